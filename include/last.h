@@ -17,6 +17,11 @@
  *   last_select_topk  Table 5: keep the k_b highest scores (no diversity term).
  *   last_scores_rows  Table 4: scores from the attention rows of several query
  *                     positions (First, Middle, All Mean) instead of p* alone.
+ * The key-value cache of the models around the path (last section of this file; the
+ * paper has no counterpart): last_rope rotates q and K by positions on several axes,
+ * as last_scores wants them; last_cache_append also writes K and V into a paged
+ * cache; last_cache_compact cuts a cache to the kept tokens; last_cache_attention
+ * decodes over it; last_cache_copy and last_pages_* part and free its pages.
  * Deployment aids without a counterpart in the paper: last_prune_host (the
  * whole path on host buffers, copies included), last_scores_noalloc (scoring
  * without a caller workspace) and last_check_bounded_wait (exercises the
@@ -31,8 +36,8 @@
  *   - Calls are asynchronous on `stream` (a cudaStream_t; NULL = legacy
  *     default stream).  Successive calls on one stream may reuse one
  *     workspace; concurrent calls need distinct workspaces.
- *   - No entry point may be captured into a CUDA graph: each call copies its
- *     plan from pageable host memory that it owns and releases on return, so
+ *   - No entry point but those of the key-value cache may be captured into a
+ *     CUDA graph: each call copies its plan from pageable host memory that it owns and releases on return, so
  *     a captured copy would replay freed memory.  Launch-bound callers batch
  *     requests into one call instead (one launch per kernel for the batch).
  *   - Argument errors are detected on the host before any launch; the call
@@ -91,7 +96,8 @@ typedef enum {
   LAST_ERR_WORKSPACE_TOO_SMALL = 3,  /* ws_bytes below what the call needs at least */
   LAST_ERR_CUDA = 4,                 /* a CUDA runtime call failed */
   LAST_ERR_DEVICE_INDEX = 5,         /* last_poll: a caller index was out of range */
-  LAST_ERR_TIMEOUT = 6               /* last_poll: a bounded device wait expired; outputs invalid */
+  LAST_ERR_TIMEOUT = 6,              /* last_poll: a bounded device wait expired; outputs invalid */
+  LAST_ERR_NO_PAGES = 7              /* last_pages_take: fewer pages are free than asked for */
 } last_status;
 
 typedef enum { LAST_DTYPE_F32 = 0, LAST_DTYPE_BF16 = 1 } last_dtype;
@@ -237,6 +243,148 @@ last_status last_scores_noalloc(const last_problem *p, const void *q, const void
  * device wait of the library takes when a wait expires, without hanging or
  * faulting the GPU. */
 last_status last_check_bounded_wait(void *ws, void *stream);
+
+/* ---- rotary positions and the key-value cache ----
+ *
+ * What a model around the path needs beside it: rotary positions before last_scores,
+ * and a paged cache of K and V after it.  These calls read lengths, page tables and
+ * positions on the DEVICE and copy nothing from host memory, so that they may be
+ * captured into a CUDA graph and replayed while lengths and tables change in place.
+ * dtype (last_dtype) is that of q, K, V and the outputs; sums and rotations are
+ * formed in fp32 and rounded once.  What cannot be checked on the host (a page, an
+ * index or a length out of range) is checked on the device: it is skipped, and
+ * last_poll on the call's workspace returns LAST_ERR_DEVICE_INDEX. */
+
+/* Rotary positions on several axes (time, height, width; one axis for text): token t's
+ * pair i < rot_dim / 2 turns by positions[axis[i]][t] * inv_freq[i].  Elements past
+ * rot_dim are copied.  The arrays are HOST memory, read during the call only. */
+typedef enum {
+  LAST_ROPE_HALF = 0,        /* pair i: elements i and i + rot_dim / 2 */
+  LAST_ROPE_ADJACENT = 1     /* pair i: elements 2i and 2i + 1 */
+} last_rope_pairs;
+typedef struct {
+  int32_t rot_dim;           /* even, 2 .. head_dim */
+  int32_t num_axes;          /* 1 .. 4 */
+  int32_t pairs;             /* last_rope_pairs */
+  const float *inv_freq;     /* [rot_dim / 2], 0 <= f <= 65536 */
+  const int32_t *axis;       /* [rot_dim / 2], each in 0 .. num_axes - 1; NULL: all on axis 0 */
+} last_rotary;
+
+/* Heads of a token tensor [num_tokens][heads][head_dim]: strides in elements, head_dim
+ * contiguous.  out may be in, with the same strides. */
+typedef struct {
+  const void *in;
+  void *out;
+  int32_t heads;
+  int64_t in_token, in_head;
+  int64_t out_token, out_head;
+} last_heads;
+
+/* Rotates q and, unless NULL, k.  positions: int32 [num_axes][axis_stride >= num_tokens],
+ * any value (angles are formed modulo one turn in 64-bit integers, so that long
+ * positions lose nothing).  Any strides and alignment of whole elements; head_dim 2 .. 256.
+ * last_rope_backward turns by the opposite angles: with the gradient with respect to the
+ * rotated heads as `in`, `out` receives the gradient with respect to the heads. */
+last_status last_rope(const last_rotary *r, int32_t dtype, int32_t num_tokens, int32_t head_dim,
+                      const int32_t *positions, int64_t axis_stride, const last_heads *q,
+                      const last_heads *k, void *stream);
+last_status last_rope_backward(const last_rotary *r, int32_t dtype, int32_t num_tokens,
+                               int32_t head_dim, const int32_t *positions, int64_t axis_stride,
+                               const last_heads *q, const last_heads *k, void *stream);
+
+/* A paged cache: K and V of num_layers layers in num_pages pages of page_size tokens.
+ * Element (layer, page, head, token, c) of either lies at layer * layer_stride +
+ * page * page_stride + head * head_stride + token * token_stride + c (strides in elements,
+ * each a multiple of 16 bytes; k and v 16-byte aligned).  page_size a multiple of 8;
+ * head_dim * elem_bytes a multiple of 16, head_dim <= 256. */
+typedef struct {
+  void *k, *v;
+  int32_t num_layers, num_pages, page_size, num_kv_heads, head_dim;
+  int32_t dtype;
+  int64_t layer_stride, page_stride, head_stride, token_stride;
+} last_cache;
+
+/* Sequences of a cache, all DEVICE int32: token i of sequence b lies in page
+ * page_table[b * table_stride + i / page_size], slot i % page_size; lens[b] tokens are held. */
+typedef struct {
+  int32_t batch;
+  int32_t max_pages;         /* entries of a page table row */
+  int64_t table_stride;
+  const int32_t *page_table;
+  const int32_t *lens;
+  const int32_t *key_begin;  /* first key that last_cache_attention reads; NULL: 0 */
+} last_sequences;
+
+/* Bytes of device workspace (256-byte aligned) for the calls below with up to `batch`
+ * sequences and num_q_heads query heads.  Its contents need no initialisation. */
+last_status last_cache_workspace_size(const last_cache *c, int32_t batch, int32_t num_q_heads,
+                                      size_t *bytes);
+
+/* Writes new tokens behind the sequences' cached ones, in one layer.  Sequence b's new tokens are
+ * cu_new[b] .. cu_new[b+1]-1 (DEVICE int32 [batch+1], cu_new[batch] = num_tokens; NULL: one
+ * token per sequence) and s->lens[b] counts them already: the last one goes to slot
+ * lens[b] - 1.  With r, the tokens' K (and q, unless NULL) are rotated on the way as in
+ * last_rope and q's heads written to q->out; without r, K is copied and q must be NULL.
+ * The out fields of k and v are not used. */
+last_status last_cache_append(const last_cache *c, int32_t layer, const last_sequences *s,
+                              int32_t num_tokens, const int32_t *cu_new, const last_rotary *r,
+                              const int32_t *positions, int64_t axis_stride, const last_heads *q,
+                              const last_heads *k, const last_heads *v, void *ws,
+                              size_t ws_bytes, void *stream);
+
+/* Attention of one new token per sequence over its cached keys key_begin[b] .. lens[b]-1, in
+ * one layer: out = sum_p softmax_p(scale q.k_p) v_p for every q-head, lse (may be NULL) [batch]
+ * [num_q_heads] fp32 = log sum_p exp(scale q.k_p).  A sequence without such a key gets out = 0
+ * and lse = -inf; keys whose logits are -inf take no part.  Slots outside the range are
+ * never used, whatever they hold, and pages wholly outside it are not read (their table entries
+ * may be anything).  q-head h reads kv-head h / (num_q_heads / num_kv_heads).  q and out:
+ * [batch][num_q_heads][head_dim], sequences q_stride and out_stride elements apart, both multiples
+ * of 16 bytes, 16-byte aligned.  scale <= 0 selects 1/sqrt(head_dim).  Results do not depend on
+ * other calls or on timing: repeated calls give the same bits. */
+last_status last_cache_attention(const last_cache *c, int32_t layer, const last_sequences *s,
+                                 int32_t num_q_heads, float scale, const void *q, int64_t q_stride,
+                                 void *out, int64_t out_stride, float *lse, void *ws,
+                                 size_t ws_bytes, void *stream);
+
+/* Copies page src[i] to page dst[i], i < num_copies (DEVICE int32), in every layer, K and V.  No
+ * page may be written twice, nor written and read, by one call; src[i] == dst[i] does nothing. */
+last_status last_cache_copy(const last_cache *c, int32_t num_copies, const int32_t *src,
+                            const int32_t *dst, void *ws, size_t ws_bytes, void *stream);
+
+/* The pruning applied to a cache (Eq. 12 on K and V): sequence b keeps its tokens before
+ * span_begin[b], of the span_len[b] tokens after that the span-local ones idx[cu_keep[b]] ..
+ * idx[cu_keep[b+1]-1] (as last_select writes them), and all tokens behind the span; they are
+ * copied, in that order and in every layer, to the front of the pages that row b of dst_table
+ * ([batch][dst_max_pages], rows dst_stride apart) names, and lens_out[b] receives their number.
+ * All arrays are DEVICE int32; span_begin and span_len NULL: the whole sequence is the span.
+ * num_idx is the length of idx.  Pages that are written may not be read for another token in the
+ * same call, but a page may stand in both tables where its tokens keep their slots (those before
+ * the first dropped one): a token that would be copied onto itself is left alone.  A
+ * sequence whose span, cu_keep or dst_table cannot hold is skipped, lens_out[b] included;
+ * so is a single token whose idx or page is out of range.  lens_out may not be s->lens. */
+last_status last_cache_compact(const last_cache *c, const last_sequences *s,
+                               const int32_t *dst_table, int32_t dst_max_pages,
+                               int64_t dst_stride, const int32_t *span_begin,
+                               const int32_t *span_len, const int32_t *cu_keep,
+                               const int32_t *idx, int32_t num_idx, int32_t *lens_out, void *ws,
+                               size_t ws_bytes, void *stream);
+
+/* Who holds which page, on the HOST: holders [num_pages] counts the sequences that hold a page (0: free)
+ * and free_pages [num_pages] is a stack of the num_free free ones; both arrays belong to the caller.
+ * last_pages_init frees every page.  last_pages_take hands out n free pages (one holder each) or,
+ * with fewer free, none: LAST_ERR_NO_PAGES.  last_pages_share adds a holder to each page of a list
+ * (a fork), last_pages_release takes one away and frees what nobody holds.  A page that is out of
+ * range or free makes either return LAST_ERR_INVALID_ARG, with nothing changed. */
+typedef struct {
+  int32_t num_pages;
+  int32_t num_free;
+  int32_t *holders;
+  int32_t *free_pages;
+} last_page_pool;
+last_status last_pages_init(last_page_pool *p);
+last_status last_pages_take(last_page_pool *p, int32_t n, int32_t *pages);
+last_status last_pages_share(last_page_pool *p, int32_t n, const int32_t *pages);
+last_status last_pages_release(last_page_pool *p, int32_t n, const int32_t *pages);
 
 /* Synchronises `stream`, then reports the device-side flags of the last call
  * that used `ws`: LAST_OK, LAST_ERR_DEVICE_INDEX, or LAST_ERR_TIMEOUT (a wait

@@ -2,14 +2,19 @@
 
 Every step of the path runs in the CUDA kernels of liblast.so; this module
 only turns torch tensors (and, for last_prune_host, host buffers) into pointers
-and host offset arrays into the C problem struct.  There is no CPU fallback: if
+and host offset arrays into the C problem struct.  The handles of the key-value
+cache (Rope, Cache, Sequences, PagePool) are such structs too, checked once and
+reused by every call on them.  There is no CPU fallback: if
 the library is missing, every call raises.
 
 Functions carry the names of the C entry points in include/last.h:
   last_workspace_size, last_scores, last_select, last_select_topk, last_gather,
   last_prune, last_host_workspace_size, last_prune_host, last_scores_rows,
   last_scores_rows_workspace_size, last_scores_noalloc, last_check_bounded_wait,
-  last_poll, last_budget, last_status_string, last_error_message.
+  last_poll, last_budget, last_status_string, last_error_message,
+  last_rope, last_rope_backward, last_cache_workspace_size, last_cache_append,
+  last_cache_attention, last_cache_copy, last_cache_compact, last_pages_init,
+  last_pages_take, last_pages_share, last_pages_release.
 """
 from __future__ import annotations
 
@@ -29,15 +34,22 @@ LAST_ERR_WORKSPACE_TOO_SMALL = 3
 LAST_ERR_CUDA = 4
 LAST_ERR_DEVICE_INDEX = 5
 LAST_ERR_TIMEOUT = 6
+LAST_ERR_NO_PAGES = 7
 
 LAST_DTYPE_F32 = 0
 LAST_DTYPE_BF16 = 1
+
+LAST_ROPE_HALF = 0
+LAST_ROPE_ADJACENT = 1
 
 EXPORTED = ("last_workspace_size", "last_scores", "last_select", "last_gather", "last_prune",
             "last_poll", "last_budget", "last_status_string", "last_error_message",
             "last_scores_noalloc", "last_select_topk", "last_scores_rows",
             "last_scores_rows_workspace_size", "last_check_bounded_wait",
-            "last_host_workspace_size", "last_prune_host")
+            "last_host_workspace_size", "last_prune_host", "last_rope", "last_rope_backward",
+            "last_cache_workspace_size", "last_cache_append", "last_cache_attention",
+            "last_cache_copy", "last_cache_compact", "last_pages_init", "last_pages_take",
+            "last_pages_share", "last_pages_release")
 
 
 class LastError(RuntimeError):
@@ -55,6 +67,39 @@ class _Problem(ctypes.Structure):
                 ("vis_start", ctypes.POINTER(ctypes.c_int32)),
                 ("cu_vis", ctypes.POINTER(ctypes.c_int32)),
                 ("cu_keep", ctypes.POINTER(ctypes.c_int32))]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("pairs", ctypes.c_int32),
+                ("inv_freq", ctypes.POINTER(ctypes.c_float)),
+                ("axis", ctypes.POINTER(ctypes.c_int32))]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("heads", ctypes.c_int32),
+                ("in_token", ctypes.c_int64), ("in_head", ctypes.c_int64),
+                ("out_token", ctypes.c_int64), ("out_head", ctypes.c_int64)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("num_layers", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("layer_stride", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64)]
+
+
+class _Sequences(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("table_stride", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("key_begin", ctypes.c_void_p)]
+
+
+class _PagePool(ctypes.Structure):
+    _fields_ = [("num_pages", ctypes.c_int32), ("num_free", ctypes.c_int32),
+                ("holders", ctypes.POINTER(ctypes.c_int32)),
+                ("free_pages", ctypes.POINTER(ctypes.c_int32))]
 
 
 _lib = None
@@ -95,6 +140,23 @@ def load_library(path: str = LIB_PATH):
     lib.last_status_string.restype = ctypes.c_char_p
     lib.last_error_message.argtypes = []
     lib.last_error_message.restype = ctypes.c_char_p
+    I, L, F, Z = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+    PR, PH, PC = (ctypes.POINTER(t) for t in (_Rotary, _Heads, _Cache))
+    PS, PG = ctypes.POINTER(_Sequences), ctypes.POINTER(_PagePool)
+    lib.last_rope.argtypes = lib.last_rope_backward.argtypes = [PR, I, I, I, P, L, PH, PH, P]
+    lib.last_cache_workspace_size.argtypes = [PC, I, I, ctypes.POINTER(Z)]
+    lib.last_cache_append.argtypes = [PC, I, PS, I, P, PR, P, L, PH, PH, PH, P, Z, P]
+    lib.last_cache_attention.argtypes = [PC, I, PS, I, F, P, L, P, L, P, P, Z, P]
+    lib.last_cache_copy.argtypes = [PC, I, P, P, P, Z, P]
+    lib.last_cache_compact.argtypes = [PC, PS, P, I, L, P, P, P, P, I, P, P, Z, P]
+    lib.last_pages_init.argtypes = [PG]
+    for name in ("last_pages_take", "last_pages_share", "last_pages_release"):
+        getattr(lib, name).argtypes = [PG, I, PI]
+    for name in ("last_rope", "last_rope_backward", "last_cache_workspace_size", "last_cache_append",
+                 "last_cache_attention", "last_cache_copy", "last_cache_compact",
+                 "last_pages_init", "last_pages_take", "last_pages_share", "last_pages_release",
+                 "last_host_workspace_size", "last_prune_host"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("last_workspace_size", "last_scores", "last_select", "last_gather",
                  "last_prune", "last_poll", "last_scores_noalloc", "last_select_topk",
                  "last_scores_rows", "last_scores_rows_workspace_size",
@@ -334,3 +396,271 @@ def last_budget(n_vis: int, num: int, den: int) -> int:
 
 def last_status_string(st: int) -> str:
     return load_library().last_status_string(st).decode()
+
+
+# ---- rotary positions and the key-value cache ----
+
+_CODES = {"float32": LAST_DTYPE_F32, "bfloat16": LAST_DTYPE_BF16}
+
+
+def _code(dtype) -> int:
+    name = str(dtype).rpartition(".")[2]
+    if name not in _CODES:
+        raise ValueError(f"liblast takes float32 and bfloat16 tensors, not {name}")
+    return _CODES[name]
+
+
+def _on_device(t, name: str, shape=None):
+    if not t.is_cuda:
+        raise ValueError(f"{name}: liblast takes device tensors")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return t
+
+
+def _int32(t, name: str, shape=None):
+    """A device int32 tensor whose last dimension is contiguous."""
+    _on_device(t, name, shape)
+    if _dtype_name(t) != "int32" or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: int32 with a contiguous last dimension expected")
+    return t
+
+
+def _dtype_name(t) -> str:
+    return str(t.dtype).rpartition(".")[2]
+
+
+class Rope:
+    """Rotary positions on several axes (include/last.h `last_rotary`).  inv_freq: one frequency per
+    pair; axis: the axis of each (default: all on axis 0); pairs: "half" for elements
+    (i, i + rot_dim/2), "adjacent" for (2i, 2i + 1)."""
+
+    def __init__(self, inv_freq: Sequence[float], axis: Optional[Sequence[int]] = None, pairs: str = "half",
+                 num_axes: Optional[int] = None):
+        self.inv_freq = np.ascontiguousarray(np.asarray(inv_freq, dtype=np.float32))
+        n = len(self.inv_freq)
+        self.axis = np.ascontiguousarray(np.zeros(n) if axis is None else np.asarray(axis), dtype=np.int32)
+        if self.inv_freq.shape != (n,) or self.axis.shape != (n,):
+            raise ValueError("inv_freq and axis must hold one value per pair")
+        if num_axes is None:
+            num_axes = int(self.axis.max()) + 1 if n else 1
+        code = {"half": LAST_ROPE_HALF, "adjacent": LAST_ROPE_ADJACENT}[pairs]
+        self.num_axes = num_axes
+        self.c = _Rotary(2 * n, num_axes, code, self.inv_freq.ctypes.data_as(ctypes.POINTER(ctypes.c_float)),
+                         self.axis.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)))
+        self.ref = ctypes.byref(self.c)
+
+    @classmethod
+    def sections(cls, sections: Sequence[int], base: float = 10000.0, pairs: str = "half"):
+        """sections[a] consecutive frequencies on axis a, frequency i = base^(-2i/rot_dim)."""
+        n = int(sum(sections))
+        return cls(base ** (-np.arange(n, dtype=np.float64) / max(n, 1)),
+                   np.repeat(np.arange(len(sections)), sections), pairs, len(sections))
+
+
+class Cache:
+    """A paged key-value cache (include/last.h `last_cache`) over two tensors of the caller's, k and v,
+    [layers][pages][kv_heads][page_size][head_dim]; views with other strides (e.g. pages that hold
+    tokens outside heads, transposed) do as well, of both tensors alike."""
+
+    def __init__(self, k, v):
+        for t, name in ((_on_device(k, "k"), "k"), (_on_device(v, "v", k.shape), "v")):
+            if t.dim() != 5:
+                raise ValueError(f"{name}: [layers][pages][kv_heads][page_size][head_dim] expected")
+        if k.dtype != v.dtype or k.stride() != v.stride() or (k.shape[4] > 1 and k.stride(4) != 1):
+            raise ValueError("k and v must have one dtype and the same strides, head_dim contiguous")
+        self.k, self.v, self.dtype = k, v, k.dtype
+        layers, pages, heads, size, dim = k.shape
+        self.page_size, self.kv_heads, self.head_dim = size, heads, dim
+        sl, sp, sh, st, _ = k.stride()
+        self.c = _Cache(k.data_ptr(), v.data_ptr(), layers, pages, size, heads, dim, _code(k.dtype), sl, sp, sh, st)
+        self.ref = ctypes.byref(self.c)
+
+
+class Sequences:
+    """Sequences of a cache (include/last.h `last_sequences`): device int32 tensors page_table
+    [batch][max_pages], lens [batch] and, optionally, key_begin [batch].  Their contents may change
+    between calls; a program keeps one for as long as it keeps the tensors."""
+
+    def __init__(self, page_table, lens, key_begin=None):
+        if page_table.dim() != 2:
+            raise ValueError("page_table: [batch][max_pages] expected")
+        b, n = page_table.shape
+        self.page_table = _int32(page_table, "page_table")
+        self.lens = _int32(lens, "lens", (b,))
+        self.key_begin = None if key_begin is None else _int32(key_begin, "key_begin", (b,))
+        self.batch = b
+        self.c = _Sequences(b, n, page_table.stride(0), page_table.data_ptr(), lens.data_ptr(),
+                            None if key_begin is None else key_begin.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+
+def _heads(x, out, dtype, dim, name):
+    """last_heads of a [tokens][heads][dim] tensor and, optionally, its output."""
+    if not x.is_cuda or x.dim() != 3 or x.dtype != dtype or x.shape[2] != dim:
+        raise ValueError(f"{name}: a device tensor [tokens][heads][{dim}] of {dtype} expected")
+    st, sh, sd = x.stride()
+    if sd != 1 and dim > 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    if out is None:
+        return _Heads(x.data_ptr(), None, x.shape[1], st, sh, 0, 0)
+    if not out.is_cuda or out.shape != x.shape or out.dtype != dtype or (out.stride(2) != 1 and dim > 1):
+        raise ValueError(f"{name}_out: a tensor like {name} expected")
+    ot, oh, _ = out.stride()
+    return _Heads(x.data_ptr(), out.data_ptr(), x.shape[1], st, sh, ot, oh)
+
+
+def _positions(positions, num_axes, tokens):
+    if positions is None:
+        raise ValueError("positions are required")
+    if positions.dim() == 1:
+        positions = positions[None]
+    _int32(positions, "positions", (num_axes, tokens))
+    return positions.data_ptr(), positions.stride(0) if num_axes > 1 else tokens
+
+
+def _rope(call, rope: Rope, positions, q, q_out, k, k_out, stream):
+    t, _, d = q.shape
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out go together")
+    if k is not None and k.shape[0] != t:
+        raise ValueError("q and k must have the same tokens")
+    qh = _heads(q, q_out, q.dtype, d, "q")
+    kh = None if k is None else ctypes.byref(_heads(k, k_out, q.dtype, d, "k"))
+    pos, stride = _positions(positions, rope.num_axes, t)
+    _check(call(rope.ref, _code(q.dtype), t, d, pos, stride, ctypes.byref(qh), kh, _stream(stream)))
+
+
+def last_rope(rope: Rope, positions, q, q_out, k=None, k_out=None, stream=None):
+    """q and k [tokens][heads][head_dim] rotated by positions [axes][tokens] (int32) into q_out and k_out,
+    which may be q and k themselves."""
+    _rope(load_library().last_rope, rope, positions, q, q_out, k, k_out, stream)
+
+
+def last_rope_backward(rope: Rope, positions, q, q_out, k=None, k_out=None, stream=None):
+    """The gradients q and k of the rotated heads turned back into the heads' gradients q_out and k_out."""
+    _rope(load_library().last_rope_backward, rope, positions, q, q_out, k, k_out, stream)
+
+
+def last_cache_workspace_size(cache: Cache, batch: int, num_q_heads: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().last_cache_workspace_size(cache.ref, batch, num_q_heads, ctypes.byref(n)))
+    return n.value
+
+
+def cache_workspace(cache: Cache, batch: int, num_q_heads: int):
+    """A torch uint8 tensor of last_cache_workspace_size bytes beside the cache."""
+    import torch
+    return torch.empty(last_cache_workspace_size(cache, batch, num_q_heads), dtype=torch.uint8,
+                       device=cache.k.device)
+
+
+def last_cache_append(cache: Cache, layer: int, seqs: Sequences, k, v, ws, cu_new=None, rope: Optional[Rope] = None,
+                      positions=None, q=None, q_out=None, stream=None):
+    """New tokens' k and v [tokens][kv_heads][head_dim] written behind the sequences' cached ones (seqs.lens
+    counts them already); with a rope, k is rotated on the way and q into q_out."""
+    t = k.shape[0]
+    if v.shape[0] != t or (q is not None and q.shape[0] != t):
+        raise ValueError("q, k and v must have the same tokens")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if cu_new is not None:
+        _int32(cu_new, "cu_new", (seqs.batch + 1,))
+    d = cache.head_dim
+    kh, vh = _heads(k, None, cache.dtype, d, "k"), _heads(v, None, cache.dtype, d, "v")
+    qh = None if q is None else ctypes.byref(_heads(q, q_out, cache.dtype, d, "q"))
+    pos, stride = (None, 0) if rope is None else _positions(positions, rope.num_axes, t)
+    p, n = _ws(ws)
+    _check(load_library().last_cache_append(
+        cache.ref, layer, seqs.ref, t, None if cu_new is None else cu_new.data_ptr(),
+        None if rope is None else rope.ref, pos, stride, qh, ctypes.byref(kh), ctypes.byref(vh), p, n, _stream(stream)))
+
+
+def last_cache_attention(cache: Cache, layer: int, seqs: Sequences, q, out, ws, lse=None, softmax_scale: float = 0.0,
+                         stream=None):
+    """out = attention of q [batch][q_heads][head_dim] over the sequences' cached keys of one layer; lse
+    [batch][q_heads] fp32 receives the log of the softmax's denominator."""
+    if q.dim() != 3 or q.shape[0] != seqs.batch or q.shape[2] != cache.head_dim or out.shape != q.shape:
+        raise ValueError(f"q and out: [{seqs.batch}][q_heads][{cache.head_dim}] expected")
+    heads = q.shape[1]
+    for t, name in ((q, "q"), (out, "out")):
+        if not t.is_cuda or t.dtype != cache.dtype or t.stride(2) != 1 or (heads > 1 and t.stride(1) != cache.head_dim):
+            raise ValueError(f"{name}: a device tensor of the cache's dtype, [q_heads][head_dim] contiguous, expected")
+    if lse is not None and (not lse.is_cuda or _dtype_name(lse) != "float32" or tuple(lse.shape) != (seqs.batch, heads)
+                            or not lse.is_contiguous()):
+        raise ValueError("lse: a contiguous device float32 tensor [batch][q_heads] expected")
+    p, n = _ws(ws)
+    _check(load_library().last_cache_attention(
+        cache.ref, layer, seqs.ref, heads, float(softmax_scale), q.data_ptr(), q.stride(0), out.data_ptr(),
+        out.stride(0), None if lse is None else lse.data_ptr(), p, n, _stream(stream)))
+
+
+def last_cache_copy(cache: Cache, src, dst, ws, stream=None):
+    """Pages src[i] copied to pages dst[i] (device int32), every layer, K and V."""
+    n = src.shape[0]
+    _int32(src, "src", (n,))
+    _int32(dst, "dst", (n,))
+    p, nb = _ws(ws)
+    _check(load_library().last_cache_copy(cache.ref, n, src.data_ptr(), dst.data_ptr(), p, nb, _stream(stream)))
+
+
+def last_cache_compact(cache: Cache, seqs: Sequences, dst_table, cu_keep, idx, lens_out, ws, span_begin=None,
+                       span_len=None, stream=None):
+    """The sequences' tokens outside their spans and the spans' tokens idx (as last_select writes them),
+    in order, copied to the pages of dst_table [batch][max_pages]; lens_out [batch] receives the new lengths."""
+    b = seqs.batch
+    if dst_table.dim() != 2 or dst_table.shape[0] != b or idx.dim() != 1:
+        raise ValueError("dst_table: [batch][max_pages], idx: one dimension expected")
+    _int32(dst_table, "dst_table")
+    _int32(cu_keep, "cu_keep", (b + 1,))
+    _int32(idx, "idx")
+    _int32(lens_out, "lens_out", (b,))
+    for t, name in ((span_begin, "span_begin"), (span_len, "span_len")):
+        if t is not None:
+            _int32(t, name, (b,))
+    p, n = _ws(ws)
+    _check(load_library().last_cache_compact(
+        cache.ref, seqs.ref, dst_table.data_ptr(), dst_table.shape[1], dst_table.stride(0),
+        None if span_begin is None else span_begin.data_ptr(), None if span_len is None else span_len.data_ptr(),
+        cu_keep.data_ptr(), idx.data_ptr(), idx.shape[0], lens_out.data_ptr(), p, n, _stream(stream)))
+
+
+class PagePool:
+    """Who holds which page of a cache (include/last.h `last_page_pool`), in host memory."""
+
+    def __init__(self, num_pages: int):
+        self.holders = np.zeros(max(num_pages, 1), dtype=np.int32)
+        self.free_pages = np.zeros(max(num_pages, 1), dtype=np.int32)
+        I = ctypes.POINTER(ctypes.c_int32)
+        self.c = _PagePool(num_pages, 0, self.holders.ctypes.data_as(I), self.free_pages.ctypes.data_as(I))
+        last_pages_init(self)
+
+    @property
+    def num_free(self) -> int:
+        return self.c.num_free
+
+
+def _page_list(pages):
+    a = np.ascontiguousarray(np.asarray(pages, dtype=np.int32).reshape(-1))
+    return a, a.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
+
+
+def last_pages_init(pool: PagePool):
+    _check(load_library().last_pages_init(ctypes.byref(pool.c)))
+
+
+def last_pages_take(pool: PagePool, n: int) -> np.ndarray:
+    """n free pages, one holder each."""
+    a, ptr = _page_list(np.zeros(max(n, 0)))
+    _check(load_library().last_pages_take(ctypes.byref(pool.c), n, ptr))
+    return a
+
+
+def last_pages_share(pool: PagePool, pages):
+    a, ptr = _page_list(pages)
+    _check(load_library().last_pages_share(ctypes.byref(pool.c), len(a), ptr))
+
+
+def last_pages_release(pool: PagePool, pages):
+    a, ptr = _page_list(pages)
+    _check(load_library().last_pages_release(ctypes.byref(pool.c), len(a), ptr))

@@ -1,5 +1,6 @@
 // C-ABI entry points of liblast: argument validation, workspace layout, the
 // small host->device plan copy, and the kernel launch sequence.
+#include "cache_internal.h"
 #include "last_internal.h"
 
 #include <algorithm>
@@ -519,6 +520,15 @@ last_status last_poll(const void *ws, void *stream) {
   unsigned flag = 0;
   cudaError_t e = cudaMemcpyAsync(&flag, ws, sizeof flag, cudaMemcpyDeviceToHost, s);
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e == cudaSuccess && (flag & kErrList)) {   // a cache call: one word per CTA
+    unsigned words[kMaxStatus];
+    const unsigned n = std::min(flag & ~kErrList, (unsigned)kMaxStatus);
+    e = cudaMemcpyAsync(words, static_cast<const unsigned *>(ws) + kStatusBegin, n * sizeof(unsigned),
+                        cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    flag = 0;
+    for (unsigned i = 0; e == cudaSuccess && i < n; ++i) flag |= words[i];
+  }
   if (e != cudaSuccess) return cuda_fail(e, "poll");
   if (flag & kErrConfig)
     return fail(LAST_ERR_CUDA, "internal error: a kernel's shared-memory plan exceeded its launch; "
@@ -527,6 +537,8 @@ last_status last_poll(const void *ws, void *stream) {
     return fail(LAST_ERR_TIMEOUT, "a bounded device wait expired; outputs of that call are invalid");
   if (flag & kErrGatherIndex)
     return fail(LAST_ERR_DEVICE_INDEX, "a gather index was outside [0, N_b)");
+  if (flag & kErrCacheIndex)
+    return fail(LAST_ERR_DEVICE_INDEX, "a page, an index or a length of a cache call was out of range");
   return LAST_OK;
 }
 
@@ -547,6 +559,7 @@ const char *last_status_string(last_status s) {
     case LAST_ERR_CUDA: return "LAST_ERR_CUDA";
     case LAST_ERR_DEVICE_INDEX: return "LAST_ERR_DEVICE_INDEX";
     case LAST_ERR_TIMEOUT: return "LAST_ERR_TIMEOUT";
+    case LAST_ERR_NO_PAGES: return "LAST_ERR_NO_PAGES";
   }
   return "LAST_ERR_UNKNOWN";
 }

@@ -1,0 +1,273 @@
+"""CPU-side checks of the rotary positions and the key-value cache: arguments are refused on
+the host before any launch, and the page pool is host code (no compute call runs here)."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import paper_2607_27952_gb300 as last
+
+ONE_PAIR = (ctypes.c_float * 4)(1.0, 0.5, 0.25, 0.125)
+AXES = (ctypes.c_int32 * 4)(0, 1, 2, 0)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2607_27952_gb300.build import build
+    build()
+    return last.load_library()
+
+
+def _rotary(**kw):
+    f = dict(rot_dim=8, num_axes=3, pairs=0, inv_freq=ONE_PAIR, axis=AXES)
+    f.update(kw)
+    return last._Rotary(f["rot_dim"], f["num_axes"], f["pairs"],
+                        ctypes.cast(f["inv_freq"], ctypes.POINTER(ctypes.c_float)),
+                        ctypes.cast(f["axis"], ctypes.POINTER(ctypes.c_int32)))
+
+
+def _heads(**kw):
+    f = dict(in_=16, out=16, heads=2, in_token=128, in_head=64, out_token=128, out_head=64)
+    f.update(kw)
+    return last._Heads(*f.values())
+
+
+def _cache(**kw):
+    f = dict(k=4096, v=8192, num_layers=2, num_pages=10, page_size=16, num_kv_heads=2, head_dim=64, dtype=1,
+             layer_stride=20480, page_stride=2048, head_stride=1024, token_stride=64)
+    f.update(kw)
+    return last._Cache(*f.values())
+
+
+def _seqs(**kw):
+    f = dict(batch=3, max_pages=4, table_stride=4, page_table=512, lens=256, key_begin=None)
+    f.update(kw)
+    return last._Sequences(*f.values())
+
+
+def _status(st):
+    return st, last.load_library().last_error_message().decode()
+
+
+def _rope(lib, r=None, h=None, k=None, dtype=1, tokens=5, dim=64, pos=16, stride=5, back=False):
+    r, h = r or _rotary(), h or _heads()
+    call = lib.last_rope_backward if back else lib.last_rope
+    return call(ctypes.byref(r), dtype, tokens, dim, pos, stride, ctypes.byref(h),
+                ctypes.byref(k) if k else None, 0)
+
+
+BAD_AXES = (ctypes.c_int32 * 4)(0, 3, 0, 0)
+BAD_FREQ = (ctypes.c_float * 4)(1.0, float("nan"), 0, 0)
+BIG_FREQ = (ctypes.c_float * 4)(1.0, 65537.0, 0, 0)
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=2), last.LAST_ERR_INVALID_ARG),
+    (dict(tokens=-1), last.LAST_ERR_INVALID_ARG),
+    (dict(dim=264), last.LAST_ERR_UNSUPPORTED),
+    (dict(dim=1), last.LAST_ERR_INVALID_ARG),
+    (dict(dim=6), last.LAST_ERR_INVALID_ARG),                        # rot_dim > head_dim
+    (dict(pos=None), last.LAST_ERR_INVALID_ARG),
+    (dict(stride=4), last.LAST_ERR_INVALID_ARG),                     # axes overlap
+    (dict(r=_rotary(rot_dim=7)), last.LAST_ERR_INVALID_ARG),
+    (dict(r=_rotary(rot_dim=0)), last.LAST_ERR_INVALID_ARG),
+    (dict(r=_rotary(num_axes=0)), last.LAST_ERR_INVALID_ARG),
+    (dict(r=_rotary(num_axes=5)), last.LAST_ERR_INVALID_ARG),
+    (dict(r=_rotary(pairs=2)), last.LAST_ERR_INVALID_ARG),
+    (dict(r=_rotary(axis=BAD_AXES)), last.LAST_ERR_INVALID_ARG),
+    (dict(r=_rotary(inv_freq=BAD_FREQ)), last.LAST_ERR_INVALID_ARG),
+    (dict(r=_rotary(inv_freq=BIG_FREQ)), last.LAST_ERR_INVALID_ARG),
+    (dict(h=_heads(in_=None)), last.LAST_ERR_INVALID_ARG),
+    (dict(h=_heads(out=None)), last.LAST_ERR_INVALID_ARG),
+    (dict(h=_heads(heads=0)), last.LAST_ERR_INVALID_ARG),
+    (dict(h=_heads(in_=17)), last.LAST_ERR_INVALID_ARG),             # not a whole element
+    (dict(k=_heads(heads=-1)), last.LAST_ERR_INVALID_ARG),
+])
+def test_rope_refuses(lib, kw, status, back):
+    st, msg = _status(_rope(lib, back=back, **kw))
+    assert st == status and msg
+
+
+def test_rope_of_no_tokens_is_nothing(lib):
+    assert _rope(lib, tokens=0, pos=None, h=_heads(in_=None, out=None)) == last.LAST_OK
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=7), last.LAST_ERR_INVALID_ARG),
+    (dict(num_layers=0), last.LAST_ERR_INVALID_ARG),
+    (dict(num_pages=0), last.LAST_ERR_INVALID_ARG),
+    (dict(num_kv_heads=0), last.LAST_ERR_INVALID_ARG),
+    (dict(page_size=0), last.LAST_ERR_INVALID_ARG),
+    (dict(page_size=12), last.LAST_ERR_INVALID_ARG),
+    (dict(head_dim=0), last.LAST_ERR_INVALID_ARG),
+    (dict(head_dim=60), last.LAST_ERR_UNSUPPORTED),                  # 120-byte rows
+    (dict(head_dim=320, token_stride=320), last.LAST_ERR_UNSUPPORTED),
+    (dict(k=None), last.LAST_ERR_INVALID_ARG),
+    (dict(v=8), last.LAST_ERR_INVALID_ARG),
+    (dict(page_stride=2044), last.LAST_ERR_INVALID_ARG),             # 4088 bytes
+    (dict(page_stride=-2048), last.LAST_ERR_INVALID_ARG),
+    (dict(token_stride=56), last.LAST_ERR_INVALID_ARG),
+])
+def test_cache_calls_refuse_a_bad_cache(lib, kw, status):
+    c, s, h = ctypes.byref(_cache(**kw)), ctypes.byref(_seqs()), ctypes.byref(_heads())
+    n = ctypes.c_size_t(0)
+    big = 1 << 30
+    for st in (lib.last_cache_workspace_size(c, 3, 4, ctypes.byref(n)),
+               lib.last_cache_append(c, 0, s, 3, None, None, None, 0, None, h, h, 256, big, 0),
+               lib.last_cache_attention(c, 0, s, 4, 0.0, 256, 256, 256, 256, None, 256, big, 0),
+               lib.last_cache_copy(c, 1, 256, 256, 256, big, 0),
+               lib.last_cache_compact(c, s, 256, 4, 4, None, None, 256, 256, 5, 512, 256, big, 0)):
+        assert st == status and last.load_library().last_error_message()
+
+
+@pytest.mark.parametrize("kw", [dict(batch=-1), dict(page_table=None), dict(lens=None), dict(max_pages=-1),
+                                dict(table_stride=3)])
+def test_cache_calls_refuse_bad_sequences(lib, kw):
+    c, s, h = ctypes.byref(_cache()), ctypes.byref(_seqs(**kw)), ctypes.byref(_heads())
+    big = 1 << 30
+    for st in (lib.last_cache_append(c, 0, s, 3, 256, None, None, 0, None, h, h, 256, big, 0),
+               lib.last_cache_attention(c, 0, s, 4, 0.0, 256, 256, 256, 256, None, 256, big, 0),
+               lib.last_cache_compact(c, s, 256, 4, 4, None, None, 256, 256, 5, 512, 256, big, 0)):
+        assert st == last.LAST_ERR_INVALID_ARG
+
+
+def _append(lib, layer=0, tokens=3, cu=None, r=None, pos=None, q=None, k=None, v=None, ws=256, ws_bytes=1 << 30, s=None):
+    ref = lambda x: ctypes.byref(x) if x else None  # noqa: E731
+    return lib.last_cache_append(ctypes.byref(_cache()), layer, ctypes.byref(s or _seqs()), tokens, cu, ref(r), pos, 3,
+                                 ref(q), ref(k or _heads()), ref(v or _heads()), ws, ws_bytes, 0)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(layer=-1), last.LAST_ERR_INVALID_ARG),
+    (dict(layer=2), last.LAST_ERR_INVALID_ARG),
+    (dict(tokens=-1), last.LAST_ERR_INVALID_ARG),
+    (dict(tokens=4), last.LAST_ERR_INVALID_ARG),                     # one per sequence without cu_new
+    (dict(q=_heads()), last.LAST_ERR_INVALID_ARG),                   # q without a rotation
+    (dict(r=_rotary(), q=_heads()), last.LAST_ERR_INVALID_ARG),      # no positions
+    (dict(r=_rotary(rot_dim=66), pos=16), last.LAST_ERR_INVALID_ARG),
+    (dict(k=_heads(heads=3)), last.LAST_ERR_INVALID_ARG),
+    (dict(v=_heads(in_=None)), last.LAST_ERR_INVALID_ARG),
+    (dict(ws=None), last.LAST_ERR_INVALID_ARG),
+    (dict(ws=128), last.LAST_ERR_INVALID_ARG),
+    (dict(ws_bytes=1024), last.LAST_ERR_WORKSPACE_TOO_SMALL),
+])
+def test_append_refuses(lib, kw, status):
+    assert _append(lib, **kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(heads=3), last.LAST_ERR_INVALID_ARG),                      # not a multiple of the kv-heads
+    (dict(heads=0), last.LAST_ERR_INVALID_ARG),
+    (dict(heads=8194), last.LAST_ERR_UNSUPPORTED),
+    (dict(q=None), last.LAST_ERR_INVALID_ARG),
+    (dict(out=None), last.LAST_ERR_INVALID_ARG),
+    (dict(q=264), last.LAST_ERR_INVALID_ARG),
+    (dict(qs=257), last.LAST_ERR_INVALID_ARG),
+    (dict(os=248), last.LAST_ERR_INVALID_ARG),                       # sequences overlap
+    (dict(lse=2), last.LAST_ERR_INVALID_ARG),
+    (dict(ws_bytes=1024), last.LAST_ERR_WORKSPACE_TOO_SMALL),
+])
+def test_attention_refuses(lib, kw, status):
+    f = dict(heads=4, q=256, qs=256, out=256, os=256, lse=None, ws_bytes=1 << 40)
+    f.update(kw)
+    assert lib.last_cache_attention(ctypes.byref(_cache()), 0, ctypes.byref(_seqs()), f["heads"], 0.0, f["q"], f["qs"],
+                                    f["out"], f["os"], f["lse"], 256, f["ws_bytes"], 0) == status
+
+
+def test_copy_and_compact_refuse(lib):
+    c, s = ctypes.byref(_cache()), ctypes.byref(_seqs())
+    big = 1 << 30
+    bad = last.LAST_ERR_INVALID_ARG
+    assert lib.last_cache_copy(c, -1, 256, 256, 256, big, 0) == bad
+    assert lib.last_cache_copy(c, 1, None, 256, 256, big, 0) == bad
+    assert lib.last_cache_copy(c, 1, 256, None, 256, big, 0) == bad
+    assert lib.last_cache_copy(c, 1, 256, 256, 256, 1024, 0) == last.LAST_ERR_WORKSPACE_TOO_SMALL
+    ok = dict(dst=512, pages=4, stride=4, begin=256, span=256, cu=256, idx=256, n=5, out=512, ws=256, size=big)
+    for kw in (dict(dst=None), dict(pages=0), dict(stride=3), dict(begin=None), dict(span=None), dict(cu=None),
+               dict(idx=None), dict(n=-1), dict(out=None), dict(out=256), dict(ws=None), dict(ws=8)):
+        a = {**ok, **kw}
+        assert lib.last_cache_compact(c, s, a["dst"], a["pages"], a["stride"], a["begin"], a["span"], a["cu"], a["idx"],
+                                      a["n"], a["out"], a["ws"], a["size"], 0) == bad, kw
+
+
+def test_workspace_size_of_a_cache(lib):
+    n, m = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    assert lib.last_cache_workspace_size(ctypes.byref(_cache()), 3, 4, ctypes.byref(n)) == last.LAST_OK
+    assert lib.last_cache_workspace_size(ctypes.byref(_cache()), 4000, 4, ctypes.byref(m)) == last.LAST_OK
+    assert 0 < n.value <= m.value
+    for batch, heads in ((-1, 4), (3, 0), (3, 3)):
+        assert lib.last_cache_workspace_size(ctypes.byref(_cache()), batch, heads, ctypes.byref(n)) == last.LAST_ERR_INVALID_ARG
+    assert lib.last_cache_workspace_size(ctypes.byref(_cache()), 3, 4, None) == last.LAST_ERR_INVALID_ARG
+
+
+# ---- the page pool ----
+
+def test_pool_against_counts(lib):
+    """Random takes, forks and releases against a plain count per page."""
+    rng = np.random.default_rng(3)
+    pool, counts, lists = last.PagePool(37), np.zeros(37, int), []
+    for _ in range(2000):
+        what = rng.integers(3)
+        if what == 0:
+            n = int(rng.integers(0, 9))
+            if n > pool.num_free:
+                with pytest.raises(last.LastError) as e:
+                    last.last_pages_take(pool, n)
+                assert e.value.status == last.LAST_ERR_NO_PAGES
+            else:
+                pages = last.last_pages_take(pool, n)
+                assert len(set(pages.tolist())) == n and (counts[pages] == 0).all()
+                counts[pages] = 1
+                lists.append(pages)
+        elif lists and what == 1:
+            pages = lists[int(rng.integers(len(lists)))]
+            last.last_pages_share(pool, pages)
+            counts[pages] += 1
+            lists.append(pages)
+        elif lists:
+            pages = lists.pop(int(rng.integers(len(lists))))
+            last.last_pages_release(pool, pages)
+            counts[pages] -= 1
+        assert (pool.holders == counts).all() and pool.num_free == (counts == 0).sum()
+        assert sorted(pool.free_pages[:pool.num_free]) == np.flatnonzero(counts == 0).tolist()
+
+
+def test_pool_changes_nothing_when_it_refuses(lib):
+    pool = last.PagePool(4)
+    a = last.last_pages_take(pool, 3)
+    last.last_pages_share(pool, a[:1])
+    before = pool.holders.copy(), pool.free_pages.copy(), pool.num_free
+    free = int(np.flatnonzero(pool.holders == 0)[0])
+    for call, pages in ((last.last_pages_share, [a[0], free]), (last.last_pages_share, [a[0], 4]),
+                        (last.last_pages_release, [a[0], a[1], a[1]]),       # once too often
+                        (last.last_pages_release, [a[0], free]), (last.last_pages_release, [-1])):
+        with pytest.raises(last.LastError) as e:
+            call(pool, pages)
+        assert e.value.status == last.LAST_ERR_INVALID_ARG
+        assert (pool.holders == before[0]).all() and (pool.free_pages == before[1]).all() and pool.num_free == before[2]
+    last.last_pages_release(pool, [a[0], a[1], a[0]])      # both holders of one page at once
+    assert pool.num_free == 3 and pool.holders[a[0]] == 0
+    assert len(set(pool.free_pages[:3].tolist())) == 3
+
+
+def test_pool_refuses_bad_structs(lib):
+    bad = last.LAST_ERR_INVALID_ARG
+    assert lib.last_pages_init(None) == bad
+    p = last._PagePool(3, 0, None, None)
+    assert lib.last_pages_init(ctypes.byref(p)) == bad
+    pool = last.PagePool(3)
+    assert lib.last_pages_take(ctypes.byref(pool.c), -1, None) == bad
+    assert lib.last_pages_take(ctypes.byref(pool.c), 1, None) == bad
+    empty = last.PagePool(0)
+    assert empty.num_free == 0 and len(last.last_pages_take(empty, 0)) == 0
+
+
+def test_rope_handle_of_sections():
+    r = last.Rope.sections([2, 3, 3], base=10000.0, pairs="adjacent")
+    assert r.num_axes == 3 and r.axis.tolist() == [0, 0, 1, 1, 1, 2, 2, 2]
+    assert np.allclose(r.inv_freq, 10000.0 ** (-np.arange(8) / 8), rtol=1e-6)
+    with pytest.raises(ValueError):
+        last.Rope([1.0, 0.5], axis=[0])
+    with pytest.raises(KeyError):
+        last.Rope([1.0], pairs="other")

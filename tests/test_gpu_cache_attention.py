@@ -1,0 +1,265 @@
+"""Attention of one new token over a paged cache against softmax in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+
+import paper_2607_27952_gb300 as last
+
+pytestmark = pytest.mark.gpu
+
+
+def _setup(lens, hq, hkv, d, dtype, size, order, seed=0, begin=None, stale=None, qscale=1.0):
+    import torch
+    import cache_util as cu
+    pool = sum(-(-int(n) // size) for n in lens) + 2
+    k, v = cu.pages(1, pool, hkv, size, d, dtype, order, seed + 1)
+    table, rest = cu.table(lens, size, pool, seed)
+    if stale is not None:      # what no sequence's keys are
+        used = torch.zeros((pool, size), dtype=torch.bool, device="cuda")
+        for b, n in enumerate(lens):
+            i = torch.arange(0 if begin is None else min(int(begin[b]), int(n)), int(n), device="cuda")
+            used[table[b].long()[i // size], i % size] = True
+        for t in (k, v):
+            t[0].transpose(1, 2)[~used] = stale
+    q = cu.randn((len(lens), hq, d), dtype, seed + 3, qscale)
+    cache = last.Cache(k, v)
+    seqs = last.Sequences(table, cu.ints(lens), None if begin is None else cu.ints(begin))
+    return cache, seqs, q
+
+
+def _run(cache, seqs, q, scale=0.0, stream=None):
+    import torch
+    import cache_util as cu
+    out = torch.full_like(q, float("nan"))
+    lse = torch.full(q.shape[:2], float("nan"), dtype=torch.float32, device="cuda")
+    ws = cu.workspace(cache, seqs.batch, q.shape[1])
+    last.last_cache_attention(cache, 0, seqs, q, out, ws, lse=lse, softmax_scale=scale, stream=stream)
+    last.last_poll(ws, stream)
+    return out, lse
+
+
+def _check(cache, seqs, q, out, lse, lens, begin=None, scale=None):
+    import torch
+    import cache_util as cu
+    scale = 1 / math.sqrt(cache.head_dim) if scale is None else scale
+    dtype = str(q.dtype).rpartition(".")[2]
+    for b, n in enumerate(lens):
+        first = 0 if begin is None else min(int(begin[b]), int(n))
+        k, v = (cu.rows(t, seqs.page_table[b], int(n), cache.page_size)[0][:, first:] for t in (cache.k, cache.v))
+        want, want_lse, size = cu.attention(q[b], k, v, scale)
+        ez, rel, u = cu.attention_bounds(q[b], k, scale, int(n) - first, dtype)
+        err = (out[b].double() - want).abs()
+        tol = rel * size + u * want.abs()
+        assert (err <= tol).all(), f"sequence {b} ({n} keys): worst {(err - tol).max():.3e} past the bound"
+        if n == first:
+            assert (lse[b] == -math.inf).all()
+        else:
+            assert ((lse[b].double() - want_lse).abs() <= 2 * ez + 2.0 ** -20 * (1 + want_lse.abs())
+                    + (n / 8 + 64) * 2.0 ** -24).all()
+
+
+LENS = [0, 1, 2, 15, 16, 17, 63, 64, 65, 127, 129, 500]
+
+
+@pytest.mark.parametrize("order", ["head", "token"])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("hq,hkv,d,size", [
+    (1, 1, 64, 16), (4, 4, 128, 16), (12, 2, 128, 32), (14, 2, 64, 8), (16, 2, 80, 24), (9, 1, 128, 64),
+    (16, 1, 128, 48), (32, 2, 64, 96), (34, 2, 72, 16), (40, 1, 128, 128), (6, 2, 256, 16), (20, 2, 192, 40),
+    (3, 1, 8, 256), (10, 5, 16, 16), (5, 1, 136, 72), (48, 1, 256, 56),
+])
+def test_lengths_heads_and_pages(hq, hkv, d, size, dtype, order):
+    cache, seqs, q = _setup(LENS, hq, hkv, d, dtype, size, order, stale=float("nan"))
+    out, lse = _run(cache, seqs, q)
+    _check(cache, seqs, q, out, lse, LENS)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("size", [8, 16, 64, 80])
+def test_key_begin(size, dtype):
+    """Windows that start anywhere, end anywhere, hold one key or none; what lies before them is never used."""
+    import torch
+    lens = [100, 100, 100, 100, 700, 700, 700, 64, 64, 65, 5]
+    begin = [0, 1, 99, 100, 64, 65, 640, 63, 64, 64, 9]
+    cache, seqs, q = _setup(lens, 8, 2, 128, dtype, size, "head", begin=begin, stale=float("inf"))
+    table = seqs.page_table
+    for b, f in enumerate(begin):      # pages before the window have been given back
+        table[b, :min(f, lens[b]) // size] = -7
+    out, lse = _run(cache, seqs, q)
+    table.clamp_(min=0)                # for the plain form, which gathers them and leaves them out
+    _check(cache, seqs, q, out, lse, lens, begin)
+    assert (out[3] == 0).all() and (out[10] == 0).all() and torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_many_sequences_and_long_ones(dtype):
+    rng = np.random.default_rng(5)
+    for lens in (rng.integers(0, 40, 700), [20011, 1, 0, 9000, 30000], [70001]):
+        cache, seqs, q = _setup(lens, 4, 2, 64, dtype, 16, "head", seed=9)
+        out, lse = _run(cache, seqs, q)
+        _check(cache, seqs, q, out, lse, lens)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_large_and_rising_logits(dtype):
+    """Logits of hundreds, the largest last or first, and an explicit scale."""
+    import torch
+    lens = [300, 300]
+    cache, seqs, q = _setup(lens, 4, 1, 64, dtype, 16, "head", qscale=4.0)
+    i = torch.arange(300, device="cuda")
+    for b, w in ((0, i / 30.0), (1, (299 - i) / 30.0)):
+        p = seqs.page_table[b].long()[i // 16]
+        cache.k[0, p, 0, i % 16] = (q[b, 0].float()[None] * w[:, None].float()).to(q.dtype)
+    for scale in (0.0, 0.75):
+        out, lse = _run(cache, seqs, q, scale)
+        _check(cache, seqs, q, out, lse, lens, scale=scale or None)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_infinite_logits(dtype):
+    """Keys whose logits are -inf take no part, a sequence of nothing else is empty; NaN and +inf show."""
+    import torch
+    lens = [200, 200, 70, 130]
+    cache, seqs, q = _setup(lens, 2, 1, 64, dtype, 16, "head")
+    q[:] = q.abs() + 0.01
+    def put(b, at, x):
+        at = torch.as_tensor(at, device="cuda")
+        cache.k[0, seqs.page_table[b].long()[at // 16], 0, at % 16] = x
+    dead = [*range(0, 64), *range(70, 90), 199]
+    put(0, dead, -float("inf"))
+    put(1, list(range(200)), -float("inf"))
+    put(2, [69], float("nan"))
+    put(3, [3], float("inf"))
+    out, lse = _run(cache, seqs, q)
+    assert (out[1] == 0).all() and (lse[1] == -math.inf).all()
+    assert out[2].isnan().all() and lse[2].isnan().all()
+    assert out[3].isnan().all() and not torch.isfinite(lse[3]).any()
+    import cache_util as cu
+    live = [i for i in range(200) if i not in dead]
+    k, v = (cu.rows(t, seqs.page_table[0], 200, 16)[0][:, live] for t in (cache.k, cache.v))
+    want, want_lse, size = cu.attention(q[0], k, v, 0.125)
+    ez, rel, u = cu.attention_bounds(q[0], k, 0.125, len(live), dtype)
+    assert ((out[0].double() - want).abs() <= rel * size + u * want.abs()).all()
+    assert ((lse[0].double() - want_lse).abs() <= 2 * ez + 2.0 ** -18).all()
+
+
+def test_infinite_values_of_live_keys_show():
+    import torch
+    cache, seqs, q = _setup([40], 2, 1, 64, "bfloat16", 16, "head")
+    cache.v[0, seqs.page_table[0, 1].long(), 0, 3, 5] = float("inf")
+    out, lse = _run(cache, seqs, q)
+    assert (out[0, :, 5] == math.inf).all() and torch.isfinite(out[0, :, 6:]).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_views_and_layers(dtype):
+    """q inside a fused projection, out inside a wider row, K and V of one tensor, a layer of several."""
+    import torch
+    import cache_util as cu
+    lens, hq, hkv, d, size = [33, 0, 150], 6, 2, 64, 16
+    kv = cu.randn((3, 20, 2, size, hkv, d), dtype, 1)
+    cache = last.Cache(kv[:, :, 0].transpose(2, 3), kv[:, :, 1].transpose(2, 3))
+    table, _ = cu.table(lens, size, 20, 2)
+    wide = torch.nn.functional.pad(table, (0, 5), value=-1)[:, :table.shape[1]]
+    seqs = last.Sequences(wide, cu.ints(lens))
+    fused = cu.randn((3, (hq + 2 * hkv) * d), dtype, 3)
+    q = fused[:, :hq * d].unflatten(1, (hq, d))
+    out = torch.zeros((3, hq * d + 64), dtype=q.dtype, device="cuda")
+    ws = cu.workspace(cache, 3, hq)
+    for layer in range(3):
+        o = out[:, 64:].unflatten(1, (hq, d))
+        lse = torch.zeros((3, hq), device="cuda")
+        last.last_cache_attention(cache, layer, seqs, q, o, ws, lse=lse)
+        last.last_poll(ws)
+        part = last.Cache(cache.k[layer:layer + 1], cache.v[layer:layer + 1])
+        _check(part, seqs, q, o, lse, lens)
+    assert (out[:, :64] == 0).all()
+    last.last_cache_attention(cache, 0, seqs, q, o, ws)      # without lse
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_offsets_past_32_bits(dtype):
+    """Pages 5 GB apart (3 of them, most of the storage never touched)."""
+    import torch
+    import cache_util as cu
+    e = 4 if dtype == "float32" else 2
+    far = 5 * 2**30 // e
+    base = [torch.empty(2 * far + 4096, dtype=getattr(torch, dtype), device="cuda") for _ in range(2)]
+    k, v = (b.as_strided((1, 3, 2, 16, 64), (0, far, 1024, 64, 1)) for b in base)
+    for i, t in enumerate((k, v)):
+        t.copy_(cu.randn((1, 3, 2, 16, 64), dtype, i))
+    cache, seqs = last.Cache(k, v), last.Sequences(cu.ints([[2, 0, 1]]), cu.ints([47]))
+    q = cu.randn((1, 4, 64), dtype, 5)
+    out, lse = _run(cache, seqs, q)
+    _check(cache, seqs, q, out, lse, [47])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_repeats_and_streams_give_the_same_bits(dtype):
+    import torch
+    rng = np.random.default_rng(1)
+    lens = rng.integers(1, 3000, 20)
+    cache, seqs, q = _setup(lens, 8, 2, 128, dtype, 16, "token", seed=4)
+    want = _run(cache, seqs, q)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for stream in (None, s, None):
+        with torch.cuda.stream(stream):
+            got = _run(cache, seqs, q, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_empty_batch_and_refusals():
+    import torch
+    import cache_util as cu
+    cache, seqs, q = _setup([10, 20], 4, 2, 64, "bfloat16", 16, "head")
+    out, ws = torch.empty_like(q), cu.workspace(cache, 2, 4)
+    none = last.Sequences(seqs.page_table[:0], seqs.lens[:0])
+    last.last_cache_attention(cache, 0, none, q[:0], out[:0], ws)
+    last.last_poll(ws)
+    for args in ((q[:1], out), (q.float(), out.float()), (q[:, :, :32], out[:, :, :32]), (q, out[:, ::2]),
+                 (q.cpu(), out.cpu()), (q.transpose(0, 1), out)):
+        with pytest.raises(ValueError):
+            last.last_cache_attention(cache, 0, seqs, *args, ws)
+    with pytest.raises(ValueError):
+        last.last_cache_attention(cache, 0, seqs, q, out, ws, lse=torch.empty(2, 4, dtype=torch.float64, device="cuda"))
+    with pytest.raises(ValueError):
+        last.Sequences(seqs.page_table.long(), seqs.lens)
+    with pytest.raises(ValueError):
+        last.Sequences(seqs.page_table, seqs.lens[:1])
+    with pytest.raises(ValueError):
+        last.Cache(cache.k, cache.v.float())
+    with pytest.raises(ValueError):
+        last.Cache(cache.k, cache.v[:, :-1])
+    with pytest.raises(last.LastError) as e:
+        last.last_cache_attention(cache, 1, seqs, q, out, ws)
+    assert e.value.status == last.LAST_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_bad_pages_and_lengths_are_reported(dtype):
+    """The call flags them, leaves the other sequences right, and the next good call on the workspace is clean."""
+    import torch
+    import cache_util as cu
+    lens = [100, 300, 50]
+    cache, seqs, q = _setup(lens, 4, 2, 64, dtype, 16, "head")
+    out, ws = torch.zeros_like(q), cu.workspace(cache, 3, 4)
+    good = torch.zeros_like(q)
+    last.last_cache_attention(cache, 0, seqs, q, good, ws)
+    last.last_poll(ws)
+    pool = cache.k.shape[1]
+    for where, value in (("table", -1), ("table", pool), ("table", 2**31 - 1), ("lens", 10**6), ("lens", -3),
+                         ("begin", -1)):
+        t, n = seqs.page_table.clone(), seqs.lens.clone()
+        begin = torch.zeros_like(n) if where == "begin" else None
+        {"table": t[1, 7:8], "lens": n[1:2], "begin": begin[1:2] if begin is not None else None}[where].fill_(value)
+        last.last_cache_attention(cache, 0, last.Sequences(t, n, begin), q, out, ws)
+        with pytest.raises(last.LastError) as e:
+            last.last_poll(ws)
+        assert e.value.status == last.LAST_ERR_DEVICE_INDEX
+        assert torch.equal(out[0], good[0]) and torch.equal(out[2], good[2])
+        last.last_cache_attention(cache, 0, seqs, q, out, ws)
+        last.last_poll(ws)
+        assert torch.equal(out, good)
