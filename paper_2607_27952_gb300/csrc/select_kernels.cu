@@ -134,12 +134,12 @@ int active_clusters(void *fn, int csize, size_t smem, int threads) {
   return active;
 }
 
-bool encode_bf16_map(CUtensorMap *m, const void *base, int rank, const uint64_t *dims,
+bool encode_rows_map(CUtensorMap *m, const void *base, bool f32, int rank, const uint64_t *dims,
                      const uint64_t *strides, const uint32_t *box) {
   EncodeTiledFn fn = encode_tiled();
   if (fn == nullptr) return false;
-  cuuint64_t d[3], st[2];
-  cuuint32_t bx[3], es[3];
+  cuuint64_t d[4], st[3];
+  cuuint32_t bx[4], es[4];
   for (int i = 0; i < rank; ++i) {
     if (dims[i] == 0) return false;
     d[i] = dims[i];
@@ -147,9 +147,14 @@ bool encode_bf16_map(CUtensorMap *m, const void *base, int rank, const uint64_t 
     es[i] = 1;
     if (i + 1 < rank) st[i] = strides[i];
   }
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), d, st, bx, es,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  return fn(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
+            const_cast<void *>(base), d, st, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool encode_bf16_map(CUtensorMap *m, const void *base, int rank, const uint64_t *dims,
+                     const uint64_t *strides, const uint32_t *box) {
+  return encode_rows_map(m, base, false, rank, dims, strides, box);
 }
 
 // X as a [rows][dv] bf16 tensor, 64-element x box_rows boxes, 128-byte swizzle.
