@@ -1,0 +1,173 @@
+// Cache attention over fp32 keys and values: the products on the CUDA cores.
+#include "attend_impl.cuh"
+
+namespace last {
+
+namespace {
+
+// ---- consumers: fp32, on the CUDA cores ----
+// Logits: 4 lanes a key, 8 keys a warp, the heads' q broadcast from shared memory.  O: the lanes
+// across the row's columns (with short rows several keys at once), the weights broadcast.
+template <int HEADS, int WIDE>   // heads held; 128-column blocks of a row
+struct F32Part {
+  static constexpr int kTile = 32, kWarpKeys = 8;
+  static constexpr int kHeadRows = HEADS;
+  float o[HEADS][WIDE][4], m[HEADS], l[HEADS];
+
+  static __device__ __forceinline__ int lanes_across(int D) {   // lanes that share a row of V
+    const int n = D / 4;
+    return n > 16 ? 32 : n > 8 ? 16 : n > 4 ? 8 : n > 2 ? 4 : n;
+  }
+  __device__ void start(const Shape &, const char *, int) {
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      m[h] = -INFINITY;
+      l[h] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WIDE; ++w) o[h][w][0] = o[h][w][1] = o[h][w][2] = o[h][w][3] = 0.0f;
+    }
+  }
+  // Weights of the tile's 8 keys from row0 on, kept in this warp's ps [8 keys][HEADS]; keys lo <= i < hi of
+  // the tile count.  q: the heads' rows (past the pass's heads anything: their sums are not used).
+  __device__ void logits(const Shape &p, const char *q, float *ps, const char *k, int row0, int lo, int hi) {
+    const int lane = threadIdx.x & 31, D = p.a.cache.dim, cols = D / 4, column = 128 << p.box_log;
+    const float4 *qs = reinterpret_cast<const float4 *>(q);
+    const int row = row0 + (lane & 7);
+    const char *kr = k + row_at(p, row);
+    float s[HEADS] = {};
+    for (int c = lane >> 3; c < cols; c += 4) {
+      const float4 x = *reinterpret_cast<const float4 *>(kr + (c >> 3) * column + (((c & 7) ^ (row & 7)) << 4));
+#pragma unroll
+      for (int h = 0; h < HEADS; ++h) {
+        const float4 y = qs[h * cols + c];
+        s[h] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[h]))));
+      }
+    }
+    const bool counts = row >= lo && row < hi;
+    bool moved = false;
+    float alpha[HEADS];
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      s[h] += __shfl_xor_sync(~0u, s[h], 8);
+      s[h] += __shfl_xor_sync(~0u, s[h], 16);
+      if (!counts) s[h] = -INFINITY;
+      float x = s[h] * p.scale2;
+      x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
+      x = fmaxf(x, __shfl_xor_sync(~0u, x, 2));
+      x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+      alpha[h] = 1.0f;
+      if (x > m[h]) {
+        alpha[h] = exp2_fast(m[h] - x);
+        m[h] = x;
+        moved = true;
+      }
+      s[h] = exp2_fast(fmaf(s[h], p.scale2, m[h] == -INFINITY ? 0.0f : -m[h]));
+      l[h] = l[h] * alpha[h] + s[h];
+    }
+    if (moved) {   // the same in every lane
+#pragma unroll
+      for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+        for (int w = 0; w < WIDE; ++w)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[h][w][e] *= alpha[h];
+    }
+    __syncwarp();
+    if (lane < 8) {
+#pragma unroll
+      for (int h = 0; h < HEADS; ++h) ps[lane * HEADS + h] = s[h];
+    }
+    __syncwarp();
+  }
+  __device__ void values(const Shape &p, const float *ps, const char *v, int row0, int lo, int hi) {
+    const int lane = threadIdx.x & 31, D = p.a.cache.dim, cols = D / 4, column = 128 << p.box_log;
+    const int across = lanes_across(D), c0 = lane & (across - 1);
+    for (int i = lane / across; i < 8; i += 32 / across) {
+      const int r = row0 + i;
+      if (r < lo || r >= hi) continue;
+      const char *vr = v + row_at(p, r);
+#pragma unroll
+      for (int w = 0; w < WIDE; ++w) {
+        const int c = c0 + 32 * w;
+        if (c >= cols) break;
+        const float4 x = *reinterpret_cast<const float4 *>(vr + (c >> 3) * column + (((c & 7) ^ (r & 7)) << 4));
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h) {
+          const float y = ps[i * HEADS + h];
+          o[h][w][0] = fmaf(y, x.x, o[h][w][0]);
+          o[h][w][1] = fmaf(y, x.y, o[h][w][1]);
+          o[h][w][2] = fmaf(y, x.z, o[h][w][2]);
+          o[h][w][3] = fmaf(y, x.w, o[h][w][3]);
+        }
+      }
+    }
+  }
+  __device__ void stats(float *top, float *sum) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      float x = l[h] + __shfl_xor_sync(~0u, l[h], 1);
+      x += __shfl_xor_sync(~0u, x, 2);
+      x += __shfl_xor_sync(~0u, x, 4);
+      if (lane == 0) {
+        top[h] = m[h];
+        sum[h] = x;
+      }
+    }
+  }
+  __device__ void put(int row0, int col0, const float *factor, float (*to)[kMergeLd], int D) {
+    const int lane = threadIdx.x & 31, across = lanes_across(D);
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      if (h < row0 || h >= row0 + kMergeRows) continue;
+      const float f = factor[h];
+#pragma unroll
+      for (int w = 0; w < WIDE; ++w) {
+        if (w != col0 / 128) continue;
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = o[h][w][e];
+          for (int d = across; d < 32; d <<= 1) x[e] += __shfl_xor_sync(~0u, x[e], d);
+        }
+        const int c = w * 128 + lane * 4 - col0;
+        if (lane < across && c >= 0 && c < kMergeCols) *reinterpret_cast<float4 *>(&to[h - row0][c]) = make_float4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+      }
+    }
+  }
+};
+template <int WIDE>
+cudaError_t launch_heads(const Shape &p, cudaStream_t s) {
+  if (p.rows <= 1) return launch<F32Part<1, WIDE>, float>(p, s);
+  if (p.rows <= 4) return launch<F32Part<4, WIDE>, float>(p, s);
+  if (p.rows <= 8) return launch<F32Part<8, WIDE>, float>(p, s);
+  return launch<F32Part<16, WIDE>, float>(p, s);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_f32(const Shape &p, cudaStream_t s) {
+  return p.chunks <= 4 ? launch_heads<1>(p, s) : launch_heads<2>(p, s);
+}
+
+size_t attend_scratch_bytes(int batch, int q_heads, int kv_heads, int dim) {
+  const int group = q_heads / kv_heads, rows = group < kRows ? group : kRows;
+  return align256(sizeof(long long) * ((size_t)batch + 1)) + align256(sizeof(float) * kMaxWorkers * 2 * (kStatFloats + (size_t)rows * dim));
+}
+
+cudaError_t launch_attend(const AttendArgs &a, cudaStream_t s) {
+  Shape p{};
+  p.a = a;
+  p.group = a.q_heads / a.cache.heads;
+  p.passes = (p.group + kRows - 1) / kRows;
+  p.heads = p.passes * a.cache.heads;
+  p.rows = p.group < kRows ? p.group : kRows;
+  p.chunks = (a.cache.dim * a.elem + 127) / 128;
+  p.scale2 = a.scale * kLog2e;
+  p.first = reinterpret_cast<long long *>(a.ws + kStatusBytes);
+  p.parts = reinterpret_cast<float *>(a.ws + kStatusBytes + align256(sizeof(long long) * ((size_t)a.seq.batch + 1)));
+  if ((long long)a.seq.batch * a.q_heads > 0x7fffffffLL) return cudaErrorInvalidValue;
+  return a.elem == 4 ? launch_attend_f32(p, s) : launch_attend_bf16(p, s);
+}
+
+}  // namespace last

@@ -1,0 +1,529 @@
+// Attention of one new token per sequence over a paged cache (last_cache_attention).
+//
+// With z_p = scale q.k_p in units of log 2 and the running maximum m of the keys seen so far,
+//   l <- l 2^(m - m') + sum 2^(z_p - m'),  o <- o 2^(m - m') + sum 2^(z_p - m') v_p
+// is one pass over K and V; sums over parts of the keys join by the same rule, so that the
+// keys of all sequences and kv-heads are cut into equal shares, one per CTA, wherever the
+// cuts fall (join_kernel adds up what a cut has parted).  The work is reading K and V: each
+// is read once for up to 16 query heads of its kv-head.
+//
+// A CTA: one warp keeps a ring of tiles filled with TMA boxes of the pages (128-byte swizzle),
+// four take a quarter of every tile each, with sums of their own, and add them up where
+// the CTA's part of a (sequence, head) ends.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "cache_internal.h"
+#include "last_device.cuh"
+#include "last_internal.h"
+#include "tensor_map.h"
+
+namespace last {
+
+struct Shape {      // the same for every CTA
+  AttendArgs a;
+  int group, passes, heads;   // q-heads per kv-head, passes over a kv-head, passes in all
+  int box_log, chunks;        // rows of a TMA box; 128-byte columns of a row
+  int stages, slots;          // ring; parts whose q is kept
+  bool joined;                // a box holds all of them
+  int tile;                   // keys
+  int rows;                   // heads of a pass at most
+  float scale2;               // scale log2 e
+  long long *first;           // [batch + 1] first tile of each sequence (in the workspace)
+  float *parts;               // [workers][2] sums that a cut has parted
+};
+
+cudaError_t launch_attend_bf16(const Shape &p, cudaStream_t s);
+
+namespace {
+
+constexpr int kWarps = 4;                      // consumers: a quarter of every tile each
+constexpr int kThreads = 32 * (kWarps + 1);
+constexpr int kRows = 16;                      // query heads of one pass over a kv-head
+constexpr int kMaxWorkers = 320;               // CTAs
+constexpr int kMaxStages = 12;                 // of the ring: K or V of a tile each
+constexpr int kMergeRows = 8, kMergeCols = 64, kMergeLd = kMergeCols + 8;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct TileInfo {   // what the producer says of a tile
+  int seq, head;    // head: pass over a kv-head
+  int lo, hi;       // keys of the tile that count
+  int flags, slot;  // slot: of the part's q
+};
+// First and last tile of the CTA's part of a (sequence, head); the part is all of it; it is not the
+// CTA's first one.
+constexpr int kFirst = 1, kLast = 2, kWhole = 4, kLater = 8;
+constexpr int kStatFloats = 2 * kRows;   // of a parted sum: maximum and denominator per head, then the rows
+
+struct alignas(16) Shared {
+  unsigned long long full[kMaxStages], empty[kMaxStages], sync, never;
+  TileInfo info[kMaxStages];
+  float top[2][kWarps][kRows], sum[2][kWarps][kRows];   // by turns
+  float factor[kWarps][kRows], all[kRows], total[kRows];
+  float merge[kWarps][kMergeRows][kMergeLd];
+  long long warp_tiles[kWarps + 1], start_first;
+  int start_seq;
+  unsigned flags;
+  volatile unsigned dead;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A whole warp waits, with a limit; the first to give up has every other wait of the CTA end too.
+__device__ __forceinline__ bool wait(Shared &sm, unsigned long long *bar, uint32_t parity) {
+  bool ok = false;
+  for (uint32_t i = 0; i < kWaitLimit && !ok; ++i) {
+    ok = mbar_try_wait(bar, parity);
+    if ((i & 31) == 31 && sm.dead) break;
+  }
+  if (__all_sync(~0u, ok)) return true;
+  sm.dead = 1;
+  return false;
+}
+
+// The consumers' barrier (bounded, unlike a hardware one).
+__device__ __forceinline__ bool consumers_sync(Shared &sm, uint32_t &parity) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(&sm.sync);
+  parity ^= 1;
+  return wait(sm, &sm.sync, parity ^ 1);
+}
+
+struct Keys {
+  int begin, end;
+};
+__device__ __forceinline__ Keys keys_of(const AttendArgs &a, int b, unsigned *bad) {
+  const long long room = (long long)a.seq.max_pages * a.cache.page_size;
+  int end = a.seq.lens[b], begin = a.seq.begin ? a.seq.begin[b] : 0;
+  if (end < 0 || end > room || begin < 0) *bad = kErrCacheIndex;
+  end = end > room ? (int)room : end;
+  begin = begin < 0 ? 0 : begin;
+  return Keys{begin, end};
+}
+__device__ __forceinline__ int tiles_of(Keys k, int tile) {
+  return k.begin < k.end ? (k.end - 1) / tile - k.begin / tile + 1 : 0;
+}
+
+// Where a row of a tile lies: boxes of 2^box_log rows, in each the 128-byte columns one after the other.
+__device__ __forceinline__ uint32_t row_at(const Shape &p, int row) {
+  return ((row >> p.box_log) * p.chunks << (p.box_log + 7)) + (row & ((1 << p.box_log) - 1)) * 128;
+}
+
+// Two values rounded to bf16, the first in the low half.
+__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ float join_factor(float top, float all) { return top == -INFINITY ? 1.0f : exp2_fast(top - all); }
+__device__ __forceinline__ float lse_of(float top, float sum) { return sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * kLn2; }
+
+// Adds up the warps' sums of the CTA's part of a (sequence, head): to the output where the part is
+// all of it, else to the workspace.
+template <typename Part, typename T>
+__device__ bool finish(const Shape &p, Shared &sm, Part &part, const TileInfo &ti, int turn, uint32_t &parity) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = p.a.cache.dim;
+  const int kv = ti.head / p.passes, pass = ti.head - kv * p.passes;
+  const int h0 = kv * p.group + pass * kRows, n = min(kRows, p.group - pass * kRows);
+  float (*top)[kRows] = sm.top[turn], (*sum)[kRows] = sm.sum[turn];
+  part.stats(top[warp], sum[warp]);
+  if (!consumers_sync(sm, parity)) return false;   // and everybody has done with the last part's sums
+  if (lane < Part::kHeadRows) {
+    float all = top[0][lane], total = 0.0f;
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) all = fmaxf(all, top[w][lane]);
+    sm.factor[warp][lane] = join_factor(top[warp][lane], all);
+    if (warp == 0) {
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) total += sum[w][lane] * join_factor(top[w][lane], all);
+      sm.all[lane] = all;
+      sm.total[lane] = total;
+    }
+  }
+  __syncwarp();
+  float *slot = p.parts + ((long long)blockIdx.x * 2 + (ti.flags & kLater ? 1 : 0)) * (kStatFloats + p.rows * D);
+  for (int row0 = 0; row0 < n; row0 += kMergeRows)
+    for (int col0 = 0; col0 < D; col0 += kMergeCols) {
+      if (row0 + col0 > 0 && !consumers_sync(sm, parity)) return false;
+      part.put(row0, col0, sm.factor[warp], sm.merge[warp], D);
+      if (!consumers_sync(sm, parity)) return false;
+      for (int i = threadIdx.x; i < kMergeRows * kMergeCols / 2; i += kWarps * 32) {
+        const int rr = i / (kMergeCols / 2), r = row0 + rr, cc = (i % (kMergeCols / 2)) * 2, c = col0 + cc;
+        if (r >= n || c >= D) continue;
+        float2 x = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float2 y = *reinterpret_cast<const float2 *>(&sm.merge[w][rr][cc]);
+          x.x += y.x;
+          x.y += y.y;
+        }
+        const float total = sm.total[r];
+        if (ti.flags & kWhole) {
+          const float f = total == 0.0f ? 0.0f : 1.0f / total;
+          T *out = reinterpret_cast<T *>(p.a.out + ti.seq * p.a.out_stride) + (long long)(h0 + r) * D + c;
+          if (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(out) = pack_bf16(x.x * f, x.y * f);
+          else *reinterpret_cast<float2 *>(out) = make_float2(x.x * f, x.y * f);
+          if (p.a.lse != nullptr && c == 0) p.a.lse[(long long)ti.seq * p.a.q_heads + h0 + r] = lse_of(sm.all[r], total);
+        } else {
+          *reinterpret_cast<float2 *>(slot + kStatFloats + r * D + c) = x;
+          if (c == 0) *reinterpret_cast<float2 *>(slot + 2 * r) = make_float2(sm.all[r], total);
+        }
+      }
+    }
+  return true;
+}
+
+// Rows of a slot for q: the fp32 consumers read as many heads as they hold.
+template <typename Part, typename T>
+__host__ __device__ __forceinline__ int slot_rows(const Shape &p) { return sizeof(T) == 4 ? Part::kHeadRows : p.rows; }
+
+template <typename Part, typename T>
+__device__ void consume(const Shape &p, Shared &sm, char *ring, char *qs, float *weights, int tiles) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = p.chunks * Part::kTile * 128;
+  const int q_bytes = slot_rows<Part, T>(p) * p.a.cache.dim * (int)sizeof(T);
+  Part part;
+  uint32_t parity = 0;
+  int stage = 0, round = 0, turn = 0;
+  auto give_back = [&]() {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sm.empty[stage]);
+    if (++stage == p.stages) {
+      stage = 0;
+      ++round;
+    }
+  };
+  weights += warp * 8 * Part::kHeadRows;
+  for (int it = 0; it < tiles; ++it) {
+    if (!wait(sm, &sm.full[stage], round & 1)) return;
+    const TileInfo ti = sm.info[stage];
+    const char *q = qs + ti.slot * q_bytes;
+    if (ti.flags & kFirst) part.start(p, q, min(kRows, p.group - ti.head % p.passes * kRows));
+    const bool mine = warp * Part::kWarpKeys < ti.hi && (warp + 1) * Part::kWarpKeys > ti.lo;
+    if (mine) part.logits(p, q, weights, ring + (long long)stage * half, warp * Part::kWarpKeys, ti.lo, ti.hi);
+    give_back();
+    if (!wait(sm, &sm.full[stage], round & 1)) return;
+    if (mine) part.values(p, weights, ring + (long long)stage * half, warp * Part::kWarpKeys, ti.lo, ti.hi);
+    give_back();
+    if (ti.flags & kLast) {
+      if (!finish<Part, T>(p, sm, part, ti, turn, parity)) return;
+      turn ^= 1;
+    }
+  }
+}
+
+struct Walk {   // tile `at` of the `tiles` of sequence seq, pass head
+  int seq, head, at, tiles;
+  Keys keys;
+};
+__device__ __forceinline__ void advance(const Shape &p, Walk &w) {
+  unsigned bad = 0;
+  if (++w.at < w.tiles) return;
+  w.at = 0;
+  if (++w.head < p.heads) return;
+  w.head = 0;
+  do {
+    if (++w.seq >= p.a.seq.batch) return;
+    w.keys = keys_of(p.a, w.seq, &bad);
+    w.tiles = tiles_of(w.keys, p.tile);
+  } while (w.tiles == 0);
+}
+
+// One warp fills the ring, K and V of a tile by turns.  A tile's boxes (whole pages, or parts of them) are spread
+// over the lanes, and the next tile's pages are looked up while this one waits for room.  The heads' rows of q
+// come with the K of a part's first tile.  They have a slot for every K the ring can hold: when a slot's turn
+// comes again, as many tiles lie between and the last K of its part has been given back.
+template <typename Part, typename T>
+__device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const CUtensorMap *kmap, const CUtensorMap *vmap,
+                        Walk w, int tiles) {
+  constexpr int kTile = Part::kTile;
+  const int lane = threadIdx.x & 31, box = 1 << p.box_log, boxes = kTile >> p.box_log, mine = lane & (boxes - 1);
+  const int ops = boxes * (p.joined ? 1 : p.chunks), half = p.chunks * kTile * 128;
+  const int size = p.a.cache.page_size, row_bytes = p.a.cache.dim * (int)sizeof(T);
+  auto box_key = [&](const Walk &x) { return (x.keys.begin / kTile + x.at) * kTile + mine * box; };
+  auto counts = [&](const Walk &x) { return box_key(x) < x.keys.end && box_key(x) + box > x.keys.begin; };
+  auto lookup = [&](const Walk &x) {   // page of this lane's box, as the table has it
+    return counts(x) ? p.a.seq.table[x.seq * p.a.seq.table_stride + box_key(x) / size] : 0;
+  };
+  int page = lookup(w), next_page = 0, stage = 0, round = 0, slot = 0;
+  bool fresh = true, later = false, begun = false;
+  for (int it = 0; it < tiles; ++it) {
+    Walk next = w;
+    if (it + 1 < tiles) {
+      advance(p, next);
+      next_page = lookup(next);   // not looked at before its own turn
+    }
+    const bool last = it + 1 == tiles || w.at + 1 == w.tiles, here = counts(w);
+    if (fresh) begun = w.at == 0;
+    const int bytes = __popc(__ballot_sync(~0u, lane < boxes && here)) * p.chunks * box * 128;
+    const int kv = w.head / p.passes, row = box_key(w) % size;
+#pragma unroll
+    for (int is_v = 0; is_v < 2; ++is_v) {
+      if (round > 0 && !wait(sm, &sm.empty[stage], (round & 1) ^ 1)) return;
+      if (is_v == 0 && here && (unsigned)page >= (unsigned)p.a.cache.num_pages) {
+        atomicOr(&sm.flags, kErrCacheIndex);
+        page = 0;   // any page will do: the call is reported
+      }
+      if (lane == 0) {
+        if (is_v == 0) {
+          const int k0 = (w.keys.begin / kTile + w.at) * kTile, pass = w.head - kv * p.passes;
+          TileInfo ti;
+          ti.seq = w.seq;
+          ti.head = w.head;
+          ti.lo = w.keys.begin - k0;
+          ti.hi = w.keys.end - k0;
+          ti.flags = (fresh ? kFirst : 0) | (last ? kLast : 0) | (begun && w.at + 1 == w.tiles ? kWhole : 0) | (later ? kLater : 0);
+          ti.slot = slot;
+          sm.info[stage] = ti;
+          const int q_bytes = fresh ? min(kRows, p.group - pass * kRows) * row_bytes : 0;
+          mbar_expect_tx(&sm.full[stage], bytes + q_bytes);
+          if (fresh)
+            bulk_g2s(qs + slot * slot_rows<Part, T>(p) * row_bytes,
+                     p.a.q + w.seq * p.a.q_stride + (long long)(kv * p.group + pass * kRows) * row_bytes, q_bytes, &sm.full[stage]);
+        } else {
+          mbar_expect_tx(&sm.full[stage], bytes);
+        }
+      }
+      __syncwarp();
+      if (here) {
+        const CUtensorMap *map = is_v ? vmap : kmap;
+        char *to = ring + (long long)stage * half + (mine * p.chunks << (p.box_log + 7));
+        if (p.joined) {
+          if (lane < boxes) tma_load_5d(to, map, 0, row, 0, kv, page, &sm.full[stage]);
+        } else {
+          for (int o = lane; o < ops; o += 32) {
+            const int c = o / boxes;
+            tma_load_4d(to + (c << (p.box_log + 7)), map, c * (128 / (int)sizeof(T)), row, kv, page, &sm.full[stage]);
+          }
+        }
+      }
+      if (++stage == p.stages) {
+        stage = 0;
+        ++round;
+      }
+    }
+    fresh = last;
+    later |= last;
+    if (last && ++slot == p.slots) slot = 0;
+    w = next;
+    page = next_page;
+  }
+}
+
+template <typename Part, typename T>
+__global__ void __launch_bounds__(kThreads, 2)
+attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
+  extern __shared__ char smem_raw[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.a.seq.batch;
+  char *ring = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+  Shared &sm = *reinterpret_cast<Shared *>(ring + (long long)p.stages * p.chunks * Part::kTile * 128);
+  char *qs = reinterpret_cast<char *>(&sm + 1);
+  float *weights = reinterpret_cast<float *>(qs + p.slots * slot_rows<Part, T>(p) * p.a.cache.dim * (int)sizeof(T));
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (tid == 0) {
+    for (int i = 0; i < p.stages; ++i) {
+      mbar_init(&sm.full[i], 1);
+      mbar_init(&sm.empty[i], kWarps);
+    }
+    mbar_init(&sm.sync, kWarps);
+    mbar_init(&sm.never, 1);
+    fence_mbar_init();
+    sm.flags = 0;
+    sm.dead = 0;
+    sm.start_seq = -1;
+  }
+
+  // this CTA's share of all tiles: each thread counts some sequences' tiles
+  unsigned bad = 0;
+  const int per = (B + kThreads - 1) / kThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) mine += (long long)tiles_of(keys_of(p.a, b, &bad), p.tile) * p.heads;
+  long long upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long x = __shfl_up_sync(~0u, upto, d);
+    if (lane >= d) upto += x;
+  }
+  if (lane == 31) sm.warp_tiles[warp] = upto;
+  __syncthreads();
+  if (bad) atomicOr(&sm.flags, bad);
+  long long total = 0;
+  for (int w = 0; w <= kWarps; ++w) {
+    if (w < warp) upto += sm.warp_tiles[w];
+    total += sm.warp_tiles[w];
+  }
+  // no share is empty: with fewer tiles than CTAs the last CTAs have none
+  const long long shares = total < gridDim.x ? total : gridDim.x;
+  const long long t0 = blockIdx.x < shares ? total * blockIdx.x / shares : total;
+  const long long t1 = blockIdx.x < shares ? total * (blockIdx.x + 1) / shares : total;
+  const bool here = t0 < t1 && t0 >= upto - mine && t0 < upto;
+  if (here || blockIdx.x == 0) {
+    long long at = upto - mine;
+    for (int b = b0; b < b1; ++b) {
+      const long long n = (long long)tiles_of(keys_of(p.a, b, &bad), p.tile) * p.heads;
+      if (blockIdx.x == 0) p.first[b] = at;
+      if (here && t0 >= at && t0 < at + n) {
+        sm.start_seq = b;
+        sm.start_first = at;
+      }
+      at += n;
+    }
+  }
+  if (blockIdx.x == 0 && tid == 0) p.first[B] = total;
+  __syncthreads();
+
+  const int tiles = (int)(t1 - t0);
+  if (tiles > 0) {
+    if (warp == kWarps) {
+      Walk w;
+      w.seq = sm.start_seq;
+      w.keys = keys_of(p.a, w.seq, &bad);
+      w.tiles = tiles_of(w.keys, p.tile);
+      const long long at = t0 - sm.start_first;
+      w.head = (int)(at / w.tiles);
+      w.at = (int)(at - (long long)w.head * w.tiles);
+      produce<Part, T>(p, sm, ring, qs, &kmap, &vmap, w, tiles);
+    } else {
+      consume<Part, T>(p, sm, ring, qs, weights, tiles);
+    }
+  }
+  __syncthreads();
+  if (sm.dead && tid < 32) wait_out(&sm.never);   // copies that nobody waited for
+  if (tid == 0) post_status(reinterpret_cast<unsigned *>(p.a.ws), blockIdx.x, gridDim.x, sm.flags | (sm.dead ? kErrTimeout : 0u));
+}
+
+// What the cuts between the CTAs' shares have parted, one query head per CTA; and the outputs of sequences
+// without a key.
+constexpr int kJoinThreads = 256;
+
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Shape p, int workers) {
+  __shared__ float factor[kMaxWorkers], red[kJoinThreads / 32];
+  __shared__ float4 rows[kJoinThreads / 32][64];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = p.a.cache.dim;
+  const int b = blockIdx.x / p.a.q_heads, h = blockIdx.x - b * p.a.q_heads;
+  const int kv = h / p.group, pass = (h - kv * p.group) / kRows, r = h - kv * p.group - pass * kRows;
+  const long long total = p.first[p.a.seq.batch], tiles = (p.first[b + 1] - p.first[b]) / p.heads;
+  const long long begin = p.first[b] + (kv * p.passes + pass) * tiles;
+  T *out = reinterpret_cast<T *>(p.a.out + b * p.a.out_stride) + (long long)h * D;
+  float *lse = p.a.lse == nullptr ? nullptr : p.a.lse + (long long)b * p.a.q_heads + h;
+  if (tiles == 0) {
+    for (int d = tid; d < D; d += kJoinThreads) out[d] = (T)0.0f;
+    if (lse != nullptr && tid == 0) *lse = -INFINITY;
+    return;
+  }
+  // share w: the tiles total w / workers up to total (w + 1) / workers
+  if (workers > total) workers = (int)total;
+  const int w0 = (int)(((begin + 1) * workers - 1) / total), w1 = (int)(((begin + tiles) * workers - 1) / total);
+  if (w0 == w1) return;   // one CTA wrote the output
+  const long long stride = kStatFloats + p.rows * D;
+  auto part = [&](int w) {   // a CTA's first part unless its share begins before the (sequence, head)
+    return p.parts + (2LL * w + (total * w / workers < begin ? 1 : 0)) * stride;
+  };
+  float all = -INFINITY, sum = 0.0f;
+  for (int w = w0 + tid; w <= w1; w += kJoinThreads) all = fmaxf(all, part(w)[2 * r]);
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) all = fmaxf(all, __shfl_xor_sync(~0u, all, x));
+  if (lane == 0) red[warp] = all;
+  __syncthreads();
+  all = red[0];
+#pragma unroll
+  for (int w = 1; w < kJoinThreads / 32; ++w) all = fmaxf(all, red[w]);
+  for (int w = w0 + tid; w <= w1; w += kJoinThreads) {
+    const float2 x = *reinterpret_cast<const float2 *>(part(w) + 2 * r);
+    const float f = join_factor(x.x, all);
+    factor[w - w0] = f;
+    sum += x.y * f;
+  }
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(~0u, sum, x);
+  __syncthreads();
+  if (lane == 0) red[warp] = sum;
+  float4 acc[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
+#pragma unroll 4
+  for (int w = w0 + warp; w <= w1; w += kJoinThreads / 32) {
+    const float4 *x = reinterpret_cast<const float4 *>(part(w) + kStatFloats + r * D);
+    const float g = factor[w - w0];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (lane + 32 * i < D / 4) {
+        const float4 y = x[lane + 32 * i];
+        acc[i].x = fmaf(y.x, g, acc[i].x);
+        acc[i].y = fmaf(y.y, g, acc[i].y);
+        acc[i].z = fmaf(y.z, g, acc[i].z);
+        acc[i].w = fmaf(y.w, g, acc[i].w);
+      }
+  }
+  rows[warp][lane] = acc[0];
+  rows[warp][lane + 32] = acc[1];
+  __syncthreads();
+  sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kJoinThreads / 32; ++w) sum += red[w];
+  for (int d = tid; d < D; d += kJoinThreads) {
+    float x = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 32; ++w) x += reinterpret_cast<const float *>(rows[w])[d];
+    out[d] = (T)(sum == 0.0f ? 0.0f : x / sum);
+  }
+  if (lse != nullptr && tid == 0) *lse = lse_of(all, sum);
+}
+
+constexpr size_t kHalfSm = 113 * 1024;   // of shared memory, for one of two CTAs
+constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
+
+template <typename Part, typename T>
+cudaError_t launch(Shape p, cudaStream_t s) {
+  const AttendArgs &a = p.a;
+  const CacheLayer &c = a.cache;
+  p.tile = Part::kTile;
+  p.box_log = 0;
+  while ((2 << p.box_log) <= Part::kTile && c.page_size % (2 << p.box_log) == 0) ++p.box_log;
+  p.joined = c.dim * (int)sizeof(T) % 128 == 0;
+  // two CTAs share an SM
+  const size_t half = (size_t)p.chunks * Part::kTile * 128, q_slot = (size_t)slot_rows<Part, T>(p) * c.dim * sizeof(T);
+  const size_t fixed = 1024 + sizeof(Shared) + (sizeof(T) == 4 ? kWarps * 8 * Part::kHeadRows * sizeof(float) : 0);
+  auto smem_of = [&](int stages) { return fixed + stages * half + (stages + 1) / 2 * q_slot; };
+  p.stages = kMaxStages;
+  while (p.stages > 2 && smem_of(p.stages) > kHalfSm) --p.stages;
+  p.slots = (p.stages + 1) / 2;
+  const size_t smem = smem_of(p.stages);
+  CUtensorMap maps[2];
+  const uint64_t row = (uint64_t)c.dim * sizeof(T), head = c.heads > 1 ? (uint64_t)c.head_stride : row,
+                 page = c.num_pages > 1 ? (uint64_t)c.page_stride : row, token = (uint64_t)c.token_stride;
+  const uint64_t inner = 128 / sizeof(T);
+  const uint64_t dims[4] = {(uint64_t)c.dim, (uint64_t)c.page_size, (uint64_t)c.heads, (uint64_t)c.num_pages};
+  const uint64_t dims5[5] = {inner, (uint64_t)c.page_size, (uint64_t)p.chunks, (uint64_t)c.heads, (uint64_t)c.num_pages};
+  const uint64_t strides[3] = {token, head, page}, strides5[4] = {token, 128, head, page};
+  const uint32_t rows = 1u << p.box_log, box[4] = {(uint32_t)inner, rows, 1, 1}, box5[5] = {(uint32_t)inner, rows, (uint32_t)p.chunks, 1, 1};
+  for (int i = 0; i < 2; ++i)
+    if (!encode_rows_map(&maps[i], i ? c.v : c.k, sizeof(T) == 4, p.joined ? 5 : 4, p.joined ? dims5 : dims,
+                         p.joined ? strides5 : strides, p.joined ? box5 : box))
+      return cudaErrorInvalidValue;
+  const void *fn = reinterpret_cast<const void *>(&attend_kernel<Part, T>);
+  cudaError_t e = allow_smem(fn, smem);
+  if (e != cudaSuccess) return e;
+  int workers = sm_count() * 2;
+  workers = workers < kMaxWorkers ? workers : kMaxWorkers;
+  attend_kernel<Part, T><<<workers, kThreads, smem, s>>>(p, maps[0], maps[1]);
+  if ((e = cudaGetLastError()) != cudaSuccess || a.seq.batch == 0) return e;
+  cudaLaunchConfig_t q = {};
+  q.gridDim = dim3((unsigned)(a.seq.batch * (long long)a.q_heads));
+  q.blockDim = dim3(kJoinThreads);
+  q.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // its launch overlaps the kernel it waits for
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  q.attrs = at;
+  q.numAttrs = 1;
+  return cudaLaunchKernelEx(&q, join_kernel<T>, p, workers);
+}
+
+}  // namespace
+}  // namespace last

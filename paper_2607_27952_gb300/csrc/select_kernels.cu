@@ -138,8 +138,8 @@ bool encode_rows_map(CUtensorMap *m, const void *base, bool f32, int rank, const
                      const uint64_t *strides, const uint32_t *box) {
   EncodeTiledFn fn = encode_tiled();
   if (fn == nullptr) return false;
-  cuuint64_t d[4], st[3];
-  cuuint32_t bx[4], es[4];
+  cuuint64_t d[5], st[4];
+  cuuint32_t bx[5], es[5];
   for (int i = 0; i < rank; ++i) {
     if (dims[i] == 0) return false;
     d[i] = dims[i];

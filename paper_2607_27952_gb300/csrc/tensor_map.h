@@ -11,7 +11,7 @@ namespace last {
 bool encode_bf16_map(CUtensorMap *m, const void *base, int rank, const uint64_t *dims,
                      const uint64_t *strides, const uint32_t *box);
 
-// The same for bf16 or fp32 and up to four dimensions; the box's inner extent is 128 bytes.
+// The same for bf16 or fp32 and up to five dimensions; the box's inner extent is 128 bytes.
 bool encode_rows_map(CUtensorMap *m, const void *base, bool f32, int rank, const uint64_t *dims,
                      const uint64_t *strides, const uint32_t *box);
 
