@@ -239,17 +239,29 @@ def _host_ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+def _current_stream() -> int:
+    """The current stream's handle without building a torch.cuda.Stream (3 us on a GB300's host)."""
+    global _current_stream
+    import torch
+    get, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    torch.cuda.current_stream()      # CUDA is up
+    if get is None or device is None:
+        _current_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    else:
+        _current_stream = lambda: get(device())  # noqa: E731
+    return _current_stream()
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def _ws(ws):
     if isinstance(ws, tuple):
         return ws
-    return _ptr(ws), ws.numel() * ws.element_size()
+    return _ptr(ws), ws.nbytes
 
 
 def last_workspace_size(problem: Problem) -> int:
@@ -400,34 +412,33 @@ def last_status_string(st: int) -> str:
 
 # ---- rotary positions and the key-value cache ----
 
-_CODES = {"float32": LAST_DTYPE_F32, "bfloat16": LAST_DTYPE_BF16}
+_CODES, _INT32 = {}, None
 
 
 def _code(dtype) -> int:
-    name = str(dtype).rpartition(".")[2]
-    if name not in _CODES:
-        raise ValueError(f"liblast takes float32 and bfloat16 tensors, not {name}")
-    return _CODES[name]
-
-
-def _on_device(t, name: str, shape=None):
-    if not t.is_cuda:
-        raise ValueError(f"{name}: liblast takes device tensors")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    return t
-
-
-def _int32(t, name: str, shape=None):
-    """A device int32 tensor whose last dimension is contiguous."""
-    _on_device(t, name, shape)
-    if _dtype_name(t) != "int32" or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{name}: int32 with a contiguous last dimension expected")
-    return t
+    if not _CODES:
+        import torch
+        _CODES.update({torch.float32: LAST_DTYPE_F32, torch.bfloat16: LAST_DTYPE_BF16})
+    if dtype not in _CODES:
+        raise ValueError(f"liblast takes float32 and bfloat16 tensors, not {dtype}")
+    return _CODES[dtype]
 
 
 def _dtype_name(t) -> str:
     return str(t.dtype).rpartition(".")[2]
+
+
+def _int32(t, name: str, shape=None):
+    """A device int32 tensor whose last dimension is contiguous."""
+    global _INT32
+    if _INT32 is None:
+        import torch
+        _INT32 = torch.int32
+    if t.dtype != _INT32 or not t.is_cuda or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise ValueError(f"{name}: a device int32 tensor with a contiguous last dimension expected")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return t
 
 
 class Rope:
@@ -464,9 +475,8 @@ class Cache:
     tokens outside heads, transposed) do as well, of both tensors alike."""
 
     def __init__(self, k, v):
-        for t, name in ((_on_device(k, "k"), "k"), (_on_device(v, "v", k.shape), "v")):
-            if t.dim() != 5:
-                raise ValueError(f"{name}: [layers][pages][kv_heads][page_size][head_dim] expected")
+        if k.dim() != 5 or v.shape != k.shape or not k.is_cuda or not v.is_cuda:
+            raise ValueError("k and v: device tensors [layers][pages][kv_heads][page_size][head_dim] expected")
         if k.dtype != v.dtype or k.stride() != v.stride() or (k.shape[4] > 1 and k.stride(4) != 1):
             raise ValueError("k and v must have one dtype and the same strides, head_dim contiguous")
         self.k, self.v, self.dtype = k, v, k.dtype
@@ -497,17 +507,15 @@ class Sequences:
 
 def _heads(x, out, dtype, dim, name):
     """last_heads of a [tokens][heads][dim] tensor and, optionally, its output."""
-    if not x.is_cuda or x.dim() != 3 or x.dtype != dtype or x.shape[2] != dim:
-        raise ValueError(f"{name}: a device tensor [tokens][heads][{dim}] of {dtype} expected")
-    st, sh, sd = x.stride()
-    if sd != 1 and dim > 1:
-        raise ValueError(f"{name}: the last dimension must be contiguous")
+    shape, strides = x.shape, x.stride()
+    if len(shape) != 3 or shape[2] != dim or x.dtype != dtype or not x.is_cuda or (strides[2] != 1 and dim > 1):
+        raise ValueError(f"{name}: a device tensor [tokens][heads][{dim}] of {dtype}, the last dimension contiguous, expected")
     if out is None:
-        return _Heads(x.data_ptr(), None, x.shape[1], st, sh, 0, 0)
-    if not out.is_cuda or out.shape != x.shape or out.dtype != dtype or (out.stride(2) != 1 and dim > 1):
+        return _Heads(x.data_ptr(), None, shape[1], strides[0], strides[1], 0, 0)
+    outs = out.stride()
+    if out.shape != shape or out.dtype != dtype or not out.is_cuda or (outs[2] != 1 and dim > 1):
         raise ValueError(f"{name}_out: a tensor like {name} expected")
-    ot, oh, _ = out.stride()
-    return _Heads(x.data_ptr(), out.data_ptr(), x.shape[1], st, sh, ot, oh)
+    return _Heads(x.data_ptr(), out.data_ptr(), shape[1], strides[0], strides[1], outs[0], outs[1])
 
 
 def _positions(positions, num_axes, tokens):
@@ -520,15 +528,16 @@ def _positions(positions, num_axes, tokens):
 
 
 def _rope(call, rope: Rope, positions, q, q_out, k, k_out, stream):
-    t, _, d = q.shape
+    shape, dtype = q.shape, q.dtype
+    t, d = shape[0], shape[-1]
     if (k is None) != (k_out is None):
         raise ValueError("k and k_out go together")
     if k is not None and k.shape[0] != t:
         raise ValueError("q and k must have the same tokens")
-    qh = _heads(q, q_out, q.dtype, d, "q")
-    kh = None if k is None else ctypes.byref(_heads(k, k_out, q.dtype, d, "k"))
+    qh = _heads(q, q_out, dtype, d, "q")
+    kh = None if k is None else ctypes.byref(_heads(k, k_out, dtype, d, "k"))
     pos, stride = _positions(positions, rope.num_axes, t)
-    _check(call(rope.ref, _code(q.dtype), t, d, pos, stride, ctypes.byref(qh), kh, _stream(stream)))
+    _check(call(rope.ref, _code(dtype), t, d, pos, stride, ctypes.byref(qh), kh, _stream(stream)))
 
 
 def last_rope(rope: Rope, positions, q, q_out, k=None, k_out=None, stream=None):
@@ -559,20 +568,17 @@ def last_cache_append(cache: Cache, layer: int, seqs: Sequences, k, v, ws, cu_ne
                       positions=None, q=None, q_out=None, stream=None):
     """New tokens' k and v [tokens][kv_heads][head_dim] written behind the sequences' cached ones (seqs.lens
     counts them already); with a rope, k is rotated on the way and q into q_out."""
-    t = k.shape[0]
+    dtype, d, t = cache.dtype, cache.head_dim, k.shape[0]
     if v.shape[0] != t or (q is not None and q.shape[0] != t):
         raise ValueError("q, k and v must have the same tokens")
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
-    if cu_new is not None:
-        _int32(cu_new, "cu_new", (seqs.batch + 1,))
-    d = cache.head_dim
-    kh, vh = _heads(k, None, cache.dtype, d, "k"), _heads(v, None, cache.dtype, d, "v")
-    qh = None if q is None else ctypes.byref(_heads(q, q_out, cache.dtype, d, "q"))
+    kh, vh = _heads(k, None, dtype, d, "k"), _heads(v, None, dtype, d, "v")
+    qh = None if q is None else ctypes.byref(_heads(q, q_out, dtype, d, "q"))
     pos, stride = (None, 0) if rope is None else _positions(positions, rope.num_axes, t)
     p, n = _ws(ws)
     _check(load_library().last_cache_append(
-        cache.ref, layer, seqs.ref, t, None if cu_new is None else cu_new.data_ptr(),
+        cache.ref, layer, seqs.ref, t, None if cu_new is None else _int32(cu_new, "cu_new", (seqs.batch + 1,)).data_ptr(),
         None if rope is None else rope.ref, pos, stride, qh, ctypes.byref(kh), ctypes.byref(vh), p, n, _stream(stream)))
 
 
@@ -580,49 +586,46 @@ def last_cache_attention(cache: Cache, layer: int, seqs: Sequences, q, out, ws, 
                          stream=None):
     """out = attention of q [batch][q_heads][head_dim] over the sequences' cached keys of one layer; lse
     [batch][q_heads] fp32 receives the log of the softmax's denominator."""
-    if q.dim() != 3 or q.shape[0] != seqs.batch or q.shape[2] != cache.head_dim or out.shape != q.shape:
-        raise ValueError(f"q and out: [{seqs.batch}][q_heads][{cache.head_dim}] expected")
-    heads = q.shape[1]
-    for t, name in ((q, "q"), (out, "out")):
-        if not t.is_cuda or t.dtype != cache.dtype or t.stride(2) != 1 or (heads > 1 and t.stride(1) != cache.head_dim):
-            raise ValueError(f"{name}: a device tensor of the cache's dtype, [q_heads][head_dim] contiguous, expected")
-    if lse is not None and (not lse.is_cuda or _dtype_name(lse) != "float32" or tuple(lse.shape) != (seqs.batch, heads)
-                            or not lse.is_contiguous()):
+    shape, d, dtype = q.shape, cache.head_dim, cache.dtype
+    if len(shape) != 3 or shape[0] != seqs.batch or shape[2] != d or out.shape != shape:
+        raise ValueError(f"q and out: [{seqs.batch}][q_heads][{d}] expected")
+    heads, qs, os_ = shape[1], q.stride(), out.stride()
+    if (q.dtype != dtype or out.dtype != dtype or not q.is_cuda or not out.is_cuda or qs[2] != 1 or os_[2] != 1
+            or (heads > 1 and (qs[1] != d or os_[1] != d))):
+        raise ValueError("q and out: device tensors of the cache's dtype, [q_heads][head_dim] contiguous, expected")
+    if lse is not None and (lse.shape != shape[:2] or not lse.is_contiguous() or not lse.is_cuda
+                            or _dtype_name(lse) != "float32"):
         raise ValueError("lse: a contiguous device float32 tensor [batch][q_heads] expected")
     p, n = _ws(ws)
     _check(load_library().last_cache_attention(
-        cache.ref, layer, seqs.ref, heads, float(softmax_scale), q.data_ptr(), q.stride(0), out.data_ptr(),
-        out.stride(0), None if lse is None else lse.data_ptr(), p, n, _stream(stream)))
+        cache.ref, layer, seqs.ref, heads, softmax_scale, q.data_ptr(), qs[0], out.data_ptr(), os_[0],
+        None if lse is None else lse.data_ptr(), p, n, _stream(stream)))
 
 
 def last_cache_copy(cache: Cache, src, dst, ws, stream=None):
     """Pages src[i] copied to pages dst[i] (device int32), every layer, K and V."""
     n = src.shape[0]
-    _int32(src, "src", (n,))
-    _int32(dst, "dst", (n,))
     p, nb = _ws(ws)
-    _check(load_library().last_cache_copy(cache.ref, n, src.data_ptr(), dst.data_ptr(), p, nb, _stream(stream)))
+    _check(load_library().last_cache_copy(cache.ref, n, _int32(src, "src", (n,)).data_ptr(),
+                                          _int32(dst, "dst", (n,)).data_ptr(), p, nb, _stream(stream)))
 
 
 def last_cache_compact(cache: Cache, seqs: Sequences, dst_table, cu_keep, idx, lens_out, ws, span_begin=None,
                        span_len=None, stream=None):
     """The sequences' tokens outside their spans and the spans' tokens idx (as last_select writes them),
     in order, copied to the pages of dst_table [batch][max_pages]; lens_out [batch] receives the new lengths."""
-    b = seqs.batch
-    if dst_table.dim() != 2 or dst_table.shape[0] != b or idx.dim() != 1:
+    b, shape = seqs.batch, dst_table.shape
+    if len(shape) != 2 or shape[0] != b or idx.dim() != 1:
         raise ValueError("dst_table: [batch][max_pages], idx: one dimension expected")
-    _int32(dst_table, "dst_table")
-    _int32(cu_keep, "cu_keep", (b + 1,))
-    _int32(idx, "idx")
-    _int32(lens_out, "lens_out", (b,))
-    for t, name in ((span_begin, "span_begin"), (span_len, "span_len")):
-        if t is not None:
-            _int32(t, name, (b,))
+
+    def per_sequence(t, name):
+        return None if t is None else _int32(t, name, (b,)).data_ptr()
     p, n = _ws(ws)
     _check(load_library().last_cache_compact(
-        cache.ref, seqs.ref, dst_table.data_ptr(), dst_table.shape[1], dst_table.stride(0),
-        None if span_begin is None else span_begin.data_ptr(), None if span_len is None else span_len.data_ptr(),
-        cu_keep.data_ptr(), idx.data_ptr(), idx.shape[0], lens_out.data_ptr(), p, n, _stream(stream)))
+        cache.ref, seqs.ref, _int32(dst_table, "dst_table").data_ptr(), shape[1], dst_table.stride(0),
+        per_sequence(span_begin, "span_begin"), per_sequence(span_len, "span_len"),
+        _int32(cu_keep, "cu_keep", (b + 1,)).data_ptr(), _int32(idx, "idx").data_ptr(), idx.shape[0],
+        per_sequence(lens_out, "lens_out"), p, n, _stream(stream)))
 
 
 class PagePool:

@@ -64,12 +64,13 @@ unsigned long long turn_of(float f) {
   const unsigned long long w[3] = {(unsigned long long)lo, (unsigned long long)hi, (unsigned long long)(hi >> 64)};
   const int shift = 64 - e - 1;                       // one bit more, to round
   if (shift >= 192) return 0;
-  unsigned long long out = 0;
-  for (int i = 63; i >= 0; --i) {                     // bits shift + 1 + i of the product
-    const int at = shift + 1 + i;
-    if (at < 192 && (w[at / 64] >> (at % 64) & 1)) out |= 1ull << i;
-  }
-  return out + (w[shift / 64] >> (shift % 64) & 1);
+  auto bits = [&](int at) -> unsigned long long {     // 64 bits of the product from bit `at` on
+    const int word = at / 64, off = at % 64;
+    if (word >= 3) return 0;
+    const unsigned long long above = word + 1 < 3 ? w[word + 1] : 0;
+    return off == 0 ? w[word] : w[word] >> off | above << (64 - off);
+  };
+  return bits(shift + 1) + (bits(shift) & 1);
 }
 
 last_status make_rotary(const last_rotary *r, int head_dim, RotaryTable *t) {
@@ -128,8 +129,8 @@ last_status check_cache(const last_cache *c) {
   const int e = elem_bytes(c->dtype);
   if (c->head_dim * (long long)e % 16 != 0 || c->head_dim > 256)
     return fail(LAST_ERR_UNSUPPORTED, "head_dim * elem_bytes must be a multiple of 16 and head_dim <= 256");
-  if (c->page_size > (1 << 20) || c->num_kv_heads > 4096)
-    return fail(LAST_ERR_UNSUPPORTED, "page_size must be at most 2^20, num_kv_heads at most 4096");
+  if (c->page_size > (1 << 20) || c->num_kv_heads > 4096 || c->num_layers > 4096)
+    return fail(LAST_ERR_UNSUPPORTED, "page_size must be at most 2^20, num_kv_heads and num_layers at most 4096");
   if (c->k == nullptr || c->v == nullptr) return invalid("k and v are required");
   if (!aligned(c->k, 16) || !aligned(c->v, 16)) return invalid("k and v must be 16-byte aligned");
   const int64_t strides[4] = {c->layer_stride, c->page_stride, c->head_stride, c->token_stride};

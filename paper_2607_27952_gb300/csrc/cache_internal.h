@@ -78,6 +78,7 @@ struct PagesArgs {   // copy and compact: every layer
   char *k, *v;
   long long layer_stride, page_stride, head_stride, token_stride;   // bytes
   int layers, num_pages, page_size, heads, row_bytes;
+  bool packed;   // copy: a page's rows follow each other without a gap
   unsigned *status;
 };
 

@@ -8,6 +8,12 @@ namespace last {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kBatch = 4;   // 16-byte pieces of a thread in flight
+
+// x / n; m = ceil(2^32 / n) where x n < 2^32 for every x, else 0.
+__device__ __forceinline__ int quotient(int x, int n, uint32_t m) {
+  return n == 1 ? x : m != 0 ? (int)__umulhi((uint32_t)x, m) : x / n;
+}
 
 // One page of one layer of K or V per step.
 __global__ void __launch_bounds__(kThreads) copy_kernel(const __grid_constant__ PagesArgs p, int n, const int32_t *src,
@@ -26,62 +32,102 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(const __grid_constant__ 
     char *base = (lk & 1 ? p.v : p.k) + (lk >> 1) * p.layer_stride;
     const char *x = base + from * p.page_stride;
     char *y = base + to * p.page_stride;
-    for (int e = threadIdx.x; e < per_page; e += kThreads) {
+    auto at = [&](int e) {
+      if (p.packed) return e * 16LL;
       const int r = e / vec, h = r / p.page_size;
-      const long long at = h * p.head_stride + (r - h * p.page_size) * p.token_stride + (e - r * vec) * 16;
-      *reinterpret_cast<uint4 *>(y + at) = *reinterpret_cast<const uint4 *>(x + at);
+      return h * p.head_stride + (r - h * p.page_size) * p.token_stride + (e - r * vec) * 16;
+    };
+    for (int e = threadIdx.x; e < per_page; e += kThreads * kBatch) {
+      uint4 v[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        if (e + u * kThreads < per_page) v[u] = *reinterpret_cast<const uint4 *>(x + at(e + u * kThreads));
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        if (e + u * kThreads < per_page) *reinterpret_cast<uint4 *>(y + at(e + u * kThreads)) = v[u];
     }
   }
   if (threadIdx.x == 0) post_status(p.status, blockIdx.x, gridDim.x, flags);
 }
 
-// One destination page of one layer of K or V per step.
-__global__ void __launch_bounds__(kThreads) compact_kernel(const __grid_constant__ CompactArgs a) {
+// A warp takes a token of a shortened sequence (or, of few tokens, a part of its rows): its place and its
+// source are looked up once for all layers and heads.  The tokens of 32 sequences at a time are counted by
+// the lanes, every warp alike, and dealt out in turn.
+__global__ void __launch_bounds__(kThreads) compact_kernel(const __grid_constant__ CompactArgs a, int rows, uint32_t vec_m,
+                                                           uint32_t heads_m) {
   const PagesArgs &p = a.p;
+  const int lane = threadIdx.x & 31, ps = p.page_size, vec = p.row_bytes / 16, items = rows * vec;
+  const int warps = gridDim.x * (kThreads / 32), me = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   unsigned flags = 0;
-  const int vec = p.row_bytes / 16, ps = p.page_size;
-  const long long items = (long long)a.seq.batch * a.dst_max_pages * p.layers * 2;
-  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-    const int lk = (int)(it % (2 * p.layers));
-    const long long bp = it / (2 * p.layers);
-    const int b = (int)(bp / a.dst_max_pages), page = (int)(bp - (long long)b * a.dst_max_pages);
-    const int len = a.seq.lens[b], k0 = a.cu_keep[b], k1 = a.cu_keep[b + 1];
-    const int first = a.span_begin ? a.span_begin[b] : 0, span = a.span_len ? a.span_len[b] : len;
-    const bool ok = len >= 0 && first >= 0 && span >= 0 && first <= len && span <= len - first && k0 >= 0 && k0 <= k1 &&
-                    k1 <= a.num_idx && len <= (long long)a.seq.max_pages * ps &&
-                    (long long)len - span + (k1 - k0) <= (long long)a.dst_max_pages * ps;
-    if (!ok) {
-      flags |= kErrCacheIndex;
-      continue;
+  long long dealt = 0;   // units of the sequences before
+  for (int b0 = 0; b0 < a.seq.batch; b0 += 32) {
+    const int mine = b0 + lane;
+    int len = 0, first = 0, span = 0, kept = 0, k0 = 0, total = 0;
+    if (mine < a.seq.batch) {
+      len = a.seq.lens[mine];
+      k0 = a.cu_keep[mine];
+      const int k1 = a.cu_keep[mine + 1];
+      first = a.span_begin ? a.span_begin[mine] : 0;
+      span = a.span_len ? a.span_len[mine] : len;
+      const bool ok = len >= 0 && first >= 0 && span >= 0 && first <= len && span <= len - first && k0 >= 0 && k0 <= k1 &&
+                      k1 <= a.num_idx && len <= (long long)a.seq.max_pages * ps &&
+                      (long long)len - span + (k1 - k0) <= (long long)a.dst_max_pages * ps;
+      kept = k1 - k0;
+      total = ok ? len - span + kept : 0;
+      if (!ok) flags = kErrCacheIndex;
+      else if (me == 0) a.lens_out[mine] = total;
     }
-    const int kept = k1 - k0, total = len - span + kept;
-    if (page == 0 && lk == 0 && threadIdx.x == 0) a.lens_out[b] = total;
-    const int rows = min(ps, total - page * ps);
-    if (rows <= 0) continue;
-    const int to = a.dst_table[b * a.dst_stride + page];
-    if (to < 0 || to >= p.num_pages) {
-      flags |= kErrCacheIndex;
-      continue;
+    long long upto = total;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long x = __shfl_up_sync(~0u, upto, d);
+      if (lane >= d) upto += x;
     }
-    char *base = (lk & 1 ? p.v : p.k) + (lk >> 1) * p.layer_stride;
-    for (int e = threadIdx.x; e < rows * p.heads * vec; e += kThreads) {
-      const int r = e / vec, h = r / rows, j = page * ps + (r - h * rows);
+    const long long tokens = __shfl_sync(~0u, upto, 31);
+    if (tokens == 0) continue;
+    // of few tokens, parts of no less than 4 pieces a lane
+    const int most = items / (32 * kBatch);
+    int parts = tokens < warps ? (int)(warps / tokens) : 1;
+    parts = parts > most ? (most > 1 ? most : 1) : parts;
+    const long long units = tokens * parts;
+    for (long long u = ((long long)me - dealt % warps + warps) % warps; u < units; u += warps) {
+      const long long tok = parts == 1 ? u : u / parts;
+      const int part = (int)(u - tok * parts);
+      const int own = __popc(__ballot_sync(~0u, upto <= tok));   // the sequence whose tokens hold it
+      const int b = b0 + own, j = (int)(tok - (__shfl_sync(~0u, upto, own) - __shfl_sync(~0u, total, own)));
+      const int f = __shfl_sync(~0u, first, own), sp = __shfl_sync(~0u, span, own), kp = __shfl_sync(~0u, kept, own);
       int from = j;
-      if (j >= first + kept) from = j + span - kept;
-      else if (j >= first) {
-        const int i = a.idx[k0 + j - first];
-        from = i >= 0 && i < span ? first + i : -1;
+      if (j >= f + kp) from = j + sp - kp;
+      else if (j >= f) {
+        const int i = a.idx[__shfl_sync(~0u, k0, own) + j - f];
+        from = i >= 0 && i < sp ? f + i : -1;
       }
-      const int sp = from >= 0 ? a.seq.table[b * a.seq.table_stride + from / ps] : -1;
-      if (sp < 0 || sp >= p.num_pages) {
-        flags |= kErrCacheIndex;
+      const int to_page = a.dst_table[b * a.dst_stride + j / ps];
+      const int page = from >= 0 ? a.seq.table[b * a.seq.table_stride + from / ps] : -1;
+      if (page < 0 || page >= p.num_pages || to_page < 0 || to_page >= p.num_pages) {
+        flags = kErrCacheIndex;
         continue;
       }
-      const long long x = sp * p.page_stride + (from % ps) * p.token_stride, y = to * p.page_stride + (j % ps) * p.token_stride;
+      const long long x = page * p.page_stride + (from % ps) * p.token_stride;
+      const long long y = to_page * p.page_stride + (j % ps) * p.token_stride;
       if (x == y) continue;
-      const long long in = h * p.head_stride + (e - r * vec) * 16;
-      *reinterpret_cast<uint4 *>(base + y + in) = *reinterpret_cast<const uint4 *>(base + x + in);
+      const int i0 = parts == 1 ? 0 : (int)((long long)items * part / parts);
+      const int i1 = parts == 1 ? items : (int)((long long)items * (part + 1) / parts);
+      auto at = [&](int i) {   // piece i of the token: K or V, layer, head, 16 bytes
+        const int r = quotient(i, vec, vec_m), lk = quotient(r, p.heads, heads_m);
+        return (lk & 1 ? p.v : p.k) + (lk >> 1) * p.layer_stride + (r - lk * p.heads) * p.head_stride + (i - r * vec) * 16;
+      };
+      for (int i = i0 + lane; i < i1; i += 32 * kBatch) {
+        uint4 v[kBatch];
+#pragma unroll
+        for (int n = 0; n < kBatch; ++n)
+          if (i + n * 32 < i1) v[n] = *reinterpret_cast<const uint4 *>(at(i + n * 32) + x);
+#pragma unroll
+        for (int n = 0; n < kBatch; ++n)
+          if (i + n * 32 < i1) *reinterpret_cast<uint4 *>(at(i + n * 32) + y) = v[n];
+      }
     }
+    dealt += units;
   }
   flags = __syncthreads_or((int)flags);
   if (threadIdx.x == 0) post_status(p.status, blockIdx.x, gridDim.x, flags ? kErrCacheIndex : 0u);
@@ -94,13 +140,23 @@ int grid_of(long long items) {
 
 }  // namespace
 
-cudaError_t launch_page_copy(const PagesArgs &p, int n, const int32_t *src, const int32_t *dst, cudaStream_t s) {
+cudaError_t launch_page_copy(const PagesArgs &args, int n, const int32_t *src, const int32_t *dst, cudaStream_t s) {
+  PagesArgs p = args;
+  // a page's rows one after the other, in either order
+  const long long row = p.row_bytes, ps = p.page_size;
+  p.packed = (p.token_stride == row && (p.heads == 1 || p.head_stride == row * ps)) ||
+             (p.token_stride == row * p.heads && (p.heads == 1 || p.head_stride == row));
   copy_kernel<<<grid_of((long long)n * p.layers * 2), kThreads, 0, s>>>(p, n, src, dst);
   return cudaGetLastError();
 }
 
 cudaError_t launch_compact(const CompactArgs &a, cudaStream_t s) {
-  compact_kernel<<<grid_of((long long)a.seq.batch * a.dst_max_pages * a.p.layers * 2), kThreads, 0, s>>>(a);
+  const int rows = a.p.layers * 2 * a.p.heads, vec = a.p.row_bytes / 16;
+  auto magic = [](long long most, int n) {
+    return most * n < 1LL << 32 ? (uint32_t)(((1ull << 32) + (unsigned)n - 1) / (unsigned)n) : 0u;
+  };
+  const long long most = (long long)a.seq.batch * a.dst_max_pages * a.p.page_size * rows * vec / (32 * kBatch);   // units
+  compact_kernel<<<grid_of(most / (kThreads / 32) + 1), kThreads, 0, s>>>(a, rows, magic((long long)rows * vec, vec), magic(rows, a.p.heads));
   return cudaGetLastError();
 }
 

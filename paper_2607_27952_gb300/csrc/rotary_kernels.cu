@@ -17,8 +17,7 @@ namespace last {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBatch = 4;        // loads a thread has in flight
-constexpr int kMaxTokens = 16;   // per CTA
+constexpr int kBatch = 4;        // items of a lane in flight
 
 template <int BYTES> struct Pack;
 template <> struct Pack<16> { using type = uint4; };
@@ -33,10 +32,18 @@ template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float v) { return __float2bfloat16_rn(v); }
 
-// x / n for 0 <= x < 2^17, 1 <= n <= 2^14, with m = ceil(2^32 / n).
+// x / n for x n < 2^32, with m = ceil(2^32 / n).
 __device__ __forceinline__ int quotient(int x, int n, uint32_t m) {
   return n == 1 ? x : (int)__umulhi((uint32_t)x, m);
 }
+uint32_t magic(int n) { return (uint32_t)(((1ull << 32) + (unsigned)n - 1) / (unsigned)(n > 0 ? n : 1)); }
+
+struct Split {       // of a token's work
+  int parts;         // warps per token
+  int rounds;        // of 32 items (pairs of VEC-element pieces) per part
+  int chunks, tail;  // items and single pieces behind them of a row
+  uint32_t chunks_m, tail_m;
+};
 
 // Byte offset of new token t's slot in its cache layer; -1 (and a flag) if it has none.
 __device__ long long slot_of(const RotaryArgs &p, int t, unsigned *bad) {
@@ -62,139 +69,156 @@ __device__ long long slot_of(const RotaryArgs &p, int t, unsigned *bad) {
   return -1;
 }
 
-// Heads of a few tokens per CTA: the angles' sines and cosines go to shared memory while
-// the first loads are under way, then every thread turns VEC pairs of one row at a time.
+// A warp takes a token (or, of few tokens, a part of its rows) at a time.  Its lanes turn VEC pairs of a row
+// in each round and load those of the fourth round from there, of the next token if need be, so that loads
+// are always under way; the sines and cosines of a token lie in the warp's own shared memory, and warps do
+// not wait for each other.  Rows are q's, k's and, for a cache, v's heads, which are copied.
 template <typename T, int VEC, bool ADJACENT, bool APPEND>
-__global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ RotaryArgs p, int per_cta, uint32_t rows_m,
-                                                          uint32_t kv_m, bool wide) {
+__global__ void __launch_bounds__(kThreads, 3) rotary_kernel(const __grid_constant__ RotaryArgs p, const Split w) {
   using V = typename Pack<VEC * (int)sizeof(T)>::type;
-  __shared__ float2 turn[kMaxTokens * kMaxRotPairs];   // (cos, sin) [token][pair]
-  __shared__ long long slot[kMaxTokens];
+  constexpr int kSets = kMaxRotPairs / 32;
+  __shared__ float2 tables[kThreads / 32][kMaxRotPairs];   // (cos, sin) of pair c VEC + e at [e chunks + c]
   __shared__ unsigned flags;
-  const int tid = threadIdx.x, half = p.rot.half, heads = p.q.heads + p.k.heads;
-  if (APPEND && tid == 0) flags = 0;
-  const int chunks = half / VEC;   // of a row, side by side in a warp
-  const int c = chunks > 0 ? tid % chunks : 0, pass = chunks > 0 ? kThreads / chunks : 1;
-  const int first = chunks > 0 ? tid / chunks : 0;
-  const int ia = (ADJACENT ? 2 * c : c) * VEC, ib = ADJACENT ? ia + VEC : half + ia;   // elements
-  const int groups = (p.tokens + per_cta - 1) / per_cta;
-
-  for (int g = blockIdx.x; g < groups; g += gridDim.x) {
-    const int t0 = g * per_cta, nt = min(per_cta, p.tokens - t0);
-    // rows: the rotated heads of the tokens, token-major
-    const int rows = first < pass && chunks > 0 ? nt * heads : 0;
-    auto row_in = [&](int t, int h) -> const char * {
-      return h < p.q.heads ? p.q.in + (t0 + t) * p.q.in_token + h * p.q.in_head
-                           : p.k.in + (t0 + t) * p.k.in_token + (h - p.q.heads) * p.k.in_head;
-    };
-    V a[kBatch], b[kBatch];
-    auto load = [&](int at) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, half = p.rot.half, warps = gridDim.x * (kThreads / 32);
+  const int turned = p.q.heads + p.k.heads, rows = turned + (APPEND ? p.v.heads : 0), items = rows * w.chunks;
+  float2 *turn = tables[warp];
+  if (APPEND) {
+    if (threadIdx.x == 0) flags = 0;
+    __syncthreads();
+  }
+  auto share = [&](int n, int part, int &i0, int &i1) {
+    i0 = w.parts == 1 ? 0 : (int)((long long)n * part / w.parts);
+    i1 = w.parts == 1 ? n : (int)((long long)n * (part + 1) / w.parts);
+  };
+  auto row_in = [&](int t, int h) -> const char * {
+    if (h < p.q.heads) return p.q.in + t * p.q.in_token + h * p.q.in_head;
+    if (!APPEND || h < turned) return p.k.in + t * p.k.in_token + (h - p.q.heads) * p.k.in_head;
+    return p.v.in + t * p.v.in_token + (h - turned) * p.v.in_head;
+  };
+  // a lane's frequencies, read once: lanes reading parameters at different places do so one by one
+  unsigned long long freq[kSets];
+  uint32_t axes = 0;
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int r = at + u * pass;
-        if (r < rows) {
-          const int t = quotient(r, heads, rows_m);
-          const char *x = row_in(t, r - t * heads);
-          a[u] = *reinterpret_cast<const V *>(x + ia * sizeof(T));
-          b[u] = *reinterpret_cast<const V *>(x + ib * sizeof(T));
-        }
-      }
-    };
-    load(first);
+  for (int n = 0; n < kSets; ++n) {
+    const int i = lane + 32 * n;
+    freq[n] = i < half ? p.rot.turn[i] : 0;
+    axes |= i < half ? (uint32_t)p.rot.axis[i] << (8 * n) : 0u;
+  }
 
-    __syncthreads();   // the previous tokens' angles and slots are read, flags is zero
-    if (half > 0) {
-      const int lanes = kThreads / half, i = tid % half;
-      if (tid / half < lanes) {
-        const unsigned long long f = p.rot.turn[i];
-        const int32_t *pos = p.positions + p.rot.axis[i] * p.axis_stride + t0;
-        for (int t = tid / half; t < nt; t += lanes) {
-          const long long phase = (long long)((unsigned long long)(long long)pos[t] * f);
+  const int units = p.tokens * w.parts;
+  int load_unit = blockIdx.x * (kThreads / 32) + warp, load_round = 0;
+  V a[kBatch], b[kBatch];
+  auto load = [&](int n) {   // the next round's items
+    if (load_unit >= units) return;
+    const int t = w.parts == 1 ? load_unit : load_unit / w.parts;
+    int i0, i1;
+    share(items, load_unit - t * w.parts, i0, i1);
+    const int i = i0 + load_round * 32 + lane;
+    if (i < i1) {
+      const int h = quotient(i, w.chunks, w.chunks_m), c = i - h * w.chunks;
+      const T *x = reinterpret_cast<const T *>(row_in(t, h)) + (ADJACENT ? 2 * c : c) * VEC;
+      a[n] = *reinterpret_cast<const V *>(x);
+      b[n] = *reinterpret_cast<const V *>(x + (ADJACENT ? VEC : half));
+    }
+    if (++load_round == w.rounds) {
+      load_round = 0;
+      load_unit += warps;
+    }
+  };
+#pragma unroll
+  for (int n = 0; n < kBatch; ++n) load(n);
+
+  int unit = blockIdx.x * (kThreads / 32) + warp, round = 0, t = 0, i0 = 0, i1 = 0;
+  long long slot = 0;
+  while (unit < units) {
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) {
+      if (unit >= units) break;
+      if (round == 0) {   // a new token
+        t = w.parts == 1 ? unit : unit / w.parts;
+        share(items, unit - t * w.parts, i0, i1);
+        __syncwarp();
+#pragma unroll
+        for (int m = 0; m < kSets; ++m) {
+          const int i = lane + 32 * m;
+          if (i >= half) break;
+          const long long at = p.positions[(long long)(axes >> (8 * m) & 255) * p.axis_stride + t];
+          const long long phase = (long long)((unsigned long long)at * freq[m]);
           float sn, cs;
           sincospif((float)phase * 0x1p-63f, &sn, &cs);   // phase: 2^-64 turns
-          turn[t * half + i] = make_float2(cs, p.backward ? -sn : sn);
+          turn[(i % VEC) * w.chunks + i / VEC] = make_float2(cs, p.backward ? -sn : sn);
         }
+        if (APPEND) {
+          unsigned bad = 0;
+          slot = slot_of(p, t, &bad);
+          if (bad && lane == 0) atomicOr(&flags, bad);
+        }
+        __syncwarp();
       }
-    }
-    if (APPEND && tid < nt) {
-      unsigned bad = 0;
-      slot[tid] = slot_of(p, t0 + tid, &bad);
-      if (bad) atomicOr(&flags, bad);
-    }
-    __syncthreads();
-
-    auto row_out = [&](int t, int h) -> char * {
-      if (h < p.q.heads) return p.q.out + (t0 + t) * p.q.out_token + h * p.q.out_head;
-      if (!APPEND) return p.k.out + (t0 + t) * p.k.out_token + (h - p.q.heads) * p.k.out_head;
-      return slot[t] < 0 ? nullptr : p.cache.k + slot[t] + (h - p.q.heads) * p.cache.head_stride;
-    };
-    for (int base = first; base < rows; base += pass * kBatch) {
-      if (base != first) load(base);
+      auto row_out = [&](int h) -> char * {
+        if (h < p.q.heads) return p.q.out + t * p.q.out_token + h * p.q.out_head;
+        if (!APPEND) return p.k.out + t * p.k.out_token + (h - p.q.heads) * p.k.out_head;
+        if (slot < 0) return nullptr;
+        return h < turned ? p.cache.k + slot + (h - p.q.heads) * p.cache.head_stride
+                          : p.cache.v + slot + (h - turned) * p.cache.head_stride;
+      };
+      const int i = i0 + round * 32 + lane;
+      if (i < i1) {
+        const int h = quotient(i, w.chunks, w.chunks_m), c = i - h * w.chunks;
+        char *y = row_out(h);
+        V va = a[n], vb = b[n];
+        if (!APPEND || h < turned) {
+          T ea[VEC], eb[VEC];
+          memcpy(ea, &va, sizeof(V));
+          memcpy(eb, &vb, sizeof(V));
+          if (!ADJACENT || VEC == 1) {
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int r = base + u * pass;
-        if (r >= rows) break;
-        const int t = quotient(r, heads, rows_m);
-        char *y = row_out(t, r - t * heads);
-        T ea[VEC], eb[VEC];
-        memcpy(ea, &a[u], sizeof(V));
-        memcpy(eb, &b[u], sizeof(V));
-        const float2 *cs = turn + t * half + c * VEC;
-        if (!ADJACENT || VEC == 1) {
+            for (int e = 0; e < VEC; ++e) {
+              const float2 cs = turn[e * w.chunks + c];
+              const float x0 = to_f32(ea[e]), x1 = to_f32(eb[e]);
+              ea[e] = from_f32<T>(x0 * cs.x - x1 * cs.y);
+              eb[e] = from_f32<T>(x0 * cs.y + x1 * cs.x);
+            }
+          } else {
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            const float x0 = to_f32(ea[e]), x1 = to_f32(eb[e]);
-            ea[e] = from_f32<T>(x0 * cs[e].x - x1 * cs[e].y);
-            eb[e] = from_f32<T>(x0 * cs[e].y + x1 * cs[e].x);
+            for (int e = 0; e + 1 < VEC; e += 2) {
+              const float2 w0 = turn[e / 2 * w.chunks + c], w1 = turn[(VEC / 2 + e / 2) * w.chunks + c];
+              const float x0 = to_f32(ea[e]), x1 = to_f32(ea[e + 1]), z0 = to_f32(eb[e]), z1 = to_f32(eb[e + 1]);
+              ea[e] = from_f32<T>(x0 * w0.x - x1 * w0.y);
+              ea[e + 1] = from_f32<T>(x0 * w0.y + x1 * w0.x);
+              eb[e] = from_f32<T>(z0 * w1.x - z1 * w1.y);
+              eb[e + 1] = from_f32<T>(z0 * w1.y + z1 * w1.x);
+            }
           }
-        } else {
-#pragma unroll
-          for (int e = 0; e + 1 < VEC; e += 2) {
-            const float2 w0 = cs[e / 2], w1 = cs[VEC / 2 + e / 2];
-            const float x0 = to_f32(ea[e]), x1 = to_f32(ea[e + 1]), z0 = to_f32(eb[e]), z1 = to_f32(eb[e + 1]);
-            ea[e] = from_f32<T>(x0 * w0.x - x1 * w0.y);
-            ea[e + 1] = from_f32<T>(x0 * w0.y + x1 * w0.x);
-            eb[e] = from_f32<T>(z0 * w1.x - z1 * w1.y);
-            eb[e + 1] = from_f32<T>(z0 * w1.y + z1 * w1.x);
-          }
-        }
-        if (y != nullptr) {
-          V va, vb;
           memcpy(&va, ea, sizeof(V));
           memcpy(&vb, eb, sizeof(V));
-          *reinterpret_cast<V *>(y + ia * sizeof(T)) = va;
-          *reinterpret_cast<V *>(y + ib * sizeof(T)) = vb;
+        }
+        if (!APPEND || y != nullptr) {
+          T *to = reinterpret_cast<T *>(y) + (ADJACENT ? 2 * c : c) * VEC;
+          *reinterpret_cast<V *>(to) = va;
+          *reinterpret_cast<V *>(to + (ADJACENT ? VEC : half)) = vb;
         }
       }
-    }
-
-    // elements past the rotated ones are copied
-    const int tail = (p.dim - 2 * half) / VEC;
-    for (int i = tid; i < nt * heads * tail; i += kThreads) {
-      const int r = i / tail, e = 2 * half + (i - r * tail) * VEC;
-      const int t = quotient(r, heads, rows_m), h = r - t * heads;
-      char *y = row_out(t, h);
-      if (y != nullptr)
-        *reinterpret_cast<V *>(y + e * sizeof(T)) = *reinterpret_cast<const V *>(row_in(t, h) + e * sizeof(T));
-    }
-    if (APPEND) {   // V, in 16-byte pieces where its alignment allows
-      auto copy_v = [&](auto piece) {
-        using P = decltype(piece);
-        const int n = p.dim * (int)sizeof(T) / (int)sizeof(P);
-        for (int i = tid; i < nt * p.v.heads * n; i += kThreads) {
-          const int r = i / n, t = quotient(r, p.v.heads, kv_m), h = r - t * p.v.heads;
-          if (slot[t] >= 0)
-            reinterpret_cast<P *>(p.cache.v + slot[t] + h * p.cache.head_stride)[i - r * n] =
-                reinterpret_cast<const P *>(p.v.in + (t0 + t) * p.v.in_token + h * p.v.in_head)[i - r * n];
+      load(n);
+      if (++round >= w.rounds) {
+        if (w.tail > 0) {   // elements past the rotated ones are copied
+          int j0, j1;
+          share(rows * w.tail, unit - t * w.parts, j0, j1);
+          for (int j = j0 + lane; j < j1; j += 32) {
+            const int h = quotient(j, w.tail, w.tail_m), e = 2 * half + (j - h * w.tail) * VEC;
+            char *y = row_out(h);
+            if (y != nullptr)
+              *reinterpret_cast<V *>(y + e * sizeof(T)) = *reinterpret_cast<const V *>(row_in(t, h) + e * sizeof(T));
+          }
         }
-      };
-      if (wide) copy_v(uint4{});
-      else copy_v(typename Pack<sizeof(T)>::type{});
+        round = 0;
+        unit += warps;
+      }
     }
   }
   if (APPEND) {
     __syncthreads();
-    if (tid == 0) post_status(p.status, blockIdx.x, gridDim.x, flags);
+    if (threadIdx.x == 0) post_status(p.status, blockIdx.x, gridDim.x, flags);
   }
 }
 
@@ -206,10 +230,8 @@ bool rows_aligned(const HeadRows &h, int bytes, bool out) {
 }
 
 template <typename T, int VEC>
-void launch(const RotaryArgs &a, int grid, int per_cta, bool wide, cudaStream_t s) {
-  auto magic = [](int n) { return (uint32_t)(((1ull << 32) + (unsigned)n - 1) / (unsigned)(n > 0 ? n : 1)); };
-  const uint32_t rm = magic(a.q.heads + a.k.heads), km = magic(a.v.heads);
-  auto go = [&](auto kernel) { kernel<<<grid, kThreads, 0, s>>>(a, per_cta, rm, km, wide); };
+void launch(const RotaryArgs &a, int grid, const Split &w, cudaStream_t s) {
+  auto go = [&](auto kernel) { kernel<<<grid, kThreads, 0, s>>>(a, w); };
   if (a.rot.adjacent)
     a.append ? go(rotary_kernel<T, VEC, true, true>) : go(rotary_kernel<T, VEC, true, false>);
   else
@@ -222,25 +244,31 @@ cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t s) {
   // the widest vector that every row's parts are whole numbers of, up to 16 bytes
   int vec = 16 / a.elem;
   while (vec > 1 && (a.rot.half % vec != 0 || a.dim % vec != 0 || !rows_aligned(a.q, vec * a.elem, true) ||
-                     !rows_aligned(a.k, vec * a.elem, !a.append)))
+                     !rows_aligned(a.k, vec * a.elem, !a.append) || !rows_aligned(a.v, vec * a.elem, false)))
     vec /= 2;
-  const bool wide = a.append && rows_aligned(a.v, 16, false);
-  // tokens per CTA: as many as its threads hold in one batch of loads, fewer where the GPU would not be full
-  const int heads = a.q.heads + a.k.heads, chunks = a.rot.half / vec;
-  int per = kThreads * kBatch / (heads * (chunks > 0 ? chunks : 1));
-  per = per < 1 ? 1 : per > kMaxTokens ? kMaxTokens : per;
-  const int sms = sm_count();
-  while (per > 1 && (a.tokens + per - 1) / per < 2 * sms) --per;
-  int grid = (a.tokens + per - 1) / per;
+  Split w;
+  w.chunks = a.rot.half / vec;
+  w.tail = (a.dim - 2 * a.rot.half) / vec;
+  w.chunks_m = magic(w.chunks);
+  w.tail_m = magic(w.tail);
+  // one warp a token, or as many as leave each one a round, where the SMs would not have eight each
+  const int rows = a.q.heads + a.k.heads + a.v.heads, items = rows * (w.chunks > w.tail ? w.chunks : w.tail);
+  const int sms = sm_count(), most = items > 32 ? items / 32 : 1;
+  w.parts = a.tokens > 0 && a.tokens < sms * 8 ? sms * 8 / a.tokens : 1;
+  if (w.parts > most) w.parts = most;
+  w.rounds = ((rows * w.chunks + w.parts - 1) / w.parts + 31) / 32;
+  const long long units = (long long)a.tokens * w.parts, per = kThreads / 32;
+  long long grid = (units + per - 1) / per;
+  if (grid > sms * 3) grid = sms * 3;
   if (a.append && grid > kMaxStatus) grid = kMaxStatus;   // a status word each
   if (grid < 1) grid = 1;
+  const int g = (int)grid;
   if (a.elem == 4) {
-    vec == 4 ? launch<float, 4>(a, grid, per, wide, s) : vec == 2 ? launch<float, 2>(a, grid, per, wide, s)
-                                                                 : launch<float, 1>(a, grid, per, wide, s);
+    vec == 4 ? launch<float, 4>(a, g, w, s) : vec == 2 ? launch<float, 2>(a, g, w, s) : launch<float, 1>(a, g, w, s);
   } else {
     using B = __nv_bfloat16;
-    vec == 8 ? launch<B, 8>(a, grid, per, wide, s) : vec == 4 ? launch<B, 4>(a, grid, per, wide, s)
-    : vec == 2 ? launch<B, 2>(a, grid, per, wide, s) : launch<B, 1>(a, grid, per, wide, s);
+    vec == 8 ? launch<B, 8>(a, g, w, s) : vec == 4 ? launch<B, 4>(a, g, w, s)
+    : vec == 2 ? launch<B, 2>(a, g, w, s) : launch<B, 1>(a, g, w, s);
   }
   return cudaGetLastError();
 }
