@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBatch = 4;        // items of a lane in flight
+constexpr int kCtas = 3;         // per SM
 
 template <int BYTES> struct Pack;
 template <> struct Pack<16> { using type = uint4; };
@@ -38,11 +39,42 @@ __device__ __forceinline__ int quotient(int x, int n, uint32_t m) {
 }
 uint32_t magic(int n) { return (uint32_t)(((1ull << 32) + (unsigned)n - 1) / (unsigned)(n > 0 ? n : 1)); }
 
-struct Split {       // of a token's work
-  int parts;         // warps per token
-  int rounds;        // of 32 items (pairs of VEC-element pieces) per part
-  int chunks, tail;  // items and single pieces behind them of a row
-  uint32_t chunks_m, tail_m;
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\t"
+      "mov.b64 {%0, %1}, z;\n\t}" : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+template <typename T> __device__ __forceinline__ float2 get2(const T *x);
+template <> __device__ __forceinline__ float2 get2(const float *x) { return make_float2(x[0], x[1]); }
+template <> __device__ __forceinline__ float2 get2(const __nv_bfloat16 *x) {
+  uint32_t v;
+  memcpy(&v, x, 4);
+  return make_float2(bf16lo(v), bf16hi(v));
+}
+template <typename T> __device__ __forceinline__ void set2(T *x, float2 v);
+template <> __device__ __forceinline__ void set2(float *x, float2 v) { x[0] = v.x; x[1] = v.y; }
+template <> __device__ __forceinline__ void set2(__nv_bfloat16 *x, float2 v) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(v.y), "f"(v.x));
+  memcpy(x, &r, 4);
+}
+
+// A row's items (pairs of VEC-element pieces) lie side by side in a warp, `heads` rows at a time.
+struct Split {
+  int parts;            // warps per token
+  int items, columns;   // of a row; passes over rows of more than 32
+  int heads;
+  int tail;             // pieces behind a row's items
+  uint32_t tail_m;
 };
 
 // Byte offset of new token t's slot in its cache layer; -1 (and a flag) if it has none.
@@ -69,84 +101,127 @@ __device__ long long slot_of(const RotaryArgs &p, int t, unsigned *bad) {
   return -1;
 }
 
-// A warp takes a token (or, of few tokens, a part of its rows) at a time.  Its lanes turn VEC pairs of a row
-// in each round and load those of the fourth round from there, of the next token if need be, so that loads
-// are always under way; the sines and cosines of a token lie in the warp's own shared memory, and warps do
-// not wait for each other.  Rows are q's, k's and, for a cache, v's heads, which are copied.
+// The cosines and sines of a lane's VEC pairs.
+template <int VEC, bool ADJACENT> struct Turns {
+  static constexpr bool kPacked = !ADJACENT && VEC > 1;
+  float2 c[VEC > 1 ? VEC / 2 : 1], s[VEC > 1 ? VEC / 2 : 1];   // of two pairs; adjacent: pairs e < VEC / 2 and the rest
+  __device__ __forceinline__ void load(const float *table, int items, int column) {
+    if constexpr (kPacked) {
+#pragma unroll
+      for (int e = 0; e < VEC / 2; ++e) {
+        const float4 x = reinterpret_cast<const float4 *>(table)[e * items + column];
+        c[e] = make_float2(x.x, x.y);
+        s[e] = make_float2(x.z, x.w);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < (VEC > 1 ? VEC / 2 : 1); ++e) {
+        const float2 x = reinterpret_cast<const float2 *>(table)[e * items + column];
+        const float2 y = VEC > 1 ? reinterpret_cast<const float2 *>(table)[(VEC / 2 + e) * items + column] : x;
+        c[e] = make_float2(x.x, y.x);
+        s[e] = make_float2(x.y, y.y);
+      }
+    }
+  }
+  template <typename T> __device__ __forceinline__ void apply(T *a, T *b) const {
+    if constexpr (kPacked) {
+#pragma unroll
+      for (int e = 0; e < VEC / 2; ++e) {
+        const float2 x = get2(a + 2 * e), y = get2(b + 2 * e), ys = mul2(y, s[e]);
+        set2(a + 2 * e, fma2(x, c[e], make_float2(-ys.x, -ys.y)));
+        set2(b + 2 * e, fma2(x, s[e], mul2(y, c[e])));
+      }
+    } else if constexpr (VEC == 1) {
+      const float x = to_f32(a[0]), y = to_f32(b[0]);
+      a[0] = from_f32<T>(fmaf(x, c[0].x, -y * s[0].x));
+      b[0] = from_f32<T>(fmaf(x, s[0].x, y * c[0].x));
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC / 2; ++e) {
+        const float2 x = get2(a + 2 * e), y = get2(b + 2 * e);
+        set2(a + 2 * e, make_float2(fmaf(x.x, c[e].x, -x.y * s[e].x), fmaf(x.x, s[e].x, x.y * c[e].x)));
+        set2(b + 2 * e, make_float2(fmaf(y.x, c[e].y, -y.y * s[e].y), fmaf(y.x, s[e].y, y.y * c[e].y)));
+      }
+    }
+  }
+};
+
+// A warp takes a token, or, of few tokens, every `parts`-th group of its rows.  The first loads of all its
+// tensors are under way while the token's sines and cosines go to the warp's own shared memory; from there
+// each lane keeps those of its column for all heads.  Warps do not wait for each other.
 template <typename T, int VEC, bool ADJACENT, bool APPEND>
-__global__ void __launch_bounds__(kThreads, 3) rotary_kernel(const __grid_constant__ RotaryArgs p, const Split w) {
+__global__ void __launch_bounds__(kThreads, kCtas) rotary_kernel(const __grid_constant__ RotaryArgs p, const Split w) {
   using V = typename Pack<VEC * (int)sizeof(T)>::type;
-  constexpr int kSets = kMaxRotPairs / 32;
-  __shared__ float2 tables[kThreads / 32][kMaxRotPairs];   // (cos, sin) of pair c VEC + e at [e chunks + c]
+  using R = Turns<VEC, ADJACENT>;
+  // of pair c VEC + e: cosine and sine at [e items + c], or, two pairs a time, both cosines and both sines at
+  // [e / 2 items + c]
+  __shared__ alignas(16) float tables[kThreads / 32][2 * kMaxRotPairs];
+  __shared__ unsigned long long freqs[kMaxRotPairs];
+  __shared__ uint8_t axes[kMaxRotPairs];
   __shared__ unsigned flags;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, half = p.rot.half, warps = gridDim.x * (kThreads / 32);
-  const int turned = p.q.heads + p.k.heads, rows = turned + (APPEND ? p.v.heads : 0), items = rows * w.chunks;
-  float2 *turn = tables[warp];
-  if (APPEND) {
-    if (threadIdx.x == 0) flags = 0;
-    __syncthreads();
+  float *table = tables[warp];
+  for (int i = threadIdx.x; i < half; i += kThreads) {
+    // through memory addresses: a warp's lanes would read parameters at different places one by one
+    const RotaryTable *rot = &p.rot;
+    asm("mov.b64 %0, %0;" : "+l"(rot));
+    freqs[i] = rot->turn[i];
+    axes[i] = rot->axis[i];
   }
-  auto share = [&](int n, int part, int &i0, int &i1) {
-    i0 = w.parts == 1 ? 0 : (int)((long long)n * part / w.parts);
-    i1 = w.parts == 1 ? n : (int)((long long)n * (part + 1) / w.parts);
-  };
-  auto row_in = [&](int t, int h) -> const char * {
-    if (h < p.q.heads) return p.q.in + t * p.q.in_token + h * p.q.in_head;
-    if (!APPEND || h < turned) return p.k.in + t * p.k.in_token + (h - p.q.heads) * p.k.in_head;
-    return p.v.in + t * p.v.in_token + (h - turned) * p.v.in_head;
-  };
-  // a lane's frequencies, read once: lanes reading parameters at different places do so one by one
-  unsigned long long freq[kSets];
-  uint32_t axes = 0;
-#pragma unroll
-  for (int n = 0; n < kSets; ++n) {
-    const int i = lane + 32 * n;
-    freq[n] = i < half ? p.rot.turn[i] : 0;
-    axes |= i < half ? (uint32_t)p.rot.axis[i] << (8 * n) : 0u;
-  }
+  if (APPEND && threadIdx.x == 0) flags = 0;
+  __syncthreads();
 
-  const int units = p.tokens * w.parts;
-  int load_unit = blockIdx.x * (kThreads / 32) + warp, load_round = 0;
-  V a[kBatch], b[kBatch];
-  auto load = [&](int n) {   // the next round's items
-    if (load_unit >= units) return;
-    const int t = w.parts == 1 ? load_unit : load_unit / w.parts;
-    int i0, i1;
-    share(items, load_unit - t * w.parts, i0, i1);
-    const int i = i0 + load_round * 32 + lane;
-    if (i < i1) {
-      const int h = quotient(i, w.chunks, w.chunks_m), c = i - h * w.chunks;
-      const T *x = reinterpret_cast<const T *>(row_in(t, h)) + (ADJACENT ? 2 * c : c) * VEC;
-      a[n] = *reinterpret_cast<const V *>(x);
-      b[n] = *reinterpret_cast<const V *>(x + (ADJACENT ? VEC : half));
-    }
-    if (++load_round == w.rounds) {
-      load_round = 0;
-      load_unit += warps;
-    }
-  };
+  const bool across = w.columns > 1;
+  const int sub = across ? 0 : lane / w.items;                       // row of the group
+  const bool idle = sub >= w.heads;
+  const int step = w.heads * w.parts, units = p.tokens * w.parts;
+  const int far = (ADJACENT ? VEC : half) * (int)sizeof(T);          // from an item's first piece to its second
+  for (int unit = blockIdx.x * (kThreads / 32) + warp; unit < units; unit += warps) {
+    const int t = w.parts == 1 ? unit : unit / w.parts, first = sub + (unit - t * w.parts) * w.heads;
+    long long slot = 0;
+    for (int col = 0; col < w.columns; ++col) {
+      const int c = across ? lane + 32 * col : lane - sub * w.items;
+      const bool off = idle || c >= w.items || half == 0;
+      const int at = (ADJACENT ? 2 * c : c) * VEC * (int)sizeof(T);
+      const int nq = off || first >= p.q.heads ? 0 : (p.q.heads - first + step - 1) / step;
+      const int nk = off || first >= p.k.heads ? 0 : (p.k.heads - first + step - 1) / step;
+      const char *q = p.q.in + t * p.q.in_token + first * p.q.in_head + at, *k = p.k.in + t * p.k.in_token + first * p.k.in_head + at;
+      const char *v = APPEND ? p.v.in + t * p.v.in_token + first * p.v.in_head + at : nullptr;
+      const long long q_step = step * p.q.in_head, k_step = step * p.k.in_head, v_step = step * p.v.in_head;
+      V a[kBatch], b[kBatch], ka, kb, va, vb;
+      auto load_q = [&](int r) {
 #pragma unroll
-  for (int n = 0; n < kBatch; ++n) load(n);
-
-  int unit = blockIdx.x * (kThreads / 32) + warp, round = 0, t = 0, i0 = 0, i1 = 0;
-  long long slot = 0;
-  while (unit < units) {
-#pragma unroll
-    for (int n = 0; n < kBatch; ++n) {
-      if (unit >= units) break;
-      if (round == 0) {   // a new token
-        t = w.parts == 1 ? unit : unit / w.parts;
-        share(items, unit - t * w.parts, i0, i1);
+        for (int n = 0; n < kBatch; ++n)
+          if (r + n < nq) {
+            a[n] = *reinterpret_cast<const V *>(q + n * q_step);
+            b[n] = *reinterpret_cast<const V *>(q + n * q_step + far);
+          }
+        q += kBatch * q_step;
+      };
+      load_q(0);
+      if (nk > 0) {
+        ka = *reinterpret_cast<const V *>(k);
+        kb = *reinterpret_cast<const V *>(k + far);
+        if (APPEND) {
+          va = *reinterpret_cast<const V *>(v);
+          vb = *reinterpret_cast<const V *>(v + far);
+        }
+      }
+      if (col == 0) {   // the token's angles, and its slot
         __syncwarp();
-#pragma unroll
-        for (int m = 0; m < kSets; ++m) {
-          const int i = lane + 32 * m;
-          if (i >= half) break;
-          const long long at = p.positions[(long long)(axes >> (8 * m) & 255) * p.axis_stride + t];
-          const long long phase = (long long)((unsigned long long)at * freq[m]);
+        for (int i = lane; i < half; i += 32) {
+          const long long phase = (long long)((unsigned long long)(long long)p.positions[axes[i] * p.axis_stride + t] * freqs[i]);
           float sn, cs;
           sincospif((float)phase * 0x1p-63f, &sn, &cs);   // phase: 2^-64 turns
-          turn[(i % VEC) * w.chunks + i / VEC] = make_float2(cs, p.backward ? -sn : sn);
+          sn = p.backward ? -sn : sn;
+          const int e = i % VEC, j = i / VEC;
+          if (R::kPacked) {
+            float *to = table + ((e / 2) * w.items + j) * 4 + (e & 1);
+            to[0] = cs;
+            to[2] = sn;
+          } else {
+            *reinterpret_cast<float2 *>(table + (e * w.items + j) * 2) = make_float2(cs, sn);
+          }
         }
         if (APPEND) {
           unsigned bad = 0;
@@ -155,64 +230,69 @@ __global__ void __launch_bounds__(kThreads, 3) rotary_kernel(const __grid_consta
         }
         __syncwarp();
       }
-      auto row_out = [&](int h) -> char * {
-        if (h < p.q.heads) return p.q.out + t * p.q.out_token + h * p.q.out_head;
-        if (!APPEND) return p.k.out + t * p.k.out_token + (h - p.q.heads) * p.k.out_head;
-        if (slot < 0) return nullptr;
-        return h < turned ? p.cache.k + slot + (h - p.q.heads) * p.cache.head_stride
-                          : p.cache.v + slot + (h - turned) * p.cache.head_stride;
+      R turns;
+      if (!off) turns.load(table, w.items, c);
+      auto turn = [&](V &x, V &y) {
+        T ex[VEC], ey[VEC];
+        memcpy(ex, &x, sizeof(V));
+        memcpy(ey, &y, sizeof(V));
+        turns.apply(ex, ey);
+        memcpy(&x, ex, sizeof(V));
+        memcpy(&y, ey, sizeof(V));
       };
-      const int i = i0 + round * 32 + lane;
-      if (i < i1) {
-        const int h = quotient(i, w.chunks, w.chunks_m), c = i - h * w.chunks;
-        char *y = row_out(h);
-        V va = a[n], vb = b[n];
-        if (!APPEND || h < turned) {
-          T ea[VEC], eb[VEC];
-          memcpy(ea, &va, sizeof(V));
-          memcpy(eb, &vb, sizeof(V));
-          if (!ADJACENT || VEC == 1) {
+      char *qo = p.q.out + t * p.q.out_token + first * p.q.out_head + at;
+      const long long qo_step = step * p.q.out_head;
+      for (int r = 0; r < nq; r += kBatch) {
+        if (r > 0) load_q(r);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-              const float2 cs = turn[e * w.chunks + c];
-              const float x0 = to_f32(ea[e]), x1 = to_f32(eb[e]);
-              ea[e] = from_f32<T>(x0 * cs.x - x1 * cs.y);
-              eb[e] = from_f32<T>(x0 * cs.y + x1 * cs.x);
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e + 1 < VEC; e += 2) {
-              const float2 w0 = turn[e / 2 * w.chunks + c], w1 = turn[(VEC / 2 + e / 2) * w.chunks + c];
-              const float x0 = to_f32(ea[e]), x1 = to_f32(ea[e + 1]), z0 = to_f32(eb[e]), z1 = to_f32(eb[e + 1]);
-              ea[e] = from_f32<T>(x0 * w0.x - x1 * w0.y);
-              ea[e + 1] = from_f32<T>(x0 * w0.y + x1 * w0.x);
-              eb[e] = from_f32<T>(z0 * w1.x - z1 * w1.y);
-              eb[e + 1] = from_f32<T>(z0 * w1.y + z1 * w1.x);
-            }
+        for (int n = 0; n < kBatch; ++n)
+          if (r + n < nq) {
+            turn(a[n], b[n]);
+            *reinterpret_cast<V *>(qo + n * qo_step) = a[n];
+            *reinterpret_cast<V *>(qo + n * qo_step + far) = b[n];
           }
-          memcpy(&va, ea, sizeof(V));
-          memcpy(&vb, eb, sizeof(V));
+        qo += kBatch * qo_step;
+      }
+      if (APPEND && slot < 0) continue;
+      char *ko = APPEND ? p.cache.k + slot + first * p.cache.head_stride + at : p.k.out + t * p.k.out_token + first * p.k.out_head + at;
+      char *vo = APPEND ? p.cache.v + slot + first * p.cache.head_stride + at : nullptr;
+      const long long ko_step = step * (APPEND ? p.cache.head_stride : p.k.out_head);
+      for (int r = 0; r < nk; ++r) {
+        if (r > 0) {
+          k += k_step;
+          ka = *reinterpret_cast<const V *>(k);
+          kb = *reinterpret_cast<const V *>(k + far);
+          if (APPEND) {
+            v += v_step;
+            va = *reinterpret_cast<const V *>(v);
+            vb = *reinterpret_cast<const V *>(v + far);
+          }
         }
-        if (!APPEND || y != nullptr) {
-          T *to = reinterpret_cast<T *>(y) + (ADJACENT ? 2 * c : c) * VEC;
-          *reinterpret_cast<V *>(to) = va;
-          *reinterpret_cast<V *>(to + (ADJACENT ? VEC : half)) = vb;
+        turn(ka, kb);
+        *reinterpret_cast<V *>(ko) = ka;
+        *reinterpret_cast<V *>(ko + far) = kb;
+        ko += ko_step;
+        if (APPEND) {
+          *reinterpret_cast<V *>(vo) = va;
+          *reinterpret_cast<V *>(vo + far) = vb;
+          vo += ko_step;
         }
       }
-      load(n);
-      if (++round >= w.rounds) {
-        if (w.tail > 0) {   // elements past the rotated ones are copied
-          int j0, j1;
-          share(rows * w.tail, unit - t * w.parts, j0, j1);
-          for (int j = j0 + lane; j < j1; j += 32) {
-            const int h = quotient(j, w.tail, w.tail_m), e = 2 * half + (j - h * w.tail) * VEC;
-            char *y = row_out(h);
-            if (y != nullptr)
-              *reinterpret_cast<V *>(y + e * sizeof(T)) = *reinterpret_cast<const V *>(row_in(t, h) + e * sizeof(T));
-          }
+    }
+    if (w.tail > 0) {   // elements past the rotated ones are copied
+      const int part = unit - t * w.parts;
+      auto copy = [&](const char *in, long long in_head, char *out, long long out_head, int heads) {
+        const int all = heads * w.tail;
+        for (int j = (int)((long long)all * part / w.parts) + lane; j < (int)((long long)all * (part + 1) / w.parts); j += 32) {
+          const int h = quotient(j, w.tail, w.tail_m), e = (2 * half + (j - h * w.tail) * VEC) * (int)sizeof(T);
+          *reinterpret_cast<V *>(out + h * out_head + e) = *reinterpret_cast<const V *>(in + h * in_head + e);
         }
-        round = 0;
-        unit += warps;
+      };
+      copy(p.q.in + t * p.q.in_token, p.q.in_head, p.q.out + t * p.q.out_token, p.q.out_head, p.q.heads);
+      if (!APPEND) copy(p.k.in + t * p.k.in_token, p.k.in_head, p.k.out + t * p.k.out_token, p.k.out_head, p.k.heads);
+      if (APPEND && slot >= 0) {
+        copy(p.k.in + t * p.k.in_token, p.k.in_head, p.cache.k + slot, p.cache.head_stride, p.k.heads);
+        copy(p.v.in + t * p.v.in_token, p.v.in_head, p.cache.v + slot, p.cache.head_stride, p.v.heads);
       }
     }
   }
@@ -247,19 +327,29 @@ cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t s) {
                      !rows_aligned(a.k, vec * a.elem, !a.append) || !rows_aligned(a.v, vec * a.elem, false)))
     vec /= 2;
   Split w;
-  w.chunks = a.rot.half / vec;
+  const int pairs = a.rot.half / vec;
+  w.items = pairs > 0 ? pairs : 1;
+  w.columns = (w.items + 31) / 32;
+  w.heads = w.columns > 1 ? 1 : 32 / w.items;
   w.tail = (a.dim - 2 * a.rot.half) / vec;
-  w.chunks_m = magic(w.chunks);
   w.tail_m = magic(w.tail);
-  // one warp a token, or as many as leave each one a round, where the SMs would not have eight each
-  const int rows = a.q.heads + a.k.heads + a.v.heads, items = rows * (w.chunks > w.tail ? w.chunks : w.tail);
-  const int sms = sm_count(), most = items > 32 ? items / 32 : 1;
-  w.parts = a.tokens > 0 && a.tokens < sms * 8 ? sms * 8 / a.tokens : 1;
-  if (w.parts > most) w.parts = most;
-  w.rounds = ((rows * w.chunks + w.parts - 1) / w.parts + 31) / 32;
+  // Parts of a token per warp: the fewest rounds on the busiest warp, its angles (and slot) taken for two
+  const int sms = sm_count(), warps = sms * kCtas * (kThreads / 32);
+  auto rounds = [&](int heads, int parts) { return (heads + w.heads * parts - 1) / (w.heads * parts); };
+  const int most = rounds(a.q.heads > a.k.heads ? a.q.heads : a.k.heads, 1);
+  w.parts = 1;
+  long long best = -1;
+  for (int parts = 1; parts <= most && parts <= 32; ++parts) {
+    const int work = rounds(a.q.heads, parts) + rounds(a.k.heads, parts) + rounds(a.v.heads, parts);
+    const long long cost = ((long long)a.tokens * parts + warps - 1) / warps * (w.columns * work + 2);
+    if (best < 0 || cost < best) {
+      best = cost;
+      w.parts = parts;
+    }
+  }
   const long long units = (long long)a.tokens * w.parts, per = kThreads / 32;
   long long grid = (units + per - 1) / per;
-  if (grid > sms * 3) grid = sms * 3;
+  if (grid > sms * kCtas) grid = sms * kCtas;
   if (a.append && grid > kMaxStatus) grid = kMaxStatus;   // a status word each
   if (grid < 1) grid = 1;
   const int g = (int)grid;
