@@ -150,9 +150,9 @@ cudaError_t launch_attend_f32(const Shape &p, cudaStream_t s) {
   return p.chunks <= 4 ? launch_heads<1>(p, s) : launch_heads<2>(p, s);
 }
 
-size_t attend_scratch_bytes(int batch, int q_heads, int kv_heads, int dim) {
+size_t attend_scratch_bytes(int q_heads, int kv_heads, int dim) {
   const int group = q_heads / kv_heads, rows = group < kRows ? group : kRows;
-  return align256(sizeof(long long) * ((size_t)batch + 1)) + align256(sizeof(float) * kMaxWorkers * 2 * (kStatFloats + (size_t)rows * dim));
+  return align256(sizeof(int4) * kMaxWorkers) + align256(sizeof(float) * kMaxWorkers * 2 * (kStatFloats + (size_t)rows * dim));
 }
 
 cudaError_t launch_attend(const AttendArgs &a, cudaStream_t s) {
@@ -164,9 +164,8 @@ cudaError_t launch_attend(const AttendArgs &a, cudaStream_t s) {
   p.rows = p.group < kRows ? p.group : kRows;
   p.chunks = (a.cache.dim * a.elem + 127) / 128;
   p.scale2 = a.scale * kLog2e;
-  p.first = reinterpret_cast<long long *>(a.ws + kStatusBytes);
-  p.parts = reinterpret_cast<float *>(a.ws + kStatusBytes + align256(sizeof(long long) * ((size_t)a.seq.batch + 1)));
-  if ((long long)a.seq.batch * a.q_heads > 0x7fffffffLL) return cudaErrorInvalidValue;
+  p.jobs = reinterpret_cast<int4 *>(a.ws + kStatusBytes);
+  p.parts = reinterpret_cast<float *>(a.ws + kStatusBytes + align256(sizeof(int4) * kMaxWorkers));
   return a.elem == 4 ? launch_attend_f32(p, s) : launch_attend_bf16(p, s);
 }
 

@@ -30,8 +30,8 @@ struct Shape {      // the same for every CTA
   int tile;                   // keys
   int rows;                   // heads of a pass at most
   float scale2;               // scale log2 e
-  long long *first;           // [batch + 1] first tile of each sequence (in the workspace)
-  float *parts;               // [workers][2] sums that a cut has parted
+  int4 *jobs;                 // [CTAs] sequence, head, parts (0: nothing to join), slot of the first
+  float *parts;               // [CTAs][2] sums that a cut has parted
 };
 
 cudaError_t launch_attend_bf16(const Shape &p, cudaStream_t s);
@@ -62,6 +62,7 @@ struct alignas(16) Shared {
   float top[2][kWarps][kRows], sum[2][kWarps][kRows];   // by turns
   float factor[kWarps][kRows], all[kRows], total[kRows];
   float merge[kWarps][kMergeRows][kMergeLd];
+  int4 job;
   long long warp_tiles[kWarps + 1], start_first;
   int start_seq;
   unsigned flags;
@@ -240,7 +241,7 @@ __device__ __forceinline__ void advance(const Shape &p, Walk &w) {
 // comes again, as many tiles lie between and the last K of its part has been given back.
 template <typename Part, typename T>
 __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const CUtensorMap *kmap, const CUtensorMap *vmap,
-                        Walk w, int tiles) {
+                        Walk w, int tiles, long long upto, long long total, long long shares) {
   constexpr int kTile = Part::kTile;
   const int lane = threadIdx.x & 31, box = 1 << p.box_log, boxes = kTile >> p.box_log, mine = lane & (boxes - 1);
   const int ops = boxes * (p.joined ? 1 : p.chunks), half = p.chunks * kTile * 128;
@@ -307,6 +308,10 @@ __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const 
         ++round;
       }
     }
+    if (it + 1 == tiles && begun && w.at + 1 < w.tiles && lane == 0) {   // begun here, goes on in the next shares
+      const long long end = upto + (w.tiles - 1 - w.at);
+      sm.job = make_int4(w.seq, w.head, (int)((end * shares - 1) / total) - (int)blockIdx.x + 1, later);
+    }
     fresh = last;
     later |= last;
     if (last && ++slot == p.slots) slot = 0;
@@ -335,14 +340,24 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
     fence_mbar_init();
     sm.flags = 0;
     sm.dead = 0;
-    sm.start_seq = -1;
+    sm.start_seq = 0;
+    sm.job = make_int4(0, 0, 0, 0);
   }
 
-  // this CTA's share of all tiles: each thread counts some sequences' tiles
+  // this CTA's share of all tiles: each thread counts some sequences' tiles; sequences without one have
+  // their outputs from the CTA whose turn it is
   unsigned bad = 0;
   const int per = (B + kThreads - 1) / kThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
   long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += (long long)tiles_of(keys_of(p.a, b, &bad), p.tile) * p.heads;
+  for (int b = b0; b < b1; ++b) {
+    const int n = tiles_of(keys_of(p.a, b, &bad), p.tile);
+    mine += (long long)n * p.heads;
+    if (n == 0 && b % gridDim.x == blockIdx.x) {
+      uint4 *out = reinterpret_cast<uint4 *>(p.a.out + b * p.a.out_stride);
+      for (int i = 0; i < p.a.q_heads * p.a.cache.dim * (int)sizeof(T) / 16; ++i) out[i] = make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < p.a.q_heads && p.a.lse != nullptr; ++i) p.a.lse[(long long)b * p.a.q_heads + i] = -INFINITY;
+    }
+  }
   long long upto = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -357,24 +372,23 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
     if (w < warp) upto += sm.warp_tiles[w];
     total += sm.warp_tiles[w];
   }
-  // no share is empty: with fewer tiles than CTAs the last CTAs have none
+  // share w: the tiles total w / shares up to total (w + 1) / shares.  None is empty: with fewer tiles than
+  // CTAs the last CTAs have none
   const long long shares = total < gridDim.x ? total : gridDim.x;
   const long long t0 = blockIdx.x < shares ? total * blockIdx.x / shares : total;
   const long long t1 = blockIdx.x < shares ? total * (blockIdx.x + 1) / shares : total;
-  const bool here = t0 < t1 && t0 >= upto - mine && t0 < upto;
-  if (here || blockIdx.x == 0) {
+  if (t0 < t1 && t0 >= upto - mine && t0 < upto) {
     long long at = upto - mine;
     for (int b = b0; b < b1; ++b) {
       const long long n = (long long)tiles_of(keys_of(p.a, b, &bad), p.tile) * p.heads;
-      if (blockIdx.x == 0) p.first[b] = at;
-      if (here && t0 >= at && t0 < at + n) {
+      if (t0 < at + n) {
         sm.start_seq = b;
         sm.start_first = at;
+        break;
       }
       at += n;
     }
   }
-  if (blockIdx.x == 0 && tid == 0) p.first[B] = total;
   __syncthreads();
 
   const int tiles = (int)(t1 - t0);
@@ -387,95 +401,94 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
       const long long at = t0 - sm.start_first;
       w.head = (int)(at / w.tiles);
       w.at = (int)(at - (long long)w.head * w.tiles);
-      produce<Part, T>(p, sm, ring, qs, &kmap, &vmap, w, tiles);
+      produce<Part, T>(p, sm, ring, qs, &kmap, &vmap, w, tiles, t1, total, shares);
     } else {
       consume<Part, T>(p, sm, ring, qs, weights, tiles);
     }
   }
   __syncthreads();
   if (sm.dead && tid < 32) wait_out(&sm.never);   // copies that nobody waited for
+  if (tid == 0) p.jobs[blockIdx.x] = sm.job;
   if (tid == 0) post_status(reinterpret_cast<unsigned *>(p.a.ws), blockIdx.x, gridDim.x, sm.flags | (sm.dead ? kErrTimeout : 0u));
 }
 
-// What the cuts between the CTAs' shares have parted, one query head per CTA; and the outputs of sequences
-// without a key.
-constexpr int kJoinThreads = 256;
+// What the cuts between the CTAs' shares have parted: CTA (w, r) joins head r of the (sequence, head) that
+// begins in share w and ends in a later one.  Most have nothing to do.
+constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kJoinBatch = 4;
 
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Shape p, int workers) {
-  __shared__ float factor[kMaxWorkers], red[kJoinThreads / 32];
-  __shared__ float4 rows[kJoinThreads / 32][64];
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Shape p) {
+  __shared__ float factor[kMaxWorkers], red[kJoinWarps], sums[kJoinWarps][256];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = p.a.cache.dim;
-  const int b = blockIdx.x / p.a.q_heads, h = blockIdx.x - b * p.a.q_heads;
-  const int kv = h / p.group, pass = (h - kv * p.group) / kRows, r = h - kv * p.group - pass * kRows;
-  const long long total = p.first[p.a.seq.batch], tiles = (p.first[b + 1] - p.first[b]) / p.heads;
-  const long long begin = p.first[b] + (kv * p.passes + pass) * tiles;
-  T *out = reinterpret_cast<T *>(p.a.out + b * p.a.out_stride) + (long long)h * D;
-  float *lse = p.a.lse == nullptr ? nullptr : p.a.lse + (long long)b * p.a.q_heads + h;
-  if (tiles == 0) {
-    for (int d = tid; d < D; d += kJoinThreads) out[d] = (T)0.0f;
-    if (lse != nullptr && tid == 0) *lse = -INFINITY;
-    return;
-  }
-  // share w: the tiles total w / workers up to total (w + 1) / workers
-  if (workers > total) workers = (int)total;
-  const int w0 = (int)(((begin + 1) * workers - 1) / total), w1 = (int)(((begin + tiles) * workers - 1) / total);
-  if (w0 == w1) return;   // one CTA wrote the output
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = p.a.cache.dim, first = blockIdx.x;
+  const int4 job = p.jobs[first];
+  const int parts = job.z, kv = job.y / p.passes, pass = job.y - kv * p.passes, r = blockIdx.y;
+  if (parts == 0 || r >= p.group - pass * kRows) return;
   const long long stride = kStatFloats + p.rows * D;
-  auto part = [&](int w) {   // a CTA's first part unless its share begins before the (sequence, head)
-    return p.parts + (2LL * w + (total * w / workers < begin ? 1 : 0)) * stride;
-  };
-  float all = -INFINITY, sum = 0.0f;
-  for (int w = w0 + tid; w <= w1; w += kJoinThreads) all = fmaxf(all, part(w)[2 * r]);
+  auto part = [&](int i) { return p.parts + (2LL * (first + i) + (i == 0 ? job.w : 0)) * stride; };
+  float4 x[kJoinBatch][2];
+  auto load = [&](int i0) {   // this warp's next parts
 #pragma unroll
-  for (int x = 16; x > 0; x >>= 1) all = fmaxf(all, __shfl_xor_sync(~0u, all, x));
+    for (int n = 0; n < kJoinBatch; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        if (i0 + n * kJoinWarps < parts && lane + 32 * c < D / 4)
+          x[n][c] = reinterpret_cast<const float4 *>(part(i0 + n * kJoinWarps) + kStatFloats + r * D)[lane + 32 * c];
+  };
+  load(warp);
+  float all = -INFINITY, sum = 0.0f;
+  for (int i = tid; i < parts; i += kJoinThreads) all = fmaxf(all, part(i)[2 * r]);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor_sync(~0u, all, d));
   if (lane == 0) red[warp] = all;
   __syncthreads();
   all = red[0];
 #pragma unroll
-  for (int w = 1; w < kJoinThreads / 32; ++w) all = fmaxf(all, red[w]);
-  for (int w = w0 + tid; w <= w1; w += kJoinThreads) {
-    const float2 x = *reinterpret_cast<const float2 *>(part(w) + 2 * r);
-    const float f = join_factor(x.x, all);
-    factor[w - w0] = f;
-    sum += x.y * f;
+  for (int w = 1; w < kJoinWarps; ++w) all = fmaxf(all, red[w]);
+  for (int i = tid; i < parts; i += kJoinThreads) {
+    const float2 s = *reinterpret_cast<const float2 *>(part(i) + 2 * r);
+    factor[i] = join_factor(s.x, all);
+    sum += s.y * factor[i];
   }
 #pragma unroll
-  for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(~0u, sum, x);
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
   __syncthreads();
   if (lane == 0) red[warp] = sum;
   float4 acc[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
-#pragma unroll 4
-  for (int w = w0 + warp; w <= w1; w += kJoinThreads / 32) {
-    const float4 *x = reinterpret_cast<const float4 *>(part(w) + kStatFloats + r * D);
-    const float g = factor[w - w0];
+  for (int i0 = warp; i0 < parts; i0 += kJoinWarps * kJoinBatch) {
+    if (i0 != warp) load(i0);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (lane + 32 * i < D / 4) {
-        const float4 y = x[lane + 32 * i];
-        acc[i].x = fmaf(y.x, g, acc[i].x);
-        acc[i].y = fmaf(y.y, g, acc[i].y);
-        acc[i].z = fmaf(y.z, g, acc[i].z);
-        acc[i].w = fmaf(y.w, g, acc[i].w);
-      }
+    for (int n = 0; n < kJoinBatch; ++n) {
+      if (i0 + n * kJoinWarps >= parts) break;
+      const float f = factor[i0 + n * kJoinWarps];
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        if (lane + 32 * c < D / 4) {
+          acc[c].x = fmaf(x[n][c].x, f, acc[c].x);
+          acc[c].y = fmaf(x[n][c].y, f, acc[c].y);
+          acc[c].z = fmaf(x[n][c].z, f, acc[c].z);
+          acc[c].w = fmaf(x[n][c].w, f, acc[c].w);
+        }
+    }
   }
-  rows[warp][lane] = acc[0];
-  rows[warp][lane + 32] = acc[1];
+  reinterpret_cast<float4 *>(sums[warp])[lane] = acc[0];
+  reinterpret_cast<float4 *>(sums[warp])[lane + 32] = acc[1];
   __syncthreads();
   sum = 0.0f;
 #pragma unroll
-  for (int w = 0; w < kJoinThreads / 32; ++w) sum += red[w];
+  for (int w = 0; w < kJoinWarps; ++w) sum += red[w];
+  const int h = kv * p.group + pass * kRows + r;
+  T *out = reinterpret_cast<T *>(p.a.out + job.x * p.a.out_stride) + (long long)h * D;
   for (int d = tid; d < D; d += kJoinThreads) {
-    float x = 0.0f;
+    float y = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kJoinThreads / 32; ++w) x += reinterpret_cast<const float *>(rows[w])[d];
-    out[d] = (T)(sum == 0.0f ? 0.0f : x / sum);
+    for (int w = 0; w < kJoinWarps; ++w) y += sums[w][d];
+    out[d] = (T)(sum == 0.0f ? 0.0f : y / sum);
   }
-  if (lse != nullptr && tid == 0) *lse = lse_of(all, sum);
+  if (p.a.lse != nullptr && tid == 0) p.a.lse[(long long)job.x * p.a.q_heads + h] = lse_of(all, sum);
 }
 
-constexpr size_t kHalfSm = 113 * 1024;   // of shared memory, for one of two CTAs
+constexpr size_t kHalfSm = 109 * 1024;   // of shared memory for one of two CTAs; the rest is room for join_kernel
 constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 template <typename Part, typename T>
@@ -514,7 +527,7 @@ cudaError_t launch(Shape p, cudaStream_t s) {
   attend_kernel<Part, T><<<workers, kThreads, smem, s>>>(p, maps[0], maps[1]);
   if ((e = cudaGetLastError()) != cudaSuccess || a.seq.batch == 0) return e;
   cudaLaunchConfig_t q = {};
-  q.gridDim = dim3((unsigned)(a.seq.batch * (long long)a.q_heads));
+  q.gridDim = dim3(workers, p.rows);
   q.blockDim = dim3(kJoinThreads);
   q.stream = s;
   cudaLaunchAttribute at[1];
@@ -522,7 +535,7 @@ cudaError_t launch(Shape p, cudaStream_t s) {
   at[0].val.programmaticStreamSerializationAllowed = 1;
   q.attrs = at;
   q.numAttrs = 1;
-  return cudaLaunchKernelEx(&q, join_kernel<T>, p, workers);
+  return cudaLaunchKernelEx(&q, join_kernel<T>, p);
 }
 
 }  // namespace

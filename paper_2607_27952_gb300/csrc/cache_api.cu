@@ -255,7 +255,7 @@ last_status last_cache_workspace_size(const last_cache *c, int32_t batch, int32_
     if (batch < 0) return invalid("batch < 0");
     if (num_q_heads < 1 || num_q_heads % c->num_kv_heads != 0)
       return invalid("num_q_heads must be a positive multiple of num_kv_heads");
-    *bytes = kStatusBytes + attend_scratch_bytes(batch, num_q_heads, c->num_kv_heads, c->head_dim);
+    *bytes = kStatusBytes + attend_scratch_bytes(num_q_heads, c->num_kv_heads, c->head_dim);
     return LAST_OK;
   });
 }
@@ -316,7 +316,7 @@ last_status last_cache_attention(const last_cache *c, int32_t layer, const last_
     if (s->batch > 1 && out_stride < (int64_t)num_q_heads * c->head_dim)
       return invalid("out_stride must be at least num_q_heads * head_dim");
     if (!aligned(lse, 4)) return invalid("lse is misaligned");
-    const size_t need = kStatusBytes + attend_scratch_bytes(s->batch, num_q_heads, c->num_kv_heads, c->head_dim);
+    const size_t need = kStatusBytes + attend_scratch_bytes(num_q_heads, c->num_kv_heads, c->head_dim);
     if ((st = check_cache_ws(ws, ws_bytes, need)) != LAST_OK) return st;
     AttendArgs a{};
     a.cache = layer_of(c, layer);

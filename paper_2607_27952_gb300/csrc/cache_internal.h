@@ -98,7 +98,7 @@ cudaError_t launch_attend(const AttendArgs &a, cudaStream_t s);
 cudaError_t launch_page_copy(const PagesArgs &a, int n, const int32_t *src, const int32_t *dst, cudaStream_t s);
 cudaError_t launch_compact(const CompactArgs &a, cudaStream_t s);
 // Workspace of the attention behind the status words.
-size_t attend_scratch_bytes(int batch, int q_heads, int kv_heads, int dim);
+size_t attend_scratch_bytes(int q_heads, int kv_heads, int dim);
 
 // SMs of the current device.
 int sm_count();
