@@ -178,18 +178,19 @@ struct Bf16Part {
       }
     }
   }
-  // Rows row0 .. row0 + 7 and columns col0 .. col0 + 63 of the sums times factor[row].
-  __device__ void put(int row0, int col0, const float *factor, float (*to)[kMergeLd], int) {
+  // Rows row0 .. row0 + rows - 1 and columns col0 .. col0 + cols - 1 of the sums.
+  __device__ void put(int row0, int rows, int col0, int cols, int ld, float *to, int) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const float f = factor[row0 + g];
 #pragma unroll
-    for (int i = 0; i < CHUNKS * 8; ++i) {
-      const int c = i * 8 + 2 * t - col0;
-      if (i * 8 < col0 || i * 8 >= col0 + kMergeCols) continue;
-      float2 x;
-      if (FEW) x = make_float2(o[i][0] + o[i][2], o[i][1] + o[i][3]);
-      else x = row0 == 0 ? make_float2(o[i][0], o[i][1]) : make_float2(o[i][2], o[i][3]);
-      *reinterpret_cast<float2 *>(&to[g][c]) = make_float2(x.x * f, x.y * f);
+    for (int r = 0; r < (FEW ? 1 : 2); ++r) {
+      const int row = g + 8 * r - row0;
+      if (row < 0 || row >= rows) continue;
+#pragma unroll
+      for (int i = 0; i < CHUNKS * 8; ++i) {
+        if (i * 8 < col0 || i * 8 >= col0 + cols) continue;
+        const float2 x = FEW ? make_float2(o[i][0] + o[i][2], o[i][1] + o[i][3]) : make_float2(o[i][2 * r], o[i][2 * r + 1]);
+        *reinterpret_cast<float2 *>(to + row * ld + i * 8 + 2 * t - col0) = x;
+      }
     }
   }
 };

@@ -115,15 +115,14 @@ struct F32Part {
       }
     }
   }
-  __device__ void put(int row0, int col0, const float *factor, float (*to)[kMergeLd], int D) {
+  // Rows row0 .. row0 + rows - 1 and columns col0 .. col0 + cols - 1 of the sums.
+  __device__ void put(int row0, int rows, int col0, int cols, int ld, float *to, int D) {
     const int lane = threadIdx.x & 31, across = lanes_across(D);
 #pragma unroll
     for (int h = 0; h < HEADS; ++h) {
-      if (h < row0 || h >= row0 + kMergeRows) continue;
-      const float f = factor[h];
+      if (h < row0 || h >= row0 + rows) continue;
 #pragma unroll
       for (int w = 0; w < WIDE; ++w) {
-        if (w != col0 / 128) continue;
         float x[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -131,11 +130,12 @@ struct F32Part {
           for (int d = across; d < 32; d <<= 1) x[e] += __shfl_xor_sync(~0u, x[e], d);
         }
         const int c = w * 128 + lane * 4 - col0;
-        if (lane < across && c >= 0 && c < kMergeCols) *reinterpret_cast<float4 *>(&to[h - row0][c]) = make_float4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+        if (lane < across && c >= 0 && c < cols) *reinterpret_cast<float4 *>(to + (h - row0) * ld + c) = make_float4(x[0], x[1], x[2], x[3]);
       }
     }
   }
 };
+
 template <int WIDE>
 cudaError_t launch_heads(const Shape &p, cudaStream_t s) {
   if (p.rows <= 1) return launch<F32Part<1, WIDE>, float>(p, s);

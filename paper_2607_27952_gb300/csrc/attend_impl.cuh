@@ -43,7 +43,7 @@ constexpr int kThreads = 32 * (kWarps + 1);
 constexpr int kRows = 16;                      // query heads of one pass over a kv-head
 constexpr int kMaxWorkers = 320;               // CTAs
 constexpr int kMaxStages = 12;                 // of the ring: K or V of a tile each
-constexpr int kMergeRows = 8, kMergeCols = 64, kMergeLd = kMergeCols + 8;
+constexpr int kMergeFloats = 512;              // of each warp's sums laid down at a time: 8 x 64, 4 x 128 or 2 x 256
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct TileInfo {   // what the producer says of a tile
@@ -57,11 +57,10 @@ constexpr int kFirst = 1, kLast = 2, kWhole = 4, kLater = 8;
 constexpr int kStatFloats = 2 * kRows;   // of a parted sum: maximum and denominator per head, then the rows
 
 struct alignas(16) Shared {
-  unsigned long long full[kMaxStages], empty[kMaxStages], sync, never;
+  unsigned long long full[kMaxStages], empty[kMaxStages], laid, read, never;
   TileInfo info[kMaxStages];
-  float top[2][kWarps][kRows], sum[2][kWarps][kRows];   // by turns
-  float factor[kWarps][kRows], all[kRows], total[kRows];
-  float merge[kWarps][kMergeRows][kMergeLd];
+  float top[kWarps][kRows], sum[kWarps][kRows];
+  alignas(16) float merge[kWarps][kMergeFloats + 8 * 8];   // rows 8 floats apart
   int4 job;
   long long warp_tiles[kWarps + 1], start_first;
   int start_seq;
@@ -85,14 +84,6 @@ __device__ __forceinline__ bool wait(Shared &sm, unsigned long long *bar, uint32
   if (__all_sync(~0u, ok)) return true;
   sm.dead = 1;
   return false;
-}
-
-// The consumers' barrier (bounded, unlike a hardware one).
-__device__ __forceinline__ bool consumers_sync(Shared &sm, uint32_t &parity) {
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) mbar_arrive(&sm.sync);
-  parity ^= 1;
-  return wait(sm, &sm.sync, parity ^ 1);
 }
 
 struct Keys {
@@ -126,56 +117,53 @@ __device__ __forceinline__ float join_factor(float top, float all) { return top 
 __device__ __forceinline__ float lse_of(float top, float sum) { return sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * kLn2; }
 
 // Adds up the warps' sums of the CTA's part of a (sequence, head): to the output where the part is
-// all of it, else to the workspace.
+// all of it, else to the workspace.  As many rows and columns at a time as the buffer holds: each warp
+// lays its own down, one barrier, and every thread scales and adds what it writes.  A second barrier
+// says that the buffer has been read; it is waited for at the next use.
 template <typename Part, typename T>
-__device__ bool finish(const Shape &p, Shared &sm, Part &part, const TileInfo &ti, int turn, uint32_t &parity) {
+__device__ bool finish(const Shape &p, Shared &sm, Part &part, const TileInfo &ti, int &passes) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = p.a.cache.dim;
   const int kv = ti.head / p.passes, pass = ti.head - kv * p.passes;
   const int h0 = kv * p.group + pass * kRows, n = min(kRows, p.group - pass * kRows);
-  float (*top)[kRows] = sm.top[turn], (*sum)[kRows] = sm.sum[turn];
-  part.stats(top[warp], sum[warp]);
-  if (!consumers_sync(sm, parity)) return false;   // and everybody has done with the last part's sums
-  if (lane < Part::kHeadRows) {
-    float all = top[0][lane], total = 0.0f;
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) all = fmaxf(all, top[w][lane]);
-    sm.factor[warp][lane] = join_factor(top[warp][lane], all);
-    if (warp == 0) {
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) total += sum[w][lane] * join_factor(top[w][lane], all);
-      sm.all[lane] = all;
-      sm.total[lane] = total;
-    }
-  }
-  __syncwarp();
+  const int row_log = n > 4 ? 3 : n > 2 ? 2 : 1, cols = kMergeFloats >> row_log, ld = cols + 8;
   float *slot = p.parts + ((long long)blockIdx.x * 2 + (ti.flags & kLater ? 1 : 0)) * (kStatFloats + p.rows * D);
-  for (int row0 = 0; row0 < n; row0 += kMergeRows)
-    for (int col0 = 0; col0 < D; col0 += kMergeCols) {
-      if (row0 + col0 > 0 && !consumers_sync(sm, parity)) return false;
-      part.put(row0, col0, sm.factor[warp], sm.merge[warp], D);
-      if (!consumers_sync(sm, parity)) return false;
-      for (int i = threadIdx.x; i < kMergeRows * kMergeCols / 2; i += kWarps * 32) {
-        const int rr = i / (kMergeCols / 2), r = row0 + rr, cc = (i % (kMergeCols / 2)) * 2, c = col0 + cc;
+  for (int row0 = 0; row0 < n; row0 += 1 << row_log)
+    for (int col0 = 0; col0 < D; col0 += cols, ++passes) {
+      if (passes > 0 && !wait(sm, &sm.read, (passes & 1) ^ 1)) return false;
+      if (row0 + col0 == 0) part.stats(sm.top[warp], sm.sum[warp]);
+      part.put(row0, 1 << row_log, col0, cols, ld, sm.merge[warp], D);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.laid);
+      if (!wait(sm, &sm.laid, passes & 1)) return false;
+      const int pairs_log = 31 - __clz(cols) - 1;
+      for (int i = threadIdx.x; i < kMergeFloats / 2; i += kWarps * 32) {
+        const int rr = i >> pairs_log, r = row0 + rr, cc = (i & ((1 << pairs_log) - 1)) * 2, c = col0 + cc;
         if (r >= n || c >= D) continue;
+        float all = sm.top[0][r], total = 0.0f;
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) all = fmaxf(all, sm.top[w][r]);
         float2 x = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-          const float2 y = *reinterpret_cast<const float2 *>(&sm.merge[w][rr][cc]);
-          x.x += y.x;
-          x.y += y.y;
+          const float f = join_factor(sm.top[w][r], all);
+          const float2 y = *reinterpret_cast<const float2 *>(&sm.merge[w][rr * ld + cc]);
+          x.x = fmaf(y.x, f, x.x);
+          x.y = fmaf(y.y, f, x.y);
+          total = fmaf(sm.sum[w][r], f, total);
         }
-        const float total = sm.total[r];
         if (ti.flags & kWhole) {
           const float f = total == 0.0f ? 0.0f : 1.0f / total;
           T *out = reinterpret_cast<T *>(p.a.out + ti.seq * p.a.out_stride) + (long long)(h0 + r) * D + c;
           if (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(out) = pack_bf16(x.x * f, x.y * f);
           else *reinterpret_cast<float2 *>(out) = make_float2(x.x * f, x.y * f);
-          if (p.a.lse != nullptr && c == 0) p.a.lse[(long long)ti.seq * p.a.q_heads + h0 + r] = lse_of(sm.all[r], total);
+          if (p.a.lse != nullptr && c == 0) p.a.lse[(long long)ti.seq * p.a.q_heads + h0 + r] = lse_of(all, total);
         } else {
           *reinterpret_cast<float2 *>(slot + kStatFloats + r * D + c) = x;
-          if (c == 0) *reinterpret_cast<float2 *>(slot + 2 * r) = make_float2(sm.all[r], total);
+          if (c == 0) *reinterpret_cast<float2 *>(slot + 2 * r) = make_float2(all, total);
         }
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.read);
     }
   return true;
 }
@@ -189,8 +177,7 @@ __device__ void consume(const Shape &p, Shared &sm, char *ring, char *qs, float 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = p.chunks * Part::kTile * 128;
   const int q_bytes = slot_rows<Part, T>(p) * p.a.cache.dim * (int)sizeof(T);
   Part part;
-  uint32_t parity = 0;
-  int stage = 0, round = 0, turn = 0;
+  int stage = 0, round = 0, passes = 0;
   auto give_back = [&]() {
     __syncwarp();
     if (lane == 0) mbar_arrive(&sm.empty[stage]);
@@ -211,10 +198,7 @@ __device__ void consume(const Shape &p, Shared &sm, char *ring, char *qs, float 
     if (!wait(sm, &sm.full[stage], round & 1)) return;
     if (mine) part.values(p, weights, ring + (long long)stage * half, warp * Part::kWarpKeys, ti.lo, ti.hi);
     give_back();
-    if (ti.flags & kLast) {
-      if (!finish<Part, T>(p, sm, part, ti, turn, parity)) return;
-      turn ^= 1;
-    }
+    if ((ti.flags & kLast) && !finish<Part, T>(p, sm, part, ti, passes)) return;
   }
 }
 
@@ -329,13 +313,15 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
   Shared &sm = *reinterpret_cast<Shared *>(ring + (long long)p.stages * p.chunks * Part::kTile * 128);
   char *qs = reinterpret_cast<char *>(&sm + 1);
   float *weights = reinterpret_cast<float *>(qs + p.slots * slot_rows<Part, T>(p) * p.a.cache.dim * (int)sizeof(T));
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (tid == 0) {
+    asm volatile("prefetch.tensormap [%0];" :: "l"(&kmap) : "memory");
+    asm volatile("prefetch.tensormap [%0];" :: "l"(&vmap) : "memory");
     for (int i = 0; i < p.stages; ++i) {
       mbar_init(&sm.full[i], 1);
       mbar_init(&sm.empty[i], kWarps);
     }
-    mbar_init(&sm.sync, kWarps);
+    mbar_init(&sm.laid, kWarps);
+    mbar_init(&sm.read, kWarps);
     mbar_init(&sm.never, 1);
     fence_mbar_init();
     sm.flags = 0;
@@ -343,6 +329,7 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
     sm.start_seq = 0;
     sm.job = make_int4(0, 0, 0, 0);
   }
+  grid_begins();
 
   // this CTA's share of all tiles: each thread counts some sequences' tiles; sequences without one have
   // their outputs from the CTA whose turn it is
@@ -419,7 +406,7 @@ constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kJoinBatch = 4
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Shape p) {
   __shared__ float factor[kMaxWorkers], red[kJoinWarps], sums[kJoinWarps][256];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  grid_begins();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = p.a.cache.dim, first = blockIdx.x;
   const int4 job = p.jobs[first];
   const int parts = job.z, kv = job.y / p.passes, pass = job.y - kv * p.passes, r = blockIdx.y;
@@ -524,18 +511,9 @@ cudaError_t launch(Shape p, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   int workers = sm_count() * 2;
   workers = workers < kMaxWorkers ? workers : kMaxWorkers;
-  attend_kernel<Part, T><<<workers, kThreads, smem, s>>>(p, maps[0], maps[1]);
-  if ((e = cudaGetLastError()) != cudaSuccess || a.seq.batch == 0) return e;
-  cudaLaunchConfig_t q = {};
-  q.gridDim = dim3(workers, p.rows);
-  q.blockDim = dim3(kJoinThreads);
-  q.stream = s;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // its launch overlaps the kernel it waits for
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  q.attrs = at;
-  q.numAttrs = 1;
-  return cudaLaunchKernelEx(&q, join_kernel<T>, p);
+  e = launch_early(attend_kernel<Part, T>, dim3(workers), kThreads, smem, s, p, maps[0], maps[1]);
+  if (e != cudaSuccess || a.seq.batch == 0) return e;
+  return launch_early(join_kernel<T>, dim3(workers, p.rows), kJoinThreads, 0, s, p);
 }
 
 }  // namespace

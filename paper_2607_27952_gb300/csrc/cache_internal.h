@@ -104,6 +104,26 @@ size_t attend_scratch_bytes(int q_heads, int kv_heads, int dim);
 int sm_count();
 
 #ifdef __CUDACC__
+// Kernels of the cache are launched as soon as the one before them in the stream has all its CTAs running, and
+// wait here, before they touch memory, for it to end: the launch itself costs nothing then.
+__device__ __forceinline__ void grid_begins() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, const A &...args) {
+  cudaLaunchConfig_t c = {};
+  c.gridDim = grid;
+  c.blockDim = dim3(threads);
+  c.dynamicSmemBytes = smem;
+  c.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = at;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, P(args)...);
+}
 __device__ __forceinline__ void post_status(unsigned *status, unsigned cta, unsigned ctas, unsigned flags) {
   status[kStatusBegin + cta] = flags;
   if (cta == 0) status[0] = kErrList | ctas;

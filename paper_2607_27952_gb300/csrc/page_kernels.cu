@@ -18,6 +18,7 @@ __device__ __forceinline__ int quotient(int x, int n, uint32_t m) {
 // One page of one layer of K or V per step.
 __global__ void __launch_bounds__(kThreads) copy_kernel(const __grid_constant__ PagesArgs p, int n, const int32_t *src,
                                                         const int32_t *dst) {
+  grid_begins();
   unsigned flags = 0;
   const int vec = p.row_bytes / 16, per_page = p.heads * p.page_size * vec;
   const long long items = (long long)n * p.layers * 2;
@@ -55,6 +56,7 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(const __grid_constant__ 
 // the lanes, every warp alike, and dealt out in turn.
 __global__ void __launch_bounds__(kThreads) compact_kernel(const __grid_constant__ CompactArgs a, int rows, uint32_t vec_m,
                                                            uint32_t heads_m) {
+  grid_begins();
   const PagesArgs &p = a.p;
   const int lane = threadIdx.x & 31, ps = p.page_size, vec = p.row_bytes / 16, items = rows * vec;
   const int warps = gridDim.x * (kThreads / 32), me = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
@@ -146,8 +148,7 @@ cudaError_t launch_page_copy(const PagesArgs &args, int n, const int32_t *src, c
   const long long row = p.row_bytes, ps = p.page_size;
   p.packed = (p.token_stride == row && (p.heads == 1 || p.head_stride == row * ps)) ||
              (p.token_stride == row * p.heads && (p.heads == 1 || p.head_stride == row));
-  copy_kernel<<<grid_of((long long)n * p.layers * 2), kThreads, 0, s>>>(p, n, src, dst);
-  return cudaGetLastError();
+  return launch_early(copy_kernel, dim3(grid_of((long long)n * p.layers * 2)), kThreads, 0, s, p, n, src, dst);
 }
 
 cudaError_t launch_compact(const CompactArgs &a, cudaStream_t s) {
@@ -156,8 +157,8 @@ cudaError_t launch_compact(const CompactArgs &a, cudaStream_t s) {
     return most * n < 1LL << 32 ? (uint32_t)(((1ull << 32) + (unsigned)n - 1) / (unsigned)n) : 0u;
   };
   const long long most = (long long)a.seq.batch * a.dst_max_pages * a.p.page_size * rows * vec / (32 * kBatch);   // units
-  compact_kernel<<<grid_of(most / (kThreads / 32) + 1), kThreads, 0, s>>>(a, rows, magic((long long)rows * vec, vec), magic(rows, a.p.heads));
-  return cudaGetLastError();
+  return launch_early(compact_kernel, dim3(grid_of(most / (kThreads / 32) + 1)), kThreads, 0, s, a, rows,
+                      magic((long long)rows * vec, vec), magic(rows, a.p.heads));
 }
 
 }  // namespace last

@@ -171,6 +171,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) rotary_kernel(const __grid_co
   }
   if (APPEND && threadIdx.x == 0) flags = 0;
   __syncthreads();
+  grid_begins();
 
   const bool across = w.columns > 1;
   const int sub = across ? 0 : lane / w.items;                       // row of the group
@@ -311,12 +312,11 @@ bool rows_aligned(const HeadRows &h, int bytes, bool out) {
 }
 
 template <typename T, int VEC>
-void launch(const RotaryArgs &a, int grid, const Split &w, cudaStream_t s) {
-  auto go = [&](auto kernel) { kernel<<<grid, kThreads, 0, s>>>(a, w); };
+cudaError_t launch(const RotaryArgs &a, int grid, const Split &w, cudaStream_t s) {
+  auto go = [&](auto kernel) { return launch_early(kernel, dim3(grid), kThreads, 0, s, a, w); };
   if (a.rot.adjacent)
-    a.append ? go(rotary_kernel<T, VEC, true, true>) : go(rotary_kernel<T, VEC, true, false>);
-  else
-    a.append ? go(rotary_kernel<T, VEC, false, true>) : go(rotary_kernel<T, VEC, false, false>);
+    return a.append ? go(rotary_kernel<T, VEC, true, true>) : go(rotary_kernel<T, VEC, true, false>);
+  return a.append ? go(rotary_kernel<T, VEC, false, true>) : go(rotary_kernel<T, VEC, false, false>);
 }
 
 }  // namespace
@@ -354,14 +354,11 @@ cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t s) {
   if (a.append && grid > kMaxStatus) grid = kMaxStatus;   // a status word each
   if (grid < 1) grid = 1;
   const int g = (int)grid;
-  if (a.elem == 4) {
-    vec == 4 ? launch<float, 4>(a, g, w, s) : vec == 2 ? launch<float, 2>(a, g, w, s) : launch<float, 1>(a, g, w, s);
-  } else {
-    using B = __nv_bfloat16;
-    vec == 8 ? launch<B, 8>(a, g, w, s) : vec == 4 ? launch<B, 4>(a, g, w, s)
-    : vec == 2 ? launch<B, 2>(a, g, w, s) : launch<B, 1>(a, g, w, s);
-  }
-  return cudaGetLastError();
+  if (a.elem == 4)
+    return vec == 4 ? launch<float, 4>(a, g, w, s) : vec == 2 ? launch<float, 2>(a, g, w, s) : launch<float, 1>(a, g, w, s);
+  using B = __nv_bfloat16;
+  return vec == 8 ? launch<B, 8>(a, g, w, s) : vec == 4 ? launch<B, 4>(a, g, w, s)
+         : vec == 2 ? launch<B, 2>(a, g, w, s) : launch<B, 1>(a, g, w, s);
 }
 
 }  // namespace last
