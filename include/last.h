@@ -340,7 +340,8 @@ last_status last_cache_append(const last_cache *c, int32_t layer, const last_seq
  * may be anything).  q-head h reads kv-head h / (num_q_heads / num_kv_heads).  q and out:
  * [batch][num_q_heads][head_dim], sequences q_stride and out_stride elements apart, both multiples
  * of 16 bytes, 16-byte aligned.  scale <= 0 selects 1/sqrt(head_dim).  Results do not depend on
- * other calls or on timing: repeated calls give the same bits. */
+ * other calls or on timing: repeated calls give the same bits.  batch * num_q_heads *
+ * (max_pages * page_size / 32 + 1) must stay below 2^31 (LAST_ERR_UNSUPPORTED). */
 last_status last_cache_attention(const last_cache *c, int32_t layer, const last_sequences *s,
                                  int32_t num_q_heads, float scale, const void *q, int64_t q_stride,
                                  void *out, int64_t out_stride, float *lse, void *ws,

@@ -27,6 +27,7 @@ struct Shape {      // the same for every CTA
   int box_log, chunks;        // rows of a TMA box; 128-byte columns of a row
   int stages, slots;          // ring; parts whose q is kept
   bool joined;                // a box holds all of them
+  int page_log;               // of the page size, -1 if it is no power of two
   int tile;                   // keys
   int rows;                   // heads of a pass at most
   float scale2;               // scale log2 e
@@ -56,14 +57,22 @@ struct TileInfo {   // what the producer says of a tile
 constexpr int kFirst = 1, kLast = 2, kWhole = 4, kLater = 8;
 constexpr int kStatFloats = 2 * kRows;   // of a parted sum: maximum and denominator per head, then the rows
 
+struct Keys {
+  int begin, end;
+};
+struct Walk {   // tile `at` of the `tiles` of sequence seq, pass head
+  int seq, head, at, tiles;
+  Keys keys;
+};
+
 struct alignas(16) Shared {
   unsigned long long full[kMaxStages], empty[kMaxStages], laid, read, never;
   TileInfo info[kMaxStages];
   float top[kWarps][kRows], sum[kWarps][kRows];
   alignas(16) float merge[kWarps][kMergeFloats + 8 * 8];   // rows 8 floats apart
   int4 job;
-  long long warp_tiles[kWarps + 1], start_first;
-  int start_seq;
+  Walk start;
+  unsigned warp_tiles[kWarps + 1];
   unsigned flags;
   volatile unsigned dead;
 };
@@ -86,9 +95,6 @@ __device__ __forceinline__ bool wait(Shared &sm, unsigned long long *bar, uint32
   return false;
 }
 
-struct Keys {
-  int begin, end;
-};
 __device__ __forceinline__ Keys keys_of(const AttendArgs &a, int b, unsigned *bad) {
   const long long room = (long long)a.seq.max_pages * a.cache.page_size;
   int end = a.seq.lens[b], begin = a.seq.begin ? a.seq.begin[b] : 0;
@@ -202,10 +208,6 @@ __device__ void consume(const Shape &p, Shared &sm, char *ring, char *qs, float 
   }
 }
 
-struct Walk {   // tile `at` of the `tiles` of sequence seq, pass head
-  int seq, head, at, tiles;
-  Keys keys;
-};
 __device__ __forceinline__ void advance(const Shape &p, Walk &w) {
   unsigned bad = 0;
   if (++w.at < w.tiles) return;
@@ -225,7 +227,7 @@ __device__ __forceinline__ void advance(const Shape &p, Walk &w) {
 // comes again, as many tiles lie between and the last K of its part has been given back.
 template <typename Part, typename T>
 __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const CUtensorMap *kmap, const CUtensorMap *vmap,
-                        Walk w, int tiles, long long upto, long long total, long long shares) {
+                        Walk w, int tiles, unsigned upto, unsigned total, unsigned shares) {
   constexpr int kTile = Part::kTile;
   const int lane = threadIdx.x & 31, box = 1 << p.box_log, boxes = kTile >> p.box_log, mine = lane & (boxes - 1);
   const int ops = boxes * (p.joined ? 1 : p.chunks), half = p.chunks * kTile * 128;
@@ -233,7 +235,8 @@ __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const 
   auto box_key = [&](const Walk &x) { return (x.keys.begin / kTile + x.at) * kTile + mine * box; };
   auto counts = [&](const Walk &x) { return box_key(x) < x.keys.end && box_key(x) + box > x.keys.begin; };
   auto lookup = [&](const Walk &x) {   // page of this lane's box, as the table has it
-    return counts(x) ? p.a.seq.table[x.seq * p.a.seq.table_stride + box_key(x) / size] : 0;
+    const int key = box_key(x);
+    return counts(x) ? p.a.seq.table[x.seq * p.a.seq.table_stride + (p.page_log >= 0 ? key >> p.page_log : key / size)] : 0;
   };
   int page = lookup(w), next_page = 0, stage = 0, round = 0, slot = 0;
   bool fresh = true, later = false, begun = false;
@@ -246,7 +249,8 @@ __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const 
     const bool last = it + 1 == tiles || w.at + 1 == w.tiles, here = counts(w);
     if (fresh) begun = w.at == 0;
     const int bytes = __popc(__ballot_sync(~0u, lane < boxes && here)) * p.chunks * box * 128;
-    const int kv = w.head / p.passes, row = box_key(w) % size;
+    const int kv = p.passes == 1 ? w.head : w.head / p.passes;
+    const int row = p.page_log >= 0 ? box_key(w) & (size - 1) : box_key(w) % size;
 #pragma unroll
     for (int is_v = 0; is_v < 2; ++is_v) {
       if (round > 0 && !wait(sm, &sm.empty[stage], (round & 1) ^ 1)) return;
@@ -293,7 +297,7 @@ __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const 
       }
     }
     if (it + 1 == tiles && begun && w.at + 1 < w.tiles && lane == 0) {   // begun here, goes on in the next shares
-      const long long end = upto + (w.tiles - 1 - w.at);
+      const unsigned long long end = (unsigned long long)upto + (unsigned)(w.tiles - 1 - w.at);
       sm.job = make_int4(w.seq, w.head, (int)((end * shares - 1) / total) - (int)blockIdx.x + 1, later);
     }
     fresh = last;
@@ -326,54 +330,59 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
     fence_mbar_init();
     sm.flags = 0;
     sm.dead = 0;
-    sm.start_seq = 0;
     sm.job = make_int4(0, 0, 0, 0);
   }
   grid_begins();
 
   // this CTA's share of all tiles: each thread counts some sequences' tiles; sequences without one have
   // their outputs from the CTA whose turn it is
-  unsigned bad = 0;
+  unsigned bad = 0, mine = 0;
   const int per = (B + kThreads - 1) / kThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
-  long long mine = 0;
   for (int b = b0; b < b1; ++b) {
     const int n = tiles_of(keys_of(p.a, b, &bad), p.tile);
-    mine += (long long)n * p.heads;
+    mine += (unsigned)n * p.heads;
     if (n == 0 && b % gridDim.x == blockIdx.x) {
       uint4 *out = reinterpret_cast<uint4 *>(p.a.out + b * p.a.out_stride);
+#pragma unroll 1
       for (int i = 0; i < p.a.q_heads * p.a.cache.dim * (int)sizeof(T) / 16; ++i) out[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll 1
       for (int i = 0; i < p.a.q_heads && p.a.lse != nullptr; ++i) p.a.lse[(long long)b * p.a.q_heads + i] = -INFINITY;
     }
   }
-  long long upto = mine;
+  unsigned upto = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const long long x = __shfl_up_sync(~0u, upto, d);
+    const unsigned x = __shfl_up_sync(~0u, upto, d);
     if (lane >= d) upto += x;
   }
   if (lane == 31) sm.warp_tiles[warp] = upto;
   __syncthreads();
   if (bad) atomicOr(&sm.flags, bad);
-  long long total = 0;
+  unsigned total = 0;
   for (int w = 0; w <= kWarps; ++w) {
     if (w < warp) upto += sm.warp_tiles[w];
     total += sm.warp_tiles[w];
   }
   // share w: the tiles total w / shares up to total (w + 1) / shares.  None is empty: with fewer tiles than
   // CTAs the last CTAs have none
-  const long long shares = total < gridDim.x ? total : gridDim.x;
-  const long long t0 = blockIdx.x < shares ? total * blockIdx.x / shares : total;
-  const long long t1 = blockIdx.x < shares ? total * (blockIdx.x + 1) / shares : total;
-  if (t0 < t1 && t0 >= upto - mine && t0 < upto) {
-    long long at = upto - mine;
+  const unsigned shares = min(total, gridDim.x), whole = shares > 0 ? total / shares : 0, rest = total - whole * shares;
+  const bool some = blockIdx.x < shares;
+  const unsigned t0 = some ? whole * blockIdx.x + rest * blockIdx.x / shares : total;
+  const unsigned t1 = some ? whole * (blockIdx.x + 1) + rest * (blockIdx.x + 1) / shares : total;
+  if (some && t0 >= upto - mine && t0 < upto) {
+    unsigned at = t0 - (upto - mine);
     for (int b = b0; b < b1; ++b) {
-      const long long n = (long long)tiles_of(keys_of(p.a, b, &bad), p.tile) * p.heads;
-      if (t0 < at + n) {
-        sm.start_seq = b;
-        sm.start_first = at;
+      Walk w;
+      w.keys = keys_of(p.a, b, &bad);
+      w.tiles = tiles_of(w.keys, p.tile);
+      if (at < (unsigned)w.tiles * p.heads) {
+        w.seq = b;
+        w.head = (int)(at / (unsigned)w.tiles);
+        w.at = (int)(at - (unsigned)w.head * w.tiles);
+        sm.start = w;
         break;
       }
-      at += n;
+      at -= (unsigned)w.tiles * p.heads;
     }
   }
   __syncthreads();
@@ -381,14 +390,7 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
   const int tiles = (int)(t1 - t0);
   if (tiles > 0) {
     if (warp == kWarps) {
-      Walk w;
-      w.seq = sm.start_seq;
-      w.keys = keys_of(p.a, w.seq, &bad);
-      w.tiles = tiles_of(w.keys, p.tile);
-      const long long at = t0 - sm.start_first;
-      w.head = (int)(at / w.tiles);
-      w.at = (int)(at - (long long)w.head * w.tiles);
-      produce<Part, T>(p, sm, ring, qs, &kmap, &vmap, w, tiles, t1, total, shares);
+      produce<Part, T>(p, sm, ring, qs, &kmap, &vmap, sm.start, tiles, t1, total, shares);
     } else {
       consume<Part, T>(p, sm, ring, qs, weights, tiles);
     }
@@ -486,6 +488,7 @@ cudaError_t launch(Shape p, cudaStream_t s) {
   p.box_log = 0;
   while ((2 << p.box_log) <= Part::kTile && c.page_size % (2 << p.box_log) == 0) ++p.box_log;
   p.joined = c.dim * (int)sizeof(T) % 128 == 0;
+  p.page_log = (c.page_size & (c.page_size - 1)) == 0 ? __builtin_ctz((unsigned)c.page_size) : -1;
   // two CTAs share an SM
   const size_t half = (size_t)p.chunks * Part::kTile * 128, q_slot = (size_t)slot_rows<Part, T>(p) * c.dim * sizeof(T);
   const size_t fixed = 1024 + sizeof(Shared) + (sizeof(T) == 4 ? kWarps * 8 * Part::kHeadRows * sizeof(float) : 0);

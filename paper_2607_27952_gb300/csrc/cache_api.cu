@@ -309,6 +309,10 @@ last_status last_cache_attention(const last_cache *c, int32_t layer, const last_
       return invalid("num_q_heads must be a positive multiple of num_kv_heads");
     if (num_q_heads > 8192) return fail(LAST_ERR_UNSUPPORTED, "num_q_heads must be at most 8192");
     const int e = elem_bytes(c->dtype);
+    // tiles of 32 keys and more are counted in 32 bits
+    const double tiles = ((double)s->max_pages * c->page_size / 32 + 1) * s->batch * num_q_heads;
+    if (tiles >= 2147483648.0)
+      return fail(LAST_ERR_UNSUPPORTED, "batch * num_q_heads * (max_pages * page_size / 32 + 1) must stay below 2^31");
     if (s->batch > 0 && (q == nullptr || out == nullptr)) return invalid("q and out are required");
     if (!aligned(q, 16) || !aligned(out, 16)) return invalid("q and out must be 16-byte aligned");
     if (!multiple16(q_stride * e) || !multiple16(out_stride * e))
