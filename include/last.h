@@ -335,7 +335,7 @@ last_status last_cache_append(const last_cache *c, int32_t layer, const last_seq
 /* Attention of one new token per sequence over its cached keys key_begin[b] .. lens[b]-1, in
  * one layer: out = sum_p softmax_p(scale q.k_p) v_p for every q-head, lse (may be NULL) [batch]
  * [num_q_heads] fp32 = log sum_p exp(scale q.k_p).  A sequence without such a key gets out = 0
- * and lse = -inf; keys whose logits are -inf take no part.  Slots outside the range are
+ * and lse = -inf, and so does one whose logits are all -inf; a key of logit -inf has weight 0.  Slots outside the range are
  * never used, whatever they hold, and pages wholly outside it are not read (their table entries
  * may be anything).  q-head h reads kv-head h / (num_q_heads / num_kv_heads).  q and out:
  * [batch][num_q_heads][head_dim], sequences q_stride and out_stride elements apart, both multiples

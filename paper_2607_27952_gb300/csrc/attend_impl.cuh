@@ -40,11 +40,11 @@ cudaError_t launch_attend_bf16(const Shape &p, cudaStream_t s);
 namespace {
 
 constexpr int kWarps = 4;                      // consumers: a quarter of every tile each
-constexpr int kThreads = 32 * (kWarps + 1);
+constexpr int kThreads = 32 * (kWarps + 2);    // and one to load, one to add up
 constexpr int kRows = 16;                      // query heads of one pass over a kv-head
 constexpr int kMaxWorkers = 320;               // CTAs
 constexpr int kMaxStages = 12;                 // of the ring: K or V of a tile each
-constexpr int kMergeFloats = 512;              // of each warp's sums laid down at a time: 8 x 64, 4 x 128 or 2 x 256
+constexpr int kMergeFloats = 512;              // of a warp's sums laid down at a time: 8 x 64, 4 x 128 or 2 x 256
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct TileInfo {   // what the producer says of a tile
@@ -54,7 +54,7 @@ struct TileInfo {   // what the producer says of a tile
 };
 // First and last tile of the CTA's part of a (sequence, head); the part is all of it; it is not the
 // CTA's first one.
-constexpr int kFirst = 1, kLast = 2, kWhole = 4, kLater = 8;
+constexpr int kFirst = 1, kLast = 2, kWhole = 4, kLater = 8, kEnd = 16;   // kEnd: the CTA's last tile
 constexpr int kStatFloats = 2 * kRows;   // of a parted sum: maximum and denominator per head, then the rows
 
 struct Keys {
@@ -65,14 +65,20 @@ struct Walk {   // tile `at` of the `tiles` of sequence seq, pass head
   Keys keys;
 };
 
-struct alignas(16) Shared {
-  unsigned long long full[kMaxStages], empty[kMaxStages], laid, read, never;
-  TileInfo info[kMaxStages];
+struct alignas(16) Merge {
+  float rows[kWarps][kMergeFloats + 8 * 8];   // 8 floats apart
   float top[kWarps][kRows], sum[kWarps][kRows];
-  alignas(16) float merge[kWarps][kMergeFloats + 8 * 8];   // rows 8 floats apart
+  unsigned long long laid, read;
+  TileInfo info;
+};
+
+struct alignas(16) Shared {
+  unsigned long long full[kMaxStages], empty[kMaxStages], never;
+  TileInfo info[kMaxStages];
+  Merge merge[2];
   int4 job;
   Walk start;
-  unsigned warp_tiles[kWarps + 1];
+  unsigned warp_tiles[kWarps + 2];
   unsigned flags;
   volatile unsigned dead;
 };
@@ -122,56 +128,90 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
 __device__ __forceinline__ float join_factor(float top, float all) { return top == -INFINITY ? 1.0f : exp2_fast(top - all); }
 __device__ __forceinline__ float lse_of(float top, float sum) { return sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * kLn2; }
 
-// Adds up the warps' sums of the CTA's part of a (sequence, head): to the output where the part is
-// all of it, else to the workspace.  As many rows and columns at a time as the buffer holds: each warp
-// lays its own down, one barrier, and every thread scales and adds what it writes.  A second barrier
-// says that the buffer has been read; it is waited for at the next use.
-template <typename Part, typename T>
-__device__ bool finish(const Shape &p, Shared &sm, Part &part, const TileInfo &ti, int &passes) {
+// The warps' sums of the CTA's part of a (sequence, head) are added up by a warp of its own, as many rows
+// and columns at a time as a buffer holds, while the others go on with the next part.  Two buffers by turns.
+struct Pass {   // the same sequence of passes on both sides
+  int row_log, cols, ld;   // rows and columns at a time
+  __device__ Pass(int n) : row_log(n > 4 ? 3 : n > 2 ? 2 : 1), cols(kMergeFloats >> row_log), ld(cols + 8) {}
+};
+
+template <typename Part>
+__device__ bool lay_down(const Shape &p, Shared &sm, Part &part, const TileInfo &ti, int &passes) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = p.a.cache.dim;
-  const int kv = ti.head / p.passes, pass = ti.head - kv * p.passes;
-  const int h0 = kv * p.group + pass * kRows, n = min(kRows, p.group - pass * kRows);
-  const int row_log = n > 4 ? 3 : n > 2 ? 2 : 1, cols = kMergeFloats >> row_log, ld = cols + 8;
-  float *slot = p.parts + ((long long)blockIdx.x * 2 + (ti.flags & kLater ? 1 : 0)) * (kStatFloats + p.rows * D);
-  for (int row0 = 0; row0 < n; row0 += 1 << row_log)
-    for (int col0 = 0; col0 < D; col0 += cols, ++passes) {
-      if (passes > 0 && !wait(sm, &sm.read, (passes & 1) ^ 1)) return false;
-      if (row0 + col0 == 0) part.stats(sm.top[warp], sm.sum[warp]);
-      part.put(row0, 1 << row_log, col0, cols, ld, sm.merge[warp], D);
+  const int n = min(kRows, p.group - ti.head % p.passes * kRows);
+  const Pass s(n);
+  for (int row0 = 0; row0 < n; row0 += 1 << s.row_log)
+    for (int col0 = 0; col0 < D; col0 += s.cols, ++passes) {
+      Merge &m = sm.merge[passes & 1];
+      if (passes > 1 && !wait(sm, &m.read, (passes >> 1 & 1) ^ 1)) return false;
+      part.stats(m.top[warp], m.sum[warp]);
+      part.put(row0, 1 << s.row_log, col0, s.cols, s.ld, m.rows[warp], D);
+      if (threadIdx.x == 0) m.info = ti;
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.laid);
-      if (!wait(sm, &sm.laid, passes & 1)) return false;
-      const int pairs_log = 31 - __clz(cols) - 1;
-      for (int i = threadIdx.x; i < kMergeFloats / 2; i += kWarps * 32) {
-        const int rr = i >> pairs_log, r = row0 + rr, cc = (i & ((1 << pairs_log) - 1)) * 2, c = col0 + cc;
-        if (r >= n || c >= D) continue;
-        float all = sm.top[0][r], total = 0.0f;
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) all = fmaxf(all, sm.top[w][r]);
-        float2 x = make_float2(0.0f, 0.0f);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float f = join_factor(sm.top[w][r], all);
-          const float2 y = *reinterpret_cast<const float2 *>(&sm.merge[w][rr * ld + cc]);
-          x.x = fmaf(y.x, f, x.x);
-          x.y = fmaf(y.y, f, x.y);
-          total = fmaf(sm.sum[w][r], f, total);
-        }
-        if (ti.flags & kWhole) {
-          const float f = total == 0.0f ? 0.0f : 1.0f / total;
-          T *out = reinterpret_cast<T *>(p.a.out + ti.seq * p.a.out_stride) + (long long)(h0 + r) * D + c;
-          if (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(out) = pack_bf16(x.x * f, x.y * f);
-          else *reinterpret_cast<float2 *>(out) = make_float2(x.x * f, x.y * f);
-          if (p.a.lse != nullptr && c == 0) p.a.lse[(long long)ti.seq * p.a.q_heads + h0 + r] = lse_of(all, total);
-        } else {
-          *reinterpret_cast<float2 *>(slot + kStatFloats + r * D + c) = x;
-          if (c == 0) *reinterpret_cast<float2 *>(slot + 2 * r) = make_float2(all, total);
-        }
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.read);
+      if (lane == 0) mbar_arrive(&m.laid);
     }
   return true;
+}
+
+// To the output where the part is all of its (sequence, head), else to the workspace.
+template <typename T>
+__device__ void add_up(const Shape &p, Shared &sm) {
+  const int lane = threadIdx.x & 31, D = p.a.cache.dim;
+  for (int passes = 0, flags = 0; !(flags & kEnd);) {
+    if (!wait(sm, &sm.merge[passes & 1].laid, passes >> 1 & 1)) return;
+    const TileInfo ti = sm.merge[passes & 1].info;
+    flags = ti.flags;
+    const int kv = ti.head / p.passes, pass = ti.head - kv * p.passes;
+    const int h0 = kv * p.group + pass * kRows, n = min(kRows, p.group - pass * kRows);
+    const Pass s(n);
+    float *slot = p.parts + ((long long)blockIdx.x * 2 + (flags & kLater ? 1 : 0)) * (kStatFloats + p.rows * D);
+    T *out = reinterpret_cast<T *>(p.a.out + ti.seq * p.a.out_stride) + (long long)h0 * D;
+    for (int row0 = 0; row0 < n; row0 += 1 << s.row_log)
+      for (int col0 = 0; col0 < D; col0 += s.cols, ++passes) {
+        Merge &m = sm.merge[passes & 1];
+        if (row0 + col0 > 0 && !wait(sm, &m.laid, passes >> 1 & 1)) return;
+        // lane: warp lane / 8, row lane % 8
+        const int w = lane >> 3, r = row0 + (lane & 7);
+        const bool live = r < n && (lane & 7) < 1 << s.row_log;
+        const float top = live ? m.top[w][r] : -INFINITY;
+        float all = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+        all = fmaxf(all, __shfl_xor_sync(~0u, all, 16));
+        const float f = join_factor(top, all);
+        float total = live ? m.sum[w][r] * f : 0.0f;
+        total += __shfl_xor_sync(~0u, total, 8);
+        total += __shfl_xor_sync(~0u, total, 16);
+        const float g = flags & kWhole ? 1.0f / total : 1.0f;
+        if (w == 0 && live && col0 == 0) {
+          if (!(flags & kWhole)) *reinterpret_cast<float2 *>(slot + 2 * r) = make_float2(all, total);
+          else if (p.a.lse != nullptr) p.a.lse[(long long)ti.seq * p.a.q_heads + h0 + r] = lse_of(all, total);
+        }
+        const int cols = min(s.cols, D - col0), rows = min(n - row0, 1 << s.row_log);
+        for (int rr = 0; rr < rows; ++rr) {
+          float fw[kWarps];
+#pragma unroll
+          for (int i = 0; i < kWarps; ++i) fw[i] = __shfl_sync(~0u, f * g, i * 8 + rr);
+          const bool none = (flags & kWhole) && __shfl_sync(~0u, total, rr) == 0.0f;   // no key has a weight
+          for (int c = lane * 4; c < cols; c += 128) {
+            float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) {
+              const float4 y = *reinterpret_cast<const float4 *>(&m.rows[i][rr * s.ld + c]);
+              x.x = fmaf(y.x, fw[i], x.x);
+              x.y = fmaf(y.y, fw[i], x.y);
+              x.z = fmaf(y.z, fw[i], x.z);
+              x.w = fmaf(y.w, fw[i], x.w);
+            }
+            if (none) x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            const long long at = (long long)(row0 + rr) * D + col0 + c;
+            if (!(flags & kWhole)) *reinterpret_cast<float4 *>(slot + kStatFloats + at) = x;
+            else if (sizeof(T) == 4) *reinterpret_cast<float4 *>(out + at) = x;
+            else *reinterpret_cast<uint2 *>(out + at) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&m.read);
+      }
+  }
 }
 
 // Rows of a slot for q: the fp32 consumers read as many heads as they hold.
@@ -204,7 +244,7 @@ __device__ void consume(const Shape &p, Shared &sm, char *ring, char *qs, float 
     if (!wait(sm, &sm.full[stage], round & 1)) return;
     if (mine) part.values(p, weights, ring + (long long)stage * half, warp * Part::kWarpKeys, ti.lo, ti.hi);
     give_back();
-    if ((ti.flags & kLast) && !finish<Part, T>(p, sm, part, ti, passes)) return;
+    if ((ti.flags & kLast) && !lay_down(p, sm, part, ti, passes)) return;
   }
 }
 
@@ -266,7 +306,8 @@ __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const 
           ti.head = w.head;
           ti.lo = w.keys.begin - k0;
           ti.hi = w.keys.end - k0;
-          ti.flags = (fresh ? kFirst : 0) | (last ? kLast : 0) | (begun && w.at + 1 == w.tiles ? kWhole : 0) | (later ? kLater : 0);
+          ti.flags = (fresh ? kFirst : 0) | (last ? kLast : 0) | (begun && w.at + 1 == w.tiles ? kWhole : 0) | (later ? kLater : 0) |
+                     (it + 1 == tiles ? kEnd : 0);
           ti.slot = slot;
           sm.info[stage] = ti;
           const int q_bytes = fresh ? min(kRows, p.group - pass * kRows) * row_bytes : 0;
@@ -324,8 +365,10 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
       mbar_init(&sm.full[i], 1);
       mbar_init(&sm.empty[i], kWarps);
     }
-    mbar_init(&sm.laid, kWarps);
-    mbar_init(&sm.read, kWarps);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sm.merge[i].laid, kWarps);
+      mbar_init(&sm.merge[i].read, 1);
+    }
     mbar_init(&sm.never, 1);
     fence_mbar_init();
     sm.flags = 0;
@@ -359,7 +402,7 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
   __syncthreads();
   if (bad) atomicOr(&sm.flags, bad);
   unsigned total = 0;
-  for (int w = 0; w <= kWarps; ++w) {
+  for (int w = 0; w < kWarps + 2; ++w) {
     if (w < warp) upto += sm.warp_tiles[w];
     total += sm.warp_tiles[w];
   }
@@ -389,11 +432,9 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
 
   const int tiles = (int)(t1 - t0);
   if (tiles > 0) {
-    if (warp == kWarps) {
-      produce<Part, T>(p, sm, ring, qs, &kmap, &vmap, sm.start, tiles, t1, total, shares);
-    } else {
-      consume<Part, T>(p, sm, ring, qs, weights, tiles);
-    }
+    if (warp == kWarps) produce<Part, T>(p, sm, ring, qs, &kmap, &vmap, sm.start, tiles, t1, total, shares);
+    else if (warp > kWarps) add_up<T>(p, sm);
+    else consume<Part, T>(p, sm, ring, qs, weights, tiles);
   }
   __syncthreads();
   if (sm.dead && tid < 32) wait_out(&sm.never);   // copies that nobody waited for
