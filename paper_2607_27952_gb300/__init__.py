@@ -412,29 +412,30 @@ def last_status_string(st: int) -> str:
 
 # ---- rotary positions and the key-value cache ----
 
-_CODES, _INT32 = {}, None
+_CODES, _INT32, _F32 = {}, None, None
+
+
+def _dtypes():
+    """torch's types, looked up once."""
+    global _INT32, _F32
+    import torch
+    _CODES.update({torch.float32: LAST_DTYPE_F32, torch.bfloat16: LAST_DTYPE_BF16})
+    _INT32, _F32 = torch.int32, torch.float32
 
 
 def _code(dtype) -> int:
     if not _CODES:
-        import torch
-        _CODES.update({torch.float32: LAST_DTYPE_F32, torch.bfloat16: LAST_DTYPE_BF16})
+        _dtypes()
     if dtype not in _CODES:
         raise ValueError(f"liblast takes float32 and bfloat16 tensors, not {dtype}")
     return _CODES[dtype]
 
 
-def _dtype_name(t) -> str:
-    return str(t.dtype).rpartition(".")[2]
-
-
 def _int32(t, name: str, shape=None):
     """A device int32 tensor whose last dimension is contiguous."""
-    global _INT32
     if _INT32 is None:
-        import torch
-        _INT32 = torch.int32
-    if t.dtype != _INT32 or not t.is_cuda or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        _dtypes()
+    if t.dtype is not _INT32 or not t.is_cuda or (t.stride(-1) != 1 and t.shape[-1] > 1):
         raise ValueError(f"{name}: a device int32 tensor with a contiguous last dimension expected")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
@@ -475,6 +476,7 @@ class Cache:
     tokens outside heads, transposed) do as well, of both tensors alike."""
 
     def __init__(self, k, v):
+        _code(k.dtype)
         if k.dim() != 5 or v.shape != k.shape or not k.is_cuda or not v.is_cuda:
             raise ValueError("k and v: device tensors [layers][pages][kv_heads][page_size][head_dim] expected")
         if k.dtype != v.dtype or k.stride() != v.stride() or (k.shape[4] > 1 and k.stride(4) != 1):
@@ -508,12 +510,12 @@ class Sequences:
 def _heads(x, out, dtype, dim, name):
     """last_heads of a [tokens][heads][dim] tensor and, optionally, its output."""
     shape, strides = x.shape, x.stride()
-    if len(shape) != 3 or shape[2] != dim or x.dtype != dtype or not x.is_cuda or (strides[2] != 1 and dim > 1):
+    if len(shape) != 3 or shape[2] != dim or x.dtype is not dtype or not x.is_cuda or (strides[2] != 1 and dim > 1):
         raise ValueError(f"{name}: a device tensor [tokens][heads][{dim}] of {dtype}, the last dimension contiguous, expected")
     if out is None:
         return _Heads(x.data_ptr(), None, shape[1], strides[0], strides[1], 0, 0)
     outs = out.stride()
-    if out.shape != shape or out.dtype != dtype or not out.is_cuda or (outs[2] != 1 and dim > 1):
+    if out.shape != shape or out.dtype is not dtype or not out.is_cuda or (outs[2] != 1 and dim > 1):
         raise ValueError(f"{name}_out: a tensor like {name} expected")
     return _Heads(x.data_ptr(), out.data_ptr(), shape[1], strides[0], strides[1], outs[0], outs[1])
 
@@ -590,11 +592,11 @@ def last_cache_attention(cache: Cache, layer: int, seqs: Sequences, q, out, ws, 
     if len(shape) != 3 or shape[0] != seqs.batch or shape[2] != d or out.shape != shape:
         raise ValueError(f"q and out: [{seqs.batch}][q_heads][{d}] expected")
     heads, qs, os_ = shape[1], q.stride(), out.stride()
-    if (q.dtype != dtype or out.dtype != dtype or not q.is_cuda or not out.is_cuda or qs[2] != 1 or os_[2] != 1
+    if (q.dtype is not dtype or out.dtype is not dtype or not q.is_cuda or not out.is_cuda or qs[2] != 1 or os_[2] != 1
             or (heads > 1 and (qs[1] != d or os_[1] != d))):
         raise ValueError("q and out: device tensors of the cache's dtype, [q_heads][head_dim] contiguous, expected")
-    if lse is not None and (lse.shape != shape[:2] or not lse.is_contiguous() or not lse.is_cuda
-                            or _dtype_name(lse) != "float32"):
+    if lse is not None and (lse.dtype is not _F32 or lse.shape != (shape[0], heads) or not lse.is_contiguous()
+                            or not lse.is_cuda):
         raise ValueError("lse: a contiguous device float32 tensor [batch][q_heads] expected")
     p, n = _ws(ws)
     _check(load_library().last_cache_attention(

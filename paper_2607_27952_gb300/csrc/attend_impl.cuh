@@ -550,8 +550,7 @@ cudaError_t launch(Shape p, cudaStream_t s) {
     if (!encode_rows_map(&maps[i], i ? c.v : c.k, sizeof(T) == 4, p.joined ? 5 : 4, p.joined ? dims5 : dims,
                          p.joined ? strides5 : strides, p.joined ? box5 : box))
       return cudaErrorInvalidValue;
-  const void *fn = reinterpret_cast<const void *>(&attend_kernel<Part, T>);
-  cudaError_t e = allow_smem(fn, smem);
+  cudaError_t e = allow_smem(reinterpret_cast<const void *>(&attend_kernel<Part, T>), smem);
   if (e != cudaSuccess) return e;
   int workers = sm_count() * 2;
   workers = workers < kMaxWorkers ? workers : kMaxWorkers;

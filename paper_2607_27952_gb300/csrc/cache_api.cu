@@ -55,9 +55,10 @@ last_status check_dtype(int32_t dtype) {
 // f / (2 pi) modulo 1 in units of 2^-64: the 24-bit significand times 1/(2 pi) to 128 bits
 // after the point, in integers (the same on every host).
 unsigned long long turn_of(float f) {
-  int e = 0;
-  const unsigned long long m = (unsigned long long)std::ldexp((double)std::frexp(f, &e), 24);
-  e -= 24;                                            // f = m 2^e
+  uint32_t u;
+  std::memcpy(&u, &f, sizeof u);
+  const int biased = (int)(u >> 23 & 255), e = biased == 0 ? -149 : biased - 150;   // f = m 2^e
+  const unsigned long long m = (u & 0x7fffffu) | (biased == 0 ? 0u : 0x800000u);
   constexpr unsigned long long kHi = 0x28be60db9391054aull, kLo = 0x7f09d5f47d4d3770ull;
   const unsigned __int128 lo = (unsigned __int128)m * kLo;
   const unsigned __int128 hi = (unsigned __int128)m * kHi + (unsigned long long)(lo >> 64);
