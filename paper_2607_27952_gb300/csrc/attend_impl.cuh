@@ -31,7 +31,8 @@ struct Shape {      // the same for every CTA
   int tile;                   // keys
   int rows;                   // heads of a pass at most
   float scale2;               // scale log2 e
-  int4 *jobs;                 // [CTAs] sequence, head, parts (0: nothing to join), slot of the first
+  int4 *jobs;                 // [CTAs] of the (sequence, head) that a CTA's share ends within: these, the share it
+                              // begins in, and 2 x shares it spans (0: none) + whether it is the first one's second part
   float *parts;               // [CTAs][2] sums that a cut has parted
 };
 
@@ -76,6 +77,8 @@ struct alignas(16) Shared {
   unsigned long long full[kMaxStages], empty[kMaxStages], never;
   TileInfo info[kMaxStages];
   Merge merge[2];
+  float scale[kWarps][8];   // of the pass being added up
+  bool none[8];
   int4 job;
   Walk start;
   unsigned warp_tiles[kWarps + 2];
@@ -153,6 +156,20 @@ __device__ bool lay_down(const Shape &p, Shared &sm, Part &part, const TileInfo 
   return true;
 }
 
+// The outputs of sequences without a key, a CTA after the other.
+template <typename T>
+__device__ void write_empty(const Shape &p) {
+  const int lane = threadIdx.x & 31;
+  unsigned bad = 0;
+  for (int b = blockIdx.x; b < p.a.seq.batch; b += gridDim.x) {
+    if (tiles_of(keys_of(p.a, b, &bad), p.tile) > 0) continue;
+    uint4 *out = reinterpret_cast<uint4 *>(p.a.out + b * p.a.out_stride);
+    for (int i = lane; i < p.a.q_heads * p.a.cache.dim * (int)sizeof(T) / 16; i += 32) out[i] = make_uint4(0, 0, 0, 0);
+    if (p.a.lse != nullptr)
+      for (int i = lane; i < p.a.q_heads; i += 32) p.a.lse[(long long)b * p.a.q_heads + i] = -INFINITY;
+  }
+}
+
 // To the output where the part is all of its (sequence, head), else to the workspace.
 template <typename T>
 __device__ void add_up(const Shape &p, Shared &sm) {
@@ -185,28 +202,29 @@ __device__ void add_up(const Shape &p, Shared &sm) {
           if (!(flags & kWhole)) *reinterpret_cast<float2 *>(slot + 2 * r) = make_float2(all, total);
           else if (p.a.lse != nullptr) p.a.lse[(long long)ti.seq * p.a.q_heads + h0 + r] = lse_of(all, total);
         }
-        const int cols = min(s.cols, D - col0), rows = min(n - row0, 1 << s.row_log);
-        for (int rr = 0; rr < rows; ++rr) {
-          float fw[kWarps];
+        sm.scale[w][lane & 7] = f * g;
+        if (w == 0) sm.none[lane & 7] = (flags & kWhole) && total == 0.0f;   // no key has a weight
+        __syncwarp();
+        const int fours_log = 31 - __clz(s.cols) - 2;   // of a row
 #pragma unroll
-          for (int i = 0; i < kWarps; ++i) fw[i] = __shfl_sync(~0u, f * g, i * 8 + rr);
-          const bool none = (flags & kWhole) && __shfl_sync(~0u, total, rr) == 0.0f;   // no key has a weight
-          for (int c = lane * 4; c < cols; c += 128) {
-            float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int i = lane; i < kMergeFloats / 4; i += 32) {
+          const int rr = i >> fours_log, c = (i & ((1 << fours_log) - 1)) * 4;
+          if (row0 + rr >= n || col0 + c >= D) continue;
+          float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-            for (int i = 0; i < kWarps; ++i) {
-              const float4 y = *reinterpret_cast<const float4 *>(&m.rows[i][rr * s.ld + c]);
-              x.x = fmaf(y.x, fw[i], x.x);
-              x.y = fmaf(y.y, fw[i], x.y);
-              x.z = fmaf(y.z, fw[i], x.z);
-              x.w = fmaf(y.w, fw[i], x.w);
-            }
-            if (none) x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            const long long at = (long long)(row0 + rr) * D + col0 + c;
-            if (!(flags & kWhole)) *reinterpret_cast<float4 *>(slot + kStatFloats + at) = x;
-            else if (sizeof(T) == 4) *reinterpret_cast<float4 *>(out + at) = x;
-            else *reinterpret_cast<uint2 *>(out + at) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+          for (int v = 0; v < kWarps; ++v) {
+            const float4 y = *reinterpret_cast<const float4 *>(&m.rows[v][rr * s.ld + c]);
+            const float k = sm.scale[v][rr];
+            x.x = fmaf(y.x, k, x.x);
+            x.y = fmaf(y.y, k, x.y);
+            x.z = fmaf(y.z, k, x.z);
+            x.w = fmaf(y.w, k, x.w);
           }
+          if (sm.none[rr]) x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          const int at = (row0 + rr) * D + col0 + c;
+          if (!(flags & kWhole)) *reinterpret_cast<float4 *>(slot + kStatFloats + at) = x;
+          else if (sizeof(T) == 4) *reinterpret_cast<float4 *>(out + at) = x;
+          else *reinterpret_cast<uint2 *>(out + at) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&m.read);
@@ -337,9 +355,11 @@ __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const 
         ++round;
       }
     }
-    if (it + 1 == tiles && begun && w.at + 1 < w.tiles && lane == 0) {   // begun here, goes on in the next shares
-      const unsigned long long end = (unsigned long long)upto + (unsigned)(w.tiles - 1 - w.at);
-      sm.job = make_int4(w.seq, w.head, (int)((end * shares - 1) / total) - (int)blockIdx.x + 1, later);
+    if (it + 1 == tiles && w.at + 1 < w.tiles && lane == 0) {   // goes on in the next shares
+      const unsigned long long first = upto - 1 - w.at, end = (unsigned long long)upto + (unsigned)(w.tiles - 1 - w.at);
+      const int from = begun ? (int)blockIdx.x : (int)(((first + 1) * shares - 1) / total), to = (int)((end * shares - 1) / total);
+      const bool second = begun ? later : (unsigned long long)total * from / shares < first;
+      sm.job = make_int4(w.seq, w.head, from, 2 * (to - from + 1) + second);
     }
     fresh = last;
     later |= last;
@@ -377,20 +397,11 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
   }
   grid_begins();
 
-  // this CTA's share of all tiles: each thread counts some sequences' tiles; sequences without one have
-  // their outputs from the CTA whose turn it is
+  // this CTA's share of all tiles: each thread counts some sequences' tiles
   unsigned bad = 0, mine = 0;
   const int per = (B + kThreads - 1) / kThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
   for (int b = b0; b < b1; ++b) {
-    const int n = tiles_of(keys_of(p.a, b, &bad), p.tile);
-    mine += (unsigned)n * p.heads;
-    if (n == 0 && b % gridDim.x == blockIdx.x) {
-      uint4 *out = reinterpret_cast<uint4 *>(p.a.out + b * p.a.out_stride);
-#pragma unroll 1
-      for (int i = 0; i < p.a.q_heads * p.a.cache.dim * (int)sizeof(T) / 16; ++i) out[i] = make_uint4(0, 0, 0, 0);
-#pragma unroll 1
-      for (int i = 0; i < p.a.q_heads && p.a.lse != nullptr; ++i) p.a.lse[(long long)b * p.a.q_heads + i] = -INFINITY;
-    }
+    mine += (unsigned)tiles_of(keys_of(p.a, b, &bad), p.tile) * p.heads;
   }
   unsigned upto = mine;
 #pragma unroll
@@ -431,6 +442,7 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
   __syncthreads();
 
   const int tiles = (int)(t1 - t0);
+  if (warp > kWarps) write_empty<T>(p);
   if (tiles > 0) {
     if (warp == kWarps) produce<Part, T>(p, sm, ring, qs, &kmap, &vmap, sm.start, tiles, t1, total, shares);
     else if (warp > kWarps) add_up<T>(p, sm);
@@ -442,80 +454,127 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
   if (tid == 0) post_status(reinterpret_cast<unsigned *>(p.a.ws), blockIdx.x, gridDim.x, sm.flags | (sm.dead ? kErrTimeout : 0u));
 }
 
-// What the cuts between the CTAs' shares have parted: CTA (w, r) joins head r of the (sequence, head) that
-// begins in share w and ends in a later one.  Most have nothing to do.
+// What the cuts between the CTAs' shares have parted.  CTA w belongs to the (sequence, head) that share w ends
+// within, if any, and joins some of its heads: with few parts a warp takes a head, with many the whole CTA.
 constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kJoinBatch = 4;
 
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ Shape p) {
-  __shared__ float factor[kMaxWorkers], red[kJoinWarps], sums[kJoinWarps][256];
+  __shared__ float factor[kMaxWorkers], red[2][kJoinWarps], sums[kJoinWarps][256];
   grid_begins();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = p.a.cache.dim, first = blockIdx.x;
-  const int4 job = p.jobs[first];
-  const int parts = job.z, kv = job.y / p.passes, pass = job.y - kv * p.passes, r = blockIdx.y;
-  if (parts == 0 || r >= p.group - pass * kRows) return;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = p.a.cache.dim;
+  const int4 job = p.jobs[blockIdx.x];
+  const int parts = job.w >> 1, first = job.z, kv = job.y / p.passes, pass = job.y - kv * p.passes;
+  if (parts == 0) return;
+  const int h0 = kv * p.group + pass * kRows, n = min(kRows, p.group - pass * kRows);
+  const int me = (int)blockIdx.x - first, ctas = parts - 1;   // the last share's CTA belongs elsewhere
   const long long stride = kStatFloats + p.rows * D;
-  auto part = [&](int i) { return p.parts + (2LL * (first + i) + (i == 0 ? job.w : 0)) * stride; };
-  float4 x[kJoinBatch][2];
-  auto load = [&](int i0) {   // this warp's next parts
+  auto part = [&](int i) { return p.parts + (2LL * (first + i) + (i == 0 ? job.w & 1 : 0)) * stride; };
+  float4 x[kJoinBatch][2], acc[2];
+  auto load = [&](int r, int i0, int step) {
 #pragma unroll
-    for (int n = 0; n < kJoinBatch; ++n)
+    for (int m = 0; m < kJoinBatch; ++m)
 #pragma unroll
       for (int c = 0; c < 2; ++c)
-        if (i0 + n * kJoinWarps < parts && lane + 32 * c < D / 4)
-          x[n][c] = reinterpret_cast<const float4 *>(part(i0 + n * kJoinWarps) + kStatFloats + r * D)[lane + 32 * c];
+        if (i0 + m * step < parts && lane + 32 * c < D / 4)
+          x[m][c] = reinterpret_cast<const float4 *>(part(i0 + m * step) + kStatFloats + r * D)[lane + 32 * c];
   };
-  load(warp);
-  float all = -INFINITY, sum = 0.0f;
-  for (int i = tid; i < parts; i += kJoinThreads) all = fmaxf(all, part(i)[2 * r]);
+  auto add = [&](int m, float f) {
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor_sync(~0u, all, d));
-  if (lane == 0) red[warp] = all;
-  __syncthreads();
-  all = red[0];
+    for (int c = 0; c < 2; ++c)
+      if (lane + 32 * c < D / 4) {
+        acc[c].x = fmaf(x[m][c].x, f, acc[c].x);
+        acc[c].y = fmaf(x[m][c].y, f, acc[c].y);
+        acc[c].z = fmaf(x[m][c].z, f, acc[c].z);
+        acc[c].w = fmaf(x[m][c].w, f, acc[c].w);
+      }
+  };
+  auto write = [&](int r, int c, float4 v, float sum) {
+    const float g = 1.0f / sum;
+    if (sum == 0.0f) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    else v = make_float4(v.x * g, v.y * g, v.z * g, v.w * g);
+    T *out = reinterpret_cast<T *>(p.a.out + job.x * p.a.out_stride) + (long long)(h0 + r) * D + 4 * c;
+    if (sizeof(T) == 4) *reinterpret_cast<float4 *>(out) = v;
+    else *reinterpret_cast<uint2 *>(out) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+  };
+  auto write_lse = [&](int r, float all, float sum) {
+    if (p.a.lse != nullptr) p.a.lse[(long long)job.x * p.a.q_heads + h0 + r] = lse_of(all, sum);
+  };
+
+  if (parts <= 2 * kJoinBatch) {
+    for (int r = me * kJoinWarps + warp; r < n; r += ctas * kJoinWarps) {
+      load(r, 0, 1);
+      const float2 s = lane < parts ? *reinterpret_cast<const float2 *>(part(lane) + 2 * r) : make_float2(-INFINITY, 0.0f);
+      float all = s.x;
 #pragma unroll
-  for (int w = 1; w < kJoinWarps; ++w) all = fmaxf(all, red[w]);
-  for (int i = tid; i < parts; i += kJoinThreads) {
-    const float2 s = *reinterpret_cast<const float2 *>(part(i) + 2 * r);
-    factor[i] = join_factor(s.x, all);
-    sum += s.y * factor[i];
-  }
+      for (int d = kJoinBatch; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor_sync(~0u, all, d));
+      all = __shfl_sync(~0u, all, 0);
+      const float f = join_factor(s.x, all);
+      float sum = s.y * f;
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-  __syncthreads();
-  if (lane == 0) red[warp] = sum;
-  float4 acc[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
-  for (int i0 = warp; i0 < parts; i0 += kJoinWarps * kJoinBatch) {
-    if (i0 != warp) load(i0);
+      for (int d = kJoinBatch; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+      sum = __shfl_sync(~0u, sum, 0);
+      acc[0] = acc[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (int i = 0; i < parts; i += kJoinBatch) {
+        if (i > 0) load(r, i, 1);
 #pragma unroll
-    for (int n = 0; n < kJoinBatch; ++n) {
-      if (i0 + n * kJoinWarps >= parts) break;
-      const float f = factor[i0 + n * kJoinWarps];
+        for (int m = 0; m < kJoinBatch; ++m) {
+          const float g = __shfl_sync(~0u, f, i + m);
+          if (i + m < parts) add(m, g);
+        }
+      }
 #pragma unroll
       for (int c = 0; c < 2; ++c)
-        if (lane + 32 * c < D / 4) {
-          acc[c].x = fmaf(x[n][c].x, f, acc[c].x);
-          acc[c].y = fmaf(x[n][c].y, f, acc[c].y);
-          acc[c].z = fmaf(x[n][c].z, f, acc[c].z);
-          acc[c].w = fmaf(x[n][c].w, f, acc[c].w);
-        }
+        if (lane + 32 * c < D / 4) write(r, lane + 32 * c, acc[c], sum);
+      if (lane == 0) write_lse(r, all, sum);
     }
+    return;
   }
-  reinterpret_cast<float4 *>(sums[warp])[lane] = acc[0];
-  reinterpret_cast<float4 *>(sums[warp])[lane + 32] = acc[1];
-  __syncthreads();
-  sum = 0.0f;
+  for (int r = me; r < n; r += ctas) {
+    load(r, warp, kJoinWarps);
+    float all = -INFINITY, sum = 0.0f;
+    for (int i = tid; i < parts; i += kJoinThreads) all = fmaxf(all, part(i)[2 * r]);
 #pragma unroll
-  for (int w = 0; w < kJoinWarps; ++w) sum += red[w];
-  const int h = kv * p.group + pass * kRows + r;
-  T *out = reinterpret_cast<T *>(p.a.out + job.x * p.a.out_stride) + (long long)h * D;
-  for (int d = tid; d < D; d += kJoinThreads) {
-    float y = 0.0f;
+    for (int d = 16; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor_sync(~0u, all, d));
+    if (lane == 0) red[0][warp] = all;
+    __syncthreads();
+    all = red[0][0];
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) y += sums[w][d];
-    out[d] = (T)(sum == 0.0f ? 0.0f : y / sum);
+    for (int w = 1; w < kJoinWarps; ++w) all = fmaxf(all, red[0][w]);
+    for (int i = tid; i < parts; i += kJoinThreads) {
+      const float2 s = *reinterpret_cast<const float2 *>(part(i) + 2 * r);
+      factor[i] = join_factor(s.x, all);
+      sum += s.y * factor[i];
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+    if (lane == 0) red[1][warp] = sum;
+    __syncthreads();
+    acc[0] = acc[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = warp; i < parts; i += kJoinWarps * kJoinBatch) {
+      if (i != warp) load(r, i, kJoinWarps);
+#pragma unroll
+      for (int m = 0; m < kJoinBatch; ++m)
+        if (i + m * kJoinWarps < parts) add(m, factor[i + m * kJoinWarps]);
+    }
+    reinterpret_cast<float4 *>(sums[warp])[lane] = acc[0];
+    reinterpret_cast<float4 *>(sums[warp])[lane + 32] = acc[1];
+    __syncthreads();
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) sum += red[1][w];
+    for (int c = tid; c < D / 4; c += kJoinThreads) {
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int w = 0; w < kJoinWarps; ++w) {
+        const float4 y = reinterpret_cast<const float4 *>(sums[w])[c];
+        v = make_float4(v.x + y.x, v.y + y.y, v.z + y.z, v.w + y.w);
+      }
+      write(r, c, v, sum);
+    }
+    if (tid == 0) write_lse(r, all, sum);
+    __syncthreads();
   }
-  if (p.a.lse != nullptr && tid == 0) p.a.lse[(long long)job.x * p.a.q_heads + h] = lse_of(all, sum);
 }
 
 constexpr size_t kHalfSm = 109 * 1024;   // of shared memory for one of two CTAs; the rest is room for join_kernel
@@ -556,7 +615,7 @@ cudaError_t launch(Shape p, cudaStream_t s) {
   workers = workers < kMaxWorkers ? workers : kMaxWorkers;
   e = launch_early(attend_kernel<Part, T>, dim3(workers), kThreads, smem, s, p, maps[0], maps[1]);
   if (e != cudaSuccess || a.seq.batch == 0) return e;
-  return launch_early(join_kernel<T>, dim3(workers, p.rows), kJoinThreads, 0, s, p);
+  return launch_early(join_kernel<T>, dim3(workers), kJoinThreads, 0, s, p);
 }
 
 }  // namespace

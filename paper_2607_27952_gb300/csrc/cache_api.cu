@@ -132,6 +132,8 @@ last_status check_cache(const last_cache *c) {
     return fail(LAST_ERR_UNSUPPORTED, "head_dim * elem_bytes must be a multiple of 16 and head_dim <= 256");
   if (c->page_size > (1 << 20) || c->num_kv_heads > 4096 || c->num_layers > 4096)
     return fail(LAST_ERR_UNSUPPORTED, "page_size must be at most 2^20, num_kv_heads and num_layers at most 4096");
+  if ((long long)c->page_size * c->num_kv_heads * c->head_dim * e >= 1LL << 31)
+    return fail(LAST_ERR_UNSUPPORTED, "a page of one layer must stay below 2^31 bytes");
   if (c->k == nullptr || c->v == nullptr) return invalid("k and v are required");
   if (!aligned(c->k, 16) || !aligned(c->v, 16)) return invalid("k and v must be 16-byte aligned");
   const int64_t strides[4] = {c->layer_stride, c->page_stride, c->head_stride, c->token_stride};

@@ -15,15 +15,16 @@ __device__ __forceinline__ int quotient(int x, int n, uint32_t m) {
   return n == 1 ? x : m != 0 ? (int)__umulhi((uint32_t)x, m) : x / n;
 }
 
-// One page of one layer of K or V per step.
+// A warp takes kBatch pieces a lane of one page of one layer of K or V at a time.
 __global__ void __launch_bounds__(kThreads) copy_kernel(const __grid_constant__ PagesArgs p, int n, const int32_t *src,
-                                                        const int32_t *dst) {
+                                                        const int32_t *dst, int blocks) {
   grid_begins();
   unsigned flags = 0;
-  const int vec = p.row_bytes / 16, per_page = p.heads * p.page_size * vec;
-  const long long items = (long long)n * p.layers * 2;
-  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-    const int i = (int)(it / (2 * p.layers)), lk = (int)(it - (long long)i * 2 * p.layers);
+  const int lane = threadIdx.x & 31, vec = p.row_bytes / 16, per_page = p.heads * p.page_size * vec;
+  const long long items = (long long)n * p.layers * 2 * blocks, step = (long long)gridDim.x * (kThreads / 32);
+  for (long long it = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); it < items; it += step) {
+    const long long page = blocks == 1 ? it : it / blocks;
+    const int block = (int)(it - page * blocks), i = (int)(page / (2 * p.layers)), lk = (int)(page - (long long)i * 2 * p.layers);
     const int from = src[i], to = dst[i];
     if (from < 0 || from >= p.num_pages || to < 0 || to >= p.num_pages) {
       flags = kErrCacheIndex;
@@ -38,17 +39,17 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(const __grid_constant__ 
       const int r = e / vec, h = r / p.page_size;
       return h * p.head_stride + (r - h * p.page_size) * p.token_stride + (e - r * vec) * 16;
     };
-    for (int e = threadIdx.x; e < per_page; e += kThreads * kBatch) {
-      uint4 v[kBatch];
+    const int e = block * 32 * kBatch + lane;
+    uint4 v[kBatch];
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u)
-        if (e + u * kThreads < per_page) v[u] = *reinterpret_cast<const uint4 *>(x + at(e + u * kThreads));
+    for (int u = 0; u < kBatch; ++u)
+      if (e + u * 32 < per_page) v[u] = *reinterpret_cast<const uint4 *>(x + at(e + u * 32));
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u)
-        if (e + u * kThreads < per_page) *reinterpret_cast<uint4 *>(y + at(e + u * kThreads)) = v[u];
-    }
+    for (int u = 0; u < kBatch; ++u)
+      if (e + u * 32 < per_page) *reinterpret_cast<uint4 *>(y + at(e + u * 32)) = v[u];
   }
-  if (threadIdx.x == 0) post_status(p.status, blockIdx.x, gridDim.x, flags);
+  flags = __syncthreads_or((int)flags);
+  if (threadIdx.x == 0) post_status(p.status, blockIdx.x, gridDim.x, flags ? kErrCacheIndex : 0u);
 }
 
 // A warp takes a token of a shortened sequence (or, of few tokens, a part of its rows): its place and its
@@ -148,7 +149,10 @@ cudaError_t launch_page_copy(const PagesArgs &args, int n, const int32_t *src, c
   const long long row = p.row_bytes, ps = p.page_size;
   p.packed = (p.token_stride == row && (p.heads == 1 || p.head_stride == row * ps)) ||
              (p.token_stride == row * p.heads && (p.heads == 1 || p.head_stride == row));
-  return launch_early(copy_kernel, dim3(grid_of((long long)n * p.layers * 2)), kThreads, 0, s, p, n, src, dst);
+  const long long pieces = (long long)p.heads * p.page_size * (p.row_bytes / 16);
+  const int blocks = (int)((pieces + 32 * kBatch - 1) / (32 * kBatch));
+  const long long items = (long long)n * p.layers * 2 * blocks;
+  return launch_early(copy_kernel, dim3(grid_of((items + kThreads / 32 - 1) / (kThreads / 32))), kThreads, 0, s, p, n, src, dst, blocks);
 }
 
 cudaError_t launch_compact(const CompactArgs &a, cudaStream_t s) {

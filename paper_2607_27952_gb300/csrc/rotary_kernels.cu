@@ -285,9 +285,21 @@ __global__ void __launch_bounds__(kThreads, kCtas) rotary_kernel(const __grid_co
       const int part = unit - t * w.parts;
       auto copy = [&](const char *in, long long in_head, char *out, long long out_head, int heads) {
         const int all = heads * w.tail;
-        for (int j = (int)((long long)all * part / w.parts) + lane; j < (int)((long long)all * (part + 1) / w.parts); j += 32) {
-          const int h = quotient(j, w.tail, w.tail_m), e = (2 * half + (j - h * w.tail) * VEC) * (int)sizeof(T);
-          *reinterpret_cast<V *>(out + h * out_head + e) = *reinterpret_cast<const V *>(in + h * in_head + e);
+        const int j0 = (int)((long long)all * part / w.parts) + lane, j1 = (int)((long long)all * (part + 1) / w.parts);
+        for (int j = j0; j < j1; j += 32 * kBatch) {
+          V x[kBatch];
+#pragma unroll
+          for (int n = 0; n < kBatch; ++n)
+            if (j + 32 * n < j1) {
+              const int h = quotient(j + 32 * n, w.tail, w.tail_m), e = (2 * half + (j + 32 * n - h * w.tail) * VEC) * (int)sizeof(T);
+              x[n] = *reinterpret_cast<const V *>(in + h * in_head + e);
+            }
+#pragma unroll
+          for (int n = 0; n < kBatch; ++n)
+            if (j + 32 * n < j1) {
+              const int h = quotient(j + 32 * n, w.tail, w.tail_m), e = (2 * half + (j + 32 * n - h * w.tail) * VEC) * (int)sizeof(T);
+              *reinterpret_cast<V *>(out + h * out_head + e) = x[n];
+            }
         }
       };
       copy(p.q.in + t * p.q.in_token, p.q.in_head, p.q.out + t * p.q.out_token, p.q.out_head, p.q.heads);
