@@ -6,9 +6,10 @@ namespace last {
 namespace {
 
 // ---- consumers: bf16, on the tensor cores ----
-// S = Q K^T with the heads as the 16 rows of an MMA, then O += P V.  With at most 8 heads rows 8..15
-// are free and take what the cut of P to bf16 leaves out, so that P carries 16 bits for nothing;
-// with more heads a second product adds it.
+// S^T = K Q^T with 16 keys as the rows of an MMA and 8 heads as its columns, then O^T += V^T P^T: K and V come
+// from shared memory as they lie, and eight heads fill the MMA.  P is cut to bf16 in two parts, so that it
+// carries 16 bits.  The maximum that the weights are taken against follows the logits only once one
+// exceeds it by 8 (a weight of 256): most tiles then need neither the exchange nor the rescaling.
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -17,10 +18,14 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                         uint32_t b1) {
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 // Two weights cut to bf16, and what the cut left: not negative, and not zero for a weight above zero, so
 // that an infinite value comes out as the weight times it.
@@ -33,171 +38,187 @@ __device__ __forceinline__ uint32_t pack_rest(float x, float y, uint32_t down) {
   return pack_bf16(fmaxf(x - bf16lo(down), x * 0x1p-30f), fmaxf(y - bf16hi(down), y * 0x1p-30f));
 }
 
-template <int CHUNKS, bool FEW>   // 128-byte columns of a row; at most 8 heads
+template <int CHUNKS, int EIGHTS>   // 128-byte columns of a row; groups of 8 heads
 struct Bf16Part {
-  static constexpr int kTile = 64, kWarpKeys = 16;
-  static constexpr int kHeadRows = FEW ? 8 : 16;
-  uint32_t q[CHUNKS * 4][FEW ? 2 : 4];
-  float o[CHUNKS * 8][4], m[2], l[2];
-  static constexpr int kR1 = FEW ? 0 : 1, kR2 = FEW ? 0 : 2, kR3 = FEW ? 0 : 3;
-  uint32_t w[4], rest[FEW ? 1 : 4], keep[2];   // the tile's weights; masks of its values
+  static constexpr int kTile = 64, kWarpKeys = 16, kHeadRows = 8 * EIGHTS;
+  static constexpr int kSteps = CHUNKS * 4;                           // 16-wide along a row
+  static constexpr int kAhead = CHUNKS * EIGHTS > 4 ? 2 : 4;          // fragments in flight, as registers allow
+  uint32_t q[kSteps][2 * EIGHTS];
+  float o[kSteps][EIGHTS][4];                             // (d g, head 2t), (g, 2t + 1), (g + 8, 2t), (g + 8, 2t + 1)
+  float m[EIGHTS][2], l[EIGHTS][2];                       // heads 2t, 2t + 1; l over this lane's keys
+  uint32_t w[EIGHTS][4], keep[2];                         // the tile's weights, cut and rest; masks of its values
   bool part;
 
   // q: the n heads' rows in shared memory.
   __device__ void start(const Shape &p, const char *qs, int n) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, D = p.a.cache.dim;
-    auto get = [&](int row, int d) {
-      return row < n && d < D ? *reinterpret_cast<const uint32_t *>(qs + (row * D + d) * 2) : 0u;
-    };
 #pragma unroll
-    for (int s = 0; s < CHUNKS * 4; ++s) {
-      q[s][0] = get(g, s * 16 + 2 * t);
-      q[s][1] = get(g, s * 16 + 2 * t + 8);
-      if (!FEW) {
-        q[s][2] = get(g + 8, s * 16 + 2 * t);
-        q[s][3] = get(g + 8, s * 16 + 2 * t + 8);
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int e = 0; e < 2 * EIGHTS; ++e) {
+        const int row = g + 8 * (e >> 1), d = s * 16 + 2 * t + 8 * (e & 1);
+        q[s][e] = row < n && d < D ? *reinterpret_cast<const uint32_t *>(qs + (row * D + d) * 2) : 0u;
       }
-    }
 #pragma unroll
-    for (int i = 0; i < CHUNKS * 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
-    m[0] = m[1] = -INFINITY;
-    l[0] = l[1] = 0.0f;
+    for (int e = 0; e < EIGHTS; ++e) {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) o[i][e][0] = o[i][e][1] = o[i][e][2] = o[i][e][3] = 0.0f;
+      m[e][0] = m[e][1] = -INFINITY;
+      l[e][0] = l[e][1] = 0.0f;
+    }
   }
 
   // Weights of the tile's 16 keys from row0 on; keys lo <= i < hi of the tile count.
   __device__ void logits(const Shape &p, const char *, float *, const char *k, int row0, int lo, int hi) {
-    const int lane = threadIdx.x & 31, t = lane & 3, D = p.a.cache.dim, column = 128 << p.box_log;
-    float s[2][4] = {};
-    {   // rows of K as the MMA's columns: matrices (keys 0-7 | 8-15) x (16-byte column even | odd)
-      const int row = row0 + (lane & 7) + ((lane >> 4) << 3), sub = (lane >> 3) & 1;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, D = p.a.cache.dim, column = 128 << p.box_log;
+    float s[2][EIGHTS][4] = {};   // even and odd steps
+    {   // 8 x 8 blocks (keys 0-7 | 8-15) x (16-byte column even | odd)
+      const int row = row0 + (lane & 15), sub = lane >> 4;
       const uint32_t base = smem_addr(k) + row_at(p, row);
+      auto at = [&](int i) { return base + (i >> 2) * column + ((((i & 3) * 2 + sub) ^ (row & 7)) << 4); };
+      uint32_t f[kAhead][4];
 #pragma unroll
-      for (int i = 0; i < CHUNKS * 4; ++i) {
+      for (int i = 0; i < kAhead; ++i)
+        if (i * 16 < D) ldsm4(f[i], at(i));
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
         if (i * 16 >= D) break;
-        uint32_t f[4];
-        ldsm4(f, base + (i >> 2) * column + ((((i & 3) * 2 + sub) ^ (row & 7)) << 4));
-        mma16816(s[0], q[i][0], FEW ? 0u : q[i][2], q[i][1], FEW ? 0u : q[i][3], f[0], f[1]);
-        mma16816(s[1], q[i][0], FEW ? 0u : q[i][2], q[i][1], FEW ? 0u : q[i][3], f[2], f[3]);
+#pragma unroll
+        for (int e = 0; e < EIGHTS; ++e) mma16816(s[i & 1][e], f[i % kAhead], q[i][2 * e], q[i][2 * e + 1]);
+        if (i + kAhead < kSteps && (i + kAhead) * 16 < D) ldsm4(f[i % kAhead], at(i + kAhead));
       }
     }
     part = lo > row0 || hi < row0 + 16;
     keep[0] = keep[1] = ~0u;   // halves of V's fragments whose keys count
     if (part) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < 2; ++j) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int key = row0 + j * 8 + 2 * t + e;
-          if (key < lo || key >= hi) {
-            s[j][e] = s[j][2 + e] = -INFINITY;
-            keep[j] &= e ? 0x0000ffffu : 0xffff0000u;
-          }
+          if (key < lo || key >= hi) keep[j] &= e ? 0x0000ffffu : 0xffff0000u;
         }
-    }
-    constexpr int R = FEW ? 1 : 2;
-    float alpha[2] = {1.0f, 1.0f};
-    bool moved = false;
+        const int key = row0 + j * 8 + g;
+        if (key < lo || key >= hi)
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      float x = fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1])) * p.scale2;
-      x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
-      x = fmaxf(x, __shfl_xor_sync(~0u, x, 2));
-      if (x > m[r]) {
-        alpha[r] = exp2_fast(m[r] - x);
-        m[r] = x;
-        moved = true;
-      }
-      const float ref = m[r] == -INFINITY ? 0.0f : m[r];
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) s[j][2 * r + e] = exp2_fast(fmaf(s[j][2 * r + e], p.scale2, -ref));
-      l[r] = l[r] * alpha[r] + ((s[0][2 * r] + s[0][2 * r + 1]) + (s[1][2 * r] + s[1][2 * r + 1]));
-    }
-    if (FEW) alpha[1] = alpha[0];
-    if (__any_sync(~0u, moved)) {
-#pragma unroll
-      for (int i = 0; i < CHUNKS * 8; ++i) {
-        o[i][0] *= alpha[0];
-        o[i][1] *= alpha[0];
-        o[i][2] *= alpha[1];
-        o[i][3] *= alpha[1];
+          for (int e = 0; e < EIGHTS; ++e) s[0][e][2 * j] = s[0][e][2 * j + 1] = s[1][e][2 * j] = s[1][e][2 * j + 1] = -INFINITY;
       }
     }
-    w[0] = pack_down(s[0][0], s[0][1]);
-    w[2] = pack_down(s[1][0], s[1][1]);
-    const uint32_t r0 = pack_rest(s[0][0], s[0][1], w[0]), r2 = pack_rest(s[1][0], s[1][1], w[2]);
-    if (FEW) {
-      w[1] = r0;
-      w[3] = r2;
-    } else {
-      w[1] = pack_down(s[0][2], s[0][3]);
-      w[3] = pack_down(s[1][2], s[1][3]);
-      rest[0] = r0;
-      rest[kR1] = pack_rest(s[0][2], s[0][3], w[1]);
-      rest[kR2] = r2;
-      rest[kR3] = pack_rest(s[1][2], s[1][3], w[3]);
+    float top[EIGHTS][2];
+    bool above = false;
+#pragma unroll
+    for (int e = 0; e < EIGHTS; ++e)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s[0][e][h] += s[1][e][h];
+        s[0][e][2 + h] += s[1][e][2 + h];
+        top[e][h] = fmaxf(s[0][e][h], s[0][e][2 + h]) * p.scale2;
+        above |= top[e][h] > m[e][h] + 8.0f;
+      }
+    if (__any_sync(~0u, above)) {
+#pragma unroll
+      for (int e = 0; e < EIGHTS; ++e) {
+        float alpha[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float x = top[e][h];
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
+          alpha[h] = x > m[e][h] ? exp2_fast(m[e][h] - x) : 1.0f;
+          m[e][h] = fmaxf(m[e][h], x);
+          l[e][h] *= alpha[h];
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          o[i][e][0] *= alpha[0];
+          o[i][e][1] *= alpha[1];
+          o[i][e][2] *= alpha[0];
+          o[i][e][3] *= alpha[1];
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < EIGHTS; ++e) {
+      float x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = exp2_fast(fmaf(s[0][e][i], p.scale2, m[e][i & 1] == -INFINITY ? 0.0f : -m[e][i & 1]));
+      l[e][0] += x[0] + x[2];
+      l[e][1] += x[1] + x[3];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {   // keys j * 8 + g, to keys j * 8 + 2t and 2t + 1 of head g
+        const uint32_t down = pack_down(x[2 * j], x[2 * j + 1]);
+        w[e][j] = transpose8(down);
+        w[e][2 + j] = transpose8(pack_rest(x[2 * j], x[2 * j + 1], down));
+      }
     }
   }
 
   __device__ void values(const Shape &p, const float *, const char *v, int row0, int, int) {
     const int lane = threadIdx.x & 31, D = p.a.cache.dim, column = 128 << p.box_log;
-    {   // V transposed on the way: matrices (keys 0-7 | 8-15) x (16-byte column even | odd)
-      const int row = row0 + (lane & 15), sub = lane >> 4;
-      const uint32_t base = smem_addr(v) + row_at(p, row);
+    // 8 x 8 blocks, transposed on the way: (keys 0-7 | 8-15) x (16-byte column even | odd)
+    const int row = row0 + (lane & 7) + (lane >> 4) * 8, sub = lane >> 3 & 1;
+    const uint32_t base = smem_addr(v) + row_at(p, row);
+    auto at = [&](int i) { return base + (i >> 2) * column + ((((i & 3) * 2 + sub) ^ (row & 7)) << 4); };
+    uint32_t f[kAhead][4];
 #pragma unroll
-      for (int i = 0; i < CHUNKS * 4; ++i) {
-        if (i * 16 >= D) break;
-        uint32_t f[4];
-        ldsm4t(f, base + (i >> 2) * column + ((((i & 3) * 2 + sub) ^ (row & 7)) << 4));
-        if (part) {   // an infinity or NaN times a weight of zero would still show
-          f[0] &= keep[0];
-          f[1] &= keep[1];
-          f[2] &= keep[0];
-          f[3] &= keep[1];
-        }
-        mma16816(o[2 * i], w[0], w[1], w[2], w[3], f[0], f[1]);
-        mma16816(o[2 * i + 1], w[0], w[1], w[2], w[3], f[2], f[3]);
-        if (!FEW) {
-          mma16816(o[2 * i], rest[0], rest[kR1], rest[kR2], rest[kR3], f[0], f[1]);
-          mma16816(o[2 * i + 1], rest[0], rest[kR1], rest[kR2], rest[kR3], f[2], f[3]);
-        }
+    for (int i = 0; i < kAhead; ++i)
+      if (i * 16 < D) ldsm4t(f[i], at(i));
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      if (i * 16 >= D) break;
+      uint32_t (&x)[4] = f[i % kAhead];
+      if (part) {   // an infinity or NaN times a weight of zero would still show
+        x[0] &= keep[0];
+        x[1] &= keep[0];
+        x[2] &= keep[1];
+        x[3] &= keep[1];
       }
+#pragma unroll
+      for (int e = 0; e < EIGHTS; ++e) mma16816(o[i][e], x, w[e][0], w[e][1]);
+#pragma unroll
+      for (int e = 0; e < EIGHTS; ++e) mma16816(o[i][e], x, w[e][2], w[e][3]);
+      if (i + kAhead < kSteps && (i + kAhead) * 16 < D) ldsm4t(x, at(i + kAhead));
     }
   }
 
   __device__ void stats(float *top, float *sum) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int r = 0; r < (FEW ? 1 : 2); ++r) {
-      float x = l[r] + __shfl_xor_sync(~0u, l[r], 1);
-      x += __shfl_xor_sync(~0u, x, 2);
-      if ((lane & 3) == 0) {
-        top[(lane >> 2) + 8 * r] = m[r];
-        sum[(lane >> 2) + 8 * r] = x;
+    for (int e = 0; e < EIGHTS; ++e)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float x = l[e][h];
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) x += __shfl_xor_sync(~0u, x, d);
+        if (lane < 4) {
+          top[8 * e + 2 * lane + h] = m[e][h];
+          sum[8 * e + 2 * lane + h] = x;
+        }
       }
-    }
   }
   // Rows row0 .. row0 + rows - 1 and columns col0 .. col0 + cols - 1 of the sums.
   __device__ void put(int row0, int rows, int col0, int cols, int ld, float *to, int) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
-    for (int r = 0; r < (FEW ? 1 : 2); ++r) {
-      const int row = g + 8 * r - row0;
-      if (row < 0 || row >= rows) continue;
+    for (int e = 0; e < EIGHTS; ++e)
 #pragma unroll
-      for (int i = 0; i < CHUNKS * 8; ++i) {
-        if (i * 8 < col0 || i * 8 >= col0 + cols) continue;
-        const float2 x = FEW ? make_float2(o[i][0] + o[i][2], o[i][1] + o[i][3]) : make_float2(o[i][2 * r], o[i][2 * r + 1]);
-        *reinterpret_cast<float2 *>(to + row * ld + i * 8 + 2 * t - col0) = x;
+      for (int h = 0; h < 2; ++h) {
+        const int row = 8 * e + 2 * t + h - row0;
+        if (row < 0 || row >= rows) continue;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          if (i * 16 < col0 || i * 16 >= col0 + cols) continue;
+          float *x = to + row * ld + i * 16 + g - col0;
+          x[0] = o[i][e][h];
+          x[8] = o[i][e][2 + h];
+        }
       }
-    }
   }
 };
 
 template <int CHUNKS>
 cudaError_t launch_chunks(const Shape &p, cudaStream_t s) {
-  return p.rows <= 8 ? launch<Bf16Part<CHUNKS, true>, __nv_bfloat16>(p, s) : launch<Bf16Part<CHUNKS, false>, __nv_bfloat16>(p, s);
+  return p.rows <= 8 ? launch<Bf16Part<CHUNKS, 1>, __nv_bfloat16>(p, s) : launch<Bf16Part<CHUNKS, 2>, __nv_bfloat16>(p, s);
 }
 
 }  // namespace

@@ -44,33 +44,34 @@ struct F32Part {
       }
     }
     const bool counts = row >= lo && row < hi;
-    bool moved = false;
-    float alpha[HEADS];
+    bool above = false;
 #pragma unroll
     for (int h = 0; h < HEADS; ++h) {
       s[h] += __shfl_xor_sync(~0u, s[h], 8);
       s[h] += __shfl_xor_sync(~0u, s[h], 16);
-      if (!counts) s[h] = -INFINITY;
-      float x = s[h] * p.scale2;
-      x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
-      x = fmaxf(x, __shfl_xor_sync(~0u, x, 2));
-      x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
-      alpha[h] = 1.0f;
-      if (x > m[h]) {
-        alpha[h] = exp2_fast(m[h] - x);
-        m[h] = x;
-        moved = true;
-      }
-      s[h] = exp2_fast(fmaf(s[h], p.scale2, m[h] == -INFINITY ? 0.0f : -m[h]));
-      l[h] = l[h] * alpha[h] + s[h];
+      s[h] = counts ? s[h] : -INFINITY;
+      above |= s[h] * p.scale2 > m[h] + 8.0f;   // as for bf16: the maximum follows from a weight of 256 on
     }
-    if (moved) {   // the same in every lane
+    if (__any_sync(~0u, above)) {
 #pragma unroll
-      for (int h = 0; h < HEADS; ++h)
+      for (int h = 0; h < HEADS; ++h) {
+        float x = s[h] * p.scale2;
+        x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
+        x = fmaxf(x, __shfl_xor_sync(~0u, x, 2));
+        x = fmaxf(x, __shfl_xor_sync(~0u, x, 4));
+        const float alpha = x > m[h] ? exp2_fast(m[h] - x) : 1.0f;
+        m[h] = fmaxf(m[h], x);
+        l[h] *= alpha;
 #pragma unroll
         for (int w = 0; w < WIDE; ++w)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[h][w][e] *= alpha[h];
+          for (int e = 0; e < 4; ++e) o[h][w][e] *= alpha;
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h) {
+      s[h] = exp2_fast(fmaf(s[h], p.scale2, m[h] == -INFINITY ? 0.0f : -m[h]));
+      l[h] += s[h];
     }
     __syncwarp();
     if (lane < 8) {
