@@ -164,20 +164,27 @@ struct Bf16Part {
     for (int i = 0; i < kAhead; ++i)
       if (i * 16 < D) ldsm4t(f[i], at(i));
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
+    for (int i = 0; i < kSteps; i += 2) {   // two steps together: the products of one wait for each other
       if (i * 16 >= D) break;
-      uint32_t (&x)[4] = f[i % kAhead];
+      const bool both = (i + 1) * 16 < D;
+      uint32_t (&x)[4] = f[i % kAhead], (&y)[4] = f[(i + 1) % kAhead];
       if (part) {   // an infinity or NaN times a weight of zero would still show
-        x[0] &= keep[0];
-        x[1] &= keep[0];
-        x[2] &= keep[1];
-        x[3] &= keep[1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[j] &= keep[j >> 1];
+          y[j] &= keep[j >> 1];
+        }
       }
 #pragma unroll
-      for (int e = 0; e < EIGHTS; ++e) mma16816(o[i][e], x, w[e][0], w[e][1]);
+      for (int r = 0; r < 2; ++r)
 #pragma unroll
-      for (int e = 0; e < EIGHTS; ++e) mma16816(o[i][e], x, w[e][2], w[e][3]);
-      if (i + kAhead < kSteps && (i + kAhead) * 16 < D) ldsm4t(x, at(i + kAhead));
+        for (int e = 0; e < EIGHTS; ++e) {
+          mma16816(o[i][e], x, w[e][2 * r], w[e][2 * r + 1]);
+          if (both) mma16816(o[i + 1][e], y, w[e][2 * r], w[e][2 * r + 1]);
+        }
+#pragma unroll
+      for (int j = i + kAhead; j < i + kAhead + 2; ++j)
+        if (j < kSteps && j * 16 < D) ldsm4t(f[j % kAhead], at(j));
     }
   }
 

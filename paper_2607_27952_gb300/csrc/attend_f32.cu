@@ -35,6 +35,7 @@ struct F32Part {
     const int row = row0 + (lane & 7);
     const char *kr = k + row_at(p, row);
     float s[HEADS] = {};
+#pragma unroll 2
     for (int c = lane >> 3; c < cols; c += 4) {
       const float4 x = *reinterpret_cast<const float4 *>(kr + (c >> 3) * column + (((c & 7) ^ (row & 7)) << 4));
 #pragma unroll
@@ -83,22 +84,31 @@ struct F32Part {
   __device__ void values(const Shape &p, const float *ps, const char *v, int row0, int lo, int hi) {
     const int lane = threadIdx.x & 31, D = p.a.cache.dim, cols = D / 4, column = 128 << p.box_log;
     const int across = lanes_across(D), c0 = lane & (across - 1);
+#pragma unroll 2
     for (int i = lane / across; i < 8; i += 32 / across) {
       const int r = row0 + i;
-      if (r < lo || r >= hi) continue;
+      const bool counts = r >= lo && r < hi;   // an infinity or NaN times a weight of zero would still show
       const char *vr = v + row_at(p, r);
+      float y[HEADS];
+      if constexpr (HEADS % 4 == 0) {
+#pragma unroll
+        for (int h = 0; h < HEADS; h += 4) *reinterpret_cast<float4 *>(y + h) = *reinterpret_cast<const float4 *>(ps + i * HEADS + h);
+      } else {
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h) y[h] = ps[i * HEADS + h];
+      }
 #pragma unroll
       for (int w = 0; w < WIDE; ++w) {
         const int c = c0 + 32 * w;
         if (c >= cols) break;
-        const float4 x = *reinterpret_cast<const float4 *>(vr + (c >> 3) * column + (((c & 7) ^ (r & 7)) << 4));
+        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (counts) x = *reinterpret_cast<const float4 *>(vr + (c >> 3) * column + (((c & 7) ^ (r & 7)) << 4));
 #pragma unroll
         for (int h = 0; h < HEADS; ++h) {
-          const float y = ps[i * HEADS + h];
-          o[h][w][0] = fmaf(y, x.x, o[h][w][0]);
-          o[h][w][1] = fmaf(y, x.y, o[h][w][1]);
-          o[h][w][2] = fmaf(y, x.z, o[h][w][2]);
-          o[h][w][3] = fmaf(y, x.w, o[h][w][3]);
+          o[h][w][0] = fmaf(y[h], x.x, o[h][w][0]);
+          o[h][w][1] = fmaf(y[h], x.y, o[h][w][1]);
+          o[h][w][2] = fmaf(y[h], x.z, o[h][w][2]);
+          o[h][w][3] = fmaf(y[h], x.w, o[h][w][3]);
         }
       }
     }

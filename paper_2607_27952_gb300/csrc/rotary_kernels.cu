@@ -34,12 +34,6 @@ template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float v) { return __float2bfloat16_rn(v); }
 
-// x / n for x n < 2^32, with m = ceil(2^32 / n).
-__device__ __forceinline__ int quotient(int x, int n, uint32_t m) {
-  return n == 1 ? x : (int)__umulhi((uint32_t)x, m);
-}
-uint32_t magic(int n) { return (uint32_t)(((1ull << 32) + (unsigned)n - 1) / (unsigned)(n > 0 ? n : 1)); }
-
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   float2 d;
@@ -69,13 +63,14 @@ template <> __device__ __forceinline__ void set2(__nv_bfloat16 *x, float2 v) {
   memcpy(x, &r, 4);
 }
 
-// A row's items (pairs of VEC-element pieces) lie side by side in a warp, `heads` rows at a time.
+// A row's items (pairs of VEC-element pieces, the first `turned` of them rotated, the others copied) lie side
+// by side in a warp, `heads` rows at a time.
 struct Split {
   int parts;            // warps per token
-  int items, columns;   // of a row; passes over rows of more than 32
+  int items, turned;    // of a row
+  int columns;          // passes over rows of more than 32 items
   int heads;
-  int tail;             // pieces behind a row's items
-  uint32_t tail_m;
+  bool tail;            // one piece is left behind the items
 };
 
 // Byte offset of new token t's slot in its cache layer; -1 (and a flag) if it has none.
@@ -154,8 +149,8 @@ template <typename T, int VEC, bool ADJACENT, bool APPEND>
 __global__ void __launch_bounds__(kThreads, kCtas) rotary_kernel(const __grid_constant__ RotaryArgs p, const Split w) {
   using V = typename Pack<VEC * (int)sizeof(T)>::type;
   using R = Turns<VEC, ADJACENT>;
-  // of pair c VEC + e: cosine and sine at [e items + c], or, two pairs a time, both cosines and both sines at
-  // [e / 2 items + c]
+  // of pair c VEC + e: cosine and sine at [e turned + c], or, two pairs a time, both cosines and both sines at
+  // [e / 2 turned + c]
   __shared__ alignas(16) float tables[kThreads / 32][2 * kMaxRotPairs];
   __shared__ unsigned long long freqs[kMaxRotPairs];
   __shared__ uint8_t axes[kMaxRotPairs];
@@ -174,17 +169,18 @@ __global__ void __launch_bounds__(kThreads, kCtas) rotary_kernel(const __grid_co
   grid_begins();
 
   const bool across = w.columns > 1;
-  const int sub = across ? 0 : lane / w.items;                       // row of the group
+  const int width = max(w.items, 1), sub = across ? 0 : lane / width;   // row of the group
   const bool idle = sub >= w.heads;
   const int step = w.heads * w.parts, units = p.tokens * w.parts;
-  const int far = (ADJACENT ? VEC : half) * (int)sizeof(T);          // from an item's first piece to its second
   for (int unit = blockIdx.x * (kThreads / 32) + warp; unit < units; unit += warps) {
     const int t = w.parts == 1 ? unit : unit / w.parts, first = sub + (unit - t * w.parts) * w.heads;
     long long slot = 0;
     for (int col = 0; col < w.columns; ++col) {
-      const int c = across ? lane + 32 * col : lane - sub * w.items;
-      const bool off = idle || c >= w.items || half == 0;
-      const int at = (ADJACENT ? 2 * c : c) * VEC * (int)sizeof(T);
+      const int c = across ? lane + 32 * col : lane - sub * width;
+      const bool off = idle || c >= w.items, rotated = c < w.turned;
+      // an item's first piece, and from there to its second
+      const int at = (!rotated ? 2 * half + (c - w.turned) * 2 * VEC : ADJACENT ? 2 * c * VEC : c * VEC) * (int)sizeof(T);
+      const int far = (rotated && !ADJACENT ? half : VEC) * (int)sizeof(T);
       const int nq = off || first >= p.q.heads ? 0 : (p.q.heads - first + step - 1) / step;
       const int nk = off || first >= p.k.heads ? 0 : (p.k.heads - first + step - 1) / step;
       const char *q = p.q.in + t * p.q.in_token + first * p.q.in_head + at, *k = p.k.in + t * p.k.in_token + first * p.k.in_head + at;
@@ -218,11 +214,11 @@ __global__ void __launch_bounds__(kThreads, kCtas) rotary_kernel(const __grid_co
           sn = p.backward ? -sn : sn;
           const int e = i % VEC, j = i / VEC;
           if (R::kPacked) {
-            float *to = table + ((e / 2) * w.items + j) * 4 + (e & 1);
+            float *to = table + ((e / 2) * w.turned + j) * 4 + (e & 1);
             to[0] = cs;
             to[2] = sn;
           } else {
-            *reinterpret_cast<float2 *>(table + (e * w.items + j) * 2) = make_float2(cs, sn);
+            *reinterpret_cast<float2 *>(table + (e * w.turned + j) * 2) = make_float2(cs, sn);
           }
         }
         if (APPEND) {
@@ -233,8 +229,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) rotary_kernel(const __grid_co
         __syncwarp();
       }
       R turns;
-      if (!off) turns.load(table, w.items, c);
+      if (!off && rotated) turns.load(table, w.turned, c);
       auto turn = [&](V &x, V &y) {
+        if (!rotated) return;
         T ex[VEC], ey[VEC];
         memcpy(ex, &x, sizeof(V));
         memcpy(ey, &y, sizeof(V));
@@ -281,26 +278,11 @@ __global__ void __launch_bounds__(kThreads, kCtas) rotary_kernel(const __grid_co
         }
       }
     }
-    if (w.tail > 0) {   // elements past the rotated ones are copied
-      const int part = unit - t * w.parts;
+    if (w.tail && unit - t * w.parts == 0) {   // the piece that no item holds
+      const int e = (p.dim - VEC) * (int)sizeof(T);
       auto copy = [&](const char *in, long long in_head, char *out, long long out_head, int heads) {
-        const int all = heads * w.tail;
-        const int j0 = (int)((long long)all * part / w.parts) + lane, j1 = (int)((long long)all * (part + 1) / w.parts);
-        for (int j = j0; j < j1; j += 32 * kBatch) {
-          V x[kBatch];
-#pragma unroll
-          for (int n = 0; n < kBatch; ++n)
-            if (j + 32 * n < j1) {
-              const int h = quotient(j + 32 * n, w.tail, w.tail_m), e = (2 * half + (j + 32 * n - h * w.tail) * VEC) * (int)sizeof(T);
-              x[n] = *reinterpret_cast<const V *>(in + h * in_head + e);
-            }
-#pragma unroll
-          for (int n = 0; n < kBatch; ++n)
-            if (j + 32 * n < j1) {
-              const int h = quotient(j + 32 * n, w.tail, w.tail_m), e = (2 * half + (j + 32 * n - h * w.tail) * VEC) * (int)sizeof(T);
-              *reinterpret_cast<V *>(out + h * out_head + e) = x[n];
-            }
-        }
+        for (int h = lane; h < heads; h += 32)
+          *reinterpret_cast<V *>(out + h * out_head + e) = *reinterpret_cast<const V *>(in + h * in_head + e);
       };
       copy(p.q.in + t * p.q.in_token, p.q.in_head, p.q.out + t * p.q.out_token, p.q.out_head, p.q.heads);
       if (!APPEND) copy(p.k.in + t * p.k.in_token, p.k.in_head, p.k.out + t * p.k.out_token, p.k.out_head, p.k.heads);
@@ -340,12 +322,11 @@ cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t s) {
                      !rows_aligned(a.k, vec * a.elem, !a.append) || !rows_aligned(a.v, vec * a.elem, false)))
     vec /= 2;
   Split w;
-  const int pairs = a.rot.half / vec;
-  w.items = pairs > 0 ? pairs : 1;
-  w.columns = (w.items + 31) / 32;
-  w.heads = w.columns > 1 ? 1 : 32 / w.items;
-  w.tail = (a.dim - 2 * a.rot.half) / vec;
-  w.tail_m = magic(w.tail);
+  w.turned = a.rot.half / vec;
+  w.items = w.turned + (a.dim - 2 * a.rot.half) / (2 * vec);
+  w.tail = (a.dim - 2 * a.rot.half) / vec % 2 != 0;
+  w.columns = w.items > 32 ? (w.items + 31) / 32 : 1;
+  w.heads = w.columns > 1 ? 1 : w.items > 0 ? 32 / w.items : 32;
   // Parts of a token per warp: the fewest rounds on the busiest warp, its angles (and slot) taken for two
   const int sms = sm_count(), warps = sms * kCtas * (kThreads / 32);
   auto rounds = [&](int heads, int parts) { return (heads + w.heads * parts - 1) / (w.heads * parts); };

@@ -364,3 +364,28 @@ def test_decode_loop_in_a_graph():
         graph.replay()
         assert _same(g[1], want[i]), i
     last.last_poll(g[3])
+
+
+@pytest.mark.parametrize("dtype,d,rot", [("bfloat16", 8, 0), ("bfloat16", 8, 2), ("bfloat16", 24, 0), ("float32", 4, 0), ("float32", 12, 4),
+                                         ("bfloat16", 128, 40), ("float32", 128, 40), ("bfloat16", 80, 64), ("float32", 256, 250)])
+@pytest.mark.parametrize("pairs", ["half", "adjacent"])
+def test_append_of_narrow_and_partly_rotated_rows(dtype, d, rot, pairs):
+    """Rows of one or three pieces, and rows of which a part is copied."""
+    import torch
+    import cache_util as cu
+    k, v = cu.pages(1, 5, 3, 8, d, dtype, "token", 1)
+    cache, seqs = last.Cache(k, v), last.Sequences(cu.ints([[4, 2], [1, 0]]), cu.ints([11, 6]))
+    q, kn, vn = cu.randn((5, 6, d), dtype, 2), cu.randn((5, 3, d), dtype, 3), cu.randn((5, 3, d), dtype, 4)
+    kn[..., rot:] = float("inf")                    # what is copied is only copied
+    kr, qo, want_q, kw = kn.clone(), torch.zeros_like(q), torch.zeros_like(q), {}
+    if rot:
+        rope, pos = last.Rope.sections([rot // 2], pairs=pairs), torch.arange(5, dtype=torch.int32, device="cuda")
+        last.last_rope(rope, pos, q, want_q, k=kn, k_out=kr)
+        kw = dict(rope=rope, positions=pos, q=q, q_out=qo)
+    assert _same(kr[..., rot:], kn[..., rot:])
+    k0, v0, ws = k.clone(), v.clone(), cu.workspace(cache, 2, 6)
+    last.last_cache_append(cache, 0, seqs, kn, vn, ws, cu_new=cu.ints([0, 3, 5]), **kw)
+    last.last_poll(ws)
+    for i, (page, slot) in enumerate([(2, 0), (2, 1), (2, 2), (1, 4), (1, 5)]):
+        k0[0, page, :, slot], v0[0, page, :, slot] = kr[i], vn[i]
+    assert _same(k, k0) and _same(v, v0) and _same(qo, want_q)
