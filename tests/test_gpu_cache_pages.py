@@ -389,3 +389,8 @@ def test_append_of_narrow_and_partly_rotated_rows(dtype, d, rot, pairs):
     for i, (page, slot) in enumerate([(2, 0), (2, 1), (2, 2), (1, 4), (1, 5)]):
         k0[0, page, :, slot], v0[0, page, :, slot] = kr[i], vn[i]
     assert _same(k, k0) and _same(v, v0) and _same(qo, want_q)
+
+
+def test_compaction_of_many_layers():
+    """More rows a token than a CTA keeps addresses of."""
+    _compact(24, [40, 9], [3, 0], [30, 9], [7, 2], 88, 8, 8, "bfloat16", "head", seed=7)
