@@ -282,7 +282,8 @@ typedef struct {
 
 /* Rotates q and, unless NULL, k.  positions: int32 [num_axes][axis_stride >= num_tokens],
  * any value (angles are formed modulo one turn in 64-bit integers, so that long
- * positions lose nothing).  Any strides and alignment of whole elements; head_dim 2 .. 256.
+ * positions lose nothing).  Any strides and alignment of whole elements; head_dim 2 .. 256, num_tokens
+ * at most 2^30.
  * last_rope_backward turns by the opposite angles: with the gradient with respect to the
  * rotated heads as `in`, `out` receives the gradient with respect to the heads. */
 last_status last_rope(const last_rotary *r, int32_t dtype, int32_t num_tokens, int32_t head_dim,
@@ -295,8 +296,9 @@ last_status last_rope_backward(const last_rotary *r, int32_t dtype, int32_t num_
 /* A paged cache: K and V of num_layers layers in num_pages pages of page_size tokens.
  * Element (layer, page, head, token, c) of either lies at layer * layer_stride +
  * page * page_stride + head * head_stride + token * token_stride + c (strides in elements,
- * each a multiple of 16 bytes; k and v 16-byte aligned).  page_size a multiple of 8;
- * head_dim * elem_bytes a multiple of 16, head_dim <= 256. */
+ * each a multiple of 16 bytes; k and v 16-byte aligned).  page_size a multiple of 8, at most
+ * 2^20; head_dim * elem_bytes a multiple of 16, head_dim <= 256; at most 4096 layers and
+ * kv-heads, and a page of one layer below 2^31 bytes. */
 typedef struct {
   void *k, *v;
   int32_t num_layers, num_pages, page_size, num_kv_heads, head_dim;

@@ -40,25 +40,31 @@ __device__ __forceinline__ uint32_t pack_rest(float x, float y, uint32_t down) {
 
 template <int CHUNKS, int EIGHTS>   // 128-byte columns of a row; groups of 8 heads
 struct Bf16Part {
-  static constexpr int kTile = 64, kWarpKeys = 16, kHeadRows = 8 * EIGHTS;
+  static constexpr int kTile = 64, kWarpKeys = 16, kHeadRows = 8 * EIGHTS, kCtas = CHUNKS * EIGHTS == 1 ? 3 : 2;
   static constexpr int kSteps = CHUNKS * 4;                           // 16-wide along a row
   static constexpr int kAhead = CHUNKS * EIGHTS > 4 ? 2 : 4;          // fragments in flight, as registers allow
-  uint32_t q[kSteps][2 * EIGHTS];
+  static constexpr bool kKeepQ = CHUNKS * EIGHTS < 6;                 // else its fragments are read for every tile
+  uint32_t q[kKeepQ ? kSteps : 1][2 * EIGHTS];
+  int heads;
   float o[kSteps][EIGHTS][4];                             // (d g, head 2t), (g, 2t + 1), (g + 8, 2t), (g + 8, 2t + 1)
   float m[EIGHTS][2], l[EIGHTS][2];                       // heads 2t, 2t + 1; l over this lane's keys
   uint32_t w[EIGHTS][4], keep[2];                         // the tile's weights, cut and rest; masks of its values
   bool part;
 
-  // q: the n heads' rows in shared memory.
+  // Step s of q, whose heads' rows lie in shared memory.
+  __device__ __forceinline__ void get_q(uint32_t (&x)[2 * EIGHTS], const char *qs, int s, int D) const {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int e = 0; e < 2 * EIGHTS; ++e) {
+      const int row = g + 8 * (e >> 1), d = s * 16 + 2 * t + 8 * (e & 1);
+      x[e] = row < heads && d < D ? *reinterpret_cast<const uint32_t *>(qs + (row * D + d) * 2) : 0u;
+    }
+  }
   __device__ void start(const Shape &p, const char *qs, int n) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, D = p.a.cache.dim;
+    heads = n;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-      for (int e = 0; e < 2 * EIGHTS; ++e) {
-        const int row = g + 8 * (e >> 1), d = s * 16 + 2 * t + 8 * (e & 1);
-        q[s][e] = row < n && d < D ? *reinterpret_cast<const uint32_t *>(qs + (row * D + d) * 2) : 0u;
-      }
+      if (kKeepQ) get_q(q[kKeepQ ? s : 0], qs, s, p.a.cache.dim);
 #pragma unroll
     for (int e = 0; e < EIGHTS; ++e) {
 #pragma unroll
@@ -69,7 +75,7 @@ struct Bf16Part {
   }
 
   // Weights of the tile's 16 keys from row0 on; keys lo <= i < hi of the tile count.
-  __device__ void logits(const Shape &p, const char *, float *, const char *k, int row0, int lo, int hi) {
+  __device__ void logits(const Shape &p, const char *qs, float *, const char *k, int row0, int lo, int hi) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, D = p.a.cache.dim, column = 128 << p.box_log;
     float s[2][EIGHTS][4] = {};   // even and odd steps
     {   // 8 x 8 blocks (keys 0-7 | 8-15) x (16-byte column even | odd)
@@ -83,8 +89,10 @@ struct Bf16Part {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) {
         if (i * 16 >= D) break;
+        uint32_t (&x)[2 * EIGHTS] = q[kKeepQ ? i : 0];
+        if (!kKeepQ) get_q(x, qs, i, D);
 #pragma unroll
-        for (int e = 0; e < EIGHTS; ++e) mma16816(s[i & 1][e], f[i % kAhead], q[i][2 * e], q[i][2 * e + 1]);
+        for (int e = 0; e < EIGHTS; ++e) mma16816(s[i & 1][e], f[i % kAhead], x[2 * e], x[2 * e + 1]);
         if (i + kAhead < kSteps && (i + kAhead) * 16 < D) ldsm4(f[i % kAhead], at(i + kAhead));
       }
     }

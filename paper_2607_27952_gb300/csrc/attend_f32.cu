@@ -10,7 +10,7 @@ namespace {
 // across the row's columns (with short rows several keys at once), the weights broadcast.
 template <int HEADS, int WIDE>   // heads held; 128-column blocks of a row
 struct F32Part {
-  static constexpr int kTile = 32, kWarpKeys = 8;
+  static constexpr int kTile = 32, kWarpKeys = 8, kCtas = HEADS <= 4 && WIDE == 1 ? 3 : 2;
   static constexpr int kHeadRows = HEADS;
   float o[HEADS][WIDE][4], m[HEADS], l[HEADS];
 

@@ -43,7 +43,7 @@ namespace {
 constexpr int kWarps = 4;                      // consumers: a quarter of every tile each
 constexpr int kThreads = 32 * (kWarps + 2);    // and one to load, one to add up
 constexpr int kRows = 16;                      // query heads of one pass over a kv-head
-constexpr int kMaxWorkers = 320;               // CTAs
+constexpr int kMaxWorkers = 480;               // CTAs
 constexpr int kMaxStages = 12;                 // of the ring: K or V of a tile each
 constexpr int kMergeFloats = 512;              // of a warp's sums laid down at a time: 8 x 64, 4 x 128 or 2 x 256
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -370,7 +370,7 @@ __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const 
 }
 
 template <typename Part, typename T>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, Part::kCtas)
 attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
   extern __shared__ char smem_raw[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = p.a.seq.batch;
@@ -577,7 +577,6 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   }
 }
 
-constexpr size_t kHalfSm = 109 * 1024;   // of shared memory for one of two CTAs; the rest is room for join_kernel
 constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 template <typename Part, typename T>
@@ -589,14 +588,18 @@ cudaError_t launch(Shape p, cudaStream_t s) {
   while ((2 << p.box_log) <= Part::kTile && c.page_size % (2 << p.box_log) == 0) ++p.box_log;
   p.joined = c.dim * (int)sizeof(T) % 128 == 0;
   p.page_log = (c.page_size & (c.page_size - 1)) == 0 ? __builtin_ctz((unsigned)c.page_size) : -1;
-  // two CTAs share an SM
+  // CTAs of an SM share its 228 KB: 1 KB each is the system's, 6 KB are room for join_kernel
+  constexpr size_t kShare = (size_t)(228 - 6) * 1024 / Part::kCtas / 1024 * 1024 - 2048;
   const size_t half = (size_t)p.chunks * Part::kTile * 128, q_slot = (size_t)slot_rows<Part, T>(p) * c.dim * sizeof(T);
   const size_t fixed = 1024 + sizeof(Shared) + (sizeof(T) == 4 ? kWarps * 8 * Part::kHeadRows * sizeof(float) : 0);
   auto smem_of = [&](int stages) { return fixed + stages * half + (stages + 1) / 2 * q_slot; };
   p.stages = kMaxStages;
-  while (p.stages > 2 && smem_of(p.stages) > kHalfSm) --p.stages;
+  while (p.stages > 2 && smem_of(p.stages) > kShare) --p.stages;
   p.slots = (p.stages + 1) / 2;
   const size_t smem = smem_of(p.stages);
+  // before the maps are encoded: a host thread's first runtime call gives it its context
+  cudaError_t e = allow_smem(reinterpret_cast<const void *>(&attend_kernel<Part, T>), smem);
+  if (e != cudaSuccess) return e;
   CUtensorMap maps[2];
   const uint64_t row = (uint64_t)c.dim * sizeof(T), head = c.heads > 1 ? (uint64_t)c.head_stride : row,
                  page = c.num_pages > 1 ? (uint64_t)c.page_stride : row, token = (uint64_t)c.token_stride;
@@ -609,9 +612,7 @@ cudaError_t launch(Shape p, cudaStream_t s) {
     if (!encode_rows_map(&maps[i], i ? c.v : c.k, sizeof(T) == 4, p.joined ? 5 : 4, p.joined ? dims5 : dims,
                          p.joined ? strides5 : strides, p.joined ? box5 : box))
       return cudaErrorInvalidValue;
-  cudaError_t e = allow_smem(reinterpret_cast<const void *>(&attend_kernel<Part, T>), smem);
-  if (e != cudaSuccess) return e;
-  int workers = sm_count() * 2;
+  int workers = sm_count() * Part::kCtas;
   workers = workers < kMaxWorkers ? workers : kMaxWorkers;
   e = launch_early(attend_kernel<Part, T>, dim3(workers), kThreads, smem, s, p, maps[0], maps[1]);
   if (e != cudaSuccess || a.seq.batch == 0) return e;

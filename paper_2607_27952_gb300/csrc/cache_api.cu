@@ -113,6 +113,11 @@ last_status make_rows(const last_heads *h, int elem, int tokens, bool need_out, 
   return LAST_OK;
 }
 
+last_status check_tokens(int32_t n) {
+  if (n < 0) return invalid("num_tokens < 0");
+  return n <= 1 << 30 ? LAST_OK : fail(LAST_ERR_UNSUPPORTED, "num_tokens must be at most 2^30");
+}
+
 last_status check_positions(const int32_t *positions, int64_t axis_stride, int num_axes, int tokens) {
   if (tokens > 0 && positions == nullptr) return invalid("positions are required");
   if (num_axes > 1 && axis_stride < tokens) return invalid("axis_stride must be at least num_tokens");
@@ -212,7 +217,7 @@ last_status rope(const last_rotary *r, int32_t dtype, int32_t num_tokens, int32_
   last_status st = check_dtype(dtype);
   if (st != LAST_OK) return st;
   if (r == nullptr || q == nullptr) return invalid("r and q are required");
-  if (num_tokens < 0) return invalid("num_tokens < 0");
+  if ((st = check_tokens(num_tokens)) != LAST_OK) return st;
   if (head_dim < 2) return invalid("head_dim must be at least 2");
   if (head_dim > 256) return fail(LAST_ERR_UNSUPPORTED, "head_dim must be at most 256");
   RotaryArgs a{};
@@ -270,7 +275,7 @@ last_status last_cache_append(const last_cache *c, int32_t layer, const last_seq
   return guarded([&]() -> last_status {
     last_status st = check_cache(c);
     if (st != LAST_OK || (st = check_layer(c, layer)) != LAST_OK || (st = check_sequences(s)) != LAST_OK) return st;
-    if (num_tokens < 0) return invalid("num_tokens < 0");
+    if ((st = check_tokens(num_tokens)) != LAST_OK) return st;
     if (cu_new == nullptr && num_tokens != s->batch)
       return invalid("without cu_new there is one token per sequence: num_tokens must be batch");
     if (num_tokens > 0 && s->batch == 0) return invalid("tokens without a sequence");

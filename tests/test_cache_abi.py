@@ -271,3 +271,18 @@ def test_rope_handle_of_sections():
         last.Rope([1.0, 0.5], axis=[0])
     with pytest.raises(KeyError):
         last.Rope([1.0], pairs="other")
+
+
+@pytest.mark.parametrize("kw", [dict(page_size=1 << 21), dict(num_layers=4097), dict(num_kv_heads=4097, head_dim=8, token_stride=8),
+                                dict(page_size=1 << 20, num_kv_heads=64)])
+def test_limits_of_a_cache(lib, kw):
+    n = ctypes.c_size_t(0)
+    assert lib.last_cache_workspace_size(ctypes.byref(_cache(**kw)), 3, 8194, ctypes.byref(n)) == last.LAST_ERR_UNSUPPORTED
+
+
+def test_limits_of_tokens_and_tiles(lib):
+    assert _rope(lib, tokens=(1 << 30) + 1, stride=1 << 31) == last.LAST_ERR_UNSUPPORTED
+    assert _append(lib, tokens=(1 << 30) + 1, cu=256) == last.LAST_ERR_UNSUPPORTED
+    s = _seqs(batch=1 << 20, max_pages=1 << 12, table_stride=1 << 12)
+    assert lib.last_cache_attention(ctypes.byref(_cache()), 0, ctypes.byref(s), 4, 0.0, 256, 256, 256, 256, None, 256, 1 << 40,
+                                    0) == last.LAST_ERR_UNSUPPORTED

@@ -263,3 +263,50 @@ def test_bad_pages_and_lengths_are_reported(dtype):
         last.last_cache_attention(cache, 0, seqs, q, out, ws)
         last.last_poll(ws)
         assert torch.equal(out, good)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("hq,hkv,d,lens", [(16, 1, 128, [40000]), (40, 1, 64, [25000]), (9, 3, 256, [6000, 9000]), (32, 2, 128, [3000, 0, 777])])
+def test_long_sequences_of_many_heads(hq, hkv, d, lens, dtype):
+    """A (sequence, kv-head) spread over a few CTAs or over all of them, several passes of heads."""
+    cache, seqs, q = _setup(lens, hq, hkv, d, dtype, 32, "head", seed=3)
+    out, lse = _run(cache, seqs, q)
+    _check(cache, seqs, q, out, lse, lens)
+
+
+def test_host_threads():
+    """Threads with problems of other sizes, head widths and types, each on its own stream and workspace."""
+    import threading
+    import torch
+    import cache_util as cu
+    calls = []
+    for i, (lens, hq, hkv, d, dtype) in enumerate([([700, 3], 4, 2, 128, "bfloat16"), ([90] * 40, 8, 8, 64, "float32"), ([5000], 16, 1, 256, "bfloat16"),
+                                                   ([33, 0, 2000], 12, 2, 80, "float32")]):
+        cache, seqs, q = _setup(lens, hq, hkv, d, dtype, 16, "head", seed=20 + i)
+        calls.append((cache, seqs, q, torch.empty_like(q), cu.workspace(cache, len(lens), hq), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    want = []
+    for cache, seqs, q, out, ws, _ in calls:
+        last.last_cache_attention(cache, 0, seqs, q, out, ws)
+        want.append(out.clone())
+    torch.cuda.synchronize()
+    errors, start = [], threading.Barrier(len(calls))
+
+    def work(i):
+        cache, seqs, q, out, ws, s = calls[i]
+        start.wait()
+        try:
+            for r in range(200):
+                last.last_cache_attention(cache, 0, seqs, q, out, ws, stream=s)
+                if r % 50 == 49:
+                    s.synchronize()
+        except Exception as e:   # reported by the main thread
+            errors.append(f"thread {i}: {e}")
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(calls))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors, errors
+    assert all(torch.equal(c[3], w) for c, w in zip(calls, want))
