@@ -38,6 +38,8 @@ __device__ __forceinline__ uint32_t pack_rest(float x, float y, uint32_t down) {
   return pack_bf16(fmaxf(x - bf16lo(down), x * 0x1p-30f), fmaxf(y - bf16hi(down), y * 0x1p-30f));
 }
 
+// Per tile of 64 keys by 128 a warp's logits take 700 cycles and its values 500 (with heads as rows, twice the
+// products at 8 heads, 1080 and 850).
 template <int CHUNKS, int EIGHTS>   // 128-byte columns of a row; groups of 8 heads
 struct Bf16Part {
   static constexpr int kTile = 64, kWarpKeys = 16, kHeadRows = 8 * EIGHTS, kCtas = CHUNKS * EIGHTS == 1 ? 3 : 2;

@@ -8,8 +8,13 @@
 // is read once for up to 16 query heads of its kv-head.
 //
 // A CTA: one warp keeps a ring of tiles filled with TMA boxes of the pages (128-byte swizzle),
-// four take a quarter of every tile each, with sums of their own, and add them up where
-// the CTA's part of a (sequence, head) ends.
+// four take a quarter of every tile each, with sums of their own, and one adds them up where
+// the CTA's part of a (sequence, head) ends.  Two CTAs per SM keep some 160 KB of K and V under way.
+//
+// Bound by HBM: 1.42 GB of K and V (6 sequences of about 115 thousand keys) take 209 us, 6.8 TB/s; 340 MB (64 of
+// about 650 keys, 16 kv-heads) 59 us, of which 8 are the start (lengths, page table, first tile: three reads
+// that wait for each other) and the join.  A tile of 64 keys by 128 arrives every 2600 cycles and its
+// products take 1450; one CTA of eight such warps and one loader per SM took 87 and 294 us.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -37,6 +42,7 @@ struct Shape {      // the same for every CTA
 };
 
 cudaError_t launch_attend_bf16(const Shape &p, cudaStream_t s);
+cudaError_t launch_attend_f32(const Shape &p, cudaStream_t s);
 
 namespace {
 
@@ -266,17 +272,27 @@ __device__ void consume(const Shape &p, Shared &sm, char *ring, char *qs, float 
   }
 }
 
+// The whole warp goes on to the next tile; sequences without one are passed over 32 at a time.
 __device__ __forceinline__ void advance(const Shape &p, Walk &w) {
   unsigned bad = 0;
   if (++w.at < w.tiles) return;
   w.at = 0;
   if (++w.head < p.heads) return;
   w.head = 0;
-  do {
-    if (++w.seq >= p.a.seq.batch) return;
-    w.keys = keys_of(p.a, w.seq, &bad);
-    w.tiles = tiles_of(w.keys, p.tile);
-  } while (w.tiles == 0);
+  for (int b0 = w.seq + 1; b0 < p.a.seq.batch; b0 += 32) {
+    const int b = b0 + (threadIdx.x & 31);
+    Keys k{0, 0};
+    if (b < p.a.seq.batch) k = keys_of(p.a, b, &bad);
+    const int n = tiles_of(k, p.tile);
+    const unsigned some = __ballot_sync(~0u, n > 0);
+    if (some == 0) continue;
+    const int lane = __ffs(some) - 1;
+    w.seq = b0 + lane;
+    w.keys.begin = __shfl_sync(~0u, k.begin, lane);
+    w.keys.end = __shfl_sync(~0u, k.end, lane);
+    w.tiles = __shfl_sync(~0u, n, lane);
+    return;
+  }
 }
 
 // One warp fills the ring, K and V of a tile by turns.  A tile's boxes (whole pages, or parts of them) are spread
@@ -400,9 +416,7 @@ attend_kernel(const __grid_constant__ Shape p, const __grid_constant__ CUtensorM
   // this CTA's share of all tiles: each thread counts some sequences' tiles
   unsigned bad = 0, mine = 0;
   const int per = (B + kThreads - 1) / kThreads, b0 = min(B, tid * per), b1 = min(B, b0 + per);
-  for (int b = b0; b < b1; ++b) {
-    mine += (unsigned)tiles_of(keys_of(p.a, b, &bad), p.tile) * p.heads;
-  }
+  for (int b = b0; b < b1; ++b) mine += (unsigned)tiles_of(keys_of(p.a, b, &bad), p.tile) * p.heads;
   unsigned upto = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -576,8 +590,6 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     __syncthreads();
   }
 }
-
-constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 template <typename Part, typename T>
 cudaError_t launch(Shape p, cudaStream_t s) {

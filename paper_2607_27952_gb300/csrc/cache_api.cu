@@ -139,6 +139,8 @@ last_status check_cache(const last_cache *c) {
     return fail(LAST_ERR_UNSUPPORTED, "page_size must be at most 2^20, num_kv_heads and num_layers at most 4096");
   if ((long long)c->page_size * c->num_kv_heads * c->head_dim * e >= 1LL << 31)
     return fail(LAST_ERR_UNSUPPORTED, "a page of one layer must stay below 2^31 bytes");
+  if ((long long)c->num_layers * c->num_kv_heads * c->head_dim * e >= 1LL << 31)
+    return fail(LAST_ERR_UNSUPPORTED, "a token's K of all layers must stay below 2^31 bytes");
   if (c->k == nullptr || c->v == nullptr) return invalid("k and v are required");
   if (!aligned(c->k, 16) || !aligned(c->v, 16)) return invalid("k and v must be 16-byte aligned");
   const int64_t strides[4] = {c->layer_stride, c->page_stride, c->head_stride, c->token_stride};

