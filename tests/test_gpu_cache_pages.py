@@ -394,3 +394,57 @@ def test_append_of_narrow_and_partly_rotated_rows(dtype, d, rot, pairs):
 def test_compaction_of_many_layers():
     """More rows a token than a CTA keeps addresses of."""
     _compact(24, [40, 9], [3, 0], [30, 9], [7, 2], 88, 8, 8, "bfloat16", "head", seed=7)
+
+
+def test_calls_behind_copies_and_joined_streams():
+    """The calls behind memory copies, memory sets and another stream's work, at once and in a graph."""
+    import torch
+    import cache_util as cu
+    hq, hkv, d, n = 8, 2, 128, 700
+    k, v = cu.pages(2, 120, hkv, 16, d, "bfloat16", "head", 1)
+    table, rest = cu.table([n], 16, 60, 2)
+    cache, lens = last.Cache(k, v), cu.ints([n])
+    seqs, ws, ws2 = last.Sequences(table, lens), cu.workspace(cache, 1, hq), cu.workspace(cache, 1, hq)
+    src_q, src_kv = cu.randn((40, hq, d), "bfloat16", 3), cu.randn((40, 2, hkv, d), "bfloat16", 4)
+    q, kv, out, out2 = torch.zeros_like(src_q[:1]), torch.zeros_like(src_kv[:1]), torch.zeros_like(src_q[:1]), torch.zeros_like(src_q[:1])
+    big, other = torch.empty(1 << 24, device="cuda"), torch.empty(1 << 24, device="cuda")
+    copied = cu.ints([100])
+    one = table[0, 43:44].clone()           # the last, partly filled page
+    side = torch.cuda.Stream()
+
+    def program():
+        main = torch.cuda.current_stream()
+        q.copy_(src_q[7:8])
+        kv.copy_(src_kv[7:8])               # memory copies
+        last.last_cache_append(cache, 0, seqs, kv[:, 0], kv[:, 1], ws)
+        big.zero_()                         # a memory set, or a kernel of torch
+        last.last_cache_attention(cache, 0, seqs, q, out, ws)
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            other.copy_(big)
+            last.last_cache_copy(cache, one, copied, ws2)
+        main.wait_stream(side)
+        last.last_cache_attention(cache, 1, seqs, q, out2, ws)
+
+    torch.cuda.synchronize()
+    program()
+    torch.cuda.synchronize()
+    last.last_poll(ws)
+    last.last_poll(ws2)
+    want, want2, want_k = out.clone(), out2.clone(), k.clone()
+    assert _same(k[:, 100], k[:, int(one)]) and want.abs().sum() > 0
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        program()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        program()
+    for t in (q, kv, out, out2):
+        t.zero_()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    last.last_poll(ws)
+    assert _same(out, want) and _same(out2, want2) and _same(k, want_k)
