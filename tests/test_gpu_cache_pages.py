@@ -448,3 +448,58 @@ def test_calls_behind_copies_and_joined_streams():
     torch.cuda.synchronize()
     last.last_poll(ws)
     assert _same(out, want) and _same(out2, want2) and _same(k, want_k)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_offsets_past_32_bits(dtype):
+    """Appending, cutting and copying in pages 5 GB apart (most of the storage is never touched)."""
+    import torch
+    import cache_util as cu
+    e = 4 if dtype == "float32" else 2
+    far = 5 * 2**30 // e
+    base = [torch.empty(3 * far + 8192, dtype=getattr(torch, dtype), device="cuda") for _ in range(2)]
+    k, v = (b.as_strided((1, 4, 2, 16, 64), (0, far, 1024, 64, 1)) for b in base)
+    for i, t in enumerate((k, v)):
+        t.copy_(cu.randn((1, 4, 2, 16, 64), dtype, i))
+    cache = last.Cache(k, v)
+    ws = cu.workspace(cache, 1, 2)
+    seqs = last.Sequences(cu.ints([[2, 0]]), cu.ints([20]))
+    x = cu.randn((6, 2, 64), dtype, 5)
+    last.last_cache_append(cache, 0, seqs, x, -x, ws, cu_new=cu.ints([0, 6]))
+    last.last_poll(ws)
+    assert _same(k[0, 2, :, 14:].transpose(0, 1), x[:2]) and _same(v[0, 0, :, :4].transpose(0, 1), -x[2:])
+    k0, v0, out = k.clone(), v.clone(), cu.ints([0])
+    idx = [0, 3, 15, 19]
+    last.last_cache_compact(cache, seqs, cu.ints([[3]]), cu.ints([0, 4]), cu.ints(idx), out, ws)
+    last.last_poll(ws)
+    for t, t0 in ((k, k0), (v, v0)):
+        assert _same(cu.rows(t, cu.ints([3]), 4, 16), cu.rows(t0, seqs.page_table[0], 20, 16)[:, :, idx])
+    last.last_cache_copy(cache, cu.ints([3]), cu.ints([1]), ws)
+    last.last_poll(ws)
+    assert _same(k[:, 1], k[:, 3]) and _same(v[:, 1], v[:, 3]) and _same(k[:, 0], k0[:, 0])
+
+
+def test_calls_allocate_nothing():
+    import torch
+    import cache_util as cu
+    k, v = cu.pages(2, 300, 2, 16, 128, "bfloat16", "head", 1)
+    table, rest = cu.table([900, 70], 16, 300, 2)
+    cache, seqs = last.Cache(k, v), last.Sequences(table, cu.ints([900, 70]))
+    ws = cu.workspace(cache, 2, 8)
+    q, x = cu.randn((2, 8, 128), "bfloat16", 3), cu.randn((2, 2, 128), "bfloat16", 4)
+    qo, out, rope, pos = torch.empty_like(q), torch.empty_like(q), last.Rope.sections([64]), cu.ints([5, 6])
+    dst, lens_out = cu.ints([rest[:60], rest[60:120]]), cu.ints([0, 0])
+    keep, idx, a, b = cu.ints([0, 10, 20]), cu.ints([*range(10)] * 2), cu.ints(rest[:3]), cu.ints(rest[120:123])
+
+    def calls():
+        last.last_rope(rope, pos, q, qo)
+        last.last_cache_append(cache, 0, seqs, x, x, ws, rope=rope, positions=pos, q=q, q_out=qo)
+        last.last_cache_attention(cache, 0, seqs, q, out, ws)
+        last.last_cache_compact(cache, seqs, dst, keep, idx, lens_out, ws)
+        last.last_cache_copy(cache, a, b, ws)
+        torch.cuda.synchronize()
+    calls()
+    free = torch.cuda.mem_get_info()[0]
+    for _ in range(3):
+        calls()
+    assert torch.cuda.mem_get_info()[0] == free
