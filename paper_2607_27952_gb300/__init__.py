@@ -103,11 +103,26 @@ class _PagePool(ctypes.Structure):
 
 
 _lib = None
+_fast = None   # the calls of the cache without ctypes (csrc/marshal.c), where that module has been built
+
+
+def _load_fast(lib):
+    """The marshalling module bound to the library, or None."""
+    try:
+        import torch
+        from . import _marshal
+        names = ("last_rope", "last_rope_backward", "last_cache_append", "last_cache_attention", "last_cache_copy",
+                 "last_cache_compact")
+        _marshal.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names), torch.float32, torch.bfloat16,
+                      torch.int32, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
+    except (ImportError, AttributeError):   # not built, or a torch without these
+        return None
+    return _marshal
 
 
 def load_library(path: str = LIB_PATH):
     """Loads liblast.so (raises if it has not been built)."""
-    global _lib
+    global _lib, _fast
     if _lib is not None:
         return _lib
     if not os.path.exists(path):
@@ -162,6 +177,7 @@ def load_library(path: str = LIB_PATH):
                  "last_scores_rows", "last_scores_rows_workspace_size",
                  "last_check_bounded_wait"):
         getattr(lib, name).restype = ctypes.c_int
+    _fast = _load_fast(lib)
     _lib = lib
     return lib
 
@@ -460,7 +476,7 @@ class Rope:
         self.num_axes = num_axes
         self.c = _Rotary(2 * n, num_axes, code, self.inv_freq.ctypes.data_as(ctypes.POINTER(ctypes.c_float)),
                          self.axis.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)))
-        self.ref = ctypes.byref(self.c)
+        self.ref, self.addr = ctypes.byref(self.c), ctypes.addressof(self.c)
 
     @classmethod
     def sections(cls, sections: Sequence[int], base: float = 10000.0, pairs: str = "half"):
@@ -486,7 +502,7 @@ class Cache:
         self.page_size, self.kv_heads, self.head_dim = size, heads, dim
         sl, sp, sh, st, _ = k.stride()
         self.c = _Cache(k.data_ptr(), v.data_ptr(), layers, pages, size, heads, dim, _code(k.dtype), sl, sp, sh, st)
-        self.ref = ctypes.byref(self.c)
+        self.ref, self.addr = ctypes.byref(self.c), ctypes.addressof(self.c)
 
 
 class Sequences:
@@ -504,7 +520,7 @@ class Sequences:
         self.batch = b
         self.c = _Sequences(b, n, page_table.stride(0), page_table.data_ptr(), lens.data_ptr(),
                             None if key_begin is None else key_begin.data_ptr())
-        self.ref = ctypes.byref(self.c)
+        self.ref, self.addr = ctypes.byref(self.c), ctypes.addressof(self.c)
 
 
 def _heads(x, out, dtype, dim, name):
@@ -529,7 +545,20 @@ def _positions(positions, num_axes, tokens):
     return positions.data_ptr(), positions.stride(0) if num_axes > 1 else tokens
 
 
-def _rope(call, rope: Rope, positions, q, q_out, k, k_out, stream):
+def _done(st) -> bool:
+    """Whether the marshalling module has made the call (raises if the library refused it)."""
+    if st is None:
+        return False
+    if st != LAST_OK:
+        _check(st)
+    return True
+
+
+def _rope(backward, rope: Rope, positions, q, q_out, k, k_out, stream):
+    if _fast is not None and _done(_fast.rope(backward, rope.addr, rope.num_axes, positions, q, q_out, k, k_out, stream)):
+        return
+    lib = load_library()
+    call = lib.last_rope_backward if backward else lib.last_rope
     shape, dtype = q.shape, q.dtype
     t, d = shape[0], shape[-1]
     if (k is None) != (k_out is None):
@@ -545,12 +574,12 @@ def _rope(call, rope: Rope, positions, q, q_out, k, k_out, stream):
 def last_rope(rope: Rope, positions, q, q_out, k=None, k_out=None, stream=None):
     """q and k [tokens][heads][head_dim] rotated by positions [axes][tokens] (int32) into q_out and k_out,
     which may be q and k themselves."""
-    _rope(load_library().last_rope, rope, positions, q, q_out, k, k_out, stream)
+    _rope(0, rope, positions, q, q_out, k, k_out, stream)
 
 
 def last_rope_backward(rope: Rope, positions, q, q_out, k=None, k_out=None, stream=None):
     """The gradients q and k of the rotated heads turned back into the heads' gradients q_out and k_out."""
-    _rope(load_library().last_rope_backward, rope, positions, q, q_out, k, k_out, stream)
+    _rope(1, rope, positions, q, q_out, k, k_out, stream)
 
 
 def last_cache_workspace_size(cache: Cache, batch: int, num_q_heads: int) -> int:
@@ -570,6 +599,10 @@ def last_cache_append(cache: Cache, layer: int, seqs: Sequences, k, v, ws, cu_ne
                       positions=None, q=None, q_out=None, stream=None):
     """New tokens' k and v [tokens][kv_heads][head_dim] written behind the sequences' cached ones (seqs.lens
     counts them already); with a rope, k is rotated on the way and q into q_out."""
+    if _fast is not None and _done(_fast.append(
+            cache.addr, layer, seqs.addr, seqs.batch, cache.head_dim, cache.dtype, k, v, ws, cu_new,
+            None if rope is None else rope.addr, 0 if rope is None else rope.num_axes, positions, q, q_out, stream)):
+        return
     dtype, d, t = cache.dtype, cache.head_dim, k.shape[0]
     if v.shape[0] != t or (q is not None and q.shape[0] != t):
         raise ValueError("q, k and v must have the same tokens")
@@ -588,6 +621,9 @@ def last_cache_attention(cache: Cache, layer: int, seqs: Sequences, q, out, ws, 
                          stream=None):
     """out = attention of q [batch][q_heads][head_dim] over the sequences' cached keys of one layer; lse
     [batch][q_heads] fp32 receives the log of the softmax's denominator."""
+    if _fast is not None and _done(_fast.attention(cache.addr, layer, seqs.addr, seqs.batch, cache.head_dim, cache.dtype, q, out, ws,
+                                                   lse, softmax_scale, stream)):
+        return
     shape, d, dtype = q.shape, cache.head_dim, cache.dtype
     if len(shape) != 3 or shape[0] != seqs.batch or shape[2] != d or out.shape != shape:
         raise ValueError(f"q and out: [{seqs.batch}][q_heads][{d}] expected")
@@ -606,6 +642,8 @@ def last_cache_attention(cache: Cache, layer: int, seqs: Sequences, q, out, ws, 
 
 def last_cache_copy(cache: Cache, src, dst, ws, stream=None):
     """Pages src[i] copied to pages dst[i] (device int32), every layer, K and V."""
+    if _fast is not None and _done(_fast.copy(cache.addr, src, dst, ws, stream)):
+        return
     n = src.shape[0]
     p, nb = _ws(ws)
     _check(load_library().last_cache_copy(cache.ref, n, _int32(src, "src", (n,)).data_ptr(),
@@ -616,6 +654,9 @@ def last_cache_compact(cache: Cache, seqs: Sequences, dst_table, cu_keep, idx, l
                        span_len=None, stream=None):
     """The sequences' tokens outside their spans and the spans' tokens idx (as last_select writes them),
     in order, copied to the pages of dst_table [batch][max_pages]; lens_out [batch] receives the new lengths."""
+    if _fast is not None and _done(_fast.compact(cache.addr, seqs.addr, seqs.batch, dst_table, cu_keep, idx, lens_out, ws, span_begin,
+                                                 span_len, stream)):
+        return
     b, shape = seqs.batch, dst_table.shape
     if len(shape) != 2 or shape[0] != b or idx.dim() != 1:
         raise ValueError("dst_table: [batch][max_pages], idx: one dimension expected")

@@ -1,7 +1,8 @@
 """Builds liblast.so in-tree from csrc/*.cu for sm_103a (nvcc, no cmake).
 
 Each translation unit is compiled in parallel, then linked into one shared
-library against the shared CUDA runtime.
+library against the shared CUDA runtime.  The binding's marshalling module is compiled
+with gcc beside it, where Python's headers are installed.
 """
 from __future__ import annotations
 
@@ -9,6 +10,7 @@ import concurrent.futures as cf
 import os
 import shutil
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -16,6 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liblast.so")
+MARSHAL = os.path.join(PKG, "_marshal.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
@@ -57,7 +60,7 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
-            raise RuntimeError(f"nvcc failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+            raise RuntimeError(f"compiler failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
         return r.stdout + r.stderr
 
     with cf.ThreadPoolExecutor(max_workers=max(1, min(len(jobs), os.cpu_count() or 4))) as ex:
@@ -70,7 +73,20 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
         run([nvcc, *ARCH, "-shared", "-cudart", "shared", "-o", tmp, *objs,
              "-Xlinker", "-rpath", "-Xlinker", cuda_lib])
         os.replace(tmp, LIB)
+    build_marshal(run, force)
     return LIB
+
+
+def build_marshal(run, force: bool = False):
+    """_marshal.so, without which the binding goes through ctypes."""
+    src, python = os.path.join(CSRC, "marshal.c"), sysconfig.get_paths()["include"]
+    if not os.path.exists(os.path.join(python, "Python.h")):
+        return
+    if force or _stale(MARSHAL, [src, os.path.join(INCLUDE, "last.h")]):
+        tmp = MARSHAL + f".tmp{os.getpid()}"
+        run([os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-Wall", "-Wextra", "-Wno-missing-field-initializers", "-shared",
+             "-fPIC", "-I", python, "-I", INCLUDE, src, "-o", tmp])
+        os.replace(tmp, MARSHAL)
 
 
 if __name__ == "__main__":

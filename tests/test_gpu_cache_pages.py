@@ -503,3 +503,53 @@ def test_calls_allocate_nothing():
     for _ in range(3):
         calls()
     assert torch.cuda.mem_get_info()[0] == free
+
+
+def test_both_ways_of_the_binding(monkeypatch):
+    """The marshalling module and ctypes hand the library the same arguments and refuse the same tensors."""
+    import torch
+    import cache_util as cu
+    assert last.load_library() and last._fast is not None, "the marshalling module has not been built"
+
+    def everything():
+        k, v = cu.pages(2, 60, 2, 16, 64, "bfloat16", "token", 1)
+        table, rest = cu.table([90, 33], 16, 60, 2)
+        cache, seqs = last.Cache(k, v), last.Sequences(table, cu.ints([90, 33]), cu.ints([3, 0]))
+        ws = cu.workspace(cache, 2, 6)
+        fused = cu.randn((5, 10, 64), "bfloat16", 3)
+        q, kn, vn = fused.split([6, 2, 2], dim=1)
+        qo, ko, out = torch.zeros_like(q), torch.zeros_like(kn), torch.zeros((2, 6, 64), dtype=q.dtype, device="cuda")
+        lse, rope, pos = torch.zeros((2, 6), device="cuda"), last.Rope.sections([8, 12, 12]), cu.ints(np.arange(15).reshape(3, 5))
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        last.last_rope(rope, pos, q, qo, k=kn, k_out=ko, stream=s)
+        last.last_rope_backward(rope, pos, qo, qo, stream=s.cuda_stream)
+        torch.cuda.current_stream().wait_stream(s)
+        got = [qo.clone(), ko]
+        last.last_cache_append(cache, 1, seqs, kn, vn, ws, cu_new=cu.ints([0, 3, 5]), rope=rope, positions=pos, q=q, q_out=qo)
+        last.last_cache_append(cache, 0, seqs, kn[:2], vn[:2], ws)
+        last.last_cache_attention(cache, 1, seqs, qo[[2, 4]], out, ws, lse=lse, softmax_scale=0.2)
+        lens_out, dst = cu.ints([0, 0]), cu.ints(np.stack([rest[:6], rest[6:12]]))
+        last.last_cache_compact(cache, seqs, dst, cu.ints([0, 2, 3]), cu.ints([0, 7, 1]), lens_out, ws, span_begin=cu.ints([4, 0]),
+                                span_len=cu.ints([60, 20]))
+        last.last_cache_copy(cache, dst[:, 0].contiguous(), cu.ints(rest[12:14]), ws)
+        last.last_poll(ws)
+        for call in (lambda: last.last_rope(rope, pos[:2], q, qo), lambda: last.last_rope(rope, pos, q, qo, k=kn),
+                     lambda: last.last_cache_append(cache, 0, seqs, kn[:2], vn, ws),
+                     lambda: last.last_cache_append(cache, 0, seqs, kn[:2].float(), vn[:2], ws),
+                     lambda: last.last_cache_attention(cache, 0, seqs, qo[:2].cpu(), out, ws),
+                     lambda: last.last_cache_attention(cache, 0, seqs, qo[:2], out, ws, lse=lse[:, :3]),
+                     lambda: last.last_cache_attention(cache, 0, seqs, qo[:2], out, ws.cpu()),
+                     lambda: last.last_cache_compact(cache, seqs, dst, cu.ints([0, 2]), cu.ints([0, 7, 1]), lens_out, ws),
+                     lambda: last.last_cache_copy(cache, cu.ints([1]), torch.zeros(1, dtype=torch.int64, device="cuda"), ws)):
+            with pytest.raises(ValueError):
+                call()
+        with pytest.raises(last.LastError):
+            last.last_cache_attention(cache, 2, seqs, qo[:2], out, ws)
+        with pytest.raises(last.LastError):
+            last.last_cache_copy(cache, cu.ints([1]), cu.ints([2]), ws[:512])
+        return [*got, qo, k, v, out, lse, lens_out]
+
+    want = everything()
+    monkeypatch.setattr(last, "_fast", None)
+    assert all(_same(a, b) for a, b in zip(everything(), want))
