@@ -624,8 +624,11 @@ cudaError_t launch(Shape p, cudaStream_t s) {
     if (!encode_rows_map(&maps[i], i ? c.v : c.k, sizeof(T) == 4, p.joined ? 5 : 4, p.joined ? dims5 : dims,
                          p.joined ? strides5 : strides, p.joined ? box5 : box))
       return cudaErrorInvalidValue;
+  // no more CTAs than the page tables have room for tiles
+  const long long most = (long long)a.seq.batch * p.heads * ((long long)a.seq.max_pages * c.page_size / p.tile + 2);
   int workers = sm_count() * Part::kCtas;
   workers = workers < kMaxWorkers ? workers : kMaxWorkers;
+  if (workers > most) workers = most > 0 ? (int)most : 1;
   e = launch_early(attend_kernel<Part, T>, dim3(workers), kThreads, smem, s, p, maps[0], maps[1]);
   if (e != cudaSuccess || a.seq.batch == 0) return e;
   return launch_early(join_kernel<T>, dim3(workers), kJoinThreads, 0, s, p);
