@@ -20,17 +20,18 @@ struct F32Part {
     const int n = D / 4;
     return n > 16 ? 32 : n > 8 ? 16 : n > 4 ? 8 : n > 2 ? 4 : n;
   }
-  __device__ void start(const Shape &, const char *, int) {
+  // Heads past the pass's n start from +inf: their logits, of whatever the slot holds, then never move the maxima.
+  __device__ void start(const Shape &, const char *, int n) {
 #pragma unroll
     for (int h = 0; h < HEADS; ++h) {
-      m[h] = -INFINITY;
+      m[h] = h < n ? -INFINITY : INFINITY;
       l[h] = 0.0f;
 #pragma unroll
       for (int w = 0; w < WIDE; ++w) o[h][w][0] = o[h][w][1] = o[h][w][2] = o[h][w][3] = 0.0f;
     }
   }
   // Weights of the tile's 8 keys from row0 on, kept in this warp's ps [8 keys][HEADS]; keys lo <= i < hi of
-  // the tile count.  q: the heads' rows (past the pass's heads anything: their sums are not used).
+  // the tile count.  q: the heads' rows (past the pass's heads anything: neither their sums nor their logits are used).
   __device__ void logits(const Shape &p, const char *q, float *ps, const char *k, int row0, int lo, int hi) {
     const int lane = threadIdx.x & 31, D = p.a.cache.dim, cols = D / 4, column = 128 << p.box_log;
     const float4 *qs = reinterpret_cast<const float4 *>(q);

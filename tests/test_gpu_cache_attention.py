@@ -326,3 +326,27 @@ def test_mostly_empty_batches(dtype):
     assert (out[empty] == 0).all() and (lse[empty] == -math.inf).all()
     part = last.Sequences(seqs.page_table[live.tolist()].contiguous(), seqs.lens[live.tolist()].contiguous())
     _check(cache, part, q[live.tolist()], out[live.tolist()], lse[live.tolist()], lens[live])
+
+
+# ---- what a call may not depend on ----
+
+@pytest.mark.parametrize("hq,hkv,d,dtype", [
+    (4, 2, 64, "float32"), (6, 2, 128, "float32"), (3, 1, 80, "float32"), (12, 2, 64, "float32"), (14, 2, 128, "float32"),
+    (5, 1, 256, "float32"), (20, 2, 64, "float32"), (20, 1, 128, "float32"), (9, 1, 256, "float32"),
+    (12, 2, 64, "bfloat16"), (20, 1, 128, "bfloat16"), (9, 1, 256, "bfloat16"),
+])
+def test_what_shared_memory_held_decides_no_bits(hq, hkv, d, dtype):
+    """Groups that leave some of the heads a kernel holds without a query: calls of full groups with queries of no, of
+    common and of huge size in between change nothing."""
+    import torch
+    import cache_util as cu
+    rng = np.random.default_rng(2)
+    lens = rng.integers(1, 2500, 24)
+    cache, seqs, q = _setup(lens, hq, hkv, d, dtype, 16, "head", seed=6)
+    want = _run(cache, seqs, q)
+    _check(cache, seqs, q, *want, lens)
+    for full in (4, 8, 16):
+        for scale in (0.0, 3.0, 1e4):
+            _run(cache, seqs, cu.randn((len(lens), full * hkv, d), dtype, 30 + full, scale))
+            got = _run(cache, seqs, q)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (full, scale)
