@@ -76,8 +76,11 @@ struct Bf16Part {
     }
   }
 
-  // Weights of the tile's 16 keys from row0 on; keys lo <= i < hi of the tile count.
-  __device__ void logits(const Shape &p, const char *qs, float *, const char *k, int row0, int lo, int hi) {
+  // The warp's keys may lie in two boxes: logits() looks at each.
+  static __device__ __forceinline__ bool skips(const Shape &, unsigned, int) { return false; }
+
+  // Weights of the tile's 16 keys from row0 on; keys lo <= i < hi of the tile count, but for those of the boxes in skip.
+  __device__ void logits(const Shape &p, const char *qs, float *, const char *k, int row0, int lo, int hi, unsigned skip) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, D = p.a.cache.dim, column = 128 << p.box_log;
     float s[2][EIGHTS][4] = {};   // even and odd steps
     {   // 8 x 8 blocks (keys 0-7 | 8-15) x (16-byte column even | odd)
@@ -98,18 +101,17 @@ struct Bf16Part {
         if (i + kAhead < kSteps && (i + kAhead) * 16 < D) ldsm4(f[i % kAhead], at(i + kAhead));
       }
     }
-    part = lo > row0 || hi < row0 + 16;
+    part = lo > row0 || hi < row0 + 16 || skip != 0;
+    auto counts = [&](int key) { return key >= lo && key < hi && (skip >> (key >> p.box_log) & 1) == 0; };
     keep[0] = keep[1] = ~0u;   // halves of V's fragments whose keys count
     if (part) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int key = row0 + j * 8 + 2 * t + e;
-          if (key < lo || key >= hi) keep[j] &= e ? 0x0000ffffu : 0xffff0000u;
+          if (!counts(row0 + j * 8 + 2 * t + e)) keep[j] &= e ? 0x0000ffffu : 0xffff0000u;
         }
-        const int key = row0 + j * 8 + g;
-        if (key < lo || key >= hi)
+        if (!counts(row0 + j * 8 + g))
 #pragma unroll
           for (int e = 0; e < EIGHTS; ++e) s[0][e][2 * j] = s[0][e][2 * j + 1] = s[1][e][2 * j] = s[1][e][2 * j + 1] = -INFINITY;
       }

@@ -30,9 +30,12 @@ struct F32Part {
       for (int w = 0; w < WIDE; ++w) o[h][w][0] = o[h][w][1] = o[h][w][2] = o[h][w][3] = 0.0f;
     }
   }
+  // A box holds 8 keys and more: the warp's are all in one.
+  static __device__ __forceinline__ bool skips(const Shape &p, unsigned skip, int row0) { return skip >> (row0 >> p.box_log) & 1; }
+
   // Weights of the tile's 8 keys from row0 on, kept in this warp's ps [8 keys][HEADS]; keys lo <= i < hi of
   // the tile count.  q: the heads' rows (past the pass's heads anything: neither their sums nor their logits are used).
-  __device__ void logits(const Shape &p, const char *q, float *ps, const char *k, int row0, int lo, int hi) {
+  __device__ void logits(const Shape &p, const char *q, float *ps, const char *k, int row0, int lo, int hi, unsigned) {
     const int lane = threadIdx.x & 31, D = p.a.cache.dim, cols = D / 4, column = 128 << p.box_log;
     const float4 *qs = reinterpret_cast<const float4 *>(q);
     const int row = row0 + (lane & 7);

@@ -62,6 +62,7 @@ struct TileInfo {   // what the producer says of a tile
 // First and last tile of the CTA's part of a (sequence, head); the part is all of it; it is not the
 // CTA's first one.
 constexpr int kFirst = 1, kLast = 2, kWhole = 4, kLater = 8, kEnd = 16;   // kEnd: the CTA's last tile
+constexpr int kSkip = 8;   // flags from this bit on: boxes of the tile whose page is out of range, left out
 constexpr int kStatFloats = 2 * kRows;   // of a parted sum: maximum and denominator per head, then the rows
 
 struct Keys {
@@ -262,8 +263,9 @@ __device__ void consume(const Shape &p, Shared &sm, char *ring, char *qs, float 
     const TileInfo ti = sm.info[stage];
     const char *q = qs + ti.slot * q_bytes;
     if (ti.flags & kFirst) part.start(p, q, min(kRows, p.group - ti.head % p.passes * kRows));
-    const bool mine = warp * Part::kWarpKeys < ti.hi && (warp + 1) * Part::kWarpKeys > ti.lo;
-    if (mine) part.logits(p, q, weights, ring + (long long)stage * half, warp * Part::kWarpKeys, ti.lo, ti.hi);
+    const unsigned skip = (unsigned)ti.flags >> kSkip;
+    const bool mine = warp * Part::kWarpKeys < ti.hi && (warp + 1) * Part::kWarpKeys > ti.lo && !Part::skips(p, skip, warp * Part::kWarpKeys);
+    if (mine) part.logits(p, q, weights, ring + (long long)stage * half, warp * Part::kWarpKeys, ti.lo, ti.hi, skip);
     give_back();
     if (!wait(sm, &sm.full[stage], round & 1)) return;
     if (mine) part.values(p, weights, ring + (long long)stage * half, warp * Part::kWarpKeys, ti.lo, ti.hi);
@@ -320,17 +322,22 @@ __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const 
       advance(p, next);
       next_page = lookup(next);   // not looked at before its own turn
     }
-    const bool last = it + 1 == tiles || w.at + 1 == w.tiles, here = counts(w);
+    const bool last = it + 1 == tiles || w.at + 1 == w.tiles;
+    bool here = counts(w);
+    int bytes = 0;
     if (fresh) begun = w.at == 0;
-    const int bytes = __popc(__ballot_sync(~0u, lane < boxes && here)) * p.chunks * box * 128;
     const int kv = p.passes == 1 ? w.head : w.head / p.passes;
     const int row = p.page_log >= 0 ? box_key(w) & (size - 1) : box_key(w) % size;
 #pragma unroll
     for (int is_v = 0; is_v < 2; ++is_v) {
       if (round > 0 && !wait(sm, &sm.empty[stage], (round & 1) ^ 1)) return;
-      if (is_v == 0 && here && (unsigned)page >= (unsigned)p.a.cache.num_pages) {
-        atomicOr(&sm.flags, kErrCacheIndex);
-        page = 0;   // any page will do: the call is reported
+      unsigned skip = 0;
+      if (is_v == 0) {
+        const bool bad = here && (unsigned)page >= (unsigned)p.a.cache.num_pages;
+        if (bad) atomicOr(&sm.flags, kErrCacheIndex);
+        here &= !bad;
+        skip = __ballot_sync(~0u, lane < boxes && bad);
+        bytes = __popc(__ballot_sync(~0u, lane < boxes && here)) * p.chunks * box * 128;
       }
       if (lane == 0) {
         if (is_v == 0) {
@@ -341,7 +348,7 @@ __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const 
           ti.lo = w.keys.begin - k0;
           ti.hi = w.keys.end - k0;
           ti.flags = (fresh ? kFirst : 0) | (last ? kLast : 0) | (begun && w.at + 1 == w.tiles ? kWhole : 0) | (later ? kLater : 0) |
-                     (it + 1 == tiles ? kEnd : 0);
+                     (it + 1 == tiles ? kEnd : 0) | (int)(skip << kSkip);
           ti.slot = slot;
           sm.info[stage] = ti;
           const int q_bytes = fresh ? min(kRows, p.group - pass * kRows) * row_bytes : 0;

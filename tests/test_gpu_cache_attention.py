@@ -350,3 +350,43 @@ def test_what_shared_memory_held_decides_no_bits(hq, hkv, d, dtype):
             _run(cache, seqs, cu.randn((len(lens), full * hkv, d), dtype, 30 + full, scale))
             got = _run(cache, seqs, q)
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (full, scale)
+
+
+@pytest.mark.parametrize("order", ["head", "token"])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("hq,hkv,d,size", [(4, 2, 64, 16), (6, 2, 80, 24), (1, 1, 128, 8), (16, 1, 64, 64), (3, 1, 256, 40), (20, 1, 128, 128)])
+def test_keys_of_bad_pages_are_left_out(hq, hkv, d, size, dtype, order):
+    """A sequence with pages out of range attends over its other keys alone, and is empty without any; no
+    page that it does not name (page 0 among them) is used in their place."""
+    import torch
+    import cache_util as cu
+    lens = [300, 301, 64, 257, 30, 2000]
+    pool = sum(-(-n // size) for n in lens) + 1
+    k, v = cu.pages(1, pool, hkv, size, d, dtype, order, 1)
+    table, _ = cu.table(lens, size, pool - 1, 2)
+    table = torch.where(table >= 0, table + 1, table)
+    for t in (k, v):
+        t[0, 0] = float("nan")                                    # page 0 is nobody's
+    cache, q = last.Cache(k, v), cu.randn((len(lens), hq, d), dtype, 3)
+    pages = [-(-n // size) for n in lens]
+    bad = {1: [0], 2: list(range(pages[2])), 3: [pages[3] - 1, pages[3] // 2], 5: list(range(1, pages[5], 2))}
+    broken = table.clone()
+    for b, at in bad.items():
+        for i, p in enumerate(at):
+            broken[b, p] = (-1, pool, 2**31 - 1, -2**31)[i % 4]
+    out, lse = torch.full_like(q, float("nan")), torch.full((len(lens), hq), float("nan"), device="cuda")
+    ws, scale = cu.workspace(cache, len(lens), hq), 1 / math.sqrt(d)
+    last.last_cache_attention(cache, 0, last.Sequences(broken, cu.ints(lens)), q, out, ws, lse=lse)
+    with pytest.raises(last.LastError) as e:
+        last.last_poll(ws)
+    assert e.value.status == last.LAST_ERR_DEVICE_INDEX
+    for b, n in enumerate(lens):
+        live = [i for i in range(n) if i // size not in bad.get(b, [])]
+        kb, vb = (cu.rows(t, table[b], n, size)[0][:, live] for t in (k, v))
+        want, want_lse, mass = cu.attention(q[b], kb, vb, scale)
+        if not live:
+            assert (out[b] == 0).all() and (lse[b] == -math.inf).all()
+            continue
+        ez, rel, u = cu.attention_bounds(q[b], kb, scale, len(live), dtype)
+        assert ((out[b].double() - want).abs() <= rel * mass + u * want.abs()).all(), b
+        assert ((lse[b].double() - want_lse).abs() <= 2 * ez + 2.0 ** -20 * (1 + want_lse.abs()) + (n / 8 + 64) * 2.0 ** -24).all(), b
