@@ -340,7 +340,8 @@ last_status last_cache_append(const last_cache *c, int32_t layer, const last_seq
  * and lse = -inf, and so does one whose logits are all -inf; a key of logit -inf has weight 0.
  * Slots outside the range are never used, whatever they hold, and pages wholly outside it are
  * not read (their table entries may be anything).  Keys of a page out of range are left out, as
- * if they were not cached.  q-head h reads kv-head h / (num_q_heads / num_kv_heads).  q and out:
+ * if they were not cached; a sequence is taken for one without a key where lens[b] is negative or
+ * more than its table row has room for, or key_begin[b] is negative.  q-head h reads kv-head h / (num_q_heads / num_kv_heads).  q and out:
  * [batch][num_q_heads][head_dim], sequences q_stride and out_stride elements apart, both multiples
  * of 16 bytes, 16-byte aligned.  scale <= 0 selects 1/sqrt(head_dim).  Results do not depend on
  * other calls or on timing: repeated calls give the same bits.  batch * num_q_heads *

@@ -111,13 +111,13 @@ __device__ __forceinline__ bool wait(Shared &sm, unsigned long long *bar, uint32
   return false;
 }
 
+// A sequence whose length or first key is out of range has none.
 __device__ __forceinline__ Keys keys_of(const AttendArgs &a, int b, unsigned *bad) {
   const long long room = (long long)a.seq.max_pages * a.cache.page_size;
-  int end = a.seq.lens[b], begin = a.seq.begin ? a.seq.begin[b] : 0;
-  if (end < 0 || end > room || begin < 0) *bad = kErrCacheIndex;
-  end = end > room ? (int)room : end;
-  begin = begin < 0 ? 0 : begin;
-  return Keys{begin, end};
+  const int end = a.seq.lens[b], begin = a.seq.begin ? a.seq.begin[b] : 0;
+  if (end >= 0 && end <= room && begin >= 0) return Keys{begin, end};
+  *bad = kErrCacheIndex;
+  return Keys{0, 0};
 }
 __device__ __forceinline__ int tiles_of(Keys k, int tile) {
   return k.begin < k.end ? (k.end - 1) / tile - k.begin / tile + 1 : 0;

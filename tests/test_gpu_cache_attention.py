@@ -390,3 +390,26 @@ def test_keys_of_bad_pages_are_left_out(hq, hkv, d, size, dtype, order):
         ez, rel, u = cu.attention_bounds(q[b], kb, scale, len(live), dtype)
         assert ((out[b].double() - want).abs() <= rel * mass + u * want.abs()).all(), b
         assert ((lse[b].double() - want_lse).abs() <= 2 * ez + 2.0 ** -20 * (1 + want_lse.abs()) + (n / 8 + 64) * 2.0 ** -24).all(), b
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_sequences_of_bad_length_are_empty(dtype):
+    """A length or first key out of range: the sequence gets what one without a key gets, the others theirs."""
+    import torch
+    import cache_util as cu
+    lens = [100, 300, 50, 700, 5]
+    cache, seqs, q = _setup(lens, 4, 2, 64, dtype, 16, "head")
+    room = seqs.page_table.shape[1] * 16
+    for n, begin in ((room + 1, 0), (2**31 - 1, 0), (-1, 0), (-2**31, 0), (300, -1), (300, -2**31), (room + 1, 290)):
+        lens_dev, first = cu.ints(lens), cu.ints([0] * 5)
+        lens_dev[1], first[1] = n, begin
+        out, lse = torch.full_like(q, float("nan")), torch.full(q.shape[:2], float("nan"), device="cuda")
+        ws = cu.workspace(cache, 5, 4)
+        last.last_cache_attention(cache, 0, last.Sequences(seqs.page_table, lens_dev, first), q, out, ws, lse=lse)
+        with pytest.raises(last.LastError) as e:
+            last.last_poll(ws)
+        assert e.value.status == last.LAST_ERR_DEVICE_INDEX
+        assert (out[1] == 0).all() and (lse[1] == -math.inf).all(), (n, begin)
+        others = [0, 2, 3, 4]
+        part = last.Sequences(seqs.page_table[others], seqs.lens[others])
+        _check(cache, part, q[others], out[others], lse[others], [lens[b] for b in others])
