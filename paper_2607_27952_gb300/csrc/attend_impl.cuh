@@ -309,7 +309,8 @@ __device__ void produce(const Shape &p, Shared &sm, char *ring, char *qs, const 
   const int ops = boxes * (p.joined ? 1 : p.chunks), half = p.chunks * kTile * 128;
   const int size = p.a.cache.page_size, row_bytes = p.a.cache.dim * (int)sizeof(T);
   auto box_key = [&](const Walk &x) { return (x.keys.begin / kTile + x.at) * kTile + mine * box; };
-  auto counts = [&](const Walk &x) { return box_key(x) < x.keys.end && box_key(x) + box > x.keys.begin; };
+  // begin - box, not key + box: that passes 2^31 behind the last key that a length can say
+  auto counts = [&](const Walk &x) { return box_key(x) < x.keys.end && box_key(x) > x.keys.begin - box; };
   auto lookup = [&](const Walk &x) {   // page of this lane's box, as the table has it
     const int key = box_key(x);
     return counts(x) ? p.a.seq.table[x.seq * p.a.seq.table_stride + (p.page_log >= 0 ? key >> p.page_log : key / size)] : 0;

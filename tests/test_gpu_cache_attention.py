@@ -413,3 +413,22 @@ def test_sequences_of_bad_length_are_empty(dtype):
         others = [0, 2, 3, 4]
         part = last.Sequences(seqs.page_table[others], seqs.lens[others])
         _check(cache, part, q[others], out[others], lse[others], [lens[b] for b in others])
+
+
+@pytest.mark.parametrize("size", [8, 24, 1 << 20])
+@pytest.mark.parametrize("dtype,d", [("float32", 8), ("bfloat16", 16), ("bfloat16", 64)])
+def test_the_last_keys_that_32_bits_count(size, dtype, d):
+    """A window at the end of the longest sequence that a length can say; its pages are one page over and over."""
+    import torch
+    import cache_util as cu
+    n, keys = 2**31 - 1, 90
+    k, v = cu.pages(1, 1, 1, size, d, dtype, "head", 1)
+    table = torch.zeros((1, -(-n // size)), dtype=torch.int32, device="cuda")
+    cache, q = last.Cache(k, v), cu.randn((1, 2, d), dtype, 3)
+    seqs = last.Sequences(table, cu.ints([n]), cu.ints([n - keys]))
+    out, lse = _run(cache, seqs, q)
+    at = (torch.arange(n - keys, n, device="cuda") % size).long()
+    want, want_lse, mass = cu.attention(q[0], k[0, 0][:, at], v[0, 0][:, at], 1 / math.sqrt(d))
+    ez, rel, u = cu.attention_bounds(q[0], k[0, 0][:, at], 1 / math.sqrt(d), keys, dtype)
+    assert ((out[0].double() - want).abs() <= rel * mass + u * want.abs()).all()
+    assert ((lse[0].double() - want_lse).abs() <= 2 * ez + 2.0 ** -18).all()
