@@ -366,7 +366,8 @@ last_status last_cache_copy(const last_cache *c, int32_t num_copies, const int32
  * same call, but a page may stand in both tables where its tokens keep their slots (those before
  * the first dropped one): a token that would be copied onto itself is left alone.  A
  * sequence whose span, cu_keep or dst_table cannot hold is skipped, lens_out[b] included;
- * so is a single token whose idx or page is out of range.  lens_out may not be s->lens. */
+ * so is a single token whose idx or page is out of range.  lens_out may not overlap any array that
+ * the call reads. */
 last_status last_cache_compact(const last_cache *c, const last_sequences *s,
                                const int32_t *dst_table, int32_t dst_max_pages,
                                int64_t dst_stride, const int32_t *span_begin,

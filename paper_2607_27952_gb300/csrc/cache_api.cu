@@ -176,6 +176,17 @@ last_status check_cache_ws(const void *ws, size_t ws_bytes, size_t need) {
   return LAST_OK;
 }
 
+// Whether the `bytes` from `out` on hold any of `rows` rows of `width` int32 each, `stride` of them apart.
+bool overlaps(const void *out, long long bytes, const int32_t *in, long long rows, long long stride, long long width) {
+  if (in == nullptr || bytes <= 0 || rows <= 0 || width <= 0) return false;
+  const auto begin = static_cast<__int128>(reinterpret_cast<uintptr_t>(out)) - static_cast<__int128>(reinterpret_cast<uintptr_t>(in));
+  const __int128 end = begin + bytes, w = (__int128)width * 4, step = (__int128)stride * 4;
+  if (rows == 1) return begin < w && end > 0;
+  // row i takes i step .. i step + w: the first that ends behind `begin` and whether it starts before `end`
+  __int128 i = begin < w ? 0 : (begin - w) / step + 1;
+  return i < rows && i * step < end;
+}
+
 CacheLayer layer_of(const last_cache *c, int layer) {
   const int e = elem_bytes(c->dtype);
   CacheLayer l;
@@ -374,7 +385,14 @@ last_status last_cache_compact(const last_cache *c, const last_sequences *s, con
     if (dst_max_pages < (s->batch > 0 ? 1 : 0) || (s->batch > 1 && dst_stride < dst_max_pages))
       return invalid("dst_stride must be at least dst_max_pages, which must be positive");
     if (num_idx < 0 || (num_idx > 0 && idx == nullptr)) return invalid("idx must hold num_idx >= 0 entries");
-    if (s->batch > 0 && lens_out == s->lens) return invalid("lens_out may not be lens");
+    // other CTAs still read these while lens_out is written
+    const long long b = s->batch, bytes = b * 4;
+    if (overlaps(lens_out, bytes, s->lens, 1, 0, b) || overlaps(lens_out, bytes, span_begin, 1, 0, b) ||
+        overlaps(lens_out, bytes, span_len, 1, 0, b) || overlaps(lens_out, bytes, cu_keep, 1, 0, b + 1) ||
+        overlaps(lens_out, bytes, idx, 1, 0, num_idx) ||
+        overlaps(lens_out, bytes, s->page_table, b, s->table_stride, s->max_pages) ||
+        overlaps(lens_out, bytes, dst_table, b, dst_stride, dst_max_pages))
+      return invalid("lens_out may not overlap lens, span_begin, span_len, cu_keep, idx or a page table");
     if ((st = check_cache_ws(ws, ws_bytes, kStatusBytes)) != LAST_OK) return st;
     CompactArgs a{};
     a.p = pages_of(c, ws);

@@ -286,3 +286,30 @@ def test_limits_of_tokens_and_tiles(lib):
     s = _seqs(batch=1 << 20, max_pages=1 << 12, table_stride=1 << 12)
     assert lib.last_cache_attention(ctypes.byref(_cache()), 0, ctypes.byref(s), 4, 0.0, 256, 256, 256, 256, None, 256, 1 << 40,
                                     0) == last.LAST_ERR_UNSUPPORTED
+
+
+def test_compact_refuses_lengths_over_what_it_reads(lib):
+    """lens_out on any array that other blocks still read, whole or in part.  No call has a workspace, so that one
+    whose arrays lie apart is refused too, but with another message."""
+    c, big, bad = ctypes.byref(_cache()), 1 << 30, last.LAST_ERR_INVALID_ARG
+    table, dst, lens, begin, span, keep, idx = (4096 * i for i in range(1, 8))
+    rows, pages, stride, n = 3, 4, 6, 5
+
+    def call(out, stride=stride, rows=rows):
+        s = _seqs(batch=rows, max_pages=pages, table_stride=stride, page_table=table, lens=lens)
+        st = lib.last_cache_compact(c, ctypes.byref(s), dst, pages, stride, begin, span, keep, idx, n, out, None, big, 0)
+        assert st == bad
+        return "lens_out may not overlap" in lib.last_error_message().decode()
+
+    row, out_bytes = 4 * stride, 4 * rows
+    sizes = {lens: 4 * rows, begin: 4 * rows, span: 4 * rows, keep: 4 * (rows + 1), idx: 4 * n}
+    for at, size in sizes.items():
+        for out in range(at - out_bytes - 8, at + size + 12, 4):
+            assert call(out) == (at - out_bytes < out < at + size), (at, out)
+    for at in (table, dst):
+        for out in range(at - out_bytes - 8, at + rows * row + 12, 4):
+            held = {at + i * row + 4 * j for i in range(rows) for j in range(pages)}
+            assert call(out) == any(out + 4 * i in held for i in range(rows)), (at, out)
+        # two sequences' lengths fit between the rows of a table
+        assert not call(at + 4 * pages, stride=6, rows=2) and call(at + 4 * pages, stride=5, rows=2)
+    assert not call(1 << 20)
