@@ -271,7 +271,8 @@ typedef struct {
 } last_rotary;
 
 /* Heads of a token tensor [num_tokens][heads][head_dim]: strides in elements, head_dim
- * contiguous.  out may be in, with the same strides. */
+ * contiguous.  out may be in, with the same strides; else it may overlap nothing that the call
+ * reads or writes.  Heads of `in` may overlap (one token for all, say), heads of `out` may not. */
 typedef struct {
   const void *in;
   void *out;

@@ -94,13 +94,29 @@ last_status make_rotary(const last_rotary *r, int head_dim, RotaryTable *t) {
   return LAST_OK;
 }
 
+// Whether the pieces of `width` at i s0 + j s1, i < n0, j < n1, lie apart (all in the same unit).
+bool apart(long long n0, long long s0, long long n1, long long s1, long long width) {
+  using Wide = __int128;
+  const Wide a = s0 < 0 ? -(Wide)s0 : s0, b = s1 < 0 ? -(Wide)s1 : s1;
+  if (n0 < 2 || n1 < 2) return (n0 < 2 || a >= width) && (n1 < 2 || b >= width);
+  if (a < width || b < width) return false;
+  if (a >= (n1 - 1) * b + width || b >= (n0 - 1) * a + width) return true;   // one inside the other
+  for (Wide j = 1; j < n1 && j * b < (n0 - 1) * a + width; ++j) {   // the multiples of a on either side of j b
+    const Wide i = j * b / a < n0 - 1 ? j * b / a : n0 - 1;
+    if (j * b - i * a < width || (i + 1 < n0 && (i + 1) * a - j * b < width)) return false;
+  }
+  return true;
+}
+
 // `name`: of the argument, for the message.  need_out: q and k of last_rope.
-last_status make_rows(const last_heads *h, int elem, int tokens, bool need_out, const char *name, HeadRows *o) {
+last_status make_rows(const last_heads *h, int elem, int tokens, int dim, bool need_out, const char *name, HeadRows *o) {
   const std::string n(name);
   if (h->heads < 1 || h->heads > 8192) return invalid(n + ": heads must be 1 .. 8192");
   if (tokens > 0 && (h->in == nullptr || (need_out && h->out == nullptr)))
     return invalid(n + ": in" + (need_out ? " and out are" : " is") + " required");
   if (!aligned(h->in, elem) || (need_out && !aligned(h->out, elem))) return invalid(n + ": misaligned");
+  if (need_out && !apart(tokens, h->out_token, h->heads, h->out_head, dim))
+    return invalid(n + ": heads of out overlap each other");
   o->in = static_cast<const char *>(h->in);
   o->in_token = h->in_token * elem;
   o->in_head = h->in_head * elem;
@@ -235,10 +251,10 @@ last_status rope(const last_rotary *r, int32_t dtype, int32_t num_tokens, int32_
   if (head_dim > 256) return fail(LAST_ERR_UNSUPPORTED, "head_dim must be at most 256");
   RotaryArgs a{};
   if ((st = make_rotary(r, head_dim, &a.rot)) != LAST_OK) return st;
-  if ((st = check_positions(positions, axis_stride, r->num_axes, num_tokens)) != LAST_OK) return st;
   const int e = elem_bytes(dtype);
-  if ((st = make_rows(q, e, num_tokens, true, "q", &a.q)) != LAST_OK) return st;
-  if (k != nullptr && (st = make_rows(k, e, num_tokens, true, "k", &a.k)) != LAST_OK) return st;
+  if ((st = make_rows(q, e, num_tokens, head_dim, true, "q", &a.q)) != LAST_OK) return st;
+  if (k != nullptr && (st = make_rows(k, e, num_tokens, head_dim, true, "k", &a.k)) != LAST_OK) return st;
+  if ((st = check_positions(positions, axis_stride, r->num_axes, num_tokens)) != LAST_OK) return st;
   a.positions = positions;
   a.axis_stride = axis_stride;
   a.tokens = num_tokens;
@@ -300,9 +316,9 @@ last_status last_cache_append(const last_cache *c, int32_t layer, const last_seq
       if ((st = make_rotary(r, c->head_dim, &a.rot)) != LAST_OK) return st;
       if ((st = check_positions(positions, axis_stride, r->num_axes, num_tokens)) != LAST_OK) return st;
     }
-    if (q != nullptr && (st = make_rows(q, e, num_tokens, true, "q", &a.q)) != LAST_OK) return st;
-    if ((st = make_rows(k, e, num_tokens, false, "k", &a.k)) != LAST_OK) return st;
-    if ((st = make_rows(v, e, num_tokens, false, "v", &a.v)) != LAST_OK) return st;
+    if (q != nullptr && (st = make_rows(q, e, num_tokens, c->head_dim, true, "q", &a.q)) != LAST_OK) return st;
+    if ((st = make_rows(k, e, num_tokens, c->head_dim, false, "k", &a.k)) != LAST_OK) return st;
+    if ((st = make_rows(v, e, num_tokens, c->head_dim, false, "v", &a.v)) != LAST_OK) return st;
     if (k->heads != c->num_kv_heads || v->heads != c->num_kv_heads)
       return invalid("k and v must have the cache's num_kv_heads heads");
     if ((st = check_cache_ws(ws, ws_bytes, kStatusBytes)) != LAST_OK) return st;

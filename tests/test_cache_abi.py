@@ -313,3 +313,45 @@ def test_compact_refuses_lengths_over_what_it_reads(lib):
         # two sequences' lengths fit between the rows of a table
         assert not call(at + 4 * pages, stride=6, rows=2) and call(at + 4 * pages, stride=5, rows=2)
     assert not call(1 << 20)
+
+
+def _overlap(tokens, token, heads, head, dim):
+    at = [t * token + h * head for t in range(tokens) for h in range(heads)]
+    at.sort()
+    return any(b - a < dim for a, b in zip(at, at[1:]))
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_rotation_refuses_outputs_that_overlap(lib, back):
+    """Against every element's place, tokens and heads any way round.  No call has positions or, for append, a workspace, so
+    that one whose heads lie apart is refused too, but with another message."""
+    rng = np.random.default_rng(4)
+    shapes = [(3, 0, 2, 64, 64), (3, 128, 2, 0, 64), (3, 127, 2, 64, 64), (3, 128, 2, 63, 64), (1, 0, 2, 64, 64), (3, 64, 1, 0, 64),
+              (2, 3 * 64, 2, 2 * 64, 64), (3, 3 * 64, 2, 2 * 64, 64), (4, 64, 2, 256, 64), (4, 64, 2, 192, 64), (3, -128, 2, 64, 64),
+              (3, 128, 2, -64, 64), (1 << 20, 0, 8192, 0, 8), (1 << 20, 8192 * 8, 8192, 8, 8), (1 << 20, 8192 * 8 - 1, 8192, 8, 8)]
+    for _ in range(3000):
+        d = 8 * int(rng.integers(1, 4))
+        shapes.append((int(rng.integers(1, 7)), int(rng.integers(0, 12)) * d + int(rng.integers(-2, 3)), int(rng.integers(1, 7)),
+                       int(rng.integers(0, 12)) * d + int(rng.integers(-2, 3)), d))
+    r, good = _rotary(rot_dim=8), _heads()
+    seen = set()
+    for tokens, token, heads, head, d in shapes:
+        if tokens < 100:
+            want = _overlap(tokens, token, heads, head, d)
+        else:
+            want = token != 8192 * 8
+        seen.add(want)
+        h = _heads(heads=heads, in_token=0, in_head=0, out_token=token, out_head=head)     # the input may be one head
+        fine = _heads(in_=16, out=16, heads=heads, out_token=heads * d, out_head=d)
+        messages = []
+        for q, k in ((h, None), (fine, h)):
+            st, msg = _status(_rope(lib, r=r, h=q, k=k, tokens=tokens, dim=d, pos=None, back=back))
+            assert st == last.LAST_ERR_INVALID_ARG
+            messages.append("overlap" in msg)
+        assert messages == [want, want], (tokens, token, heads, head, d)
+    assert seen == {False, True}
+    x = _heads(out_token=0)
+    assert _append(lib, r=r, pos=16, q=x, ws=None) == last.LAST_ERR_INVALID_ARG
+    assert "overlap" in lib.last_error_message().decode()
+    assert _append(lib, r=r, pos=16, q=good, k=_heads(out_token=0), ws=None) == last.LAST_ERR_INVALID_ARG     # k's out is not used
+    assert "overlap" not in lib.last_error_message().decode()
