@@ -299,7 +299,9 @@ last_status last_rope_backward(const last_rotary *r, int32_t dtype, int32_t num_
  * page * page_stride + head * head_stride + token * token_stride + c (strides in elements,
  * each a multiple of 16 bytes; k and v 16-byte aligned).  page_size a multiple of 8, at most
  * 2^20; head_dim * elem_bytes a multiple of 16, head_dim <= 256; at most 4096 layers and
- * kv-heads, and a page of one layer and a token's K of all layers below 2^31 bytes each. */
+ * kv-heads, and a page of one layer and a token's K of all layers below 2^31 bytes each.  In a
+ * cache that a call writes no two elements may share an address, whether of K or V; only layers
+ * may be one (layer_stride 0). */
 typedef struct {
   void *k, *v;
   int32_t num_layers, num_pages, page_size, num_kv_heads, head_dim;

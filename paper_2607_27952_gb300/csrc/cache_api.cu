@@ -97,6 +97,7 @@ last_status make_rotary(const last_rotary *r, int head_dim, RotaryTable *t) {
 // Whether the pieces of `width` at i s0 + j s1, i < n0, j < n1, lie apart (all in the same unit).
 bool apart(long long n0, long long s0, long long n1, long long s1, long long width) {
   using Wide = __int128;
+  if (n0 < n1) return apart(n1, s1, n0, s0, width);
   const Wide a = s0 < 0 ? -(Wide)s0 : s0, b = s1 < 0 ? -(Wide)s1 : s1;
   if (n0 < 2 || n1 < 2) return (n0 < 2 || a >= width) && (n1 < 2 || b >= width);
   if (a < width || b < width) return false;
@@ -167,6 +168,18 @@ last_status check_cache(const last_cache *c) {
   if (c->token_stride < c->head_dim || (c->num_kv_heads > 1 && c->head_stride < c->head_dim) ||
       (c->num_pages > 1 && c->page_stride < c->head_dim))
     return invalid("cache strides must not be below head_dim");
+  return LAST_OK;
+}
+
+// Of a cache that a call writes, no two of whose pages, heads and tokens (and layers, where it writes all) may share
+// an element.  Layers that are one and the same get the same bytes.
+last_status check_written(const last_cache *c, bool all_layers) {
+  const long long n[4] = {c->num_pages, c->num_kv_heads, c->page_size, all_layers && c->layer_stride > 0 ? c->num_layers : 1};
+  const long long s[4] = {c->page_stride, c->head_stride, c->token_stride, c->layer_stride};
+  for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < i; ++j)
+      if (!apart(n[i], s[i], n[j], s[j], c->head_dim))
+        return invalid("a cache that is written may not overlap itself: its strides are too small");
   return LAST_OK;
 }
 
@@ -304,6 +317,7 @@ last_status last_cache_append(const last_cache *c, int32_t layer, const last_seq
   return guarded([&]() -> last_status {
     last_status st = check_cache(c);
     if (st != LAST_OK || (st = check_layer(c, layer)) != LAST_OK || (st = check_sequences(s)) != LAST_OK) return st;
+    if ((st = check_written(c, false)) != LAST_OK) return st;
     if ((st = check_tokens(num_tokens)) != LAST_OK) return st;
     if (cu_new == nullptr && num_tokens != s->batch)
       return invalid("without cu_new there is one token per sequence: num_tokens must be batch");
@@ -380,6 +394,7 @@ last_status last_cache_copy(const last_cache *c, int32_t num_copies, const int32
   return guarded([&]() -> last_status {
     last_status st = check_cache(c);
     if (st != LAST_OK) return st;
+    if ((st = check_written(c, true)) != LAST_OK) return st;
     if (num_copies < 0) return invalid("num_copies < 0");
     if (num_copies > 0 && (src == nullptr || dst == nullptr)) return invalid("src and dst are required");
     if ((st = check_cache_ws(ws, ws_bytes, kStatusBytes)) != LAST_OK) return st;
@@ -394,7 +409,7 @@ last_status last_cache_compact(const last_cache *c, const last_sequences *s, con
                                int32_t num_idx, int32_t *lens_out, void *ws, size_t ws_bytes, void *stream) {
   return guarded([&]() -> last_status {
     last_status st = check_cache(c);
-    if (st != LAST_OK || (st = check_sequences(s)) != LAST_OK) return st;
+    if (st != LAST_OK || (st = check_sequences(s)) != LAST_OK || (st = check_written(c, true)) != LAST_OK) return st;
     if (s->batch > 0 && (dst_table == nullptr || cu_keep == nullptr || lens_out == nullptr))
       return invalid("dst_table, cu_keep and lens_out are required");
     if ((span_begin == nullptr) != (span_len == nullptr)) return invalid("span_begin and span_len go together");

@@ -355,3 +355,33 @@ def test_rotation_refuses_outputs_that_overlap(lib, back):
     assert "overlap" in lib.last_error_message().decode()
     assert _append(lib, r=r, pos=16, q=good, k=_heads(out_token=0), ws=None) == last.LAST_ERR_INVALID_ARG     # k's out is not used
     assert "overlap" not in lib.last_error_message().decode()
+
+
+@pytest.mark.parametrize("kw,reads,writes", [
+    (dict(), True, True),
+    (dict(head_stride=64, token_stride=128), True, True),                          # tokens outside heads
+    (dict(page_stride=64, head_stride=640, token_stride=1280), True, True),        # pages innermost
+    (dict(head_stride=64), True, False),                                           # heads on the tokens
+    (dict(token_stride=1024), True, False),                                        # tokens on the heads
+    (dict(page_stride=1024), True, False),                                         # pages on the heads
+    (dict(page_stride=64, num_kv_heads=1), True, False),                           # pages on the tokens
+    (dict(head_stride=960, num_pages=1), True, False),                             # heads by one token
+    (dict(num_pages=1, page_stride=0), True, True),
+    (dict(layer_stride=0), True, True),                                            # all layers are one
+    (dict(layer_stride=2048), True, None),                                         # layers on pages: append writes one alone
+])
+def test_caches_that_overlap_themselves_are_not_written(lib, kw, reads, writes):
+    """They may be read.  No call has a workspace: each is refused, the sound ones for that."""
+    c, s, h = ctypes.byref(_cache(**kw)), ctypes.byref(_seqs()), ctypes.byref(_heads())
+
+    def overlap(st):
+        assert st == last.LAST_ERR_INVALID_ARG
+        message = lib.last_error_message().decode()
+        assert "overlap itself" in message or "workspace is NULL" in message
+        return "overlap itself" in message
+
+    big = 1 << 30
+    assert overlap(lib.last_cache_attention(c, 0, s, 4, 0.0, 256, 256, 256, 256, None, None, big, 0)) is not reads
+    assert overlap(lib.last_cache_append(c, 0, s, 3, None, None, None, 0, None, h, h, None, big, 0)) is (writes is False)
+    assert overlap(lib.last_cache_copy(c, 1, 256, 256, None, big, 0)) is not bool(writes)
+    assert overlap(lib.last_cache_compact(c, s, 4096, 4, 4, None, None, 8192, 12288, 5, 16384, None, big, 0)) is not bool(writes)
