@@ -40,7 +40,9 @@ last_status guarded(F f) {
 }
 
 last_status launched(cudaError_t e, const char *what) {
-  return e == cudaSuccess ? LAST_OK : fail(LAST_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
+  if (e == cudaSuccess) return LAST_OK;
+  cudaGetLastError();   // reported here, and not by whoever asks the runtime next
+  return fail(LAST_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
 }
 
 bool multiple16(long long bytes) { return (bytes & 15) == 0; }

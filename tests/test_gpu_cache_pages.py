@@ -553,3 +553,45 @@ def test_both_ways_of_the_binding(monkeypatch):
     want = everything()
     monkeypatch.setattr(last, "_fast", None)
     assert all(_same(a, b) for a, b in zip(everything(), want))
+
+
+def test_a_failed_launch_leaves_no_error_behind():
+    """The calls' launches refused by the runtime (the stream's capture is broken): each says so once, and later
+    calls of the path start clean."""
+    import ctypes
+    import torch
+    import cache_util as cu
+    rt = ctypes.CDLL("libcudart.so.13")
+    rt.cudaStreamBeginCapture.argtypes = [ctypes.c_void_p, ctypes.c_int]
+    rt.cudaStreamEndCapture.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
+    rt.cudaStreamSynchronize.argtypes = [ctypes.c_void_p]
+    k, v = cu.pages(1, 8, 2, 16, 64, "bfloat16", "head", 1)
+    cache, seqs = last.Cache(k, v), last.Sequences(cu.ints([[0, 1]]), cu.ints([20]))
+    ws, ints, out = cu.workspace(cache, 1, 2), cu.ints([2]), cu.ints([0])
+    x, rope, pos, y = cu.randn((1, 2, 64), "bfloat16", 2), last.Rope.sections([32]), cu.ints([3]), cu.randn((1, 2, 64), "bfloat16", 3)
+    keep, idx, dst = cu.ints([0, 1]), cu.ints([0]), cu.ints([[4]])
+    calls = (lambda s: last.last_cache_copy(cache, ints, ints, ws, stream=s), lambda s: last.last_rope(rope, pos, x, y, stream=s),
+             lambda s: last.last_cache_append(cache, 0, seqs, x, x, ws, stream=s),
+             lambda s: last.last_cache_attention(cache, 0, seqs, x, y, ws, stream=s),
+             lambda s: last.last_cache_compact(cache, seqs, dst, keep, idx, out, ws, stream=s))
+    for call in calls:
+        call(None)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for call in calls:
+        assert rt.cudaStreamBeginCapture(s.cuda_stream, 2) == 0
+        graph = ctypes.c_void_p()
+        try:
+            assert rt.cudaStreamSynchronize(s.cuda_stream) != 0      # not allowed: breaks the capture
+            rt.cudaGetLastError()
+            with pytest.raises(last.LastError) as e:
+                call(s)
+            left = rt.cudaGetLastError()
+        finally:
+            rt.cudaStreamEndCapture(s.cuda_stream, ctypes.byref(graph))
+            rt.cudaGetLastError()
+        assert e.value.status == last.LAST_ERR_CUDA and left == 0
+    for call in calls:
+        call(s)
+    s.synchronize()
+    last.last_poll(ws, s)
