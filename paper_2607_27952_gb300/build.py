@@ -18,7 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liblast.so")
-MARSHAL = os.path.join(PKG, "_marshal.so")
+MARSHAL = os.path.join(PKG, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))   # no other Python's import finds it
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
@@ -78,8 +78,11 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
 
 
 def build_marshal(run, force: bool = False):
-    """_marshal.so, without which the binding goes through ctypes."""
+    """The marshalling module of this Python, without which the binding goes through ctypes."""
     src, python = os.path.join(CSRC, "marshal.c"), sysconfig.get_paths()["include"]
+    untagged = os.path.join(os.path.dirname(MARSHAL), "_marshal.so")   # as it was named before: any Python would load it
+    if os.path.exists(untagged):
+        os.remove(untagged)
     if not os.path.exists(os.path.join(python, "Python.h")):
         return
     if force or _stale(MARSHAL, [src, os.path.join(INCLUDE, "last.h")]):

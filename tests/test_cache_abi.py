@@ -385,3 +385,34 @@ def test_caches_that_overlap_themselves_are_not_written(lib, kw, reads, writes):
     assert overlap(lib.last_cache_append(c, 0, s, 3, None, None, None, 0, None, h, h, None, big, 0)) is (writes is False)
     assert overlap(lib.last_cache_copy(c, 1, 256, 256, None, big, 0)) is not bool(writes)
     assert overlap(lib.last_cache_compact(c, s, 4096, 4, 4, None, None, 8192, 12288, 5, 16384, None, big, 0)) is not bool(writes)
+
+
+# ---- the marshalling module ----
+
+def _build_marshal(monkeypatch, tmp_path):
+    """build_marshal() into tmp_path: the files there, and the commands it ran."""
+    import os
+    import subprocess
+    import sysconfig
+    from paper_2607_27952_gb300 import build
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        pytest.skip("Python's headers are not installed")
+    commands = []
+
+    def compile_it(cmd):
+        commands.append(cmd)
+        subprocess.run(cmd, check=True, capture_output=True)
+    monkeypatch.setattr(build, "MARSHAL", str(tmp_path / os.path.basename(build.MARSHAL)))
+    build.build_marshal(compile_it)
+    return sorted(f.name for f in tmp_path.iterdir()), commands
+
+
+def test_marshalling_module_is_one_pythons(lib, monkeypatch, tmp_path):
+    """Its name carries the interpreter's tag, so that no other imports it, and one without a tag is removed."""
+    import sysconfig
+    (tmp_path / "_marshal.so").write_bytes(b"")
+    suffix = sysconfig.get_config_var("EXT_SUFFIX")
+    assert suffix != ".so"
+    files, commands = _build_marshal(monkeypatch, tmp_path)
+    assert files == ["_marshal" + suffix] and len(commands) == 1
+    assert last._fast is None or last._fast.__file__.endswith(suffix)
