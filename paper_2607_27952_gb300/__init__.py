@@ -115,7 +115,7 @@ def _load_fast(lib):
                  "last_cache_compact")
         _marshal.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names), torch.float32, torch.bfloat16,
                       torch.int32, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
-    except (ImportError, AttributeError):   # not built, or a torch without these
+    except (ImportError, AttributeError, TypeError):   # not built, a torch without these, or built from older sources
         return None
     return _marshal
 

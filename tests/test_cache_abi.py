@@ -416,3 +416,14 @@ def test_marshalling_module_is_one_pythons(lib, monkeypatch, tmp_path):
     files, commands = _build_marshal(monkeypatch, tmp_path)
     assert files == ["_marshal" + suffix] and len(commands) == 1
     assert last._fast is None or last._fast.__file__.endswith(suffix)
+
+
+@pytest.mark.parametrize("error", [ImportError, AttributeError, TypeError])
+def test_a_marshalling_module_that_does_not_fit_is_left_alone(lib, monkeypatch, error):
+    """One of other sources may want other arguments: the calls then go through ctypes."""
+    class Other:
+        @staticmethod
+        def bind(*args):
+            raise error("bind")
+    monkeypatch.setattr(last, "_marshal", Other, raising=False)
+    assert last._load_fast(lib) is None
