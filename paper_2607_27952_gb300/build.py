@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import concurrent.futures as cf
 import os
+import shlex
 import shutil
 import subprocess
 import sysconfig
@@ -87,7 +88,7 @@ def build_marshal(run, force: bool = False):
         return
     if force or _stale(MARSHAL, [src, os.path.join(INCLUDE, "last.h")]):
         tmp = MARSHAL + f".tmp{os.getpid()}"
-        run([os.environ.get("CC", "gcc"), "-O2", "-std=c11", "-Wall", "-Wextra", "-Wno-missing-field-initializers", "-shared",
+        run([*(shlex.split(os.environ.get("CC", "")) or ["gcc"]), "-O2", "-std=c11", "-Wall", "-Wextra", "-Wno-missing-field-initializers", "-shared",
              "-fPIC", "-I", python, "-I", INCLUDE, src, "-o", tmp])
         os.replace(tmp, MARSHAL)
 

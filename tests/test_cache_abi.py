@@ -427,3 +427,11 @@ def test_a_marshalling_module_that_does_not_fit_is_left_alone(lib, monkeypatch, 
             raise error("bind")
     monkeypatch.setattr(last, "_marshal", Other, raising=False)
     assert last._load_fast(lib) is None
+
+
+@pytest.mark.parametrize("cc", ["gcc -pipe", "", " "])
+def test_marshalling_module_with_a_compiler_of_several_words(lib, monkeypatch, tmp_path, cc):
+    """CC as make takes it; an empty one is none."""
+    monkeypatch.setenv("CC", cc)
+    files, commands = _build_marshal(monkeypatch, tmp_path)
+    assert len(files) == 1 and commands[0][0] == "gcc"
