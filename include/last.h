@@ -253,7 +253,8 @@ last_status last_check_bounded_wait(void *ws, void *stream);
  * dtype (last_dtype) is that of q, K, V and the outputs; sums and rotations are
  * formed in fp32 and rounded once.  What cannot be checked on the host (a page, an
  * index or a length out of range) is checked on the device: it is skipped, and
- * last_poll on the call's workspace returns LAST_ERR_DEVICE_INDEX. */
+ * last_poll on the call's workspace returns LAST_ERR_DEVICE_INDEX.  What a call writes
+ * may overlap nothing else that it reads or writes unless its comment says so. */
 
 /* Rotary positions on several axes (time, height, width; one axis for text): token t's
  * pair i < rot_dim / 2 turns by positions[axis[i]][t] * inv_freq[i].  Elements past

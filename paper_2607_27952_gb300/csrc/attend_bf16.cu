@@ -44,7 +44,9 @@ template <int CHUNKS, int EIGHTS>   // 128-byte columns of a row; groups of 8 he
 struct Bf16Part {
   static constexpr int kTile = 64, kWarpKeys = 16, kHeadRows = 8 * EIGHTS, kCtas = CHUNKS * EIGHTS == 1 ? 3 : 2;
   static constexpr int kSteps = CHUNKS * 4;                           // 16-wide along a row
-  static constexpr int kAhead = CHUNKS * EIGHTS > 4 ? 2 : 4;          // fragments in flight, as registers allow
+  // Fragments in flight: four, or two where the sums take most of a thread's 168 registers.  <4, 2> (rows wider than
+  // 192, 9 to 16 heads) spills all the same, 1.8 KB: 4 x 20000 keys by 256 take 75 us with 16 heads, 30 with 8.
+  static constexpr int kAhead = CHUNKS * EIGHTS > 4 ? 2 : 4;
   static constexpr bool kKeepQ = CHUNKS * EIGHTS < 6;                 // else its fragments are read for every tile
   uint32_t q[kKeepQ ? kSteps : 1][2 * EIGHTS];
   int heads;

@@ -6,8 +6,11 @@ namespace last {
 namespace {
 
 // ---- consumers: fp32, on the CUDA cores ----
-// Bound by HBM with one or two heads a kv-head (16 kv-heads of 74010 keys by 80, 758 MB: 154 us, 4.9 TB/s); with many
-// by the reads of q and of the weights from shared memory (4 x 17970 keys by 64, 12 heads on 2: 24 us).
+// Bound by HBM with one head a kv-head and rows of whole 128-byte columns (16 kv-heads of 74010 keys by 128, 1.21 GB:
+// 180 us, 6.7 TB/s); rows of 320 bytes are fetched as 384 (the same by 80, 758 MB: 155 us, 4.9 TB/s).  With many heads
+// bound by this layout's reads of q and of the weights from shared memory (4 x 17970 keys by 64, 12 heads on 2: 35 us
+// against 11 of HBM).  16 heads spill 64 bytes up to 128 elements (4 x 20000 keys by 128: 48 us) and 660 past
+// them (by 256: 184 us; 8 heads 48).
 // Logits: 4 lanes a key, 8 keys a warp, the heads' q broadcast from shared memory.  O: the lanes
 // across the row's columns (with short rows several keys at once), the weights broadcast.
 template <int HEADS, int WIDE>   // heads held; 128-column blocks of a row

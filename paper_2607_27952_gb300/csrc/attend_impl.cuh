@@ -11,9 +11,9 @@
 // four take a quarter of every tile each, with sums of their own, and one adds them up where
 // the CTA's part of a (sequence, head) ends.  Two CTAs per SM keep some 160 KB of K and V under way.
 //
-// Bound by HBM: 1.42 GB of K and V (6 sequences of about 115 thousand keys) take 209 us, 6.8 TB/s; 340 MB (64 of
-// about 650 keys, 16 kv-heads) 59 us, of which 8 are the start (lengths, page table, first tile: three reads
-// that wait for each other) and the join.  A tile of 64 keys by 128 arrives every 2600 cycles and its
+// Bound by HBM: 1.42 GB of K and V (6 sequences of about 115 thousand keys) take 211 us, 6.7 TB/s; 340 MB (64 of
+// about 650 keys, 16 kv-heads) 59.5 us, of which 8 are the start (lengths, page table, first tile: three reads
+// that wait for each other) and the join: 6.6 TB/s in between.  A tile of 64 keys by 128 arrives every 2600 cycles and its
 // products take 1450; one CTA of eight such warps and one loader per SM took 87 and 294 us.
 #pragma once
 
