@@ -100,6 +100,7 @@ last_status make_rotary(const last_rotary *r, int head_dim, RotaryTable *t) {
 bool apart(long long n0, long long s0, long long n1, long long s1, long long width) {
   using Wide = __int128;
   if (n0 < n1) return apart(n1, s1, n0, s0, width);
+  if (n1 < 1) return true;
   const Wide a = s0 < 0 ? -(Wide)s0 : s0, b = s1 < 0 ? -(Wide)s1 : s1;
   if (n0 < 2 || n1 < 2) return (n0 < 2 || a >= width) && (n1 < 2 || b >= width);
   if (a < width || b < width) return false;

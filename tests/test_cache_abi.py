@@ -435,3 +435,8 @@ def test_marshalling_module_with_a_compiler_of_several_words(lib, monkeypatch, t
     monkeypatch.setenv("CC", cc)
     files, commands = _build_marshal(monkeypatch, tmp_path)
     assert len(files) == 1 and commands[0][0] == "gcc"
+
+
+def test_outputs_of_no_tokens_cannot_overlap(lib):
+    for h in (_heads(out_token=0, out_head=0), _heads(out_head=0)):
+        assert _rope(lib, tokens=0, pos=None, h=h, k=h) == last.LAST_OK
