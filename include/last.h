@@ -21,7 +21,9 @@
  * paper has no counterpart): last_rope rotates q and K by positions on several axes,
  * as last_scores wants them; last_cache_append also writes K and V into a paged
  * cache; last_cache_compact cuts a cache to the kept tokens; last_cache_attention
- * decodes over it; last_cache_copy and last_pages_* part and free its pages.
+ * decodes over it, last_cache_chunk_attention attends for whole prompts and drafts,
+ * last_cache_diff_attention for either with the difference of two softmax maps;
+ * last_cache_copy and last_pages_* part and free its pages.
  * Deployment aids without a counterpart in the paper: last_prune_host (the
  * whole path on host buffers, copies included), last_scores_noalloc (scoring
  * without a caller workspace) and last_check_bounded_wait (exercises the
@@ -354,6 +356,55 @@ last_status last_cache_attention(const last_cache *c, int32_t layer, const last_
                                  int32_t num_q_heads, float scale, const void *q, int64_t q_stride,
                                  void *out, int64_t out_stride, float *lse, void *ws,
                                  size_t ws_bytes, void *stream);
+
+/* Bytes of device workspace (256-byte aligned) for the two calls below, whatever their sequences and
+ * tokens.  Its contents need no initialisation. */
+last_status last_chunk_workspace_size(const last_cache *c, int32_t num_q_heads, size_t *bytes);
+
+/* Attention of several new tokens per sequence over its cached keys, in one layer: prompts, prompts
+ * behind a cached part, drafted tokens.  Sequence b's new tokens are rows cu_new[b] .. cu_new[b+1]-1
+ * of q and out (DEVICE int32 [batch+1]; NULL: one token per sequence, num_tokens = batch) and
+ * its last cached ones: lens[b] counts them already, as last_cache_append leaves it, and
+ * new token i of n has position p = lens[b] - n + i.  It sees the keys key_begin[b] .. lens[b]-1; causal
+ * (0 or 1): up to p; window > 0 (with causal alone): from p - window + 1 on.  Per row and q-head:
+ * out = sum softmax(scale q.k) v, lse (may be NULL) [num_tokens][num_q_heads] fp32 = log sum
+ * exp(scale q.k); out = 0 and lse = -inf where no key is seen or all logits are -inf.  A key of logit -inf has
+ * weight 0.  What a row does not see has no part in it, whatever it holds; pages that no row of a sequence sees
+ * are not read (their table entries may be anything).  Keys of a page out of range are left out; a sequence
+ * where lens[b] is below n, above 2^31 - 256 or more than its table row has room for, or key_begin[b] is negative,
+ * is taken for one without a key; one whose cu_new is out of range or falls is skipped, and rows of no sequence are
+ * left as they are.  q-head h reads kv-head h / (num_q_heads / num_kv_heads).  q and out: [num_tokens]
+ * [num_q_heads][head_dim], tokens q_stride and out_stride elements apart, both multiples of 16 bytes, 16-byte
+ * aligned.  scale <= 0 selects 1/sqrt(head_dim).  bf16: weights are rounded to bf16 before they meet v, with their sum.
+ * Results do not depend on other calls or on timing: repeated calls give the same bits.
+ * num_tokens * num_q_heads / num_kv_heads must stay below 2^31, num_tokens * num_q_heads * (max_pages * page_size + 256)
+ * below 2^60 (LAST_ERR_UNSUPPORTED). */
+last_status last_cache_chunk_attention(const last_cache *c, int32_t layer, const last_sequences *s,
+                                       int32_t num_tokens, const int32_t *cu_new, int32_t num_q_heads,
+                                       float scale, int32_t causal, int32_t window, const void *q,
+                                       int64_t q_stride, void *out, int64_t out_stride, float *lse, void *ws,
+                                       size_t ws_bytes, void *stream);
+
+/* Differential attention, single tokens (cu_new NULL) or chunks, in one layer.  Heads go in pairs: q-heads
+ * 2j and 2j+1 and K heads 2g and 2g+1 are the two maps of pair j, g = j / (num_q_heads / num_kv_heads), and its value
+ * at a key is V heads 2g and 2g+1 side by side, 2 head_dim wide.  With the softmax maps P1 and P2 over the keys
+ * that a row sees (as above),
+ *   x = sum P1 v - lambda[j] sum P2 v,   out = out_scale x,
+ * or, with a norm_weight, out = out_scale norm_weight x / sqrt(mean(x^2) + norm_eps) over the
+ * 2 head_dim elements of x (0 where that root is).  out: [num_tokens][num_q_heads / 2][2 head_dim].  num_kv_heads
+ * must be even, head_dim at most 128.  Everything else is as for last_cache_chunk_attention.  lambda and norm_weight are
+ * DEVICE fp32, the struct is read during the call only. */
+typedef struct {
+  const float *lambda;       /* [num_q_heads / 2] */
+  const float *norm_weight;  /* [2 head_dim]; NULL: no norm */
+  float norm_eps;            /* >= 0 */
+  float out_scale;
+} last_difference;
+last_status last_cache_diff_attention(const last_cache *c, int32_t layer, const last_sequences *s,
+                                      int32_t num_tokens, const int32_t *cu_new, int32_t num_q_heads,
+                                      float scale, int32_t causal, int32_t window, const last_difference *d,
+                                      const void *q, int64_t q_stride, void *out, int64_t out_stride, void *ws,
+                                      size_t ws_bytes, void *stream);
 
 /* Copies page src[i] to page dst[i], i < num_copies (DEVICE int32), in every layer, K and V.  No
  * page may be written twice, nor written and read, by one call; src[i] == dst[i] does nothing. */

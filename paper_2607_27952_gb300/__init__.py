@@ -13,7 +13,8 @@ Functions carry the names of the C entry points in include/last.h:
   last_scores_rows_workspace_size, last_scores_noalloc, last_check_bounded_wait,
   last_poll, last_budget, last_status_string, last_error_message,
   last_rope, last_rope_backward, last_cache_workspace_size, last_cache_append,
-  last_cache_attention, last_cache_copy, last_cache_compact, last_pages_init,
+  last_cache_attention, last_chunk_workspace_size, last_cache_chunk_attention,
+  last_cache_diff_attention, last_cache_copy, last_cache_compact, last_pages_init,
   last_pages_take, last_pages_share, last_pages_release.
 """
 from __future__ import annotations
@@ -49,7 +50,8 @@ EXPORTED = ("last_workspace_size", "last_scores", "last_select", "last_gather", 
             "last_host_workspace_size", "last_prune_host", "last_rope", "last_rope_backward",
             "last_cache_workspace_size", "last_cache_append", "last_cache_attention",
             "last_cache_copy", "last_cache_compact", "last_pages_init", "last_pages_take",
-            "last_pages_share", "last_pages_release")
+            "last_pages_share", "last_pages_release", "last_chunk_workspace_size",
+            "last_cache_chunk_attention", "last_cache_diff_attention")
 
 
 class LastError(RuntimeError):
@@ -96,6 +98,11 @@ class _Sequences(ctypes.Structure):
                 ("lens", ctypes.c_void_p), ("key_begin", ctypes.c_void_p)]
 
 
+class _Difference(ctypes.Structure):
+    _fields_ = [("lambda_", ctypes.c_void_p), ("norm_weight", ctypes.c_void_p), ("norm_eps", ctypes.c_float),
+                ("out_scale", ctypes.c_float)]
+
+
 class _PagePool(ctypes.Structure):
     _fields_ = [("num_pages", ctypes.c_int32), ("num_free", ctypes.c_int32),
                 ("holders", ctypes.POINTER(ctypes.c_int32)),
@@ -112,7 +119,7 @@ def _load_fast(lib):
         import torch
         from . import _marshal
         names = ("last_rope", "last_rope_backward", "last_cache_append", "last_cache_attention", "last_cache_copy",
-                 "last_cache_compact")
+                 "last_cache_compact", "last_cache_chunk_attention", "last_cache_diff_attention")
         _marshal.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names), torch.float32, torch.bfloat16,
                       torch.int32, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
     except (ImportError, AttributeError, TypeError):   # not built, a torch without these, or built from older sources
@@ -162,6 +169,10 @@ def load_library(path: str = LIB_PATH):
     lib.last_cache_workspace_size.argtypes = [PC, I, I, ctypes.POINTER(Z)]
     lib.last_cache_append.argtypes = [PC, I, PS, I, P, PR, P, L, PH, PH, PH, P, Z, P]
     lib.last_cache_attention.argtypes = [PC, I, PS, I, F, P, L, P, L, P, P, Z, P]
+    PD = ctypes.POINTER(_Difference)
+    lib.last_chunk_workspace_size.argtypes = [PC, I, ctypes.POINTER(Z)]
+    lib.last_cache_chunk_attention.argtypes = [PC, I, PS, I, P, I, F, I, I, P, L, P, L, P, P, Z, P]
+    lib.last_cache_diff_attention.argtypes = [PC, I, PS, I, P, I, F, I, I, PD, P, L, P, L, P, Z, P]
     lib.last_cache_copy.argtypes = [PC, I, P, P, P, Z, P]
     lib.last_cache_compact.argtypes = [PC, PS, P, I, L, P, P, P, P, I, P, P, Z, P]
     lib.last_pages_init.argtypes = [PG]
@@ -170,6 +181,7 @@ def load_library(path: str = LIB_PATH):
     for name in ("last_rope", "last_rope_backward", "last_cache_workspace_size", "last_cache_append",
                  "last_cache_attention", "last_cache_copy", "last_cache_compact",
                  "last_pages_init", "last_pages_take", "last_pages_share", "last_pages_release",
+                 "last_chunk_workspace_size", "last_cache_chunk_attention", "last_cache_diff_attention",
                  "last_host_workspace_size", "last_prune_host"):
         getattr(lib, name).restype = ctypes.c_int
     for name in ("last_workspace_size", "last_scores", "last_select", "last_gather",
@@ -638,6 +650,81 @@ def last_cache_attention(cache: Cache, layer: int, seqs: Sequences, q, out, ws, 
     _check(load_library().last_cache_attention(
         cache.ref, layer, seqs.ref, heads, softmax_scale, q.data_ptr(), qs[0], out.data_ptr(), os_[0],
         None if lse is None else lse.data_ptr(), p, n, _stream(stream)))
+
+
+def last_chunk_workspace_size(cache: Cache, num_q_heads: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().last_chunk_workspace_size(cache.ref, num_q_heads, ctypes.byref(n)))
+    return n.value
+
+
+def chunk_workspace(cache: Cache, num_q_heads: int):
+    """A torch uint8 tensor of last_chunk_workspace_size bytes beside the cache."""
+    import torch
+    return torch.empty(last_chunk_workspace_size(cache, num_q_heads), dtype=torch.uint8, device=cache.k.device)
+
+
+def _rows(x, shape, dtype, name):
+    """Token stride of a device tensor [tokens][heads][width] whose tokens are contiguous."""
+    s = x.stride()
+    if x.shape != shape or x.dtype is not dtype or not x.is_cuda or s[2] != 1 or (shape[1] > 1 and s[1] != shape[2]):
+        raise ValueError(f"{name}: a device tensor {tuple(shape)} of {dtype}, each token contiguous, expected")
+    return s[0]
+
+
+def _floats(x, shape, name):
+    if _F32 is None:
+        _dtypes()
+    if x is None:
+        return None
+    if x.dtype is not _F32 or x.shape != shape or not x.is_contiguous() or not x.is_cuda:
+        raise ValueError(f"{name}: a contiguous device float32 tensor {tuple(shape)} expected")
+    return x.data_ptr()
+
+
+def last_cache_chunk_attention(cache: Cache, layer: int, seqs: Sequences, q, out, ws, cu_new=None, lse=None,
+                               causal: bool = True, window: int = 0, softmax_scale: float = 0.0, stream=None):
+    """out = attention of the new tokens' q [tokens][q_heads][head_dim] over the sequences' cached keys of one layer (seqs.lens
+    counts the new ones already); sequence b's are rows cu_new[b] .. cu_new[b+1]-1, without cu_new there is one per sequence.
+    causal: up to the token's own position; window: only the last so many; lse [tokens][q_heads] fp32 receives
+    the log of the softmax's denominator."""
+    if _fast is not None and _done(_fast.chunk(cache.addr, layer, seqs.addr, seqs.batch, cache.head_dim, cache.dtype, q, out, ws,
+                                               cu_new, lse, causal, window, softmax_scale, stream)):
+        return
+    d = cache.head_dim
+    if q.dim() != 3 or q.shape[2] != d:
+        raise ValueError(f"q: [tokens][q_heads][{d}] expected")
+    t, heads = q.shape[0], q.shape[1]
+    qs, os_ = _rows(q, q.shape, cache.dtype, "q"), _rows(out, q.shape, cache.dtype, "out")
+    p, n = _ws(ws)
+    _check(load_library().last_cache_chunk_attention(
+        cache.ref, layer, seqs.ref, t, None if cu_new is None else _int32(cu_new, "cu_new", (seqs.batch + 1,)).data_ptr(), heads,
+        softmax_scale, int(causal), window, q.data_ptr(), qs, out.data_ptr(), os_, _floats(lse, (t, heads), "lse"), p, n,
+        _stream(stream)))
+
+
+def last_cache_diff_attention(cache: Cache, layer: int, seqs: Sequences, q, out, ws, lam, cu_new=None, norm_weight=None,
+                              norm_eps: float = 1e-5, out_scale: float = 1.0, causal: bool = True, window: int = 0,
+                              softmax_scale: float = 0.0, stream=None):
+    """Differential attention of the new tokens' q [tokens][q_heads][head_dim], heads in pairs, over a cache whose K and V heads
+    are paired too: out [tokens][q_heads / 2][2 head_dim] = softmax map 1 - lam[pair] x map 2, with norm_weight
+    [2 head_dim] RMS-normalised, times out_scale.  lam [q_heads / 2] and norm_weight: fp32.  The rest is as for
+    last_cache_chunk_attention."""
+    if _fast is not None and _done(_fast.difference(cache.addr, layer, seqs.addr, seqs.batch, cache.head_dim, cache.dtype, q, out, ws,
+                                                    cu_new, lam, norm_weight, norm_eps, out_scale, causal, window, softmax_scale, stream)):
+        return
+    d = cache.head_dim
+    if q.dim() != 3 or q.shape[2] != d or q.shape[1] % 2 != 0:
+        raise ValueError(f"q: [tokens][q_heads][{d}], an even number of heads, expected")
+    t, heads = q.shape[0], q.shape[1]
+    qs, os_ = _rows(q, q.shape, cache.dtype, "q"), _rows(out, (t, heads // 2, 2 * d), cache.dtype, "out")
+    if lam is None:
+        raise ValueError("lam is required")
+    diff = _Difference(_floats(lam, (heads // 2,), "lam"), _floats(norm_weight, (2 * d,), "norm_weight"), norm_eps, out_scale)
+    p, n = _ws(ws)
+    _check(load_library().last_cache_diff_attention(
+        cache.ref, layer, seqs.ref, t, None if cu_new is None else _int32(cu_new, "cu_new", (seqs.batch + 1,)).data_ptr(), heads,
+        softmax_scale, int(causal), window, ctypes.byref(diff), q.data_ptr(), qs, out.data_ptr(), os_, p, n, _stream(stream)))
 
 
 def last_cache_copy(cache: Cache, src, dst, ws, stream=None):

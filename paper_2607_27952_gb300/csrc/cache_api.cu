@@ -281,6 +281,72 @@ last_status rope(const last_rotary *r, int32_t dtype, int32_t num_tokens, int32_
   return launched(launch_rotary(a, static_cast<cudaStream_t>(stream)), "rotary launch");
 }
 
+last_status check_heads(const last_cache *c, int32_t num_q_heads) {
+  if (num_q_heads < 1 || num_q_heads % c->num_kv_heads != 0)
+    return invalid("num_q_heads must be a positive multiple of num_kv_heads");
+  return num_q_heads <= 8192 ? LAST_OK : fail(LAST_ERR_UNSUPPORTED, "num_q_heads must be at most 8192");
+}
+
+// Attention of several new tokens per sequence; d: the difference of two maps.
+last_status chunk(const last_cache *c, int32_t layer, const last_sequences *s, int32_t num_tokens, const int32_t *cu_new,
+                  int32_t num_q_heads, float scale, int32_t causal, int32_t window, const last_difference *d, bool diff,
+                  const void *q, int64_t q_stride, void *out, int64_t out_stride, float *lse, void *ws, size_t ws_bytes,
+                  void *stream) {
+  last_status st = check_cache(c);
+  if (st != LAST_OK || (st = check_layer(c, layer)) != LAST_OK || (st = check_sequences(s)) != LAST_OK) return st;
+  if ((st = check_tokens(num_tokens)) != LAST_OK || (st = check_heads(c, num_q_heads)) != LAST_OK) return st;
+  if (cu_new == nullptr && num_tokens != s->batch)
+    return invalid("without cu_new there is one token per sequence: num_tokens must be batch");
+  if (num_tokens > 0 && s->batch == 0) return invalid("tokens without a sequence");
+  if (causal != 0 && causal != 1) return invalid("causal must be 0 or 1");
+  if (window < 0 || (window > 0 && causal == 0)) return invalid("window must not be negative, and 0 where causal is");
+  if (diff) {
+    if (d == nullptr || d->lambda == nullptr) return invalid("the difference and its lambda are required");
+    if (!aligned(d->lambda, 4) || !aligned(d->norm_weight, 4)) return invalid("lambda or norm_weight is misaligned");
+    if (!(d->norm_eps >= 0.0f && d->norm_eps <= 3.0e38f)) return invalid("norm_eps must be finite and not negative");
+    if (!(d->out_scale >= -3.0e38f && d->out_scale <= 3.0e38f)) return invalid("out_scale must be finite");
+    if (c->num_kv_heads % 2 != 0) return invalid("num_kv_heads must be even: heads go in pairs");
+    if (c->head_dim > 128) return fail(LAST_ERR_UNSUPPORTED, "head_dim must be at most 128: values are twice as wide");
+  }
+  const int e = elem_bytes(c->dtype);
+  const double rows = (double)num_tokens * (num_q_heads / c->num_kv_heads), keys = (double)s->max_pages * c->page_size + 256.0;
+  if (rows >= 2147483648.0 || rows * c->num_kv_heads * keys >= 1152921504606846976.0)
+    return fail(LAST_ERR_UNSUPPORTED, "num_tokens * num_q_heads / num_kv_heads must stay below 2^31, "
+                                      "num_tokens * num_q_heads * (max_pages * page_size + 256) below 2^60");
+  if (num_tokens > 0 && (q == nullptr || out == nullptr)) return invalid("q and out are required");
+  if (!aligned(q, 16) || !aligned(out, 16)) return invalid("q and out must be 16-byte aligned");
+  if (!multiple16(q_stride * e) || !multiple16(out_stride * e))
+    return invalid("q_stride and out_stride must be multiples of 16 bytes");
+  if (num_tokens > 1 && out_stride < (int64_t)num_q_heads * c->head_dim)
+    return invalid("out_stride must be at least num_q_heads * head_dim");
+  if (!aligned(lse, 4)) return invalid("lse is misaligned");
+  if ((st = check_cache_ws(ws, ws_bytes, kStatusBytes + chunk_scratch_bytes(c->head_dim, e))) != LAST_OK) return st;
+  ChunkArgs a{};
+  a.cache = layer_of(c, layer);
+  a.seq = view_of(s);
+  a.cu_new = cu_new;
+  a.tokens = num_tokens;
+  a.q_heads = num_q_heads;
+  a.elem = e;
+  a.scale = scale > 0.0f ? scale : 1.0f / std::sqrt((float)c->head_dim);
+  a.causal = causal != 0;
+  a.window = window;
+  a.q = static_cast<const char *>(q);
+  a.out = static_cast<char *>(out);
+  a.q_stride = q_stride * e;
+  a.out_stride = out_stride * e;
+  a.lse = lse;
+  a.diff = diff;
+  if (diff) {
+    a.lambda = d->lambda;
+    a.norm_weight = d->norm_weight;
+    a.norm_eps = d->norm_eps;
+    a.out_scale = d->out_scale;
+  }
+  a.ws = static_cast<char *>(ws);
+  return launched(launch_chunk(a, static_cast<cudaStream_t>(stream)), diff ? "differential attention launch" : "chunk attention launch");
+}
+
 }  // namespace
 }  // namespace last
 
@@ -389,6 +455,36 @@ last_status last_cache_attention(const last_cache *c, int32_t layer, const last_
     a.lse = lse;
     a.ws = static_cast<char *>(ws);
     return launched(launch_attend(a, static_cast<cudaStream_t>(stream)), "attention launch");
+  });
+}
+
+last_status last_chunk_workspace_size(const last_cache *c, int32_t num_q_heads, size_t *bytes) {
+  return guarded([&]() -> last_status {
+    if (bytes == nullptr) return invalid("bytes is NULL");
+    last_status st = check_cache(c);
+    if (st != LAST_OK || (st = check_heads(c, num_q_heads)) != LAST_OK) return st;
+    *bytes = kStatusBytes + chunk_scratch_bytes(c->head_dim, elem_bytes(c->dtype));
+    return LAST_OK;
+  });
+}
+
+last_status last_cache_chunk_attention(const last_cache *c, int32_t layer, const last_sequences *s, int32_t num_tokens,
+                                       const int32_t *cu_new, int32_t num_q_heads, float scale, int32_t causal,
+                                       int32_t window, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                                       float *lse, void *ws, size_t ws_bytes, void *stream) {
+  return guarded([&] {
+    return chunk(c, layer, s, num_tokens, cu_new, num_q_heads, scale, causal, window, nullptr, false, q, q_stride, out,
+                 out_stride, lse, ws, ws_bytes, stream);
+  });
+}
+
+last_status last_cache_diff_attention(const last_cache *c, int32_t layer, const last_sequences *s, int32_t num_tokens,
+                                      const int32_t *cu_new, int32_t num_q_heads, float scale, int32_t causal,
+                                      int32_t window, const last_difference *d, const void *q, int64_t q_stride, void *out,
+                                      int64_t out_stride, void *ws, size_t ws_bytes, void *stream) {
+  return guarded([&] {
+    return chunk(c, layer, s, num_tokens, cu_new, num_q_heads, scale, causal, window, d, true, q, q_stride, out, out_stride,
+                 nullptr, ws, ws_bytes, stream);
   });
 }
 

@@ -74,6 +74,23 @@ struct AttendArgs {
   char *ws;
 };
 
+struct ChunkArgs {   // attention of several new tokens per sequence; diff: the difference of two maps
+  CacheLayer cache;
+  SequenceView seq;
+  const int32_t *cu_new;
+  int tokens, q_heads, elem;
+  float scale;
+  bool causal, diff;
+  int window;                       // 0: none
+  const char *q;
+  char *out;
+  long long q_stride, out_stride;   // bytes
+  float *lse;
+  const float *lambda, *norm_weight;
+  float norm_eps, out_scale;
+  char *ws;
+};
+
 struct PagesArgs {   // copy and compact: every layer
   char *k, *v;
   long long layer_stride, page_stride, head_stride, token_stride;   // bytes
@@ -95,10 +112,12 @@ struct CompactArgs {
 
 cudaError_t launch_rotary(const RotaryArgs &a, cudaStream_t s);
 cudaError_t launch_attend(const AttendArgs &a, cudaStream_t s);
+cudaError_t launch_chunk(const ChunkArgs &a, cudaStream_t s);
 cudaError_t launch_page_copy(const PagesArgs &a, int n, const int32_t *src, const int32_t *dst, cudaStream_t s);
 cudaError_t launch_compact(const CompactArgs &a, cudaStream_t s);
 // Workspace of the attention behind the status words.
 size_t attend_scratch_bytes(int q_heads, int kv_heads, int dim);
+size_t chunk_scratch_bytes(int dim, int elem);
 
 // SMs of the current device.
 int sm_count();

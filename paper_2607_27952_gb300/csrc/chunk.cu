@@ -1,0 +1,155 @@
+// Chunk and differential attention: the workspace, the choice of the kernel, and the sums that cuts have parted.
+#include "chunk_impl.cuh"
+
+namespace last {
+
+namespace {
+
+constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinCtas = 2;
+
+template <typename T>
+__device__ __forceinline__ void join_store(T *to, const float (&v)[8], int n) {   // 4 or 8 of v
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+    if (n > 4) *reinterpret_cast<float4 *>(to + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+    __nv_bfloat162 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<uint4 *>(x);
+  }
+}
+
+// CTA (w, y) belongs to the item that share w ends within, if any.  The CTAs of all its cuts divide its rows, 32 at a
+// time: a lane has a row, a warp every eighth group of 8 columns.
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const __grid_constant__ ChunkShape p) {
+  __shared__ int first_cut, last_cut, share_of[kMaxShares + 1], parts;
+  __shared__ float squares[kJoinWarps][32];
+  grid_begins();
+  const ChunkArgs &a = p.a;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, w = blockIdx.x;
+  const int4 x = p.cuts[w];
+  if (x.w == 0) return;
+  if (tid == 0) {
+    first_cut = w;
+    last_cut = w;
+  }
+  __syncthreads();
+  auto tile_at = [&](int i) {   // of the cut behind share i, if it is in this item
+    const int4 c = p.cuts[i];
+    return c.x == x.x && c.y == x.y && c.z == x.z ? c.w : 0;
+  };
+  for (int i = tid; i < p.shares; i += kJoinThreads)
+    if (tile_at(i) > 0) {
+      atomicMin(&first_cut, i);
+      atomicMax(&last_cut, i);
+    }
+  __syncthreads();
+  if (tid == 0) {
+    int n = 0;
+    for (int i = first_cut; i <= last_cut + 1; ++i) {   // the cuts in between are in the item too
+      const bool some = i == first_cut || i > last_cut || tile_at(i) != tile_at(i - 1);
+      if (some) share_of[n++] = i;
+    }
+    parts = n;
+  }
+  __syncthreads();
+  const int me = (w - first_cut) * gridDim.y + blockIdx.y, ctas = (last_cut - first_cut + 1) * gridDim.y;
+  unsigned bad = 0;
+  const ChunkSeq s = chunk_seq(a, x.x, &bad);
+  const int r0 = x.z * p.block, rows = (int)min((long long)p.block, (long long)s.n * p.group - r0);
+  for (int row0 = me * 32; row0 < rows; row0 += ctas * 32) {
+    const int r = row0 + lane;
+    const bool live = r < rows;
+    const int t = (r0 + (live ? r : 0)) / p.group, h = x.y * p.group + (r0 + (live ? r : 0)) - t * p.group;
+    float acc[4][8], sq = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[j][e] = 0.0f;
+    for (int map = 0; map < p.maps; ++map) {
+      auto slot = [&](int i) { return chunk_slot(p, share_of[i], map, i == 0); };   // an item begins in its first share
+      float all = -INFINITY, sum = 0.0f;
+      if (live) {
+        for (int i = 0; i < parts; ++i) all = fmaxf(all, slot(i)[r]);
+        for (int i = 0; i < parts; ++i) sum = fmaf(chunk_factor(slot(i)[r], all), slot(i)[p.block + r], sum);
+      }
+      const float weight = map == 0 ? 1.0f : live ? -a.lambda[h] : 0.0f;
+      if (live && p.maps == 1 && a.lse != nullptr && warp == 0) a.lse[(long long)(s.first + t) * a.q_heads + h] = chunk_lse(all, sum);
+      if (!live || sum == 0.0f) continue;
+      const float g = weight / sum;
+      for (int i = 0; i < parts; ++i) {
+        const float *from = slot(i);
+        const float f = chunk_factor(from[r], all) * g;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int four = (warp + 8 * j) * 2 + e;
+            if (four * 4 >= p.dv) continue;
+            const float4 y = reinterpret_cast<const float4 *>(from + 2 * p.block)[(long long)four * p.block + r];
+            acc[j][4 * e] = fmaf(y.x, f, acc[j][4 * e]);
+            acc[j][4 * e + 1] = fmaf(y.y, f, acc[j][4 * e + 1]);
+            acc[j][4 * e + 2] = fmaf(y.z, f, acc[j][4 * e + 2]);
+            acc[j][4 * e + 3] = fmaf(y.w, f, acc[j][4 * e + 3]);
+          }
+      }
+    }
+    if (p.maps == 2) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sq = fmaf(acc[j][e], acc[j][e], sq);
+      __syncthreads();
+      squares[warp][lane] = sq;
+      __syncthreads();
+      sq = 0.0f;
+      for (int i = 0; i < kJoinWarps; ++i) sq += squares[i][lane];
+      const float f = chunk_norm(a, sq, p.dv);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int d = (warp + 8 * j) * 8 + e;
+          if (d < p.dv) acc[j][e] *= f * (a.norm_weight ? a.norm_weight[d] : 1.0f);
+        }
+    }
+    if (!live) continue;
+    T *out = reinterpret_cast<T *>(a.out + (long long)(s.first + t) * a.out_stride) + (long long)h * p.dv;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = (warp + 8 * j) * 8;
+      if (d < p.dv) join_store(out + d, acc[j], p.dv - d);
+    }
+  }
+}
+
+}  // namespace
+
+size_t chunk_scratch_bytes(int dim, int elem) {
+  (void)elem;
+  return align256(sizeof(int4) * kMaxShares) + align256(sizeof(float) * kMaxShares * 2 * 2 * chunk_slot_floats(64, 2 * dim <= 256 ? 2 * dim : 256));
+}
+
+cudaError_t launch_chunk_join(const ChunkShape &p, cudaStream_t s) {
+  const dim3 grid(p.shares, kJoinCtas);
+  return p.a.elem == 4 ? launch_early(chunk_join_kernel<float>, grid, kJoinThreads, 0, s, p)
+                       : launch_early(chunk_join_kernel<__nv_bfloat16>, grid, kJoinThreads, 0, s, p);
+}
+
+cudaError_t launch_chunk(const ChunkArgs &a, cudaStream_t s) {
+  ChunkShape p{};
+  p.a = a;
+  p.maps = a.diff ? 2 : 1;
+  p.units = a.cache.heads / p.maps;
+  p.group = a.q_heads / a.cache.heads;
+  p.dv = a.cache.dim * p.maps;
+  p.scale2 = a.scale * kChunkLog2e;
+  p.cuts = reinterpret_cast<int4 *>(a.ws + kStatusBytes);
+  p.parts = reinterpret_cast<float *>(a.ws + kStatusBytes + align256(sizeof(int4) * kMaxShares));
+  return launch_chunk_simt(p, s);
+}
+
+}  // namespace last

@@ -16,6 +16,11 @@ typedef last_status (*append_fn)(const last_cache *, int32_t, const last_sequenc
                                  size_t, void *);
 typedef last_status (*attention_fn)(const last_cache *, int32_t, const last_sequences *, int32_t, float, const void *, int64_t,
                                     void *, int64_t, float *, void *, size_t, void *);
+typedef last_status (*chunk_fn)(const last_cache *, int32_t, const last_sequences *, int32_t, const int32_t *, int32_t, float, int32_t,
+                                int32_t, const void *, int64_t, void *, int64_t, float *, void *, size_t, void *);
+typedef last_status (*difference_fn)(const last_cache *, int32_t, const last_sequences *, int32_t, const int32_t *, int32_t, float,
+                                     int32_t, int32_t, const last_difference *, const void *, int64_t, void *, int64_t, void *,
+                                     size_t, void *);
 typedef last_status (*copy_fn)(const last_cache *, int32_t, const int32_t *, const int32_t *, void *, size_t, void *);
 typedef last_status (*compact_fn)(const last_cache *, const last_sequences *, const int32_t *, int32_t, int64_t, const int32_t *,
                                   const int32_t *, const int32_t *, const int32_t *, int32_t, int32_t *, void *, size_t, void *);
@@ -23,6 +28,8 @@ typedef last_status (*compact_fn)(const last_cache *, const last_sequences *, co
 static rope_fn f_rope[2];
 static append_fn f_append;
 static attention_fn f_attention;
+static chunk_fn f_chunk;
+static difference_fn f_difference;
 static copy_fn f_copy;
 static compact_fn f_compact;
 static PyObject *t_f32, *t_bf16, *t_int32, *get_stream, *get_device;
@@ -230,6 +237,68 @@ static PyObject *attention(PyObject *self, PyObject *const *a, Py_ssize_t n) {
                    stream));
 }
 
+/* fp32, contiguous, [n] or, with m >= 0, [n][m]. */
+static int get_floats(PyObject *o, long long n, long long m, tensor *t) {
+  return get(o, t_f32, t) && t->rank == (m < 0 ? 1 : 2) && t->shape[0] == n && (m < 0 || t->shape[1] == m) &&
+         (t->shape[t->rank - 1] <= 1 || t->stride[t->rank - 1] == 1) && (m < 0 || n <= 1 || t->stride[0] == m);
+}
+
+typedef struct {
+  long long layer, window, tokens, heads;
+  const void *c, *s;
+  tensor q, o, cu;
+  void *ws, *stream;
+  size_t bytes;
+  double scale;
+  int causal;
+} chunk_args;
+
+/* What both kinds of attention of several new tokens take: cache, layer, sequences, batch, head_dim, dtype, q, out, ws, cu_new in a;
+ * causal, window, scale, stream in z.  pairs: a value is two heads wide. */
+static int get_chunk(PyObject *const *a, PyObject *const *z, int pairs, chunk_args *g) {
+  long long batch, dim;
+  if (!address(a[0], &g->c) || !integer(a[1], &g->layer) || !address(a[2], &g->s) || !integer(a[3], &batch) || !integer(a[4], &dim) ||
+      !get(a[6], a[5], &g->q) || !get(a[7], a[5], &g->o) || g->q.rank != 3 || g->o.rank != 3 || g->q.shape[2] != dim ||
+      g->q.shape[0] > INT32_MAX || g->q.shape[1] > INT32_MAX || g->q.shape[1] % (pairs ? 2 : 1) != 0 || g->o.shape[0] != g->q.shape[0] ||
+      g->o.shape[1] != (pairs ? g->q.shape[1] / 2 : g->q.shape[1]) || g->o.shape[2] != (pairs ? 2 * dim : dim) ||
+      g->q.stride[2] != 1 || g->o.stride[2] != 1 || (g->q.shape[1] > 1 && g->q.stride[1] != dim) ||
+      (g->o.shape[1] > 1 && g->o.stride[1] != g->o.shape[2]) || g->layer != (int32_t)g->layer || !get_workspace(a[8], &g->ws, &g->bytes))
+    return 0;
+  g->cu = (tensor){0};
+  if (a[9] != Py_None && !get_ints(a[9], batch + 1, &g->cu)) return 0;
+  g->tokens = g->q.shape[0];
+  g->heads = g->q.shape[1];
+  g->scale = PyFloat_AsDouble(z[2]);
+  return (z[0] == Py_True || z[0] == Py_False) && integer(z[1], &g->window) && g->window == (int32_t)g->window && !PyErr_Occurred() &&
+         (g->causal = z[0] == Py_True, stream_of(z[3], &g->stream));
+}
+
+/* chunk(cache, layer, sequences, batch, head_dim, dtype, q, out, ws, cu_new, lse, causal, window, scale, stream) */
+static PyObject *chunk(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  chunk_args g;
+  tensor l = {0};
+  if (n != 15 || !get_chunk(a, a + 11, 0, &g) || (a[10] != Py_None && !get_floats(a[10], g.tokens, g.heads, &l))) return other_way();
+  CALL(f_chunk(g.c, (int32_t)g.layer, g.s, (int32_t)g.tokens, g.cu.ptr, (int32_t)g.heads, (float)g.scale, g.causal, (int32_t)g.window,
+               g.q.ptr, g.q.stride[0], g.o.ptr, g.o.stride[0], l.ptr, g.ws, g.bytes, g.stream));
+}
+
+/* difference(cache, layer, sequences, batch, head_dim, dtype, q, out, ws, cu_new, lam, norm_weight, norm_eps, out_scale, causal, window,
+ * scale, stream) */
+static PyObject *difference(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  chunk_args g;
+  tensor lam, w = {0};
+  if (n != 18 || !get_chunk(a, a + 14, 1, &g) || !get_floats(a[10], g.heads / 2, -1, &lam) ||
+      (a[11] != Py_None && !get_floats(a[11], g.o.shape[2], -1, &w)))
+    return other_way();
+  const double eps = PyFloat_AsDouble(a[12]), scale = PyFloat_AsDouble(a[13]);
+  if (PyErr_Occurred()) return other_way();
+  const last_difference d = {lam.ptr, w.ptr, (float)eps, (float)scale};
+  CALL(f_difference(g.c, (int32_t)g.layer, g.s, (int32_t)g.tokens, g.cu.ptr, (int32_t)g.heads, (float)g.scale, g.causal,
+                    (int32_t)g.window, &d, g.q.ptr, g.q.stride[0], g.o.ptr, g.o.stride[0], g.ws, g.bytes, g.stream));
+}
+
 /* copy(cache, src, dst, ws, stream) */
 static PyObject *copy(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   (void)self;
@@ -261,16 +330,16 @@ static PyObject *compact(PyObject *self, PyObject *const *a, Py_ssize_t n) {
                  ws, bytes, stream));
 }
 
-/* bind(rope, rope_backward, append, attention, copy, compact, float32, bfloat16, int32, get_stream, get_device): the first six are
- * addresses. */
+/* bind(rope, rope_backward, append, attention, copy, compact, chunk, difference, float32, bfloat16, int32, get_stream, get_device):
+ * the first eight are addresses. */
 static PyObject *bind(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   (void)self;
-  const void *f[6];
-  if (n != 11) {
-    PyErr_SetString(PyExc_TypeError, "bind takes 11 arguments");
+  const void *f[8];
+  if (n != 13) {
+    PyErr_SetString(PyExc_TypeError, "bind takes 13 arguments");
     return NULL;
   }
-  for (int i = 0; i < 6; ++i)
+  for (int i = 0; i < 8; ++i)
     if (!address(a[i], &f[i])) {
       PyErr_SetString(PyExc_TypeError, "an address is an int");
       return NULL;
@@ -281,13 +350,16 @@ static PyObject *bind(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   f_attention = (attention_fn)f[3];
   f_copy = (copy_fn)f[4];
   f_compact = (compact_fn)f[5];
+  f_chunk = (chunk_fn)f[6];
+  f_difference = (difference_fn)f[7];
   PyObject **to[5] = {&t_f32, &t_bf16, &t_int32, &get_stream, &get_device};
-  for (int i = 0; i < 5; ++i) Py_XSETREF(*to[i], Py_NewRef(a[6 + i]));
+  for (int i = 0; i < 5; ++i) Py_XSETREF(*to[i], Py_NewRef(a[8 + i]));
   Py_RETURN_NONE;
 }
 
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
-static PyMethodDef methods[] = {METHOD(bind), METHOD(rope), METHOD(append), METHOD(attention), METHOD(copy), METHOD(compact), {0}};
+static PyMethodDef methods[] = {METHOD(bind), METHOD(rope), METHOD(append), METHOD(attention), METHOD(copy), METHOD(compact),
+                                METHOD(chunk), METHOD(difference), {0}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__marshal(void) {
