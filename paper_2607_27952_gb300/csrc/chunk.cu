@@ -128,9 +128,24 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const __grid_c
 
 }  // namespace
 
+// Parts: a block's rows and one value more each for maximum and sum, in two slots of every share and map.
+static size_t parts_bytes(int dim, int elem) {
+  auto all = [&](int maps) -> size_t {
+    const int dv = dim * maps, columns = (dim + 15) / 16 * 16 * maps;
+    if (maps == 2 && dim > 128) return 0;
+    const size_t slots = 2 * (elem == 4 ? kMaxShares * maps : kMaxTensorCtas);
+    return align256(sizeof(float) * slots * chunk_slot_floats(elem == 4 ? 64 : columns <= 128 ? 256 : 128, dv));
+  };
+  return all(1) > all(2) ? all(1) : all(2);
+}
+// diff, bf16: half of a block's rows and 16 columns at a time, per CTA.
+static size_t exchange_bytes(int dim, int elem) {
+  const int columns = (dim + 15) / 16 * 16 * 2;
+  return elem == 4 || dim > 128 ? 0 : align256(sizeof(float) * kMaxTensorCtas * 64 * (columns <= 128 ? 2 : 1) * columns);
+}
+
 size_t chunk_scratch_bytes(int dim, int elem) {
-  (void)elem;
-  return align256(sizeof(int4) * kMaxShares) + align256(sizeof(float) * kMaxShares * 2 * 2 * chunk_slot_floats(64, 2 * dim <= 256 ? 2 * dim : 256));
+  return align256(sizeof(int4) * kMaxShares) + parts_bytes(dim, elem) + exchange_bytes(dim, elem);
 }
 
 cudaError_t launch_chunk_join(const ChunkShape &p, cudaStream_t s) {
@@ -149,7 +164,8 @@ cudaError_t launch_chunk(const ChunkArgs &a, cudaStream_t s) {
   p.scale2 = a.scale * kChunkLog2e;
   p.cuts = reinterpret_cast<int4 *>(a.ws + kStatusBytes);
   p.parts = reinterpret_cast<float *>(a.ws + kStatusBytes + align256(sizeof(int4) * kMaxShares));
-  return launch_chunk_simt(p, s);
+  float *exchange = reinterpret_cast<float *>(reinterpret_cast<char *>(p.parts) + parts_bytes(a.cache.dim, a.elem));
+  return a.elem == 4 ? launch_chunk_f32(p, s) : launch_chunk_bf16(p, exchange, s);
 }
 
 }  // namespace last

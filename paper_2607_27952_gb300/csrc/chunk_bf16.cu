@@ -1,0 +1,1002 @@
+// Chunk and differential attention over bf16 keys and values: both products on the tensor cores (tcgen05).
+//
+// A CTA holds 256 rows (two tiles of 128) where values are at most 128 wide, else 128.  Steps go key tile by key
+// tile and, within, row tile by row tile:
+//   S = Q K^T into one of two accumulators in TMEM; 8 warps turn it into weights P = 2^(scale2 S - m), rounded to
+//   bf16, a warp and its lanes' rows having 64 of the 128 keys, and put them back over S; O = O + P V in TMEM, P being
+//   read from there.
+// The next step's S is formed before this one's O, so that the tensor cores work while the weights are formed.
+// The maximum m follows a row's logits only past a factor of 2^8 (weights are then at most 2^8, and O is rescaled by those warps,
+// rarely); l sums the weights before they are rounded.
+//
+// Warps: 0-7 softmax and epilogue, 8 issues the products, 9 fills a ring of K and V panels (128 keys by up to 128 columns) with TMA
+// boxes of the pages, 10 and 11 walk the share's items and fetch rows of Q.  V rows that no row sees are zeroed in
+// shared memory before the product reads them: a weight of zero times an infinity or NaN would show.
+// diff: a cluster of two CTAs, one map each; each finishes half of the rows, with the other's half of O through L2.
+#include "chunk_impl.cuh"
+#include "tensor_map.h"
+
+namespace last {
+
+namespace {
+
+constexpr int kThreads = 384, kSoftWarps = 8, kKeys = 128, kRingMax = 12, kItems = 4, kTileInfo = 16;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10;
+constexpr uint32_t kChunkBytes = kKeys * 128;   // 128 rows of 64 elements
+constexpr int kOutColumn = 256;                 // of TMEM; S takes columns 0 - 127 and 128 - 255
+
+struct Geometry {      // the same for every CTA
+  ChunkShape p;
+  int chunks;          // 64-column chunks of a head's row
+  int panel_chunks;    // of the first panel: a panel is two chunks or one
+  int columns;         // a head's row, up to a multiple of 16
+  int slots;           // panels of the ring
+  int box_log, page_log;
+  float *exchange;     // diff: [CTAs][row tiles][columns / 4][64 rows][4]
+};
+
+struct Item {
+  int seq, unit, first, r0, rows;
+  int base, begin, lens;
+  int ka, kb;             // key tiles of the share
+  int lo, hi;             // keys that some row sees
+  int ta[2], tb[2];       // key tiles by row tile
+  int tlo[2], thi[2];     // keys by row tile
+  int whole, second;
+};
+
+struct alignas(16) Shared {   // with 1 KB to align the panels by, 3 KB: 7 panels of 32 KB stand beside it
+  unsigned long long full[kRingMax], empty[kRingMax], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2];
+  unsigned long long item_full[kItems], item_empty[kItems], x_full, x_empty, never;
+  Item items[kItems];
+  float row[2][128];      // a row's value of one half of the columns for the other
+  ChunkShare share;
+  unsigned long long sums[kThreads / 32];
+  unsigned skip[kTileInfo];   // of the key tiles on their way: groups of 8 keys whose page is out of range
+  uint32_t tmem;
+  unsigned flags;
+  volatile unsigned dead;
+};
+static_assert(sizeof(Shared) <= 2048, "no room beside seven panels");
+
+// A whole warp waits, with a limit; the first to give up has every other wait of the CTA end too.  The softmax warps go on
+// after a wait that gave up, with whatever is there, to the end of their item, so that no barrier of theirs waits for a warp
+// that has left; the others leave.
+__device__ __forceinline__ bool wait(Shared &sm, unsigned long long *bar, uint32_t parity) {
+  bool ok = mbar_try_wait(bar, parity);
+  for (uint32_t i = 0; i < kWaitLimit && !ok; ++i) {
+    if ((i & 31) == 0 && sm.dead) break;
+    ok = mbar_try_wait(bar, parity);
+  }
+  if (__all_sync(~0u, ok)) return true;
+  sm.dead = 1;
+  return false;
+}
+// For what the other CTA of the cluster has written.
+__device__ __forceinline__ bool wait_cluster(Shared &sm, unsigned long long *bar, uint32_t parity) {
+  uint32_t ok = 0;
+  for (uint32_t i = 0; i < kWaitLimit && !ok; ++i) {
+    if ((i & 31) == 1 && sm.dead) break;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+  }
+  if (__all_sync(~0u, ok != 0)) return true;
+  sm.dead = 1;
+  return false;
+}
+__device__ __forceinline__ bool passed(unsigned long long *bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\t"
+               "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+               "selp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+  return __all_sync(~0u, ok != 0);
+}
+
+// 32 columns of the warp's 32 TMEM lanes.
+__device__ __forceinline__ void tmem_ld32(uint32_t a, uint32_t *r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(a) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t *r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+      :: "r"(a), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// D[tmem] (+)= A[tmem] * B[smem], issued by one thread.
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               :: "r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Rows of 128 bytes with the 128-byte swizzle whose inner dimension is N: chunks of 64 columns kChunkBytes apart, 8 keys 1024.
+__device__ __forceinline__ uint64_t desc_n_major(uint32_t saddr) {
+  uint64_t d = (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(kChunkBytes >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+constexpr uint32_t kNMajor = 1u << 16;   // of B, in the instruction descriptor
+
+__device__ __forceinline__ uint64_t pack2(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {   // x in the low half
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+  return r;
+}
+
+// One lane of a converged warp, always the same.
+__device__ __forceinline__ bool elected() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+
+__device__ __forceinline__ int elected_lane() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync %0|p, 0xffffffff;\n\t}" : "=r"(r));
+  return (int)r;
+}
+__device__ __forceinline__ void tma_box(uint32_t dst, const void *map, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+               :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+}
+
+// The two warps that share 32 rows.
+__device__ __forceinline__ void pair_sync(int pair) { asm volatile("bar.sync %0, 64;" :: "r"(pair + 1) : "memory"); }
+__device__ __forceinline__ bool pair_any(int pair, bool x) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+               "bar.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"((uint32_t)x), "r"(pair + 1) : "memory");
+  return r != 0;
+}
+
+// Steps go key tile by key tile, in each row tile by row tile, and are counted over all items.
+__device__ __forceinline__ bool active(const Item &it, int j, int t) { return j >= it.ta[t] && j < it.tb[t]; }
+
+// A place in the ring and whether its panel is of an even or odd round.
+struct Place {
+  int slot;
+  uint32_t round;
+  __device__ __forceinline__ void skip(const Geometry &g, int n) {   // n <= slots
+    slot += n;
+    if (slot >= g.slots) {
+      slot -= g.slots;
+      round ^= 1;
+    }
+  }
+};
+
+// TILES row tiles of a block, PANELS of a head's row, MAPS: 2 for diff.
+template <int TILES, int PANELS, int MAPS>
+struct Kind {
+  static constexpr int kTiles = TILES, kPanels = PANELS, kMaps = MAPS, kValues = PANELS * MAPS;
+  // Weights in two parts (the second what rounding has left) where a difference would magnify the rounding: its terms are
+  // alike and cancel.  Else one rounding of the weights, as large as the output's own.
+  static constexpr int kParts = MAPS;
+};
+
+// Query head of map `rank` of pair h, or h.
+template <typename K>
+struct MapHead {
+  static __device__ __forceinline__ int of(int h, int rank) { return K::kMaps == 2 ? 2 * h + rank : h; }
+};
+
+// ---- warps 10 and 11: items and rows of Q ----
+template <typename K>
+__device__ void query_role(const Geometry &g, Shared &sm, char *qs, int rank) {
+  const ChunkShape &p = g.p;
+  const int lane = threadIdx.x & 31, half = (threadIdx.x >> 5) - kQueryWarp, D = p.a.cache.dim;
+  ChunkWalk walk(sm.share);
+  ChunkItem it;
+  uint32_t n = 0, tile = 0;
+  const int eights = g.chunks * 8;   // 16-byte pieces of a row, zeros past D
+  for (bool more = true; more; ++n) {
+    more = walk.next(p, &it);
+    Item o;
+    o.seq = more ? it.seq : -1;
+    if (more) {
+      o.unit = it.unit;
+      o.first = it.s.first;
+      o.r0 = it.r0;
+      o.rows = it.rows;
+      o.base = it.s.base;
+      o.begin = it.s.begin;
+      o.lens = it.s.lens;
+      const bool some = it.t.count > 0;
+      o.ka = some ? it.t.first + it.k0 : 0;
+      o.kb = some ? it.t.first + it.k1 : 0;
+      o.lo = it.t.lo;
+      o.hi = it.t.hi;
+      o.whole = it.whole;
+      o.second = it.second;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        o.ta[t] = o.tb[t] = o.tlo[t] = o.thi[t] = 0;
+        if (!some || t * 128 >= it.rows) continue;
+        const ChunkTiles x = chunk_tiles(p, it.s, it.r0 + t * 128, it.r0 + min(it.rows, t * 128 + 128));
+        o.ta[t] = max(o.ka, x.first);
+        o.tb[t] = min(o.kb, x.first + x.count);
+        o.tlo[t] = x.lo;
+        o.thi[t] = x.hi;
+      }
+    }
+    if (half == 0) {
+      const int e = n % kItems;
+      if (n >= kItems && !wait(sm, &sm.item_empty[e], (n / kItems & 1) ^ 1)) return;
+      if (lane == 0) {
+        sm.items[e] = o;
+        mbar_arrive(&sm.item_full[e]);
+      }
+      __syncwarp();
+    }
+    if (!more) return;
+#pragma unroll
+    for (int t = 0; t < K::kTiles; ++t) {
+      if (o.ta[t] >= o.tb[t]) continue;
+      const int slot = tile % K::kTiles;
+      if (tile >= (uint32_t)K::kTiles && !wait(sm, &sm.q_empty[slot], (tile / K::kTiles & 1) ^ 1)) return;
+      const uint32_t to = smem_addr(qs) + slot * g.chunks * kChunkBytes;
+      // 32 / 8 rows at a time, 8 lanes to a row's 128 bytes
+      for (int r = half * 64 + (lane >> 3); r < half * 64 + 64; r += 4) {
+        const int row = t * 128 + r;
+        const bool live = row < o.rows;
+        const int tok = (o.r0 + (live ? row : 0)) / p.group, h = o.unit * p.group + (o.r0 + (live ? row : 0)) - tok * p.group;
+        const char *from = p.a.q + (long long)(o.first + tok) * p.a.q_stride + (long long)(MapHead<K>::of(h, rank)) * D * 2;
+        for (int c = lane & 7; c < eights; c += 8) {
+          const uint32_t dst = to + (c >> 3) * kChunkBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+          const bool in = live && c * 8 < D;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(in ? from + c * 16 : from), "r"(in ? 16 : 0) : "memory");
+        }
+      }
+      cp_async_commit();
+      cp_async_wait<0>();
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.q_full[slot]);
+      ++tile;
+    }
+  }
+}
+
+// ---- warp 9: K and V ----
+// The lanes look the boxes' pages up, a tile ahead; one lane issues all boxes (25 cycles each; a lane per box took 75).
+template <typename K>
+__device__ void load_role(const Geometry &g, Shared &sm, char *ring, const CUtensorMap *kmap, const CUtensorMap *vmap, int rank) {
+  const ChunkShape &p = g.p;
+  const int lane = threadIdx.x & 31, box = 1 << g.box_log, boxes = kKeys >> g.box_log;
+  const int size = p.a.cache.page_size;
+  const uint32_t ring_at = smem_addr(ring);
+  uint32_t tile = 0;
+  Place at{0, 0};
+  bool again = false;   // the ring has been filled once
+  for (uint32_t n = 0;; ++n) {
+    const int e = n % kItems;
+    if (!wait(sm, &sm.item_full[e], n / kItems & 1)) return;
+    const Item it = sm.items[e];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sm.item_empty[e]);
+    if (it.seq < 0) return;
+    const int32_t *table = p.a.seq.table + it.seq * p.a.seq.table_stride;
+    auto counts = [&](int j) { return lane < boxes && j < it.kb && j * kKeys + lane * box < it.hi && j * kKeys + lane * box > it.lo - box; };
+    auto lookup = [&](int j) {
+      const int key = j * kKeys + lane * box;
+      return counts(j) ? table[g.page_log >= 0 ? key >> g.page_log : key / size] : -1;
+    };
+    int page = it.ka < it.kb ? lookup(it.ka) : -1;
+    for (int j = it.ka; j < it.kb; ++j, ++tile) {
+      const int next_page = lookup(j + 1);
+      const bool wanted = counts(j), here = wanted && (unsigned)page < (unsigned)p.a.cache.num_pages;
+      unsigned skip = __ballot_sync(~0u, wanted && !here);
+      const unsigned there = __ballot_sync(~0u, here);
+      if (skip) {
+        if (lane == 0) atomicOr(&sm.flags, kErrCacheIndex);
+        unsigned eights = 0;   // boxes to groups of 8 keys
+        for (int i = 0; i < 16; ++i) eights |= (skip >> (i * 8 >> g.box_log) & 1) << i;
+        skip = eights;
+      }
+      if (lane == 0) sm.skip[tile % kTileInfo] = skip;
+      const int row = g.page_log >= 0 ? (j * kKeys + lane * box) & (size - 1) : (j * kKeys + lane * box) % size;
+#pragma unroll
+      for (int i = 0; i < K::kPanels + K::kValues; ++i) {
+        const int pi = i % K::kPanels, value = i / K::kPanels - 1;   // -1: K
+        const int chunks = K::kPanels == 1 ? g.chunks : min(2, g.chunks - 2 * pi);
+        if (again && !wait(sm, &sm.empty[at.slot], at.round ^ 1)) return;
+        const uint32_t bar = smem_addr(&sm.full[at.slot]), panel = ring_at + at.slot * g.panel_chunks * kChunkBytes;
+        const int head = it.unit * K::kMaps + (value < 0 ? rank : value);
+        const CUtensorMap *map = value < 0 ? kmap : vmap;
+        const int leader = elected_lane();
+        if (lane == leader) mbar_expect_tx(&sm.full[at.slot], __popc(there) * chunks * box * 128);
+        for (unsigned left = there; left != 0; left &= left - 1) {
+          const int b = __ffs(left) - 1, its_page = __shfl_sync(~0u, page, b), its_row = __shfl_sync(~0u, row, b);
+          if (elected())
+            for (int c = 0; c < chunks; ++c)
+              tma_box(panel + c * kChunkBytes + (b << (g.box_log + 7)), map, pi * 128 + c * 64, its_row, head, its_page, bar);
+          __syncwarp();
+        }
+        const int before = at.slot;
+        at.skip(g, 1);
+        again |= at.slot < before;
+      }
+      page = next_page;
+    }
+  }
+}
+
+// ---- warp 8: the products ----
+struct Step {   // whose P V is still to come
+  bool some, first, last;  // first of its row tile in the item, last of its key tile
+  uint32_t s;
+  int t, kmin, kmax;
+  int zero_lo, zero_hi;    // rows of V that some row sees
+  unsigned skip;
+  Place at;                // of V
+};
+
+__device__ void zero_rows(uint32_t panel, int chunks, int from, int to) {
+  for (int c = 0; c < chunks; ++c)
+    for (int i = from * 8 + (threadIdx.x & 31); i < to * 8; i += 32)
+      asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" :: "r"(panel + c * kChunkBytes + i * 16), "r"(0) : "memory");
+}
+
+template <typename K>
+__device__ __forceinline__ bool values(const Geometry &g, Shared &sm, uint32_t ring, Step &x, uint32_t tmem) {
+  const int b = x.s & 1;
+  x.some = false;
+  if (!wait(sm, &sm.p_full[b], x.s >> 1 & 1)) return false;
+  tc_fence_after();
+  const uint32_t pt = tmem + b * 128, o = tmem + kOutColumn + x.t * 128;
+  const int k0 = x.kmin / 16, k1 = (x.kmax + 15) / 16;
+#pragma unroll
+  for (int i = 0; i < K::kValues; ++i) {
+    const int pi = i % K::kPanels, head = i / K::kPanels;
+    if (!wait(sm, &sm.full[x.at.slot], x.at.round)) return false;
+    const uint32_t panel = ring + x.at.slot * g.panel_chunks * kChunkBytes;
+    if (x.zero_lo > k0 * 16 || x.zero_hi < k1 * 16 || x.skip) {
+      const int chunks = K::kPanels == 1 ? g.chunks : min(2, g.chunks - 2 * pi);
+      zero_rows(panel, chunks, k0 * 16, x.zero_lo);
+      zero_rows(panel, chunks, x.zero_hi, k1 * 16);
+      for (unsigned left = x.skip; left != 0; left &= left - 1) zero_rows(panel, chunks, (__ffs(left) - 1) * 8, __ffs(left) * 8);
+      fence_proxy_async_smem();
+      __syncwarp();
+    }
+    if (elected()) {
+      const int n = K::kPanels == 1 ? g.columns : min(128, g.columns - pi * 128);
+      const uint32_t idesc = umma_idesc_bf16(128, n) | kNMajor, d = o + head * g.columns + pi * 128;
+      const uint64_t v = desc_n_major(panel);
+      if (k1 - k0 == 8) {
+        umma_bf16_ts(d, pt, v, idesc, x.first ? 0u : 1u);
+#pragma unroll
+        for (int k = 1; k < 8; ++k) umma_bf16_ts(d, pt + (k >> 2) * 64 + (k & 3) * 8, v + k * (2048 >> 4), idesc, 1u);
+        if (K::kParts == 2)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) umma_bf16_ts(d, pt + 32 + (k >> 2) * 64 + (k & 3) * 8, v + k * (2048 >> 4), idesc, 1u);
+      } else {
+        for (int k = k0; k < k1; ++k)
+#pragma unroll
+          for (int e = 0; e < K::kParts; ++e)
+            umma_bf16_ts(d, pt + 32 * e + (k >> 2) * 64 + (k & 3) * 8, v + k * (2048 >> 4), idesc, x.first && k == k0 && e == 0 ? 0u : 1u);
+      }
+      if (x.last) umma_commit(&sm.empty[x.at.slot]);
+      if (i == K::kValues - 1) umma_commit(&sm.pv_done[b]);
+    }
+    __syncwarp();
+    x.at.skip(g, 1);
+  }
+  return true;
+}
+
+template <typename K>
+__device__ void product_role(const Geometry &g, Shared &sm, char *qs_, char *ring_, uint32_t tmem) {
+  const int lane = threadIdx.x & 31, D = g.p.a.cache.dim;
+  const uint32_t qs = smem_addr(qs_), ring = smem_addr(ring_);
+  uint32_t s = 0, tile = 0, q_tile = 0;
+  Place at{0, 0};
+  Step behind;
+  behind.some = false;
+  for (uint32_t n = 0;; ++n) {
+    const int e = n % kItems;
+    // what waits for the next item must not keep the last P V back
+    if (behind.some && !passed(&sm.item_full[e], n / kItems & 1) && !values<K>(g, sm, ring, behind, tmem)) return;
+    if (!wait(sm, &sm.item_full[e], n / kItems & 1)) return;
+    const Item it = sm.items[e];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sm.item_empty[e]);
+    if (it.seq < 0) break;
+    uint32_t q_at[2] = {q_tile, q_tile + (it.ta[0] < it.tb[0])};
+    for (int j = it.ka; j < it.kb; ++j, ++tile) {
+      const int last_tile = active(it, j, 1) ? 1 : active(it, j, 0) ? 0 : -1;
+      const int key0 = j * kKeys;
+#pragma unroll
+      for (int t = 0; t < K::kTiles; ++t) {
+        if (!active(it, j, t)) continue;
+        const int q = q_at[t] % K::kTiles;
+        const uint32_t q_phase = q_at[t] / K::kTiles & 1;
+        if (j == it.ta[t]) {
+          if (behind.some && !passed(&sm.q_full[q], q_phase) && !values<K>(g, sm, ring, behind, tmem)) return;
+          if (!wait(sm, &sm.q_full[q], q_phase)) return;
+        }
+        Step x;
+        x.some = true;
+        x.s = s;
+        x.t = t;
+        x.kmin = max(0, it.tlo[t] - key0);
+        x.kmax = min(kKeys, it.thi[t] - key0);
+        x.first = j == it.ta[t];
+        x.last = t == last_tile;
+        x.zero_lo = max(0, it.lo - key0);
+        x.zero_hi = min(kKeys, it.hi - key0);
+        x.at = at;
+        const uint32_t idesc = umma_idesc_bf16(128, (x.kmax + 15) / 16 * 16), d = tmem + (s & 1) * 128;
+#pragma unroll
+        for (int pi = 0; pi < K::kPanels; ++pi) {
+          if (!wait(sm, &sm.full[x.at.slot], x.at.round)) return;
+          if (elected()) {
+            const uint64_t k_rows = umma_desc_sw128(ring + x.at.slot * g.panel_chunks * kChunkBytes);
+            const uint64_t q_rows = umma_desc_sw128(qs + (q * g.chunks + 2 * pi) * kChunkBytes);
+            const int steps = (D - pi * 128 + 15) / 16;
+            auto product = [&](int k) {
+              const int off = ((k >> 2) * (int)kChunkBytes + (k & 3) * 32) >> 4;
+              umma_bf16(d, q_rows + off, k_rows + off, idesc, (pi | k) != 0 ? 1u : 0u);
+            };
+            if (steps >= 8) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) product(k);
+            } else {
+              for (int k = 0; k < steps; ++k) product(k);
+            }
+            if (x.last) umma_commit(&sm.empty[x.at.slot]);
+            if (pi == K::kPanels - 1) {
+              umma_commit(&sm.s_full[s & 1]);
+              if (j + 1 == it.tb[t]) umma_commit(&sm.q_empty[q]);
+            }
+          }
+          __syncwarp();
+          x.at.skip(g, 1);
+        }
+        x.skip = sm.skip[tile % kTileInfo];
+        if (behind.some && !values<K>(g, sm, ring, behind, tmem)) return;
+        behind = x;
+        ++s;
+      }
+      if (last_tile < 0) {   // nobody's keys: passed on as they came
+        Place x = at;
+        for (int i = 0; i < K::kPanels + K::kValues; ++i) {
+          if (!wait(sm, &sm.full[x.slot], x.round)) return;
+          if (lane == 0) mbar_arrive(&sm.empty[x.slot]);
+          x.skip(g, 1);
+        }
+      }
+      at.skip(g, K::kPanels + K::kValues);
+    }
+    q_tile += (it.ta[0] < it.tb[0]) + (it.ta[1] < it.tb[1]);
+  }
+  if (behind.some) values<K>(g, sm, ring, behind, tmem);
+}
+
+// ---- warps 0 to 7 ----
+struct Rows {      // what a thread keeps of a row tile
+  float m, l;      // l: of this warp's keys
+  int lo, hi;      // keys that its row sees
+  bool started;
+  uint32_t last;   // its last step
+};
+
+// Weights of the warp's 32 rows and 64 of the step's keys.  from, to: columns of these that the row sees.
+template <typename K, bool MASKED>
+__device__ __forceinline__ void weights(const Geometry &g, Shared &sm, Rows &r, uint32_t s, uint32_t tmem, int t, int chunk0, int chunk1,
+                                        int from, int to, unsigned skip) {
+  const int pair = (threadIdx.x >> 5) & 3, half = (threadIdx.x >> 5) >> 2, row = pair * 32 + (threadIdx.x & 31);
+  const uint32_t lanes = (uint32_t)(pair * 32) << 16, st = tmem + lanes + (s & 1) * 128 + half * 64;
+  uint32_t v[64];
+  tmem_ld32(st, v);
+  tmem_ld32(st + 32, v + 32);
+  tmem_wait_ld();
+  if (MASKED) {
+#pragma unroll
+    for (int i = 0; i < 64; ++i) {
+      const bool sees = i >= from && i < to && !(skip >> (half * 8 + i / 8) & 1);
+      if (!sees) v[i] = __float_as_uint(-INFINITY);
+    }
+  }
+  float top[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    top[e] = fmaxf(__uint_as_float(v[e]), __uint_as_float(v[4 + e]));
+#pragma unroll
+    for (int i = 8; i < 64; i += 8) top[e] = fmaxf(fmaxf(top[e], __uint_as_float(v[i + e])), __uint_as_float(v[i + 4 + e]));
+  }
+  float mine = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * g.p.scale2;
+  if (pair_any(pair, mine > r.m + 8.0f)) {
+    sm.row[half][row] = mine;
+    pair_sync(pair);
+    mine = fmaxf(r.m, fmaxf(mine, sm.row[half ^ 1][row]));
+    const float alpha = mine > r.m ? chunk_exp2(r.m - mine) : 1.0f;
+    r.m = mine;
+    r.l *= alpha;
+    if (r.started) {
+      if (r.last + 1 == s) wait(sm, &sm.pv_done[r.last & 1], r.last >> 1 & 1);
+      tc_fence_after();
+      for (int c = chunk0; c < chunk1; ++c) {
+        uint32_t o[16];
+        const uint32_t at = tmem + lanes + kOutColumn + t * 128 + c * 16;
+        tmem_ld16(at, o);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+        tmem_st16(at, o);
+      }
+      tmem_wait_st();
+    }
+    pair_sync(pair);   // before the next maximum overwrites sm.row
+  }
+  const float off = r.m == -INFINITY ? 0.0f : -r.m;
+  const uint64_t scale = pack2(g.p.scale2, g.p.scale2), shift = pack2(off, off);
+  uint64_t sum[2] = {0, 0};
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    uint32_t w[16], rest[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int at = 32 * q + 2 * i;
+      const float2 x = unpack2(fma2(pack2(__uint_as_float(v[at]), __uint_as_float(v[at + 1])), scale, shift));
+      const float e0 = chunk_exp2(x.x), e1 = chunk_exp2(x.y);
+      w[i] = pack_bf16(e0, e1);
+      sum[i & 1] = add2(sum[i & 1], pack2(e0, e1));
+      if (K::kParts == 2) rest[i] = pack_bf16(e0 - bf16lo(w[i]), e1 - bf16hi(w[i]));
+    }
+    tmem_st16(st + 16 * q, w);
+    if (K::kParts == 2) tmem_st16(st + 32 + 16 * q, rest);
+  }
+  const float2 total = unpack2(add2(sum[0], sum[1]));
+  r.l += total.x + total.y;
+  tmem_wait_st();
+}
+
+// Column `lane` of the 32 from col on of a row of O once more, on the CUDA cores, for rows where the sums are not finite though
+// their weights are: a weight of zero times an infinity or NaN in a row of V that the row does not see leaves a NaN.  Here
+// such keys are passed over.  The row sees keys lo .. hi - 1 of the item's share; m: its maximum.
+template <typename K>
+__device__ __noinline__ float careful(const Geometry &g, const Item &it, int lo, int hi, float m, const char *q, int k_head, int v_head, int col) {
+  const ChunkShape &p = g.p;
+  const CacheLayer &c = p.a.cache;
+  const int lane = threadIdx.x & 31, D = c.dim;
+  const int begin = max(lo, it.ka * kKeys), end = (int)min((long long)hi, (long long)it.kb * kKeys);
+  float acc = 0.0f;
+  for (int k0 = begin; k0 < end; k0 += 32) {
+    const int key = k0 + min(lane, end - 1 - k0);
+    const int page = p.a.seq.table[it.seq * p.a.seq.table_stride + key / c.page_size];
+    const bool sees = lane < end - k0 && (unsigned)page < (unsigned)c.num_pages;
+    const long long at = sees ? page * c.page_stride + key % c.page_size * c.token_stride : 0;
+    float z = 0.0f;
+    for (int d = 0; d < D; d += 8) {
+      float a[8], b[8];
+      Elem<__nv_bfloat16>::widen(ldg(q + d * 2), a);
+      Elem<__nv_bfloat16>::widen(ldg(c.k + k_head * c.head_stride + at + d * 2), b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z = fmaf(a[i], b[i], z);
+    }
+    float w = chunk_exp2(fmaf(z, p.scale2, m == -INFINITY ? 0.0f : -m));
+    if (K::kParts == 1) w = bf16lo(pack_bf16(w, 0.0f));
+    for (unsigned left = __ballot_sync(~0u, sees); left != 0; left &= left - 1) {
+      const int i = __ffs(left) - 1;
+      const long long from = (long long)shfl_u64((unsigned long long)at, i);
+      const float f = __shfl_sync(~0u, w, i);
+      if (col + lane < D) acc = fmaf(f, __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(c.v + v_head * c.head_stride + from)[col + lane]), acc);
+    }
+  }
+  return acc;
+}
+
+// A row of a row tile at the end of its item.
+struct RowEnd {
+  float m, sum;    // of both warps' keys
+  int lo, hi, tok, head;
+  bool live, started;
+};
+
+// O of a warp's rows and its half of the columns: 16-column chunks chunk0 .. chunk1 - 1, `per` to a head, two of one head
+// at a time where there are two.
+template <typename K>
+struct Out {
+  const Geometry &g;
+  const Item &it;
+  const RowEnd &r;
+  int rank, t, per, chunk0, chunk1, D;
+  uint32_t tmem;
+  __device__ Out(const Geometry &g, const Item &it, const RowEnd &r, int rank, int t, uint32_t tmem)
+      : g(g), it(it), r(r), rank(rank), t(t), per(g.columns / 16), D(g.p.a.cache.dim), tmem(tmem) {
+    const int half = threadIdx.x >> 7, all = per * K::kMaps;
+    chunk0 = half ? (all + 1) / 2 : 0;
+    chunk1 = half ? all : (all + 1) / 2;
+  }
+  __device__ __forceinline__ int head(int c) const { return K::kMaps == 2 && c >= per ? 1 : 0; }
+  __device__ __forceinline__ int col(int c) const { return (c - (head(c) ? per : 0)) * 16; }   // of its head
+  __device__ __forceinline__ int column(int c) const { return head(c) * D + col(c); }          // of the value
+  __device__ __forceinline__ bool two(int c) const { return c + 1 < chunk1 && (K::kMaps == 1 || c + 1 != per); }
+  __device__ __forceinline__ int next(int c) const { return c + (two(c) ? 2 : 1); }
+  __device__ __forceinline__ int width(int c) const { return min(two(c) ? 32 : 16, D - col(c)); }
+  __device__ __forceinline__ void load(int c, float (&x)[32]) const {
+    const int lane = threadIdx.x & 31;
+    const uint32_t at = tmem + ((threadIdx.x >> 5 & 3) << 21) + kOutColumn + t * 128 + c * 16;
+    uint32_t o[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) o[i] = 0;
+    if (r.started) {
+      if (two(c)) {
+        tmem_ld32(at, o);
+        tmem_wait_ld();
+      } else {
+        tmem_ld16(at, o);
+      }
+    }
+    float zero = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      x[i] = __uint_as_float(o[i]);
+      zero = fmaf(x[i], 0.0f, zero);
+    }
+    // zero is NaN where some column is not finite
+    for (unsigned odd = __ballot_sync(~0u, r.live && zero != 0.0f && r.sum < INFINITY); odd != 0; odd &= odd - 1) {
+      const int who = __ffs(odd) - 1;
+      const char *q = g.p.a.q + (long long)(it.first + r.tok) * g.p.a.q_stride + (long long)MapHead<K>::of(r.head, rank) * D * 2;
+      const float again = careful<K>(g, it, __shfl_sync(~0u, r.lo, who), __shfl_sync(~0u, r.hi, who), __shfl_sync(~0u, r.m, who),
+                                     reinterpret_cast<const char *>(shfl_u64(reinterpret_cast<unsigned long long>(q), who)),
+                                     it.unit * K::kMaps + rank, it.unit * K::kMaps + head(c), col(c));
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const float y = __shfl_sync(~0u, again, i);
+        if (lane == who && (i < 16 || two(c))) x[i] = y;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(int c, const float (&x)[32]) const {
+    char *out = g.p.a.out + (long long)(it.first + r.tok) * g.p.a.out_stride + ((long long)r.head * g.p.dv + column(c)) * 2;
+    if (!r.live) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (8 * i < width(c))
+        *reinterpret_cast<uint4 *>(out + i * 16) =
+            make_uint4(pack_bf16(x[8 * i], x[8 * i + 1]), pack_bf16(x[8 * i + 2], x[8 * i + 3]), pack_bf16(x[8 * i + 4], x[8 * i + 5]),
+                       pack_bf16(x[8 * i + 6], x[8 * i + 7]));
+  }
+};
+
+// To the output where the share has the whole item (diff: rows that the other CTA finishes to it), else to the workspace.
+template <typename K>
+__device__ __noinline__ void finish(const Geometry &g, const Item &it, const RowEnd &r, int rank, int t, uint32_t tmem, bool sends, float *own) {
+  const ChunkShape &p = g.p;
+  const Out<K> o(g, it, r, rank, t, tmem);
+  const int half = threadIdx.x >> 7, row = threadIdx.x & 127, all = o.per * K::kMaps;
+  const float inv = r.sum == 0.0f ? 0.0f : 1.0f / r.sum;
+  float x[32];
+  if (!it.whole) {
+    float *slot = chunk_slot(p, blockIdx.x / K::kMaps, rank, it.second);
+    const int br = t * 128 + row;
+    if (r.live && half == 0) {
+      slot[br] = r.m;
+      slot[p.block + br] = r.sum;
+    }
+#pragma unroll 1
+    for (int c = o.chunk0; c < o.chunk1; c = o.next(c)) {
+      o.load(c, x);
+      float4 *to = reinterpret_cast<float4 *>(slot + 2 * p.block) + (long long)(o.column(c) / 4) * p.block + br;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r.live && i * 4 < o.width(c)) to[(long long)i * p.block] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    }
+    return;
+  }
+  if (K::kMaps == 1 && r.live && half == 0 && p.a.lse != nullptr)
+    p.a.lse[(long long)(it.first + r.tok) * p.a.q_heads + r.head] = chunk_lse(r.m, r.sum);
+  if (K::kMaps == 2 && !sends) return;
+#pragma unroll 1
+  for (int c = o.chunk0; c < o.chunk1; c = o.next(c)) {
+    o.load(c, x);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = r.sum == 0.0f ? 0.0f : x[i] * inv;
+    if (K::kMaps == 1) {
+      o.store(c, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < 4 || o.two(c)) reinterpret_cast<float4 *>(own)[((t * all + c) * 4 + i) * 64 + (row & 63)] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    }
+  }
+}
+
+// diff: the rows that this CTA finishes, with the other's half of the difference.
+template <typename K>
+__device__ __noinline__ void finish_difference(const Geometry &g, Shared &sm, const Item &it, const RowEnd &r, int rank, int t, uint32_t tmem, const float4 *theirs) {
+  const ChunkShape &p = g.p;
+  const Out<K> o(g, it, r, rank, t, tmem);
+  const int half = threadIdx.x >> 7, row = threadIdx.x & 127, pair = row >> 5, all = o.per * K::kMaps;
+  const float inv = r.sum == 0.0f ? 0.0f : 1.0f / r.sum, lam = p.a.lambda[r.head];
+  const float f0 = rank == 0 ? inv : -lam * inv, f1 = rank == 0 ? -lam : 1.0f;
+  float x[32], sq = 0.0f;
+  auto difference = [&](int c) {
+    o.load(c, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (i < 4 || o.two(c)) y = __ldcg(theirs + ((t * all + c) * 4 + i) * 64 + (row & 63));
+      const float z[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[4 * i + k] = (r.sum == 0.0f ? 0.0f : x[4 * i + k] * f0) + z[k] * f1;
+    }
+  };
+  if (p.a.norm_weight != nullptr) {   // columns past D are zeros
+#pragma unroll 1
+    for (int c = o.chunk0; c < o.chunk1; c = o.next(c)) {
+      difference(c);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) sq = fmaf(x[i], x[i], sq);
+    }
+    sm.row[half][row] = sq;
+    pair_sync(pair);
+    sq += sm.row[half ^ 1][row];
+    pair_sync(pair);
+  }
+  const float f = chunk_norm(p.a, sq, p.dv);
+#pragma unroll 1
+  for (int c = o.chunk0; c < o.chunk1; c = o.next(c)) {
+    difference(c);
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (i < o.width(c)) x[i] *= f * (p.a.norm_weight ? p.a.norm_weight[o.column(c) + i] : 1.0f);
+    o.store(c, x);
+  }
+}
+
+template <typename K>
+__device__ void soft_role(const Geometry &g, Shared &sm, uint32_t tmem, int rank) {
+  const ChunkShape &p = g.p;
+  const ChunkArgs &a = p.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp & 3, half = warp >> 2, row = pair * 32 + lane;
+  const int all = g.columns / 16 * K::kMaps, chunk0 = half ? (all + 1) / 2 : 0, chunk1 = half ? all : (all + 1) / 2;
+  uint32_t s = 0, tile = 0, crossed = 0;
+  for (uint32_t n = 0;; ++n) {
+    const int e = n % kItems;
+    const bool here = wait(sm, &sm.item_full[e], n / kItems & 1);
+    if (pair_any(pair, !here)) return;
+    const Item it = sm.items[e];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sm.item_empty[e]);
+    if (it.seq < 0) return;
+    const ChunkSeq seq{it.first, 0, it.base, it.begin, it.lens};
+    Rows r[K::kTiles];
+#pragma unroll
+    for (int t = 0; t < K::kTiles; ++t) {
+      const bool live = t * 128 + row < it.rows;
+      const int tok = (it.r0 + t * 128 + row) / p.group;
+      r[t].m = -INFINITY;
+      r[t].l = 0.0f;
+      r[t].lo = live ? chunk_lo(a, seq, tok) : 0;                // rows of no token are zeros: no mask for them
+      r[t].hi = live ? chunk_hi(a, seq, tok) : 0x7fffffff;
+      r[t].started = false;
+      r[t].last = 0;
+    }
+    for (int j = it.ka; j < it.kb; ++j, ++tile) {
+#pragma unroll
+      for (int t = 0; t < K::kTiles; ++t) {
+        if (!active(it, j, t)) continue;
+        wait(sm, &sm.s_full[s & 1], s >> 1 & 1);
+        tc_fence_after();
+        if (t * 128 + pair * 32 < it.rows) {   // else nobody's rows, whatever becomes of them
+          const int key0 = j * kKeys, kmax = min(kKeys, it.thi[t] - key0);
+          const unsigned skip = sm.skip[tile % kTileInfo];
+          // columns past kmax have not been computed
+          const int from = max(0, min(kKeys, r[t].lo - key0)) - half * 64, to = max(0, min(kmax, r[t].hi - key0)) - half * 64;
+          const bool part = __any_sync(~0u, from > 0 || to < 64) || skip != 0;
+          if (part) weights<K, true>(g, sm, r[t], s, tmem, t, chunk0, chunk1, from, to, skip);
+          else weights<K, false>(g, sm, r[t], s, tmem, t, chunk0, chunk1, 0, 64, 0);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.p_full[s & 1]);
+        r[t].started = true;
+        r[t].last = s;
+        ++s;
+      }
+    }
+    if (it.ka < it.kb) {
+      wait(sm, &sm.pv_done[(s - 1) & 1], (s - 1) >> 1 & 1);
+      tc_fence_after();
+    }
+    const bool sends = (pair >> 1) != rank;   // diff: the other CTA finishes these rows
+    if (K::kMaps == 2 && it.whole && sends && crossed > 0) wait_cluster(sm, &sm.x_empty, (crossed - 1) & 1);
+    const size_t stride = (size_t)64 * all * 16 * K::kTiles;
+    RowEnd end[K::kTiles];
+#pragma unroll
+    for (int t = 0; t < K::kTiles; ++t) {
+      if (t * 128 + pair * 32 >= it.rows) break;
+      sm.row[half][row] = r[t].l;
+      pair_sync(pair);
+      end[t].sum = r[t].l + sm.row[half ^ 1][row];
+      pair_sync(pair);
+      end[t].live = t * 128 + row < it.rows;
+      const int at = it.r0 + (end[t].live ? t * 128 + row : 0);
+      end[t].tok = at / p.group;
+      end[t].head = it.unit * p.group + at - end[t].tok * p.group;
+      end[t].m = r[t].m;
+      end[t].lo = r[t].lo;
+      end[t].hi = r[t].hi;
+      end[t].started = r[t].started;
+      finish<K>(g, it, end[t], rank, t, tmem, sends, g.exchange + blockIdx.x * stride);
+    }
+    if (K::kMaps == 1 || !it.whole) continue;
+    // ---- diff: the halves of the rows change places ----
+    const uint32_t other = rank ^ 1;
+    if (sends) {
+      __threadfence();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_shared(&sm.x_full, other));
+    } else {
+      wait_cluster(sm, &sm.x_full, crossed & 1);
+#pragma unroll
+      for (int t = 0; t < K::kTiles; ++t) {
+        if (t * 128 + pair * 32 >= it.rows) break;
+        finish_difference<K>(g, sm, it, end[t], rank, t, tmem, reinterpret_cast<const float4 *>(g.exchange + (blockIdx.x ^ 1) * stride));
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_shared(&sm.x_empty, other));
+    }
+    ++crossed;
+  }
+}
+
+template <typename K>
+__global__ void __launch_bounds__(kThreads, 1)
+chunk_bf16_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
+  extern __shared__ char smem_raw[];
+  Shared &sm = *reinterpret_cast<Shared *>(smem_raw);
+  char *qs = smem_raw + sizeof(Shared);
+  qs += (1024 - (smem_addr(qs) & 1023)) & 1023;
+  char *ring = qs + (size_t)K::kTiles * g.chunks * kChunkBytes;
+  const int tid = threadIdx.x, warp = tid >> 5;
+  const int rank = K::kMaps == 2 ? (int)cluster_ctarank() : 0, share = blockIdx.x / K::kMaps;
+  if (tid == 0) {
+    asm volatile("prefetch.tensormap [%0];" :: "l"(&kmap) : "memory");
+    asm volatile("prefetch.tensormap [%0];" :: "l"(&vmap) : "memory");
+    for (int i = 0; i < g.slots; ++i) {
+      mbar_init(&sm.full[i], 1);
+      mbar_init(&sm.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sm.q_full[i], 2);
+      mbar_init(&sm.q_empty[i], 1);
+      mbar_init(&sm.s_full[i], 1);
+      mbar_init(&sm.p_full[i], kSoftWarps);
+      mbar_init(&sm.pv_done[i], 1);
+    }
+    for (int i = 0; i < kItems; ++i) {
+      mbar_init(&sm.item_full[i], 1);
+      mbar_init(&sm.item_empty[i], kSoftWarps + 2);
+    }
+    mbar_init(&sm.x_full, kSoftWarps / 2);
+    mbar_init(&sm.x_empty, kSoftWarps / 2);
+    mbar_init(&sm.never, 1);
+    fence_mbar_init();
+    sm.flags = 0;
+    sm.dead = 0;
+  }
+  if (warp == kMmaWarp) tmem_alloc(&sm.tmem, 512);
+  tc_fence_before();
+  grid_begins();
+  __syncthreads();
+  tc_fence_after();
+  chunk_share<kThreads>(g.p, share, sm.sums, &sm.share, &sm.flags);
+  if (K::kMaps == 2) cluster_sync();   // the other CTA's barriers are there
+  const uint32_t tmem = sm.tmem;
+  if (warp < kSoftWarps) soft_role<K>(g, sm, tmem, rank);
+  else if (warp == kMmaWarp) product_role<K>(g, sm, qs, ring, tmem);
+  else if (warp == kLoadWarp) load_role<K>(g, sm, ring, &kmap, &vmap, rank);
+  else query_role<K>(g, sm, qs, rank);
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (sm.dead && warp == 0) wait_out(&sm.never);   // copies and products that nobody waited for
+  if (tid == 0) {
+    if (rank == 0) g.p.cuts[share] = chunk_cut(g.p, sm.share.end);
+    post_status(reinterpret_cast<unsigned *>(g.p.a.ws), blockIdx.x, gridDim.x, sm.flags | (sm.dead ? kErrTimeout : 0u));
+  }
+  __syncwarp();
+  if (K::kMaps == 2) cluster_sync();   // until the other one has done with this one's barriers
+  else __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <typename K>
+cudaError_t launch_kind(Geometry g, cudaStream_t s) {
+  ChunkShape &p = g.p;
+  const CacheLayer &c = p.a.cache;
+  p.block = 128 * K::kTiles;
+  constexpr size_t kMost = 227 << 10;
+  const size_t fixed = sizeof(Shared) + 1024 + (size_t)K::kTiles * g.chunks * kChunkBytes, slot = (size_t)g.panel_chunks * kChunkBytes;
+  g.slots = (int)((kMost - fixed) / slot);
+  if (g.slots > kRingMax) g.slots = kRingMax;
+  const size_t smem = fixed + g.slots * slot;
+  // before the maps are encoded: a host thread's first runtime call gives it its context
+  cudaError_t e = allow_smem(reinterpret_cast<const void *>(&chunk_bf16_kernel<K>), smem);
+  if (e != cudaSuccess) return e;
+  CUtensorMap maps[2];
+  const uint64_t row = (uint64_t)c.dim * 2, strides[3] = {(uint64_t)c.token_stride, c.heads > 1 ? (uint64_t)c.head_stride : row,
+                                                          c.num_pages > 1 ? (uint64_t)c.page_stride : row};
+  const uint64_t dims[4] = {(uint64_t)c.dim, (uint64_t)c.page_size, (uint64_t)c.heads, (uint64_t)c.num_pages};
+  const uint32_t box[4] = {64, 1u << g.box_log, 1, 1};
+  for (int i = 0; i < 2; ++i)
+    if (!encode_rows_map(&maps[i], i ? c.v : c.k, false, 4, dims, strides, box)) return cudaErrorInvalidValue;
+  int ctas = sm_count();
+  if (ctas > kMaxTensorCtas) ctas = kMaxTensorCtas;
+  p.shares = ctas / K::kMaps;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.shares * K::kMaps);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim = {2, 1, 1};
+  cfg.attrs = at;
+  cfg.numAttrs = K::kMaps;
+  e = cudaLaunchKernelEx(&cfg, chunk_bf16_kernel<K>, g, maps[0], maps[1]);
+  return e == cudaSuccess ? launch_chunk_join(p, s) : e;
+}
+
+}  // namespace
+
+cudaError_t launch_chunk_bf16(ChunkShape p, float *exchange, cudaStream_t s) {
+  const CacheLayer &c = p.a.cache;
+  Geometry g{};
+  p.tile = kKeys;
+  g.columns = (c.dim + 15) / 16 * 16;
+  g.chunks = (c.dim + 63) / 64;
+  g.panel_chunks = g.chunks < 2 ? g.chunks : 2;
+  g.exchange = exchange;
+  g.box_log = 0;
+  while ((2 << g.box_log) <= kKeys && c.page_size % (2 << g.box_log) == 0) ++g.box_log;
+  g.page_log = (c.page_size & (c.page_size - 1)) == 0 ? __builtin_ctz((unsigned)c.page_size) : -1;
+  g.p = p;
+  if (p.maps == 2) return g.columns <= 64 ? launch_kind<Kind<2, 1, 2>>(g, s) : launch_kind<Kind<1, 1, 2>>(g, s);
+  return g.columns <= 128 ? launch_kind<Kind<2, 1, 1>>(g, s) : launch_kind<Kind<1, 2, 1>>(g, s);
+}
+
+}  // namespace last

@@ -1,4 +1,4 @@
-// Chunk and differential attention on the CUDA cores.
+// Chunk and differential attention over fp32 keys and values: the products on the CUDA cores.
 //
 // A CTA holds a block of 64 rows and passes its keys in tiles of 64: S = Q K^T with 4 x 4 results a thread, a running maximum
 // and sum per row (kept by the 16 threads that share it), O = O + P V with 4 rows x 4 columns a thread and
@@ -18,20 +18,9 @@ struct alignas(16) SimtShared {
   unsigned flags;
 };
 
-__device__ __forceinline__ void simt_store(float *to, float4 v) { *reinterpret_cast<float4 *>(to) = v; }
-__device__ __forceinline__ void simt_store(__nv_bfloat16 *to, float4 v) {
-  __nv_bfloat162 x[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
-  *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<uint2 *>(x);
-}
-__device__ __forceinline__ float4 simt_load(const float *p) { return *reinterpret_cast<const float4 *>(p); }
-__device__ __forceinline__ float4 simt_load(const __nv_bfloat16 *p) {
-  const uint2 u = *reinterpret_cast<const uint2 *>(p);
-  return make_float4(bf16lo(u.x), bf16hi(u.x), bf16lo(u.y), bf16hi(u.y));
-}
-
 // NC: 64-column blocks of a value.
-template <typename T, int NC>
-__global__ void __launch_bounds__(kSimtThreads) chunk_simt_kernel(const __grid_constant__ ChunkShape p) {
+template <int NC>
+__global__ void __launch_bounds__(kSimtThreads) chunk_f32_kernel(const __grid_constant__ ChunkShape p) {
   extern __shared__ float4 smem4[];
   const ChunkArgs &a = p.a;
   const int D = a.cache.dim, ld = D + kPad, ldv = p.dv + kPad, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
@@ -55,8 +44,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_kernel(const __grid_c
         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (r < it.rows) {
           const int t = (it.r0 + r) / p.group, h = it.unit * p.group + (it.r0 + r) - t * p.group;
-          x = simt_load(reinterpret_cast<const T *>(a.q + (long long)(it.s.first + t) * a.q_stride) +
-                        (long long)(p.maps == 2 ? 2 * h + map : h) * D + d);
+          x = *reinterpret_cast<const float4 *>(a.q + (long long)(it.s.first + t) * a.q_stride + ((long long)(p.maps == 2 ? 2 * h + map : h) * D + d) * 4);
         }
         *reinterpret_cast<float4 *>(qs + r * ld + d) = x;
       }
@@ -91,7 +79,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_kernel(const __grid_c
               if ((unsigned)page < (unsigned)c.num_pages) {
                 const int head = is_v ? it.unit * p.maps + d / D : it.unit * p.maps + map;
                 const char *row = (is_v ? c.v : c.k) + page * c.page_stride + head * c.head_stride + key % c.page_size * c.token_stride;
-                x = simt_load(reinterpret_cast<const T *>(row) + (is_v ? d % D : d));
+                x = *reinterpret_cast<const float4 *>(row + (is_v ? d % D : d) * 4);
               } else {
                 skipped = kErrCacheIndex;
               }
@@ -246,10 +234,10 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_kernel(const __grid_c
       }
       if (!live) continue;
       if (p.maps == 1 && a.lse != nullptr && tx == 0) a.lse[(long long)(it.s.first + t) * a.q_heads + h] = chunk_lse(m[i], l[i]);
-      T *out = reinterpret_cast<T *>(a.out + (long long)(it.s.first + t) * a.out_stride) + (long long)h * p.dv;
+      float *out = reinterpret_cast<float *>(a.out + (long long)(it.s.first + t) * a.out_stride) + (long long)h * p.dv;
 #pragma unroll
       for (int j = 0; j < NC; ++j)
-        if (tx * 4 + 64 * j < p.dv) simt_store(out + tx * 4 + 64 * j, make_float4(o[i][j][0], o[i][j][1], o[i][j][2], o[i][j][3]));
+        if (tx * 4 + 64 * j < p.dv) *reinterpret_cast<float4 *>(out + tx * 4 + 64 * j) = make_float4(o[i][j][0], o[i][j][1], o[i][j][2], o[i][j][3]);
     }
   }
   __syncthreads();
@@ -259,8 +247,8 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_simt_kernel(const __grid_c
   }
 }
 
-template <typename T, int NC>
-cudaError_t launch_simt(ChunkShape p, cudaStream_t s) {
+template <int NC>
+cudaError_t launch_f32(ChunkShape p, cudaStream_t s) {
   const int D = p.a.cache.dim;
   const size_t smem = sizeof(SimtShared) + sizeof(float) * ((kSimtRows + kSimtKeys) * (D + kPad) + kSimtKeys * (p.dv + kPad) +
                                                              kSimtRows * (kSimtKeys + kPad) + (p.maps == 2 ? kSimtRows * (p.dv + kPad) : 0));
@@ -268,26 +256,21 @@ cudaError_t launch_simt(ChunkShape p, cudaStream_t s) {
   p.tile = kSimtKeys;
   int shares = sm_count() * (int)((227 << 10) / (smem + 1024));
   p.shares = shares < kMaxShares ? shares : kMaxShares;
-  cudaError_t e = allow_smem(reinterpret_cast<const void *>(&chunk_simt_kernel<T, NC>), smem);
+  cudaError_t e = allow_smem(reinterpret_cast<const void *>(&chunk_f32_kernel<NC>), smem);
   if (e != cudaSuccess) return e;
-  e = launch_early(chunk_simt_kernel<T, NC>, dim3(p.shares), kSimtThreads, smem, s, p);
+  e = launch_early(chunk_f32_kernel<NC>, dim3(p.shares), kSimtThreads, smem, s, p);
   return e == cudaSuccess ? launch_chunk_join(p, s) : e;
-}
-
-template <typename T>
-cudaError_t launch_columns(const ChunkShape &p, cudaStream_t s) {
-  switch ((p.dv + 63) / 64) {
-    case 1: return launch_simt<T, 1>(p, s);
-    case 2: return launch_simt<T, 2>(p, s);
-    case 3: return launch_simt<T, 3>(p, s);
-    default: return launch_simt<T, 4>(p, s);
-  }
 }
 
 }  // namespace
 
-cudaError_t launch_chunk_simt(ChunkShape p, cudaStream_t s) {
-  return p.a.elem == 4 ? launch_columns<float>(p, s) : launch_columns<__nv_bfloat16>(p, s);
+cudaError_t launch_chunk_f32(ChunkShape p, cudaStream_t s) {
+  switch ((p.dv + 63) / 64) {
+    case 1: return launch_f32<1>(p, s);
+    case 2: return launch_f32<2>(p, s);
+    case 3: return launch_f32<3>(p, s);
+    default: return launch_f32<4>(p, s);
+  }
 }
 
 }  // namespace last

@@ -33,13 +33,14 @@ struct ChunkShape {   // the same for every CTA
   float *parts;       // [shares][maps][2] parted sums: second one where an item begins in the share
 };
 
-constexpr int kMaxShares = 480;
+constexpr int kMaxShares = 480, kMaxTensorCtas = 160;   // fp32 and bf16
 constexpr int kMaxKeys = 0x7fffff00;   // of a sequence: the last key's tile ends before 2^31
 constexpr float kChunkLog2e = 1.4426950408889634f, kChunkLn2 = 0.6931471805599453f;
 // What an item costs beside its keys, in keys; parts of fewer tiles are not cut off.
 constexpr int kItemKeys = 128, kLeastTiles = 1;
 
-cudaError_t launch_chunk_simt(ChunkShape p, cudaStream_t s);
+cudaError_t launch_chunk_f32(ChunkShape p, cudaStream_t s);
+cudaError_t launch_chunk_bf16(ChunkShape p, float *exchange, cudaStream_t s);
 // Adds up what the cuts have parted.
 cudaError_t launch_chunk_join(const ChunkShape &p, cudaStream_t s);
 

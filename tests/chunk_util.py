@@ -61,10 +61,10 @@ def one_map(q, k, v, see, scale):
     return p @ v, lse, p @ v.abs(), ez
 
 
-def relative(ez, n, dtype):
-    """Of the weighted sums, times sum p |v|: the exponentials' and the sums' errors as for single tokens, and
-    for bf16 a weight rounded once, in numerator and denominator: 2 x 2^-8, a hundredth more for the square."""
-    return 4 * ez + 2.0 ** -20 + (n / 8 + 64) * 2.0 ** -24 + (2.02 * 2.0 ** -8 if dtype == "bfloat16" else 0.0)
+def relative(ez, n, dtype, parts=1):
+    """Of the weighted sums, times sum p |v|: the exponentials' and the sums' errors as for single tokens, and for bf16 a
+    weight rounded once (2^-8), or held in two parts (2^-16)."""
+    return 4 * ez + 2.0 ** -20 + (n / 8 + 64) * 2.0 ** -24 + (2.0 ** (-8 * parts) if dtype == "bfloat16" else 0.0)
 
 
 def keys_of(cache, table_row, lens, head, live=None):
@@ -97,8 +97,6 @@ def check_chunk(cache, seqs, q, cu_new, out, lse, new, lens, begin=None, causal=
             got, none = lse[t0:t0 + n, h].double(), ~see.any(1)
             assert (got[none] == -math.inf).all() and (out[t0:t0 + n, h][none] == 0).all()
             tol = 2 * ez + 2.0 ** -20 * (1 + want_lse.abs()) + (total / 8 + 64) * 2.0 ** -24
-            if dtype == "bfloat16":
-                tol = tol + 2.0 ** -8      # the sum is that of the rounded weights
             assert ((got - want_lse).abs() <= tol)[~none].all(), f"sequence {b}, head {h}: lse"
 
 
@@ -125,7 +123,7 @@ def check_diff(cache, seqs, q, cu_new, out, lam, new, lens, begin=None, causal=T
                 o, _, size, ez = one_map(q[t0:t0 + n, 2 * j + m], k, v, see, scale)
                 f = 1.0 if m == 0 else -float(lam[j])
                 x = x + f * o
-                e = e + abs(f) * relative(ez, total, dtype) * size
+                e = e + abs(f) * relative(ez, total, dtype, 2) * size
             e = e + 2.0 ** -22 * x.abs()
             if weight is None:
                 want, tol = x * out_scale, e * abs(out_scale)

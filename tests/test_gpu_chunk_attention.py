@@ -146,7 +146,7 @@ def test_single_tokens_without_cu_new(dtype):
     ch.check_chunk(cache, seqs, q, cu_new, b[0], b[1], [1] * 6, lens)
     one = torch.empty_like(q)
     last.last_cache_attention(cache, 0, seqs, q, one, cu.workspace(cache, 6, 8))
-    assert float((one.double() - b[0].double()).norm() / one.double().norm()) < 2 * 2.02 * ch.UNIT[dtype] + 2.0 ** -18
+    assert float((one.double() - b[0].double()).norm() / one.double().norm()) < 3 * ch.UNIT[dtype] + 2.0 ** -18
     lam, weight = _params(4, 64, 1)
     d1, d2 = _diff(cache, seqs, q, cu_new, lam, weight)[0], _diff(cache, seqs, q, None, lam, weight)[0]
     assert torch.equal(d1, d2)
@@ -184,30 +184,35 @@ def test_what_a_row_does_not_see_has_no_part(d, hkv, dtype):
     cache, seqs, q, cu_new = ch.setup(new, old, 4, hkv, d, dtype, 16, seed=4)
     want = _chunk(cache, seqs, q, cu_new)
     lam, weight = _params(2, d, 2)
-    diff = _diff(cache, seqs, q, cu_new, lam, weight)[0] if d <= 128 else None
+    at = {0: 150, 1: 130}                       # positions of the keys that are not finite
+    early, total = [p - o for p, o in zip(at.values(), old)], list(at.values())
     for what in ("k", "v"):
         for x in (float("nan"), float("inf")):
             t = cache.k.clone(), cache.v.clone()
-            at = {0: 150, 1: 130}                       # positions of the keys that are not finite
             for b, p in at.items():
                 page = int(seqs.page_table[b, p // 16])
                 t["kv".index(what)][0, page, :, p % 16, 3] = x
             bad = last.Cache(*t)
             out, lse, _ = _chunk(bad, seqs, q, cu_new)
-            for b, p in at.items():
-                t0, first = int(cu_new[b]), p - old[b]
-                assert torch.equal(out[t0:t0 + first], want[0][t0:t0 + first]), (what, x, b)
+            ch.check_chunk(cache, seqs, q, cu_new, out, lse, early, total)     # the rows before, over the keys before
+            for b in at:
+                t0, first = int(cu_new[b]), early[b]
                 assert torch.equal(lse[t0:t0 + first], want[1][t0:t0 + first])
                 late = out[t0 + first:t0 + new[b]]
                 if what == "v":
                     assert not torch.isfinite(late[..., 3]).any() and torch.isfinite(late[..., 4:]).all()
                 elif x != x:
                     assert late.isnan().all()
-            if diff is not None:
-                got, _ = _diff(bad, seqs, q, cu_new, lam, weight)
-                for b, p in at.items():
-                    t0, first = int(cu_new[b]), p - old[b]
-                    assert torch.equal(got[t0:t0 + first], diff[t0:t0 + first]), (what, x, b)
+            if d > 128:
+                continue
+            got, _ = _diff(bad, seqs, q, cu_new, lam, weight)
+            ch.check_diff(cache, seqs, q, cu_new, got, lam, early, total, weight=weight)
+            plain, _ = _diff(bad, seqs, q, cu_new, lam)
+            ch.check_diff(cache, seqs, q, cu_new, plain, lam, early, total)
+            if what == "v":
+                for b in at:
+                    late = plain[int(cu_new[b]) + early[b]:int(cu_new[b]) + new[b]]
+                    assert not torch.isfinite(late[..., 3]).any() and torch.isfinite(late[..., 4:d]).all()
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
