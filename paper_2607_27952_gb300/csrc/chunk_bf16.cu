@@ -45,19 +45,22 @@ struct Item {
   int whole, second;
 };
 
-struct alignas(16) Shared {   // with 1 KB to align the panels by, 3 KB: 7 panels of 32 KB stand beside it
+constexpr size_t kHead = 3072;   // shared memory before the panels, of which seven of 32 KB stand beside it
+
+struct alignas(16) Shared {
   unsigned long long full[kRingMax], empty[kRingMax], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2];
   unsigned long long item_full[kItems], item_empty[kItems], x_full, x_empty, never;
   Item items[kItems];
   float row[2][128];      // a row's value of one half of the columns for the other
   ChunkShare share;
   unsigned long long sums[kThreads / 32];
+  int2 boxes[16];             // of the key tile being fetched: first token, page
   unsigned skip[kTileInfo];   // of the key tiles on their way: groups of 8 keys whose page is out of range
   uint32_t tmem;
   unsigned flags;
   volatile unsigned dead;
 };
-static_assert(sizeof(Shared) <= 2048, "no room beside seven panels");
+static_assert(sizeof(Shared) <= kHead, "the panels begin behind it");
 
 // A whole warp waits, with a limit; the first to give up has every other wait of the CTA end too.  The softmax warps go on
 // after a wait that gave up, with whatever is there, to the end of their item, so that no barrier of theirs waits for a warp
@@ -165,11 +168,6 @@ __device__ __forceinline__ bool elected() {
   return r != 0;
 }
 
-__device__ __forceinline__ int elected_lane() {
-  uint32_t r;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync %0|p, 0xffffffff;\n\t}" : "=r"(r));
-  return (int)r;
-}
 __device__ __forceinline__ void tma_box(uint32_t dst, const void *map, int x, int y, int z, int w, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
@@ -185,8 +183,7 @@ __device__ __forceinline__ bool pair_any(int pair, bool x) {
   return r != 0;
 }
 
-// Steps go key tile by key tile, in each row tile by row tile, and are counted over all items.
-__device__ __forceinline__ bool active(const Item &it, int j, int t) { return j >= it.ta[t] && j < it.tb[t]; }
+// Steps go key tile by key tile, in each row tile by row tile (those with keys ta .. tb - 1), and are counted over all items.
 
 // A place in the ring and whether its panel is of an even or odd round.
 struct Place {
@@ -218,7 +215,7 @@ struct MapHead {
 
 // ---- warps 10 and 11: items and rows of Q ----
 template <typename K>
-__device__ void query_role(const Geometry &g, Shared &sm, char *qs, int rank) {
+__device__ __forceinline__ void query_role(const Geometry &g, Shared &sm, char *qs, int rank) {
   const ChunkShape &p = g.p;
   const int lane = threadIdx.x & 31, half = (threadIdx.x >> 5) - kQueryWarp, D = p.a.cache.dim;
   ChunkWalk walk(sm.share);
@@ -227,9 +224,14 @@ __device__ void query_role(const Geometry &g, Shared &sm, char *qs, int rank) {
   const int eights = g.chunks * 8;   // 16-byte pieces of a row, zeros past D
   for (bool more = true; more; ++n) {
     more = walk.next(p, &it);
-    Item o;
-    o.seq = more ? it.seq : -1;
-    if (more) {
+    const int e = n % kItems;
+    if (half == 0 && n >= kItems && !wait(sm, &sm.item_empty[e], (n / kItems & 1) ^ 1)) return;
+    Item &o = sm.items[e];
+    const bool writes = half == 0 && lane == 0, some = more && it.t.count > 0;
+    const int ka = some ? it.t.first + it.k0 : 0, kb = some ? it.t.first + it.k1 : 0;
+    unsigned used = 0;   // row tiles with a step
+    if (writes) {
+      o.seq = more ? it.seq : -1;
       o.unit = it.unit;
       o.first = it.s.first;
       o.r0 = it.r0;
@@ -237,46 +239,45 @@ __device__ void query_role(const Geometry &g, Shared &sm, char *qs, int rank) {
       o.base = it.s.base;
       o.begin = it.s.begin;
       o.lens = it.s.lens;
-      const bool some = it.t.count > 0;
-      o.ka = some ? it.t.first + it.k0 : 0;
-      o.kb = some ? it.t.first + it.k1 : 0;
+      o.ka = ka;
+      o.kb = kb;
       o.lo = it.t.lo;
       o.hi = it.t.hi;
       o.whole = it.whole;
       o.second = it.second;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        o.ta[t] = o.tb[t] = o.tlo[t] = o.thi[t] = 0;
-        if (!some || t * 128 >= it.rows) continue;
-        const ChunkTiles x = chunk_tiles(p, it.s, it.r0 + t * 128, it.r0 + min(it.rows, t * 128 + 128));
-        o.ta[t] = max(o.ka, x.first);
-        o.tb[t] = min(o.kb, x.first + x.count);
+    }
+#pragma unroll 1
+    for (int t = 0; t < 2; ++t) {
+      ChunkTiles x{0, 0, 0, 0};
+      int ta = 0, tb = 0;
+      if (some && t * 128 < it.rows) {
+        x = chunk_tiles(p, it.s, it.r0 + t * 128, it.r0 + min(it.rows, t * 128 + 128));
+        ta = max(ka, x.first);
+        tb = min(kb, x.first + x.count);
+      }
+      used |= (unsigned)(ta < tb) << t;
+      if (writes) {
+        o.ta[t] = ta;
+        o.tb[t] = tb;
         o.tlo[t] = x.lo;
         o.thi[t] = x.hi;
       }
     }
-    if (half == 0) {
-      const int e = n % kItems;
-      if (n >= kItems && !wait(sm, &sm.item_empty[e], (n / kItems & 1) ^ 1)) return;
-      if (lane == 0) {
-        sm.items[e] = o;
-        mbar_arrive(&sm.item_full[e]);
-      }
-      __syncwarp();
-    }
+    if (writes) mbar_arrive(&sm.item_full[e]);
+    __syncwarp();
     if (!more) return;
-#pragma unroll
+#pragma unroll 1
     for (int t = 0; t < K::kTiles; ++t) {
-      if (o.ta[t] >= o.tb[t]) continue;
+      if (!(used >> t & 1)) continue;
       const int slot = tile % K::kTiles;
       if (tile >= (uint32_t)K::kTiles && !wait(sm, &sm.q_empty[slot], (tile / K::kTiles & 1) ^ 1)) return;
       const uint32_t to = smem_addr(qs) + slot * g.chunks * kChunkBytes;
       // 32 / 8 rows at a time, 8 lanes to a row's 128 bytes
       for (int r = half * 64 + (lane >> 3); r < half * 64 + 64; r += 4) {
         const int row = t * 128 + r;
-        const bool live = row < o.rows;
-        const int tok = (o.r0 + (live ? row : 0)) / p.group, h = o.unit * p.group + (o.r0 + (live ? row : 0)) - tok * p.group;
-        const char *from = p.a.q + (long long)(o.first + tok) * p.a.q_stride + (long long)(MapHead<K>::of(h, rank)) * D * 2;
+        const bool live = row < it.rows;
+        const int at = it.r0 + (live ? row : 0), tok = at / p.group, h = it.unit * p.group + at - tok * p.group;
+        const char *from = p.a.q + (long long)(it.s.first + tok) * p.a.q_stride + (long long)(MapHead<K>::of(h, rank)) * D * 2;
         for (int c = lane & 7; c < eights; c += 8) {
           const uint32_t dst = to + (c >> 3) * kChunkBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4);
           const bool in = live && c * 8 < D;
@@ -296,7 +297,7 @@ __device__ void query_role(const Geometry &g, Shared &sm, char *qs, int rank) {
 // ---- warp 9: K and V ----
 // The lanes look the boxes' pages up, a tile ahead; one lane issues all boxes (25 cycles each; a lane per box took 75).
 template <typename K>
-__device__ void load_role(const Geometry &g, Shared &sm, char *ring, const CUtensorMap *kmap, const CUtensorMap *vmap, int rank) {
+__device__ __forceinline__ void load_role(const Geometry &g, Shared &sm, char *ring, const CUtensorMap *kmap, const CUtensorMap *vmap, int rank) {
   const ChunkShape &p = g.p;
   const int lane = threadIdx.x & 31, box = 1 << g.box_log, boxes = kKeys >> g.box_log;
   const int size = p.a.cache.page_size;
@@ -307,18 +308,18 @@ __device__ void load_role(const Geometry &g, Shared &sm, char *ring, const CUten
   for (uint32_t n = 0;; ++n) {
     const int e = n % kItems;
     if (!wait(sm, &sm.item_full[e], n / kItems & 1)) return;
-    const Item it = sm.items[e];
+    const int seq = sm.items[e].seq, unit = sm.items[e].unit, ka = sm.items[e].ka, kb = sm.items[e].kb, lo = sm.items[e].lo, hi = sm.items[e].hi;
     __syncwarp();
     if (lane == 0) mbar_arrive(&sm.item_empty[e]);
-    if (it.seq < 0) return;
-    const int32_t *table = p.a.seq.table + it.seq * p.a.seq.table_stride;
-    auto counts = [&](int j) { return lane < boxes && j < it.kb && j * kKeys + lane * box < it.hi && j * kKeys + lane * box > it.lo - box; };
+    if (seq < 0) return;
+    const int32_t *table = p.a.seq.table + seq * p.a.seq.table_stride;
+    auto counts = [&](int j) { return lane < boxes && j < kb && j * kKeys + lane * box < hi && j * kKeys + lane * box > lo - box; };
     auto lookup = [&](int j) {
       const int key = j * kKeys + lane * box;
       return counts(j) ? table[g.page_log >= 0 ? key >> g.page_log : key / size] : -1;
     };
-    int page = it.ka < it.kb ? lookup(it.ka) : -1;
-    for (int j = it.ka; j < it.kb; ++j, ++tile) {
+    int page = ka < kb ? lookup(ka) : -1;
+    for (int j = ka; j < kb; ++j, ++tile) {
       const int next_page = lookup(j + 1);
       const bool wanted = counts(j), here = wanted && (unsigned)page < (unsigned)p.a.cache.num_pages;
       unsigned skip = __ballot_sync(~0u, wanted && !here);
@@ -331,23 +332,32 @@ __device__ void load_role(const Geometry &g, Shared &sm, char *ring, const CUten
       }
       if (lane == 0) sm.skip[tile % kTileInfo] = skip;
       const int row = g.page_log >= 0 ? (j * kKeys + lane * box) & (size - 1) : (j * kKeys + lane * box) % size;
+      if (lane < boxes) sm.boxes[lane] = make_int2(row, page);
+      __syncwarp();
 #pragma unroll
       for (int i = 0; i < K::kPanels + K::kValues; ++i) {
         const int pi = i % K::kPanels, value = i / K::kPanels - 1;   // -1: K
         const int chunks = K::kPanels == 1 ? g.chunks : min(2, g.chunks - 2 * pi);
         if (again && !wait(sm, &sm.empty[at.slot], at.round ^ 1)) return;
         const uint32_t bar = smem_addr(&sm.full[at.slot]), panel = ring_at + at.slot * g.panel_chunks * kChunkBytes;
-        const int head = it.unit * K::kMaps + (value < 0 ? rank : value);
+        const int head = unit * K::kMaps + (value < 0 ? rank : value);
         const CUtensorMap *map = value < 0 ? kmap : vmap;
-        const int leader = elected_lane();
-        if (lane == leader) mbar_expect_tx(&sm.full[at.slot], __popc(there) * chunks * box * 128);
-        for (unsigned left = there; left != 0; left &= left - 1) {
-          const int b = __ffs(left) - 1, its_page = __shfl_sync(~0u, page, b), its_row = __shfl_sync(~0u, row, b);
-          if (elected())
-            for (int c = 0; c < chunks; ++c)
-              tma_box(panel + c * kChunkBytes + (b << (g.box_log + 7)), map, pi * 128 + c * 64, its_row, head, its_page, bar);
-          __syncwarp();
+        if (elected()) {
+          mbar_expect_tx(&sm.full[at.slot], __popc(there) * chunks * box * 128);
+          auto load = [&](int b) {
+            const int2 from = sm.boxes[b];
+            const uint32_t to = panel + (b << (g.box_log + 7));
+            tma_box(to, map, pi * 128, from.x, head, from.y, bar);
+            if (chunks == 2) tma_box(to + kChunkBytes, map, pi * 128 + 64, from.x, head, from.y, bar);
+          };
+          if (there == (1u << boxes) - 1) {
+#pragma unroll 4
+            for (int b = 0; b < boxes; ++b) load(b);
+          } else {
+            for (unsigned left = there; left != 0; left &= left - 1) load(__ffs(left) - 1);
+          }
         }
+        __syncwarp();
         const int before = at.slot;
         at.skip(g, 1);
         again |= at.slot < before;
@@ -358,13 +368,13 @@ __device__ void load_role(const Geometry &g, Shared &sm, char *ring, const CUten
 }
 
 // ---- warp 8: the products ----
-struct Step {   // whose P V is still to come
+struct Step {
   bool some, first, last;  // first of its row tile in the item, last of its key tile
   uint32_t s;
   int t, kmin, kmax;
   int zero_lo, zero_hi;    // rows of V that some row sees
   unsigned skip;
-  Place at;                // of V
+  Place at;                // of K, then of V
 };
 
 __device__ void zero_rows(uint32_t panel, int chunks, int from, int to) {
@@ -376,7 +386,6 @@ __device__ void zero_rows(uint32_t panel, int chunks, int from, int to) {
 template <typename K>
 __device__ __forceinline__ bool values(const Geometry &g, Shared &sm, uint32_t ring, Step &x, uint32_t tmem) {
   const int b = x.s & 1;
-  x.some = false;
   if (!wait(sm, &sm.p_full[b], x.s >> 1 & 1)) return false;
   tc_fence_after();
   const uint32_t pt = tmem + b * 128, o = tmem + kOutColumn + x.t * 128;
@@ -399,13 +408,13 @@ __device__ __forceinline__ bool values(const Geometry &g, Shared &sm, uint32_t r
       const uint32_t idesc = umma_idesc_bf16(128, n) | kNMajor, d = o + head * g.columns + pi * 128;
       const uint64_t v = desc_n_major(panel);
       if (k1 - k0 == 8) {
-        umma_bf16_ts(d, pt, v, idesc, x.first ? 0u : 1u);
 #pragma unroll
-        for (int k = 1; k < 8; ++k) umma_bf16_ts(d, pt + (k >> 2) * 64 + (k & 3) * 8, v + k * (2048 >> 4), idesc, 1u);
+        for (int k = 0; k < 8; ++k) umma_bf16_ts(d, pt + (k >> 2) * 64 + (k & 3) * 8, v + k * (2048 >> 4), idesc, k == 0 && x.first ? 0u : 1u);
         if (K::kParts == 2)
 #pragma unroll
           for (int k = 0; k < 8; ++k) umma_bf16_ts(d, pt + 32 + (k >> 2) * 64 + (k & 3) * 8, v + k * (2048 >> 4), idesc, 1u);
       } else {
+#pragma unroll 1
         for (int k = k0; k < k1; ++k)
 #pragma unroll
           for (int e = 0; e < K::kParts; ++e)
@@ -420,44 +429,51 @@ __device__ __forceinline__ bool values(const Geometry &g, Shared &sm, uint32_t r
   return true;
 }
 
+// The next step's S before this one's O; but what the next step still waits for (its item, its rows of Q) does not keep
+// this one back.
 template <typename K>
-__device__ void product_role(const Geometry &g, Shared &sm, char *qs_, char *ring_, uint32_t tmem) {
+__device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char *qs_, char *ring_, uint32_t tmem) {
   const int lane = threadIdx.x & 31, D = g.p.a.cache.dim;
   const uint32_t qs = smem_addr(qs_), ring = smem_addr(ring_);
-  uint32_t s = 0, tile = 0, q_tile = 0;
+  uint32_t s = 0, tile = 0, n = 0, q_at[2] = {0, 0}, q_tile = 0;
+  int j = 0, kb = 0, t = 0;                 // the next step: key tile, row tile
+  bool open = false, done = false;          // within item n; no item is left
   Place at{0, 0};
   Step behind;
   behind.some = false;
-  for (uint32_t n = 0;; ++n) {
-    const int e = n % kItems;
-    // what waits for the next item must not keep the last P V back
-    if (behind.some && !passed(&sm.item_full[e], n / kItems & 1) && !values<K>(g, sm, ring, behind, tmem)) return;
-    if (!wait(sm, &sm.item_full[e], n / kItems & 1)) return;
-    const Item it = sm.items[e];
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sm.item_empty[e]);
-    if (it.seq < 0) break;
-    uint32_t q_at[2] = {q_tile, q_tile + (it.ta[0] < it.tb[0])};
-    for (int j = it.ka; j < it.kb; ++j, ++tile) {
-      const int last_tile = active(it, j, 1) ? 1 : active(it, j, 0) ? 0 : -1;
-      const int key0 = j * kKeys;
-#pragma unroll
-      for (int t = 0; t < K::kTiles; ++t) {
-        if (!active(it, j, t)) continue;
-        const int q = q_at[t] % K::kTiles;
-        const uint32_t q_phase = q_at[t] / K::kTiles & 1;
-        if (j == it.ta[t]) {
-          if (behind.some && !passed(&sm.q_full[q], q_phase) && !values<K>(g, sm, ring, behind, tmem)) return;
-          if (!wait(sm, &sm.q_full[q], q_phase)) return;
-        }
-        Step x;
-        x.some = true;
+  while (!done || behind.some) {
+    Step x;
+    x.some = false;
+    const Item &it = sm.items[n % kItems];
+    if (!done && !open && (!behind.some || passed(&sm.item_full[n % kItems], n / kItems & 1))) {
+      if (!wait(sm, &sm.item_full[n % kItems], n / kItems & 1)) return;
+      open = true;
+      done = it.seq < 0;
+      j = it.ka;
+      kb = it.kb;
+      t = 0;
+      q_at[0] = q_tile;
+      q_tile += it.ta[0] < it.tb[0];
+      q_at[1] = q_tile;
+      q_tile += it.ta[1] < it.tb[1];
+    }
+    if (open && !done && j < kb) {
+      const bool on0 = j >= it.ta[0] && j < it.tb[0], on1 = j >= it.ta[1] && j < it.tb[1];
+      if (t == 0 && !on0) t = 1;
+      const bool on = t == 0 || on1;   // else nobody's keys: passed on as they came
+      const uint32_t q_turn = t == 0 ? q_at[0] : q_at[1];
+      const int q = q_turn % K::kTiles;
+      const uint32_t q_phase = q_turn / K::kTiles & 1;
+      x.first = on && j == it.ta[t];
+      if (!x.first || !behind.some || passed(&sm.q_full[q], q_phase)) {
+        if (x.first && !wait(sm, &sm.q_full[q], q_phase)) return;
+        const int key0 = j * kKeys;
+        x.some = on;
         x.s = s;
         x.t = t;
         x.kmin = max(0, it.tlo[t] - key0);
         x.kmax = min(kKeys, it.thi[t] - key0);
-        x.first = j == it.ta[t];
-        x.last = t == last_tile;
+        x.last = t == 1 || !on1;
         x.zero_lo = max(0, it.lo - key0);
         x.zero_hi = min(kKeys, it.hi - key0);
         x.at = at;
@@ -466,21 +482,24 @@ __device__ void product_role(const Geometry &g, Shared &sm, char *qs_, char *rin
         for (int pi = 0; pi < K::kPanels; ++pi) {
           if (!wait(sm, &sm.full[x.at.slot], x.at.round)) return;
           if (elected()) {
-            const uint64_t k_rows = umma_desc_sw128(ring + x.at.slot * g.panel_chunks * kChunkBytes);
-            const uint64_t q_rows = umma_desc_sw128(qs + (q * g.chunks + 2 * pi) * kChunkBytes);
-            const int steps = (D - pi * 128 + 15) / 16;
-            auto product = [&](int k) {
-              const int off = ((k >> 2) * (int)kChunkBytes + (k & 3) * 32) >> 4;
-              umma_bf16(d, q_rows + off, k_rows + off, idesc, (pi | k) != 0 ? 1u : 0u);
-            };
-            if (steps >= 8) {
+            if (on) {
+              const uint64_t k_rows = umma_desc_sw128(ring + x.at.slot * g.panel_chunks * kChunkBytes);
+              const uint64_t q_rows = umma_desc_sw128(qs + (q * g.chunks + 2 * pi) * kChunkBytes);
+              const int steps = (D - pi * 128 + 15) / 16;
+              auto product = [&](int k) {
+                const int off = ((k >> 2) * (int)kChunkBytes + (k & 3) * 32) >> 4;
+                umma_bf16(d, q_rows + off, k_rows + off, idesc, (pi | k) != 0 ? 1u : 0u);
+              };
+              if (steps >= 8) {
 #pragma unroll
-              for (int k = 0; k < 8; ++k) product(k);
-            } else {
-              for (int k = 0; k < steps; ++k) product(k);
+                for (int k = 0; k < 8; ++k) product(k);
+              } else {
+#pragma unroll 1
+                for (int k = 0; k < steps; ++k) product(k);
+              }
             }
             if (x.last) umma_commit(&sm.empty[x.at.slot]);
-            if (pi == K::kPanels - 1) {
+            if (on && pi == K::kPanels - 1) {
               umma_commit(&sm.s_full[s & 1]);
               if (j + 1 == it.tb[t]) umma_commit(&sm.q_empty[q]);
             }
@@ -488,24 +507,33 @@ __device__ void product_role(const Geometry &g, Shared &sm, char *qs_, char *rin
           __syncwarp();
           x.at.skip(g, 1);
         }
-        x.skip = sm.skip[tile % kTileInfo];
-        if (behind.some && !values<K>(g, sm, ring, behind, tmem)) return;
-        behind = x;
-        ++s;
-      }
-      if (last_tile < 0) {   // nobody's keys: passed on as they came
-        Place x = at;
-        for (int i = 0; i < K::kPanels + K::kValues; ++i) {
-          if (!wait(sm, &sm.full[x.slot], x.round)) return;
-          if (lane == 0) mbar_arrive(&sm.empty[x.slot]);
-          x.skip(g, 1);
+        x.skip = sm.skip[tile % kTileInfo];   // written before K's panels arrived
+        s += on;
+        if (!on)
+          for (int i = 0; i < K::kValues; ++i) {
+            if (!wait(sm, &sm.full[x.at.slot], x.at.round)) return;
+            if (lane == 0) mbar_arrive(&sm.empty[x.at.slot]);
+            x.at.skip(g, 1);
+          }
+        if (x.last) {
+          at.skip(g, K::kPanels + K::kValues);
+          ++tile;
+          ++j;
+          t = 0;
+        } else {
+          t = 1;
         }
       }
-      at.skip(g, K::kPanels + K::kValues);
     }
-    q_tile += (it.ta[0] < it.tb[0]) + (it.ta[1] < it.tb[1]);
+    if (open && !done && j >= kb) {   // every lane has read what it needs of the item
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm.item_empty[n % kItems]);
+      ++n;
+      open = false;
+    }
+    if (behind.some && !values<K>(g, sm, ring, behind, tmem)) return;
+    behind = x;
   }
-  if (behind.some) values<K>(g, sm, ring, behind, tmem);
 }
 
 // ---- warps 0 to 7 ----
@@ -516,21 +544,30 @@ struct Rows {      // what a thread keeps of a row tile
   uint32_t last;   // its last step
 };
 
-// Weights of the warp's 32 rows and 64 of the step's keys.  from, to: columns of these that the row sees.
-template <typename K, bool MASKED>
+// Weights of the warp's 32 rows and 64 of the step's keys.  from, to: columns of these that the row sees.  There is one
+// copy of this code for all row tiles and masks: with four of them the instruction cache missed all the time.
+template <typename K>
 __device__ __forceinline__ void weights(const Geometry &g, Shared &sm, Rows &r, uint32_t s, uint32_t tmem, int t, int chunk0, int chunk1,
                                         int from, int to, unsigned skip) {
+  const bool masked = __any_sync(~0u, from > 0 || to < 64) || skip != 0;
   const int pair = (threadIdx.x >> 5) & 3, half = (threadIdx.x >> 5) >> 2, row = pair * 32 + (threadIdx.x & 31);
   const uint32_t lanes = (uint32_t)(pair * 32) << 16, st = tmem + lanes + (s & 1) * 128 + half * 64;
   uint32_t v[64];
   tmem_ld32(st, v);
   tmem_ld32(st + 32, v + 32);
   tmem_wait_ld();
-  if (MASKED) {
+  if (masked) {
 #pragma unroll
-    for (int i = 0; i < 64; ++i) {
-      const bool sees = i >= from && i < to && !(skip >> (half * 8 + i / 8) & 1);
-      if (!sees) v[i] = __float_as_uint(-INFINITY);
+    for (int q = 0; q < 2; ++q) {
+      const int a = min(32, max(0, from - 32 * q)), b = min(32, max(0, to - 32 * q));
+      unsigned sees = (b == 32 ? ~0u : (1u << b) - 1) & (a == 32 ? 0u : ~0u << a);
+      if (skip != 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (skip >> (half * 8 + q * 4 + i) & 1) sees &= ~(0xffu << (8 * i));
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (!(sees & (1u << i))) v[32 * q + i] = __float_as_uint(-INFINITY);
     }
   }
   float top[4];
@@ -588,17 +625,16 @@ __device__ __forceinline__ void weights(const Geometry &g, Shared &sm, Rows &r, 
 
 // Column `lane` of the 32 from col on of a row of O once more, on the CUDA cores, for rows where the sums are not finite though
 // their weights are: a weight of zero times an infinity or NaN in a row of V that the row does not see leaves a NaN.  Here
-// such keys are passed over.  The row sees keys lo .. hi - 1 of the item's share; m: its maximum.
+// such keys are passed over.  The row sees keys begin .. end - 1 of the item's share; m: its maximum.
 template <typename K>
-__device__ __noinline__ float careful(const Geometry &g, const Item &it, int lo, int hi, float m, const char *q, int k_head, int v_head, int col) {
+__device__ __noinline__ float careful(const Geometry &g, int seq, int begin, int end, float m, const char *q, int k_head, int v_head, int col) {
   const ChunkShape &p = g.p;
   const CacheLayer &c = p.a.cache;
   const int lane = threadIdx.x & 31, D = c.dim;
-  const int begin = max(lo, it.ka * kKeys), end = (int)min((long long)hi, (long long)it.kb * kKeys);
   float acc = 0.0f;
   for (int k0 = begin; k0 < end; k0 += 32) {
     const int key = k0 + min(lane, end - 1 - k0);
-    const int page = p.a.seq.table[it.seq * p.a.seq.table_stride + key / c.page_size];
+    const int page = p.a.seq.table[seq * p.a.seq.table_stride + key / c.page_size];
     const bool sees = lane < end - k0 && (unsigned)page < (unsigned)c.num_pages;
     const long long at = sees ? page * c.page_stride + key % c.page_size * c.token_stride : 0;
     float z = 0.0f;
@@ -628,161 +664,192 @@ struct RowEnd {
   bool live, started;
 };
 
-// O of a warp's rows and its half of the columns: 16-column chunks chunk0 .. chunk1 - 1, `per` to a head, two of one head
-// at a time where there are two.
+// O of a warp's rows and its half of the columns: 16-column chunks chunk0 .. chunk1 - 1, for diff one of the value's two heads.
+// Blocks of 32 columns are loaded, groups of 64 stored.
 template <typename K>
 struct Out {
   const Geometry &g;
   const Item &it;
   const RowEnd &r;
-  int rank, t, per, chunk0, chunk1, D;
+  int rank, t, half, chunk0, chunk1, skipped;   // skipped: chunks of the value's heads before
   uint32_t tmem;
-  __device__ Out(const Geometry &g, const Item &it, const RowEnd &r, int rank, int t, uint32_t tmem)
-      : g(g), it(it), r(r), rank(rank), t(t), per(g.columns / 16), D(g.p.a.cache.dim), tmem(tmem) {
-    const int half = threadIdx.x >> 7, all = per * K::kMaps;
+  __device__ __forceinline__ Out(const Geometry &g, const Item &it, const RowEnd &r, int rank, int t, uint32_t tmem)
+      : g(g), it(it), r(r), rank(rank), t(t), half(threadIdx.x >> 7), tmem(tmem) {
+    const int per = g.columns / 16, all = per * K::kMaps;
     chunk0 = half ? (all + 1) / 2 : 0;
     chunk1 = half ? all : (all + 1) / 2;
+    skipped = K::kMaps == 2 && half ? per : 0;
   }
-  __device__ __forceinline__ int head(int c) const { return K::kMaps == 2 && c >= per ? 1 : 0; }
-  __device__ __forceinline__ int col(int c) const { return (c - (head(c) ? per : 0)) * 16; }   // of its head
-  __device__ __forceinline__ int column(int c) const { return head(c) * D + col(c); }          // of the value
-  __device__ __forceinline__ bool two(int c) const { return c + 1 < chunk1 && (K::kMaps == 1 || c + 1 != per); }
-  __device__ __forceinline__ int next(int c) const { return c + (two(c) ? 2 : 1); }
-  __device__ __forceinline__ int width(int c) const { return min(two(c) ? 32 : 16, D - col(c)); }
+  __device__ __forceinline__ int head() const { return K::kMaps == 2 ? half : 0; }
+  __device__ __forceinline__ int col(int c) const { return (c - skipped) * 16; }                 // of its head
+  __device__ __forceinline__ int column(int c) const { return head() * g.p.a.cache.dim + col(c); }   // of the value
+  __device__ __forceinline__ bool two(int c) const { return c + 1 < chunk1; }
+  __device__ __forceinline__ int width(int c) const { return min(two(c) ? 32 : 16, g.p.a.cache.dim - col(c)); }
   __device__ __forceinline__ void load(int c, float (&x)[32]) const {
     const int lane = threadIdx.x & 31;
     const uint32_t at = tmem + ((threadIdx.x >> 5 & 3) << 21) + kOutColumn + t * 128 + c * 16;
     uint32_t o[32];
+#pragma unroll 1
+    for (bool once_more = false;; once_more = true) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) o[i] = 0;
-    if (r.started) {
-      if (two(c)) {
-        tmem_ld32(at, o);
-        tmem_wait_ld();
-      } else {
-        tmem_ld16(at, o);
+      for (int i = 0; i < 32; ++i) o[i] = 0;
+      if (r.started) {
+        if (two(c)) {
+          tmem_ld32(at, o);
+          tmem_wait_ld();
+        } else {
+          tmem_ld16(at, o);
+        }
       }
-    }
-    float zero = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      x[i] = __uint_as_float(o[i]);
-      zero = fmaf(x[i], 0.0f, zero);
-    }
-    // zero is NaN where some column is not finite
-    for (unsigned odd = __ballot_sync(~0u, r.live && zero != 0.0f && r.sum < INFINITY); odd != 0; odd &= odd - 1) {
-      const int who = __ffs(odd) - 1;
-      const char *q = g.p.a.q + (long long)(it.first + r.tok) * g.p.a.q_stride + (long long)MapHead<K>::of(r.head, rank) * D * 2;
-      const float again = careful<K>(g, it, __shfl_sync(~0u, r.lo, who), __shfl_sync(~0u, r.hi, who), __shfl_sync(~0u, r.m, who),
-                                     reinterpret_cast<const char *>(shfl_u64(reinterpret_cast<unsigned long long>(q), who)),
-                                     it.unit * K::kMaps + rank, it.unit * K::kMaps + head(c), col(c));
+      float zero = 0.0f;   // NaN where some column is not finite
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
-        const float y = __shfl_sync(~0u, again, i);
-        if (lane == who && (i < 16 || two(c))) x[i] = y;
+        x[i] = __uint_as_float(o[i]);
+        zero = fmaf(x[i], 0.0f, zero);
+      }
+      unsigned odd = __ballot_sync(~0u, r.live && zero != 0.0f && r.sum < INFINITY);
+      if (odd == 0 || once_more) break;
+#pragma unroll 1
+      for (; odd != 0; odd &= odd - 1) {
+        const int who = __ffs(odd) - 1;
+        const char *q = g.p.a.q + (long long)(it.first + r.tok) * g.p.a.q_stride + (long long)MapHead<K>::of(r.head, rank) * g.p.a.cache.dim * 2;
+        const float again = careful<K>(g, it.seq, max(it.ka * kKeys, __shfl_sync(~0u, r.lo, who)),
+                                       (int)min((long long)it.kb * kKeys, (long long)__shfl_sync(~0u, r.hi, who)), __shfl_sync(~0u, r.m, who),
+                                       reinterpret_cast<const char *>(shfl_u64(reinterpret_cast<unsigned long long>(q), who)),
+                                       it.unit * K::kMaps + rank, it.unit * K::kMaps + head(), col(c));
+#pragma unroll 1
+        for (int i = 0; i < (two(c) ? 32 : 16); ++i) {   // the row's columns change in TMEM
+          uint32_t y;
+          tmem_ld1(at + i, &y);
+          tmem_wait_ld();
+          const float z = __shfl_sync(~0u, again, i);
+          if (lane == who) y = __float_as_uint(z);
+          asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" :: "r"(at + i), "r"(y) : "memory");
+          tmem_wait_st();
+        }
       }
     }
   }
+  // 32 columns, from chunk c on, of every lane's row.  Pieces of 16 bytes change places among 4 lanes, so that these write 64 bytes
+  // of one row: a lane per row would touch 32 lines with every store.
   __device__ __forceinline__ void store(int c, const float (&x)[32]) const {
-    char *out = g.p.a.out + (long long)(it.first + r.tok) * g.p.a.out_stride + ((long long)r.head * g.p.dv + column(c)) * 2;
-    if (!r.live) return;
+    const int lane = threadIdx.x & 31;
+    uint32_t w[16];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (8 * i < width(c))
-        *reinterpret_cast<uint4 *>(out + i * 16) =
-            make_uint4(pack_bf16(x[8 * i], x[8 * i + 1]), pack_bf16(x[8 * i + 2], x[8 * i + 3]), pack_bf16(x[8 * i + 4], x[8 * i + 5]),
-                       pack_bf16(x[8 * i + 6], x[8 * i + 7]));
+    for (int i = 0; i < 16; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+#pragma unroll
+    for (int b = 2; b > 0; b >>= 1) {
+      const bool up = lane & b;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (q & b) continue;   // pieces q and q + b: the one that is not this lane's goes
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t &low = w[4 * q + i], &high = w[4 * (q + b) + i];
+          const uint32_t got = __shfl_xor_sync(~0u, up ? low : high, b);
+          if (up) low = got;
+          else high = got;
+        }
+      }
+    }
+    // piece q is now piece lane % 4 of the row of lane (lane & 28) + q
+    const int mine = (lane & 3) * 8;
+    const bool in = mine < width(c);
+    const long long at = r.live ? (long long)(it.first + r.tok) * g.p.a.out_stride + (long long)r.head * g.p.dv * 2 : -1;
+    char *out = g.p.a.out + (column(c) + mine) * 2;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const long long to = (long long)shfl_u64((unsigned long long)at, (lane & 28) + q);
+      if (to >= 0 && in) *reinterpret_cast<uint4 *>(out + to) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+    }
   }
 };
 
 // To the output where the share has the whole item (diff: rows that the other CTA finishes to it), else to the workspace.
 template <typename K>
-__device__ __noinline__ void finish(const Geometry &g, const Item &it, const RowEnd &r, int rank, int t, uint32_t tmem, bool sends, float *own) {
+__device__ __forceinline__ void finish(const Geometry &g, const Item &it, const RowEnd &r, int rank, int t, uint32_t tmem, bool sends, float *own) {
   const ChunkShape &p = g.p;
   const Out<K> o(g, it, r, rank, t, tmem);
-  const int half = threadIdx.x >> 7, row = threadIdx.x & 127, all = o.per * K::kMaps;
-  const float inv = r.sum == 0.0f ? 0.0f : 1.0f / r.sum;
-  float x[32];
+  const int row = threadIdx.x & 127, all = g.columns / 16 * K::kMaps;
+  const bool none = it.whole && r.sum == 0.0f;
+  const float f = it.whole && !none ? 1.0f / r.sum : 1.0f;
+  if (it.whole && K::kMaps == 2 && !sends) return;
+  // a quarter of a part's or half's columns' rows lie side by side
+  float4 *to = reinterpret_cast<float4 *>(own) + (long long)t * all * 256 + (row & 63);
+  int stride = 64;
   if (!it.whole) {
     float *slot = chunk_slot(p, blockIdx.x / K::kMaps, rank, it.second);
     const int br = t * 128 + row;
-    if (r.live && half == 0) {
+    if (r.live && o.half == 0) {
       slot[br] = r.m;
       slot[p.block + br] = r.sum;
     }
-#pragma unroll 1
-    for (int c = o.chunk0; c < o.chunk1; c = o.next(c)) {
-      o.load(c, x);
-      float4 *to = reinterpret_cast<float4 *>(slot + 2 * p.block) + (long long)(o.column(c) / 4) * p.block + br;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (r.live && i * 4 < o.width(c)) to[(long long)i * p.block] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-    }
-    return;
-  }
-  if (K::kMaps == 1 && r.live && half == 0 && p.a.lse != nullptr)
+    to = reinterpret_cast<float4 *>(slot + 2 * p.block) + br;
+    stride = p.block;
+  } else if (K::kMaps == 1 && r.live && o.half == 0 && p.a.lse != nullptr) {
     p.a.lse[(long long)(it.first + r.tok) * p.a.q_heads + r.head] = chunk_lse(r.m, r.sum);
-  if (K::kMaps == 2 && !sends) return;
+  }
 #pragma unroll 1
-  for (int c = o.chunk0; c < o.chunk1; c = o.next(c)) {
+  for (int c = o.chunk0; c < o.chunk1; c += 2) {
+    float x[32];
     o.load(c, x);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) x[i] = r.sum == 0.0f ? 0.0f : x[i] * inv;
-    if (K::kMaps == 1) {
+    for (int i = 0; i < 32; ++i) x[i] = none ? 0.0f : x[i] * f;
+    if (K::kMaps == 1 && it.whole) {
       o.store(c, x);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < 4 || o.two(c)) reinterpret_cast<float4 *>(own)[((t * all + c) * 4 + i) * 64 + (row & 63)] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+      continue;
     }
+    float4 *at = to + (long long)(it.whole ? c * 4 : o.column(c) / 4) * stride;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (r.live && i * 4 < o.width(c)) at[(long long)i * stride] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
   }
 }
 
 // diff: the rows that this CTA finishes, with the other's half of the difference.
 template <typename K>
-__device__ __noinline__ void finish_difference(const Geometry &g, Shared &sm, const Item &it, const RowEnd &r, int rank, int t, uint32_t tmem, const float4 *theirs) {
+__device__ __forceinline__ void finish_difference(const Geometry &g, Shared &sm, const Item &it, const RowEnd &r, int rank, int t, uint32_t tmem, const float4 *theirs) {
   const ChunkShape &p = g.p;
   const Out<K> o(g, it, r, rank, t, tmem);
-  const int half = threadIdx.x >> 7, row = threadIdx.x & 127, pair = row >> 5, all = o.per * K::kMaps;
+  const int row = threadIdx.x & 127, pair = row >> 5, all = g.columns / 16 * K::kMaps;
   const float inv = r.sum == 0.0f ? 0.0f : 1.0f / r.sum, lam = p.a.lambda[r.head];
   const float f0 = rank == 0 ? inv : -lam * inv, f1 = rank == 0 ? -lam : 1.0f;
-  float x[32], sq = 0.0f;
-  auto difference = [&](int c) {
-    o.load(c, x);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (i < 4 || o.two(c)) y = __ldcg(theirs + ((t * all + c) * 4 + i) * 64 + (row & 63));
-      const float z[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[4 * i + k] = (r.sum == 0.0f ? 0.0f : x[4 * i + k] * f0) + z[k] * f1;
-    }
-  };
-  if (p.a.norm_weight != nullptr) {   // columns past D are zeros
+  const bool norm = p.a.norm_weight != nullptr;
+  float sq = 0.0f, f = p.a.out_scale;
 #pragma unroll 1
-    for (int c = o.chunk0; c < o.chunk1; c = o.next(c)) {
-      difference(c);
-#pragma unroll
-      for (int i = 0; i < 32; ++i) sq = fmaf(x[i], x[i], sq);
-    }
-    sm.row[half][row] = sq;
-    pair_sync(pair);
-    sq += sm.row[half ^ 1][row];
-    pair_sync(pair);
-  }
-  const float f = chunk_norm(p.a, sq, p.dv);
+  for (int pass = norm ? 0 : 1; pass < 2; ++pass) {   // the squares, then the output
 #pragma unroll 1
-  for (int c = o.chunk0; c < o.chunk1; c = o.next(c)) {
-    difference(c);
+    for (int c = o.chunk0; c < o.chunk1; c += 2) {
+      float x[32];
+      o.load(c, x);
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (i < o.width(c)) x[i] *= f * (p.a.norm_weight ? p.a.norm_weight[o.column(c) + i] : 1.0f);
-    o.store(c, x);
+      for (int i = 0; i < 8; ++i) {
+        float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (r.live && i * 4 < o.width(c)) y = __ldcg(theirs + (long long)((t * all + c) * 4 + i) * 64 + (row & 63));
+        const float z[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[4 * i + k] = (r.sum == 0.0f ? 0.0f : x[4 * i + k] * f0) + z[k] * f1;
+      }
+      if (pass == 0) {   // columns past D are zeros
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sq = fmaf(x[i], x[i], sq);
+        continue;
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] *= norm && i < o.width(c) ? f * p.a.norm_weight[o.column(c) + i] : f;
+      o.store(c, x);
+    }
+    if (pass == 1) break;
+    sm.row[o.half][row] = sq;
+    pair_sync(pair);
+    sq += sm.row[o.half ^ 1][row];
+    pair_sync(pair);
+    f = chunk_norm(p.a, sq, p.dv);
   }
 }
 
 template <typename K>
-__device__ void soft_role(const Geometry &g, Shared &sm, uint32_t tmem, int rank) {
+__device__ __forceinline__ void soft_role(const Geometry &g, Shared &sm, uint32_t tmem, int rank) {
   const ChunkShape &p = g.p;
   const ChunkArgs &a = p.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp & 3, half = warp >> 2, row = pair * 32 + lane;
@@ -797,7 +864,7 @@ __device__ void soft_role(const Geometry &g, Shared &sm, uint32_t tmem, int rank
     if (lane == 0) mbar_arrive(&sm.item_empty[e]);
     if (it.seq < 0) return;
     const ChunkSeq seq{it.first, 0, it.base, it.begin, it.lens};
-    Rows r[K::kTiles];
+    Rows r[2];
 #pragma unroll
     for (int t = 0; t < K::kTiles; ++t) {
       const bool live = t * 128 + row < it.rows;
@@ -809,26 +876,27 @@ __device__ void soft_role(const Geometry &g, Shared &sm, uint32_t tmem, int rank
       r[t].started = false;
       r[t].last = 0;
     }
+    if (K::kTiles == 1) r[1] = r[0];
+#pragma unroll 1
     for (int j = it.ka; j < it.kb; ++j, ++tile) {
-#pragma unroll
+#pragma unroll 1
       for (int t = 0; t < K::kTiles; ++t) {
-        if (!active(it, j, t)) continue;
+        if (t == 0 ? j < it.ta[0] || j >= it.tb[0] : j < it.ta[1] || j >= it.tb[1]) continue;
+        Rows x = t == 0 ? r[0] : r[1];
         wait(sm, &sm.s_full[s & 1], s >> 1 & 1);
         tc_fence_after();
         if (t * 128 + pair * 32 < it.rows) {   // else nobody's rows, whatever becomes of them
-          const int key0 = j * kKeys, kmax = min(kKeys, it.thi[t] - key0);
-          const unsigned skip = sm.skip[tile % kTileInfo];
+          const int key0 = j * kKeys, kmax = min(kKeys, (t == 0 ? it.thi[0] : it.thi[1]) - key0);
           // columns past kmax have not been computed
-          const int from = max(0, min(kKeys, r[t].lo - key0)) - half * 64, to = max(0, min(kmax, r[t].hi - key0)) - half * 64;
-          const bool part = __any_sync(~0u, from > 0 || to < 64) || skip != 0;
-          if (part) weights<K, true>(g, sm, r[t], s, tmem, t, chunk0, chunk1, from, to, skip);
-          else weights<K, false>(g, sm, r[t], s, tmem, t, chunk0, chunk1, 0, 64, 0);
+          const int from = max(0, min(kKeys, x.lo - key0)) - half * 64, to = max(0, min(kmax, x.hi - key0)) - half * 64;
+          weights<K>(g, sm, x, s, tmem, t, chunk0, chunk1, from, to, sm.skip[tile % kTileInfo]);
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.p_full[s & 1]);
-        r[t].started = true;
-        r[t].last = s;
+        x.started = true;
+        x.last = s;
+        (t == 0 ? r[0] : r[1]) = x;
         ++s;
       }
     }
@@ -839,23 +907,28 @@ __device__ void soft_role(const Geometry &g, Shared &sm, uint32_t tmem, int rank
     const bool sends = (pair >> 1) != rank;   // diff: the other CTA finishes these rows
     if (K::kMaps == 2 && it.whole && sends && crossed > 0) wait_cluster(sm, &sm.x_empty, (crossed - 1) & 1);
     const size_t stride = (size_t)64 * all * 16 * K::kTiles;
-    RowEnd end[K::kTiles];
-#pragma unroll
+    auto end_of = [&](int t) {
+      const Rows x = t == 0 ? r[0] : r[1];
+      RowEnd end;
+      sm.row[half][row] = x.l;
+      pair_sync(pair);
+      end.sum = x.l + sm.row[half ^ 1][row];
+      pair_sync(pair);
+      end.live = t * 128 + row < it.rows;
+      const int at = it.r0 + (end.live ? t * 128 + row : 0);
+      end.tok = at / p.group;
+      end.head = it.unit * p.group + at - end.tok * p.group;
+      end.m = x.m;
+      end.lo = x.lo;
+      end.hi = x.hi;
+      end.started = x.started;
+      return end;
+    };
+#pragma unroll 1
     for (int t = 0; t < K::kTiles; ++t) {
       if (t * 128 + pair * 32 >= it.rows) break;
-      sm.row[half][row] = r[t].l;
-      pair_sync(pair);
-      end[t].sum = r[t].l + sm.row[half ^ 1][row];
-      pair_sync(pair);
-      end[t].live = t * 128 + row < it.rows;
-      const int at = it.r0 + (end[t].live ? t * 128 + row : 0);
-      end[t].tok = at / p.group;
-      end[t].head = it.unit * p.group + at - end[t].tok * p.group;
-      end[t].m = r[t].m;
-      end[t].lo = r[t].lo;
-      end[t].hi = r[t].hi;
-      end[t].started = r[t].started;
-      finish<K>(g, it, end[t], rank, t, tmem, sends, g.exchange + blockIdx.x * stride);
+      const RowEnd end = end_of(t);
+      finish<K>(g, it, end, rank, t, tmem, sends, g.exchange + blockIdx.x * stride);
     }
     if (K::kMaps == 1 || !it.whole) continue;
     // ---- diff: the halves of the rows change places ----
@@ -866,10 +939,11 @@ __device__ void soft_role(const Geometry &g, Shared &sm, uint32_t tmem, int rank
       if (lane == 0) mbar_arrive_cluster(map_shared(&sm.x_full, other));
     } else {
       wait_cluster(sm, &sm.x_full, crossed & 1);
-#pragma unroll
+#pragma unroll 1
       for (int t = 0; t < K::kTiles; ++t) {
         if (t * 128 + pair * 32 >= it.rows) break;
-        finish_difference<K>(g, sm, it, end[t], rank, t, tmem, reinterpret_cast<const float4 *>(g.exchange + (blockIdx.x ^ 1) * stride));
+        const RowEnd end = end_of(t);
+        finish_difference<K>(g, sm, it, end, rank, t, tmem, reinterpret_cast<const float4 *>(g.exchange + (blockIdx.x ^ 1) * stride));
       }
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(map_shared(&sm.x_empty, other));
@@ -881,10 +955,9 @@ __device__ void soft_role(const Geometry &g, Shared &sm, uint32_t tmem, int rank
 template <typename K>
 __global__ void __launch_bounds__(kThreads, 1)
 chunk_bf16_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
-  extern __shared__ char smem_raw[];
+  extern __shared__ __align__(1024) char smem_raw[];
   Shared &sm = *reinterpret_cast<Shared *>(smem_raw);
-  char *qs = smem_raw + sizeof(Shared);
-  qs += (1024 - (smem_addr(qs) & 1023)) & 1023;
+  char *qs = smem_raw + kHead;
   char *ring = qs + (size_t)K::kTiles * g.chunks * kChunkBytes;
   const int tid = threadIdx.x, warp = tid >> 5;
   const int rank = K::kMaps == 2 ? (int)cluster_ctarank() : 0, share = blockIdx.x / K::kMaps;
@@ -913,6 +986,14 @@ chunk_bf16_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CU
     sm.flags = 0;
     sm.dead = 0;
   }
+  if ((smem_addr(smem_raw) & 1023) != 0) {   // swizzled panels want it; the declaration asks for it
+    grid_begins();
+    if (tid == 0) {
+      if (rank == 0) g.p.cuts[share] = make_int4(0, 0, 0, 0);
+      post_status(reinterpret_cast<unsigned *>(g.p.a.ws), blockIdx.x, gridDim.x, kErrConfig);
+    }
+    return;
+  }
   if (warp == kMmaWarp) tmem_alloc(&sm.tmem, 512);
   tc_fence_before();
   grid_begins();
@@ -921,10 +1002,16 @@ chunk_bf16_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CU
   chunk_share<kThreads>(g.p, share, sm.sums, &sm.share, &sm.flags);
   if (K::kMaps == 2) cluster_sync();   // the other CTA's barriers are there
   const uint32_t tmem = sm.tmem;
-  if (warp < kSoftWarps) soft_role<K>(g, sm, tmem, rank);
-  else if (warp == kMmaWarp) product_role<K>(g, sm, qs, ring, tmem);
-  else if (warp == kLoadWarp) load_role<K>(g, sm, ring, &kmap, &vmap, rank);
-  else query_role<K>(g, sm, qs, rank);
+  // 384 x 168 registers at launch = 256 x 200 + 128 x 104
+  if (warp < kSoftWarps) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    soft_role<K>(g, sm, tmem, rank);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    if (warp == kMmaWarp) product_role<K>(g, sm, qs, ring, tmem);
+    else if (warp == kLoadWarp) load_role<K>(g, sm, ring, &kmap, &vmap, rank);
+    else query_role<K>(g, sm, qs, rank);
+  }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
@@ -948,7 +1035,7 @@ cudaError_t launch_kind(Geometry g, cudaStream_t s) {
   const CacheLayer &c = p.a.cache;
   p.block = 128 * K::kTiles;
   constexpr size_t kMost = 227 << 10;
-  const size_t fixed = sizeof(Shared) + 1024 + (size_t)K::kTiles * g.chunks * kChunkBytes, slot = (size_t)g.panel_chunks * kChunkBytes;
+  const size_t fixed = kHead + (size_t)K::kTiles * g.chunks * kChunkBytes, slot = (size_t)g.panel_chunks * kChunkBytes;
   g.slots = (int)((kMost - fixed) / slot);
   if (g.slots > kRingMax) g.slots = kRingMax;
   const size_t smem = fixed + g.slots * slot;
