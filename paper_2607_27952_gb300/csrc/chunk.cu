@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const __grid_c
       float all = -INFINITY, sum = 0.0f;
       if (live) {
         for (int i = 0; i < parts; ++i) all = fmaxf(all, slot(i)[r]);
-        for (int i = 0; i < parts; ++i) sum = fmaf(chunk_factor(slot(i)[r], all), slot(i)[p.block + r], sum);
+        for (int i = 0; i < parts; ++i) sum = fmaf(chunk_factor(slot(i)[r], all), slot(i)[p.pitch + r], sum);
       }
       const float weight = map == 0 ? 1.0f : live ? -a.lambda[h] : 0.0f;
       if (live && p.maps == 1 && a.lse != nullptr && warp == 0) a.lse[(long long)(s.first + t) * a.q_heads + h] = chunk_lse(all, sum);
@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const __grid_c
           for (int e = 0; e < 2; ++e) {
             const int four = (warp + 8 * j) * 2 + e;
             if (four * 4 >= p.dv) continue;
-            const float4 y = reinterpret_cast<const float4 *>(from + 2 * p.block)[(long long)four * p.block + r];
+            const float4 y = reinterpret_cast<const float4 *>(from + 2 * p.pitch)[(long long)four * p.pitch + r];
             acc[j][4 * e] = fmaf(y.x, f, acc[j][4 * e]);
             acc[j][4 * e + 1] = fmaf(y.y, f, acc[j][4 * e + 1]);
             acc[j][4 * e + 2] = fmaf(y.z, f, acc[j][4 * e + 2]);

@@ -9,8 +9,8 @@
 // The maximum m follows a row's logits only past a factor of 2^8 (weights are then at most 2^8, and O is rescaled by those warps,
 // rarely); l sums the weights before they are rounded.
 //
-// Warps: 0-7 softmax and epilogue, 8 issues the products, 9 fills a ring of K and V panels (128 keys by up to 128 columns) with TMA
-// boxes of the pages, 10 and 11 walk the share's items and fetch rows of Q.  V rows that no row sees are zeroed in
+// Warps: 0-7 softmax and epilogue, 8 and 11 issue the products, 9 fills a ring of K and V panels (128 keys by up to 128 columns) with TMA
+// boxes of the pages, 10 walks the share's items and fetches rows of Q.  V rows that no row sees are zeroed in
 // shared memory before the product reads them: a weight of zero times an infinity or NaN would show.
 // diff: a cluster of two CTAs, one map each; each finishes half of the rows, with the other's half of O through L2.
 #include "chunk_impl.cuh"
@@ -21,7 +21,7 @@ namespace last {
 namespace {
 
 constexpr int kThreads = 384, kSoftWarps = 8, kKeys = 128, kRingMax = 12, kItems = 4, kTileInfo = 16;
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kQueryWarp = 10;
+constexpr int kMmaWarp = 8, kLoadWarp = 9;   // 8 and 11 issue products, 10 walks the items
 constexpr uint32_t kChunkBytes = kKeys * 128;   // 128 rows of 64 elements
 constexpr int kOutColumn = 256;                 // of TMEM; S takes columns 0 - 127 and 128 - 255
 
@@ -32,6 +32,8 @@ struct Geometry {      // the same for every CTA
   int columns;         // a head's row, up to a multiple of 16
   int slots;           // panels of the ring
   int box_log, page_log;
+  int rows;            // of a row tile: whole tokens where a token's heads fit one
+  bool q_boxes;        // a row tile of Q is one TMA box per chunk
   float *exchange;     // diff: [CTAs][row tiles][columns / 4][64 rows][4]
 };
 
@@ -48,13 +50,13 @@ struct Item {
 constexpr size_t kHead = 3072;   // shared memory before the panels, of which seven of 32 KB stand beside it
 
 struct alignas(16) Shared {
-  unsigned long long full[kRingMax], empty[kRingMax], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2];
+  unsigned long long full[kRingMax], empty[kRingMax], q_full[2], q_empty[2], s_full[2], p_full[2][2], pv_done[2];
   unsigned long long item_full[kItems], item_empty[kItems], x_full, x_empty, never;
   Item items[kItems];
   float row[2][128];      // a row's value of one half of the columns for the other
   ChunkShare share;
   unsigned long long sums[kThreads / 32];
-  int2 boxes[16];             // of the key tile being fetched: first token, page
+  alignas(16) int2 boxes[16];   // of the key tile being fetched: first token, page
   unsigned skip[kTileInfo];   // of the key tiles on their way: groups of 8 keys whose page is out of range
   uint32_t tmem;
   unsigned flags;
@@ -62,15 +64,26 @@ struct alignas(16) Shared {
 };
 static_assert(sizeof(Shared) <= kHead, "the panels begin behind it");
 
+// Waits end after two seconds by the clock.
+constexpr unsigned long long kWaitNanoseconds = 2000000000ull;
+struct Limit {
+  unsigned long long begin = 0;
+  uint32_t tries = 0;
+  __device__ __forceinline__ bool over(const Shared &sm) {
+    if ((tries++ & 63) != 0) return false;
+    unsigned long long now;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+    if (begin == 0) begin = now;
+    return sm.dead != 0 || now - begin > kWaitNanoseconds;
+  }
+};
 // A whole warp waits, with a limit; the first to give up has every other wait of the CTA end too.  The softmax warps go on
 // after a wait that gave up, with whatever is there, to the end of their item, so that no barrier of theirs waits for a warp
 // that has left; the others leave.
 __device__ __forceinline__ bool wait(Shared &sm, unsigned long long *bar, uint32_t parity) {
   bool ok = mbar_try_wait(bar, parity);
-  for (uint32_t i = 0; i < kWaitLimit && !ok; ++i) {
-    if ((i & 31) == 0 && sm.dead) break;
-    ok = mbar_try_wait(bar, parity);
-  }
+  if (!ok)
+    for (Limit limit; !ok && !limit.over(sm);) ok = mbar_try_wait(bar, parity);
   if (__all_sync(~0u, ok)) return true;
   sm.dead = 1;
   return false;
@@ -78,26 +91,15 @@ __device__ __forceinline__ bool wait(Shared &sm, unsigned long long *bar, uint32
 // For what the other CTA of the cluster has written.
 __device__ __forceinline__ bool wait_cluster(Shared &sm, unsigned long long *bar, uint32_t parity) {
   uint32_t ok = 0;
-  for (uint32_t i = 0; i < kWaitLimit && !ok; ++i) {
-    if ((i & 31) == 1 && sm.dead) break;
+  for (Limit limit; !ok && !limit.over(sm);)
     asm volatile("{\n\t.reg .pred p;\n\t"
                  "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
                  "selp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
-  }
   if (__all_sync(~0u, ok != 0)) return true;
   sm.dead = 1;
   return false;
 }
-__device__ __forceinline__ bool passed(unsigned long long *bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n\t.reg .pred p;\n\t"
-               "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-               "selp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
-  return __all_sync(~0u, ok != 0);
-}
-
 // 32 columns of the warp's 32 TMEM lanes.
 __device__ __forceinline__ void tmem_ld32(uint32_t a, uint32_t *r) {
   asm volatile(
@@ -213,21 +215,22 @@ struct MapHead {
   static __device__ __forceinline__ int of(int h, int rank) { return K::kMaps == 2 ? 2 * h + rank : h; }
 };
 
-// ---- warps 10 and 11: items and rows of Q ----
+// ---- warp 10: items and rows of Q ----
 template <typename K>
-__device__ __forceinline__ void query_role(const Geometry &g, Shared &sm, char *qs, int rank) {
+__device__ __forceinline__ void query_role(const Geometry &g, Shared &sm, char *qs, const CUtensorMap *qmap, int rank) {
   const ChunkShape &p = g.p;
-  const int lane = threadIdx.x & 31, half = (threadIdx.x >> 5) - kQueryWarp, D = p.a.cache.dim;
+  const int lane = threadIdx.x & 31, D = p.a.cache.dim;
   ChunkWalk walk(sm.share);
   ChunkItem it;
   uint32_t n = 0, tile = 0;
   const int eights = g.chunks * 8;   // 16-byte pieces of a row, zeros past D
+  const int four_tokens = 4 / p.group, four_rest = 4 % p.group;
   for (bool more = true; more; ++n) {
     more = walk.next(p, &it);
     const int e = n % kItems;
-    if (half == 0 && n >= kItems && !wait(sm, &sm.item_empty[e], (n / kItems & 1) ^ 1)) return;
+    if (n >= kItems && !wait(sm, &sm.item_empty[e], (n / kItems & 1) ^ 1)) return;
     Item &o = sm.items[e];
-    const bool writes = half == 0 && lane == 0, some = more && it.t.count > 0;
+    const bool writes = lane == 0, some = more && it.t.count > 0;
     const int ka = some ? it.t.first + it.k0 : 0, kb = some ? it.t.first + it.k1 : 0;
     unsigned used = 0;   // row tiles with a step
     if (writes) {
@@ -250,8 +253,8 @@ __device__ __forceinline__ void query_role(const Geometry &g, Shared &sm, char *
     for (int t = 0; t < 2; ++t) {
       ChunkTiles x{0, 0, 0, 0};
       int ta = 0, tb = 0;
-      if (some && t * 128 < it.rows) {
-        x = chunk_tiles(p, it.s, it.r0 + t * 128, it.r0 + min(it.rows, t * 128 + 128));
+      if (some && t * g.rows < it.rows) {
+        x = chunk_tiles(p, it.s, it.r0 + t * g.rows, it.r0 + min(it.rows, t * g.rows + g.rows));
         ta = max(ka, x.first);
         tb = min(kb, x.first + x.count);
       }
@@ -272,16 +275,34 @@ __device__ __forceinline__ void query_role(const Geometry &g, Shared &sm, char *
       const int slot = tile % K::kTiles;
       if (tile >= (uint32_t)K::kTiles && !wait(sm, &sm.q_empty[slot], (tile / K::kTiles & 1) ^ 1)) return;
       const uint32_t to = smem_addr(qs) + slot * g.chunks * kChunkBytes;
+      if (g.q_boxes) {   // rows of other sequences behind the last one are nobody's
+        if (elected()) {
+          mbar_expect_tx(&sm.q_full[slot], g.chunks * g.rows * 128);
+          const int tok = it.s.first + (it.r0 + t * g.rows) / p.group;
+          for (int c = 0; c < g.chunks; ++c)
+            tma_box(to + c * kChunkBytes, qmap, c * 64, it.unit * p.group, rank, tok, smem_addr(&sm.q_full[slot]));
+        }
+        __syncwarp();
+        ++tile;
+        continue;
+      }
       // 32 / 8 rows at a time, 8 lanes to a row's 128 bytes
-      for (int r = half * 64 + (lane >> 3); r < half * 64 + 64; r += 4) {
-        const int row = t * 128 + r;
-        const bool live = row < it.rows;
-        const int at = it.r0 + (live ? row : 0), tok = at / p.group, h = it.unit * p.group + at - tok * p.group;
-        const char *from = p.a.q + (long long)(it.s.first + tok) * p.a.q_stride + (long long)(MapHead<K>::of(h, rank)) * D * 2;
+      int row = t * g.rows + (lane >> 3);
+      int at = it.r0 + row, tok = at / p.group, h = at - tok * p.group;
+#pragma unroll 2
+      for (int r = lane >> 3; r < 128; r += 4, row += 4) {
+        const bool live = r < g.rows && row < it.rows;
+        const char *from = p.a.q + (live ? (long long)(it.s.first + tok) * p.a.q_stride + (long long)MapHead<K>::of(it.unit * p.group + h, rank) * D * 2 : 0);
         for (int c = lane & 7; c < eights; c += 8) {
           const uint32_t dst = to + (c >> 3) * kChunkBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4);
           const bool in = live && c * 8 < D;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(in ? from + c * 16 : from), "r"(in ? 16 : 0) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(in ? from + c * 16 : p.a.q), "r"(in ? 16 : 0) : "memory");
+        }
+        h += four_rest;   // four rows on
+        tok += four_tokens;
+        if (h >= p.group) {
+          h -= p.group;
+          ++tok;
         }
       }
       cp_async_commit();
@@ -344,17 +365,27 @@ __device__ __forceinline__ void load_role(const Geometry &g, Shared &sm, char *r
         const CUtensorMap *map = value < 0 ? kmap : vmap;
         if (elected()) {
           mbar_expect_tx(&sm.full[at.slot], __popc(there) * chunks * box * 128);
-          auto load = [&](int b) {
-            const int2 from = sm.boxes[b];
+          auto load = [&](int b, int first, int its_page) {
             const uint32_t to = panel + (b << (g.box_log + 7));
-            tma_box(to, map, pi * 128, from.x, head, from.y, bar);
-            if (chunks == 2) tma_box(to + kChunkBytes, map, pi * 128 + 64, from.x, head, from.y, bar);
+            tma_box(to, map, pi * 128, first, head, its_page, bar);
+            if (chunks == 2) tma_box(to + kChunkBytes, map, pi * 128 + 64, first, head, its_page, bar);
           };
-          if (there == (1u << boxes) - 1) {
-#pragma unroll 4
-            for (int b = 0; b < boxes; ++b) load(b);
+          if (there == (1u << boxes) - 1 && boxes >= 4) {
+#pragma unroll 1
+            for (int b = 0; b < boxes; b += 4) {
+              const int4 f0 = reinterpret_cast<const int4 *>(sm.boxes)[b / 2], f1 = reinterpret_cast<const int4 *>(sm.boxes)[b / 2 + 1];
+              load(b, f0.x, f0.y);
+              load(b + 1, f0.z, f0.w);
+              load(b + 2, f1.x, f1.y);
+              load(b + 3, f1.z, f1.w);
+            }
           } else {
-            for (unsigned left = there; left != 0; left &= left - 1) load(__ffs(left) - 1);
+#pragma unroll 1
+            for (unsigned left = there; left != 0; left &= left - 1) {
+              const int b = __ffs(left) - 1;
+              const int2 from = sm.boxes[b];
+              load(b, from.x, from.y);
+            }
           }
         }
         __syncwarp();
@@ -367,172 +398,179 @@ __device__ __forceinline__ void load_role(const Geometry &g, Shared &sm, char *r
   }
 }
 
-// ---- warp 8: the products ----
-struct Step {
-  bool some, first, last;  // first of its row tile in the item, last of its key tile
-  uint32_t s;
-  int t, kmin, kmax;
-  int zero_lo, zero_hi;    // rows of V that some row sees
-  unsigned skip;
-  Place at;                // of K, then of V
+// ---- warps 8 and 11: the products ----
+// Each has one of the two accumulators of S: its steps are those of a row tile, or, of an item with one row tile, every other
+// one.  A step's S goes to the tensor cores right behind O of the step before, whose weights lay where it goes: products
+// of one thread run in the order they are issued.  What a warp works out and waits for in between hides behind the other's
+// products.  A panel's room is free once both say so: a warp that has no use for a panel gives it back as it comes, so that neither
+// mistakes a round of the ring for another.
+struct Tiles {   // of an item, in registers
+  int ka, kb, ta[2], tb[2], tlo[2], thi[2], lo, hi;
+  __device__ __forceinline__ explicit Tiles(const Item &it) : ka(it.ka), kb(it.kb), lo(it.lo), hi(it.hi) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      ta[t] = it.ta[t];
+      tb[t] = it.tb[t];
+      tlo[t] = it.tlo[t];
+      thi[t] = it.thi[t];
+    }
+  }
+  __device__ __forceinline__ bool on(int j, int t) const { return t == 0 ? j >= ta[0] && j < tb[0] : j >= ta[1] && j < tb[1]; }
+  __device__ __forceinline__ bool two() const { return ta[0] < tb[0] && ta[1] < tb[1]; }
 };
 
-__device__ void zero_rows(uint32_t panel, int chunks, int from, int to) {
+__device__ __forceinline__ void zero_rows(uint32_t panel, int chunks, int from, int to) {
+#pragma unroll 1
   for (int c = 0; c < chunks; ++c)
+#pragma unroll 1
     for (int i = from * 8 + (threadIdx.x & 31); i < to * 8; i += 32)
       asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" :: "r"(panel + c * kChunkBytes + i * 16), "r"(0) : "memory");
 }
 
 template <typename K>
-__device__ __forceinline__ bool values(const Geometry &g, Shared &sm, uint32_t ring, Step &x, uint32_t tmem) {
-  const int b = x.s & 1;
-  if (!wait(sm, &sm.p_full[b], x.s >> 1 & 1)) return false;
-  tc_fence_after();
-  const uint32_t pt = tmem + b * 128, o = tmem + kOutColumn + x.t * 128;
-  const int k0 = x.kmin / 16, k1 = (x.kmax + 15) / 16;
-#pragma unroll
-  for (int i = 0; i < K::kValues; ++i) {
-    const int pi = i % K::kPanels, head = i / K::kPanels;
-    if (!wait(sm, &sm.full[x.at.slot], x.at.round)) return false;
-    const uint32_t panel = ring + x.at.slot * g.panel_chunks * kChunkBytes;
-    if (x.zero_lo > k0 * 16 || x.zero_hi < k1 * 16 || x.skip) {
-      const int chunks = K::kPanels == 1 ? g.chunks : min(2, g.chunks - 2 * pi);
-      zero_rows(panel, chunks, k0 * 16, x.zero_lo);
-      zero_rows(panel, chunks, x.zero_hi, k1 * 16);
-      for (unsigned left = x.skip; left != 0; left &= left - 1) zero_rows(panel, chunks, (__ffs(left) - 1) * 8, __ffs(left) * 8);
-      fence_proxy_async_smem();
-      __syncwarp();
-    }
-    if (elected()) {
-      const int n = K::kPanels == 1 ? g.columns : min(128, g.columns - pi * 128);
-      const uint32_t idesc = umma_idesc_bf16(128, n) | kNMajor, d = o + head * g.columns + pi * 128;
-      const uint64_t v = desc_n_major(panel);
-      if (k1 - k0 == 8) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) umma_bf16_ts(d, pt + (k >> 2) * 64 + (k & 3) * 8, v + k * (2048 >> 4), idesc, k == 0 && x.first ? 0u : 1u);
-        if (K::kParts == 2)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) umma_bf16_ts(d, pt + 32 + (k >> 2) * 64 + (k & 3) * 8, v + k * (2048 >> 4), idesc, 1u);
-      } else {
-#pragma unroll 1
-        for (int k = k0; k < k1; ++k)
-#pragma unroll
-          for (int e = 0; e < K::kParts; ++e)
-            umma_bf16_ts(d, pt + 32 * e + (k >> 2) * 64 + (k & 3) * 8, v + k * (2048 >> 4), idesc, x.first && k == k0 && e == 0 ? 0u : 1u);
-      }
-      if (x.last) umma_commit(&sm.empty[x.at.slot]);
-      if (i == K::kValues - 1) umma_commit(&sm.pv_done[b]);
-    }
-    __syncwarp();
-    x.at.skip(g, 1);
-  }
-  return true;
-}
-
-// The next step's S before this one's O; but what the next step still waits for (its item, its rows of Q) does not keep
-// this one back.
-template <typename K>
-__device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char *qs_, char *ring_, uint32_t tmem) {
+__device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char *qs_, char *ring_, uint32_t tmem, int w) {
   const int lane = threadIdx.x & 31, D = g.p.a.cache.dim;
-  const uint32_t qs = smem_addr(qs_), ring = smem_addr(ring_);
-  uint32_t s = 0, tile = 0, n = 0, q_at[2] = {0, 0}, q_tile = 0;
-  int j = 0, kb = 0, t = 0;                 // the next step: key tile, row tile
-  bool open = false, done = false;          // within item n; no item is left
+  const uint32_t ring = smem_addr(ring_), panel = (uint32_t)g.panel_chunks * kChunkBytes, rows = (uint32_t)g.chunks * (kChunkBytes >> 4);
+  const uint64_t q_desc = umma_desc_sw128(smem_addr(qs_)), k_desc = umma_desc_sw128(ring), v_desc = desc_n_major(ring);
+  const uint32_t st = tmem + w * 128;
+  uint32_t s = 0, others = 0, tile = 0, q_tile = 0;   // own steps and the other warp's; key tiles; row tiles
   Place at{0, 0};
-  Step behind;
-  behind.some = false;
-  while (!done || behind.some) {
-    Step x;
-    x.some = false;
-    const Item &it = sm.items[n % kItems];
-    if (!done && !open && (!behind.some || passed(&sm.item_full[n % kItems], n / kItems & 1))) {
-      if (!wait(sm, &sm.item_full[n % kItems], n / kItems & 1)) return;
-      open = true;
-      done = it.seq < 0;
-      j = it.ka;
-      kb = it.kb;
-      t = 0;
-      q_at[0] = q_tile;
-      q_tile += it.ta[0] < it.tb[0];
-      q_at[1] = q_tile;
-      q_tile += it.ta[1] < it.tb[1];
-    }
-    if (open && !done && j < kb) {
-      const bool on0 = j >= it.ta[0] && j < it.tb[0], on1 = j >= it.ta[1] && j < it.tb[1];
-      if (t == 0 && !on0) t = 1;
-      const bool on = t == 0 || on1;   // else nobody's keys: passed on as they came
-      const uint32_t q_turn = t == 0 ? q_at[0] : q_at[1];
-      const int q = q_turn % K::kTiles;
-      const uint32_t q_phase = q_turn / K::kTiles & 1;
-      x.first = on && j == it.ta[t];
-      if (!x.first || !behind.some || passed(&sm.q_full[q], q_phase)) {
-        if (x.first && !wait(sm, &sm.q_full[q], q_phase)) return;
-        const int key0 = j * kKeys;
-        x.some = on;
-        x.s = s;
-        x.t = t;
-        x.kmin = max(0, it.tlo[t] - key0);
-        x.kmax = min(kKeys, it.thi[t] - key0);
-        x.last = t == 1 || !on1;
-        x.zero_lo = max(0, it.lo - key0);
-        x.zero_hi = min(kKeys, it.hi - key0);
-        x.at = at;
-        const uint32_t idesc = umma_idesc_bf16(128, (x.kmax + 15) / 16 * 16), d = tmem + (s & 1) * 128;
-#pragma unroll
-        for (int pi = 0; pi < K::kPanels; ++pi) {
-          if (!wait(sm, &sm.full[x.at.slot], x.at.round)) return;
-          if (elected()) {
-            if (on) {
-              const uint64_t k_rows = umma_desc_sw128(ring + x.at.slot * g.panel_chunks * kChunkBytes);
-              const uint64_t q_rows = umma_desc_sw128(qs + (q * g.chunks + 2 * pi) * kChunkBytes);
-              const int steps = (D - pi * 128 + 15) / 16;
-              auto product = [&](int k) {
-                const int off = ((k >> 2) * (int)kChunkBytes + (k & 3) * 32) >> 4;
-                umma_bf16(d, q_rows + off, k_rows + off, idesc, (pi | k) != 0 ? 1u : 0u);
-              };
-              if (steps >= 8) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) product(k);
-              } else {
+  for (uint32_t n = 0;; ++n) {
+    const int e = n % kItems;
+    if (!wait(sm, &sm.item_full[e], n / kItems & 1)) return;
+    const bool end = sm.items[e].seq < 0;
+    const Tiles it(sm.items[e]);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sm.item_empty[e]);
+    if (end) return;
+    const bool two = it.two();
+    const int t = two ? w : it.ta[0] < it.tb[0] ? 0 : 1, ta = t == 0 ? it.ta[0] : it.ta[1], tb = t == 0 ? it.tb[0] : it.tb[1];
+    const int tlo = t == 0 ? it.tlo[0] : it.tlo[1], thi = t == 0 ? it.thi[0] : it.thi[1];
+    const uint32_t turn = q_tile + (two ? w : 0), q = turn % K::kTiles, o = tmem + kOutColumn + t * 128;
+    bool begun = false, waited = false;   // waited: for K of tile j
 #pragma unroll 1
-                for (int k = 0; k < steps; ++k) product(k);
+    for (int j = it.ka; j < it.kb; ++j, ++tile) {
+      const bool own = two ? j >= ta && j < tb : ((j - it.ka) & 1) == w;
+      const int key0 = j * kKeys, kmin = max(0, tlo - key0), kmax = min(kKeys, thi - key0);
+      const int k0 = kmin >> 4, k1 = (kmax + 15) >> 4;
+      if (own && !begun && !wait(sm, &sm.q_full[q], turn / K::kTiles & 1)) return;
+#pragma unroll
+      for (int pi = 0; pi < K::kPanels; ++pi) {
+        if (!waited && !wait(sm, &sm.full[at.slot], at.round)) return;
+        if (own) {
+          if (elected()) {
+            const uint64_t k_rows = k_desc + at.slot * (panel >> 4), q_rows = q_desc + q * rows + pi * 2 * (kChunkBytes >> 4);
+            const uint32_t idesc = umma_idesc_bf16(128, k1 * 16);
+            const int steps = (D - pi * 128 + 15) / 16;
+            auto product = [&](int k) {
+              const int off = ((k >> 2) * (int)kChunkBytes + (k & 3) * 32) >> 4;
+              umma_bf16(st, q_rows + off, k_rows + off, idesc, (pi | k) != 0 ? 1u : 0u);
+            };
+            if (steps >= 8) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) product(k);
+            } else {
+#pragma unroll 1
+              for (int k = 0; k < steps; ++k) product(k);
+            }
+            if (pi == K::kPanels - 1) umma_commit(&sm.s_full[w]);
+            umma_commit(&sm.empty[at.slot]);
+            if (pi == K::kPanels - 1 && j + (two ? 1 : 2) >= (two ? tb : it.kb)) {   // the row tile's last
+              umma_commit(&sm.q_empty[q]);
+              if (two) umma_commit(&sm.q_empty[q]);
+            }
+          }
+        } else if (lane == 0) {
+          mbar_arrive(&sm.empty[at.slot]);
+        }
+        __syncwarp();
+        at.skip(g, 1);
+      }
+      const Place v0 = at;
+      const unsigned skip = sm.skip[tile % kTileInfo];   // written before K's panels were asked for
+      const int from = max(0, it.lo - key0), to = min(kKeys, it.hi - key0);
+#pragma unroll
+      for (int i = 0; i < K::kValues; ++i) {
+        if (!wait(sm, &sm.full[at.slot], at.round)) return;
+        if (!own) {
+          if (lane == 0) mbar_arrive(&sm.empty[at.slot]);
+        } else if (((from | to) & 15) != 0 || skip != 0) {   // what no row sees is zeroed (by both warps alike)
+          const int chunks = K::kPanels == 1 ? g.chunks : min(2, g.chunks - 2 * (i % K::kPanels));
+          zero_rows(ring + at.slot * panel, chunks, from & ~15, from);
+          zero_rows(ring + at.slot * panel, chunks, to, (to + 15) & ~15);
+#pragma unroll 1
+          for (unsigned left = skip; left != 0; left &= left - 1)
+            zero_rows(ring + at.slot * panel, chunks, (__ffs(left) - 1) * 8, __ffs(left) * 8);
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        at.skip(g, 1);
+      }
+      waited = false;
+      if (own) {
+        const bool full = k1 - k0 == 8;
+        // with two row tiles the next step is the next tile's: its K comes before these weights (and wants no room of this V)
+        if (two && j + 1 < it.kb) {
+          Place next = at;
+#pragma unroll
+          for (int pi = 0; pi < K::kPanels; ++pi) {
+            if (!wait(sm, &sm.full[next.slot], next.round)) return;
+            next.skip(g, 1);
+          }
+          waited = true;
+        }
+        // one row tile: the other warp's O of the step before goes first
+        if (!two && j > it.ka && !wait(sm, &sm.pv_done[w ^ 1], (others - 1) & 1)) return;
+        // the first and second 32 keys of either half
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          if (!wait(sm, &sm.p_full[w][part], s & 1)) return;
+          tc_fence_after();
+          Place v = v0;
+#pragma unroll
+          for (int i = 0; i < K::kValues; ++i) {
+            const int pi = i % K::kPanels, head = i / K::kPanels;
+            const int width = K::kPanels == 1 ? g.columns : min(128, g.columns - pi * 128);
+            const uint32_t idesc = umma_idesc_bf16(128, width) | kNMajor, d = o + head * g.columns + pi * 128;
+            const uint64_t vd = v_desc + v.slot * (panel >> 4);
+            if (elected()) {
+              if (full) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                  for (int k2 = 0; k2 < 2; ++k2) {
+                    const int k = 4 * h + 2 * part + k2;
+#pragma unroll
+                    for (int x = 0; x < K::kParts; ++x)
+                      umma_bf16_ts(d, st + 64 * h + 16 * part + 8 * k2 + 32 * x, vd + k * (2048 >> 4), idesc, part == 0 && h + k2 + x == 0 && j == ta ? 0u : 1u);
+                  }
+              } else if (part == 1) {
+#pragma unroll 1
+                for (int k = k0; k < k1; ++k)
+#pragma unroll
+                  for (int x = 0; x < K::kParts; ++x)
+                    umma_bf16_ts(d, st + 32 * x + (k >> 2) * 64 + (k & 3) * 8, vd + k * (2048 >> 4), idesc, j == ta && k == k0 && x == 0 ? 0u : 1u);
+              }
+              if (part == 1) {
+                if (i == K::kValues - 1) umma_commit(&sm.pv_done[w]);
+                umma_commit(&sm.empty[v.slot]);
               }
             }
-            if (x.last) umma_commit(&sm.empty[x.at.slot]);
-            if (on && pi == K::kPanels - 1) {
-              umma_commit(&sm.s_full[s & 1]);
-              if (j + 1 == it.tb[t]) umma_commit(&sm.q_empty[q]);
-            }
+            __syncwarp();
+            v.skip(g, 1);
           }
-          __syncwarp();
-          x.at.skip(g, 1);
         }
-        x.skip = sm.skip[tile % kTileInfo];   // written before K's panels arrived
-        s += on;
-        if (!on)
-          for (int i = 0; i < K::kValues; ++i) {
-            if (!wait(sm, &sm.full[x.at.slot], x.at.round)) return;
-            if (lane == 0) mbar_arrive(&sm.empty[x.at.slot]);
-            x.at.skip(g, 1);
-          }
-        if (x.last) {
-          at.skip(g, K::kPanels + K::kValues);
-          ++tile;
-          ++j;
-          t = 0;
-        } else {
-          t = 1;
-        }
+        begun = true;
+        ++s;
       }
+      others += two ? it.on(j, w ^ 1) : !own;
     }
-    if (open && !done && j >= kb) {   // every lane has read what it needs of the item
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sm.item_empty[n % kItems]);
-      ++n;
-      open = false;
+    // an item's only step was the other warp's: it has done with the row tile when both say so
+    if (!two && !begun && it.ka < it.kb) {
+      if (!wait(sm, &sm.q_full[q], turn / K::kTiles & 1)) return;
+      if (lane == 0) mbar_arrive(&sm.q_empty[q]);
     }
-    if (behind.some && !values<K>(g, sm, ring, behind, tmem)) return;
-    behind = x;
+    q_tile += (it.ta[0] < it.tb[0]) + (it.ta[1] < it.tb[1]);
   }
 }
 
@@ -541,17 +579,16 @@ struct Rows {      // what a thread keeps of a row tile
   float m, l;      // l: of this warp's keys
   int lo, hi;      // keys that its row sees
   bool started;
-  uint32_t last;   // its last step
 };
 
 // Weights of the warp's 32 rows and 64 of the step's keys.  from, to: columns of these that the row sees.  There is one
 // copy of this code for all row tiles and masks: with four of them the instruction cache missed all the time.
 template <typename K>
-__device__ __forceinline__ void weights(const Geometry &g, Shared &sm, Rows &r, uint32_t s, uint32_t tmem, int t, int chunk0, int chunk1,
-                                        int from, int to, unsigned skip) {
+__device__ __forceinline__ void weights(const Geometry &g, Shared &sm, Rows &r, uint32_t tmem, int t, int chunk0, int chunk1,
+                                        int from, int to, unsigned skip, int b, bool two, uint32_t others) {
   const bool masked = __any_sync(~0u, from > 0 || to < 64) || skip != 0;
   const int pair = (threadIdx.x >> 5) & 3, half = (threadIdx.x >> 5) >> 2, row = pair * 32 + (threadIdx.x & 31);
-  const uint32_t lanes = (uint32_t)(pair * 32) << 16, st = tmem + lanes + (s & 1) * 128 + half * 64;
+  const uint32_t lanes = (uint32_t)(pair * 32) << 16, st = tmem + lanes + b * 128 + half * 64;
   uint32_t v[64];
   tmem_ld32(st, v);
   tmem_ld32(st + 32, v + 32);
@@ -586,7 +623,7 @@ __device__ __forceinline__ void weights(const Geometry &g, Shared &sm, Rows &r, 
     r.m = mine;
     r.l *= alpha;
     if (r.started) {
-      if (r.last + 1 == s) wait(sm, &sm.pv_done[r.last & 1], r.last >> 1 & 1);
+      if (!two) wait(sm, &sm.pv_done[b ^ 1], (others - 1) & 1);   // S of one row tile comes behind its own O
       tc_fence_after();
       for (int c = chunk0; c < chunk1; ++c) {
         uint32_t o[16];
@@ -617,10 +654,13 @@ __device__ __forceinline__ void weights(const Geometry &g, Shared &sm, Rows &r, 
     }
     tmem_st16(st + 16 * q, w);
     if (K::kParts == 2) tmem_st16(st + 32 + 16 * q, rest);
+    tmem_wait_st();
+    tc_fence_before();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(&sm.p_full[b][q]);   // of the half's first, then second 32 keys
   }
   const float2 total = unpack2(add2(sum[0], sum[1]));
   r.l += total.x + total.y;
-  tmem_wait_st();
 }
 
 // Column `lane` of the 32 from col on of a row of O once more, on the CUDA cores, for rows where the sums are not finite though
@@ -779,13 +819,13 @@ __device__ __forceinline__ void finish(const Geometry &g, const Item &it, const 
   int stride = 64;
   if (!it.whole) {
     float *slot = chunk_slot(p, blockIdx.x / K::kMaps, rank, it.second);
-    const int br = t * 128 + row;
+    const int br = t * g.rows + row;
     if (r.live && o.half == 0) {
       slot[br] = r.m;
-      slot[p.block + br] = r.sum;
+      slot[p.pitch + br] = r.sum;
     }
-    to = reinterpret_cast<float4 *>(slot + 2 * p.block) + br;
-    stride = p.block;
+    to = reinterpret_cast<float4 *>(slot + 2 * p.pitch) + br;
+    stride = p.pitch;
   } else if (K::kMaps == 1 && r.live && o.half == 0 && p.a.lse != nullptr) {
     p.a.lse[(long long)(it.first + r.tok) * p.a.q_heads + r.head] = chunk_lse(r.m, r.sum);
   }
@@ -854,7 +894,7 @@ __device__ __forceinline__ void soft_role(const Geometry &g, Shared &sm, uint32_
   const ChunkArgs &a = p.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp & 3, half = warp >> 2, row = pair * 32 + lane;
   const int all = g.columns / 16 * K::kMaps, chunk0 = half ? (all + 1) / 2 : 0, chunk1 = half ? all : (all + 1) / 2;
-  uint32_t s = 0, tile = 0, crossed = 0;
+  uint32_t steps[2] = {0, 0}, tile = 0, crossed = 0;   // of the two accumulators
   for (uint32_t n = 0;; ++n) {
     const int e = n % kItems;
     const bool here = wait(sm, &sm.item_full[e], n / kItems & 1);
@@ -867,43 +907,44 @@ __device__ __forceinline__ void soft_role(const Geometry &g, Shared &sm, uint32_
     Rows r[2];
 #pragma unroll
     for (int t = 0; t < K::kTiles; ++t) {
-      const bool live = t * 128 + row < it.rows;
-      const int tok = (it.r0 + t * 128 + row) / p.group;
-      r[t].m = -INFINITY;
+      const bool live = row < g.rows && t * g.rows + row < it.rows;
+      const int tok = (it.r0 + t * g.rows + row) / p.group;
+      r[t].m = live ? -INFINITY : INFINITY;                      // rows of no token, whatever they hold, never move the others' maxima,
       r[t].l = 0.0f;
-      r[t].lo = live ? chunk_lo(a, seq, tok) : 0;                // rows of no token are zeros: no mask for them
+      r[t].lo = live ? chunk_lo(a, seq, tok) : 0;                // and ask for no mask
       r[t].hi = live ? chunk_hi(a, seq, tok) : 0x7fffffff;
       r[t].started = false;
-      r[t].last = 0;
     }
     if (K::kTiles == 1) r[1] = r[0];
+    const bool two = it.ta[0] < it.tb[0] && it.ta[1] < it.tb[1];
 #pragma unroll 1
     for (int j = it.ka; j < it.kb; ++j, ++tile) {
 #pragma unroll 1
       for (int t = 0; t < K::kTiles; ++t) {
         if (t == 0 ? j < it.ta[0] || j >= it.tb[0] : j < it.ta[1] || j >= it.tb[1]) continue;
         Rows x = t == 0 ? r[0] : r[1];
-        wait(sm, &sm.s_full[s & 1], s >> 1 & 1);
+        const int b = two ? t : (j - it.ka) & 1;
+        const uint32_t s = b == 0 ? steps[0] : steps[1], others = b == 0 ? steps[1] : steps[0];
+        wait(sm, &sm.s_full[b], s & 1);
         tc_fence_after();
-        if (t * 128 + pair * 32 < it.rows) {   // else nobody's rows, whatever becomes of them
+        if (t * g.rows + pair * 32 < it.rows) {   // else nobody's rows, whatever becomes of them
           const int key0 = j * kKeys, kmax = min(kKeys, (t == 0 ? it.thi[0] : it.thi[1]) - key0);
           // columns past kmax have not been computed
           const int from = max(0, min(kKeys, x.lo - key0)) - half * 64, to = max(0, min(kmax, x.hi - key0)) - half * 64;
-          weights<K>(g, sm, x, s, tmem, t, chunk0, chunk1, from, to, sm.skip[tile % kTileInfo]);
+          weights<K>(g, sm, x, tmem, t, chunk0, chunk1, from, to, sm.skip[tile % kTileInfo], b, two, others);
+        } else if (lane == 0) {
+          mbar_arrive(&sm.p_full[b][0]);
+          mbar_arrive(&sm.p_full[b][1]);
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.p_full[s & 1]);
         x.started = true;
-        x.last = s;
         (t == 0 ? r[0] : r[1]) = x;
-        ++s;
+        ++(b == 0 ? steps[0] : steps[1]);
       }
     }
-    if (it.ka < it.kb) {
-      wait(sm, &sm.pv_done[(s - 1) & 1], (s - 1) >> 1 & 1);
-      tc_fence_after();
-    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      if (steps[b] > 0) wait(sm, &sm.pv_done[b], (steps[b] - 1) & 1);
+    tc_fence_after();
     const bool sends = (pair >> 1) != rank;   // diff: the other CTA finishes these rows
     if (K::kMaps == 2 && it.whole && sends && crossed > 0) wait_cluster(sm, &sm.x_empty, (crossed - 1) & 1);
     const size_t stride = (size_t)64 * all * 16 * K::kTiles;
@@ -914,8 +955,8 @@ __device__ __forceinline__ void soft_role(const Geometry &g, Shared &sm, uint32_
       pair_sync(pair);
       end.sum = x.l + sm.row[half ^ 1][row];
       pair_sync(pair);
-      end.live = t * 128 + row < it.rows;
-      const int at = it.r0 + (end.live ? t * 128 + row : 0);
+      end.live = row < g.rows && t * g.rows + row < it.rows;
+      const int at = it.r0 + (end.live ? t * g.rows + row : 0);
       end.tok = at / p.group;
       end.head = it.unit * p.group + at - end.tok * p.group;
       end.m = x.m;
@@ -926,7 +967,7 @@ __device__ __forceinline__ void soft_role(const Geometry &g, Shared &sm, uint32_
     };
 #pragma unroll 1
     for (int t = 0; t < K::kTiles; ++t) {
-      if (t * 128 + pair * 32 >= it.rows) break;
+      if (t * g.rows + pair * 32 >= it.rows) break;
       const RowEnd end = end_of(t);
       finish<K>(g, it, end, rank, t, tmem, sends, g.exchange + blockIdx.x * stride);
     }
@@ -941,7 +982,7 @@ __device__ __forceinline__ void soft_role(const Geometry &g, Shared &sm, uint32_
       wait_cluster(sm, &sm.x_full, crossed & 1);
 #pragma unroll 1
       for (int t = 0; t < K::kTiles; ++t) {
-        if (t * 128 + pair * 32 >= it.rows) break;
+        if (t * g.rows + pair * 32 >= it.rows) break;
         const RowEnd end = end_of(t);
         finish_difference<K>(g, sm, it, end, rank, t, tmem, reinterpret_cast<const float4 *>(g.exchange + (blockIdx.x ^ 1) * stride));
       }
@@ -954,7 +995,8 @@ __device__ __forceinline__ void soft_role(const Geometry &g, Shared &sm, uint32_
 
 template <typename K>
 __global__ void __launch_bounds__(kThreads, 1)
-chunk_bf16_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
+chunk_bf16_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
+                  const __grid_constant__ CUtensorMap qmap) {
   extern __shared__ __align__(1024) char smem_raw[];
   Shared &sm = *reinterpret_cast<Shared *>(smem_raw);
   char *qs = smem_raw + kHead;
@@ -964,20 +1006,22 @@ chunk_bf16_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CU
   if (tid == 0) {
     asm volatile("prefetch.tensormap [%0];" :: "l"(&kmap) : "memory");
     asm volatile("prefetch.tensormap [%0];" :: "l"(&vmap) : "memory");
+    asm volatile("prefetch.tensormap [%0];" :: "l"(&qmap) : "memory");
     for (int i = 0; i < g.slots; ++i) {
       mbar_init(&sm.full[i], 1);
-      mbar_init(&sm.empty[i], 1);
+      mbar_init(&sm.empty[i], 2);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sm.q_full[i], 2);
-      mbar_init(&sm.q_empty[i], 1);
+      mbar_init(&sm.q_full[i], 1);
+      mbar_init(&sm.q_empty[i], 2);
       mbar_init(&sm.s_full[i], 1);
-      mbar_init(&sm.p_full[i], kSoftWarps);
+      mbar_init(&sm.p_full[i][0], kSoftWarps);
+      mbar_init(&sm.p_full[i][1], kSoftWarps);
       mbar_init(&sm.pv_done[i], 1);
     }
     for (int i = 0; i < kItems; ++i) {
       mbar_init(&sm.item_full[i], 1);
-      mbar_init(&sm.item_empty[i], kSoftWarps + 2);
+      mbar_init(&sm.item_empty[i], kSoftWarps + 3);
     }
     mbar_init(&sm.x_full, kSoftWarps / 2);
     mbar_init(&sm.x_empty, kSoftWarps / 2);
@@ -1008,9 +1052,9 @@ chunk_bf16_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CU
     soft_role<K>(g, sm, tmem, rank);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    if (warp == kMmaWarp) product_role<K>(g, sm, qs, ring, tmem);
+    if (warp == kMmaWarp || warp == kMmaWarp + 3) product_role<K>(g, sm, qs, ring, tmem, warp != kMmaWarp);
     else if (warp == kLoadWarp) load_role<K>(g, sm, ring, &kmap, &vmap, rank);
-    else query_role<K>(g, sm, qs, rank);
+    else query_role<K>(g, sm, qs, &qmap, rank);
   }
   __syncwarp();
   tc_fence_before();
@@ -1033,7 +1077,10 @@ template <typename K>
 cudaError_t launch_kind(Geometry g, cudaStream_t s) {
   ChunkShape &p = g.p;
   const CacheLayer &c = p.a.cache;
-  p.block = 128 * K::kTiles;
+  const int tokens = p.group <= 128 ? 128 / p.group : 0;   // of a row tile
+  g.rows = tokens > 0 ? tokens * p.group : 128;
+  p.block = g.rows * K::kTiles;
+  p.pitch = (p.block + 3) & ~3;
   constexpr size_t kMost = 227 << 10;
   const size_t fixed = kHead + (size_t)K::kTiles * g.chunks * kChunkBytes, slot = (size_t)g.panel_chunks * kChunkBytes;
   g.slots = (int)((kMost - fixed) / slot);
@@ -1042,13 +1089,19 @@ cudaError_t launch_kind(Geometry g, cudaStream_t s) {
   // before the maps are encoded: a host thread's first runtime call gives it its context
   cudaError_t e = allow_smem(reinterpret_cast<const void *>(&chunk_bf16_kernel<K>), smem);
   if (e != cudaSuccess) return e;
-  CUtensorMap maps[2];
+  CUtensorMap maps[3];
   const uint64_t row = (uint64_t)c.dim * 2, strides[3] = {(uint64_t)c.token_stride, c.heads > 1 ? (uint64_t)c.head_stride : row,
                                                           c.num_pages > 1 ? (uint64_t)c.page_stride : row};
   const uint64_t dims[4] = {(uint64_t)c.dim, (uint64_t)c.page_size, (uint64_t)c.heads, (uint64_t)c.num_pages};
   const uint32_t box[4] = {64, 1u << g.box_log, 1, 1};
   for (int i = 0; i < 2; ++i)
     if (!encode_rows_map(&maps[i], i ? c.v : c.k, false, 4, dims, strides, box)) return cudaErrorInvalidValue;
+  // q by element, head of its map, map, token; what no map can say (tokens 0 or 2^40 bytes apart) goes by rows
+  const uint64_t q_dims[4] = {(uint64_t)c.dim, (uint64_t)p.a.q_heads / K::kMaps, (uint64_t)K::kMaps, (uint64_t)(p.a.tokens > 0 ? p.a.tokens : 1)};
+  const uint64_t q_strides[3] = {row * K::kMaps, row, p.a.tokens > 1 ? (uint64_t)p.a.q_stride : row * p.a.q_heads};
+  const uint32_t q_box[4] = {64, (uint32_t)p.group, 1, (uint32_t)tokens};
+  g.q_boxes = tokens > 0 && p.a.q != nullptr && q_strides[2] > 0 && encode_rows_map(&maps[2], p.a.q, false, 4, q_dims, q_strides, q_box);
+  if (!g.q_boxes) maps[2] = maps[0];
   int ctas = sm_count();
   if (ctas > kMaxTensorCtas) ctas = kMaxTensorCtas;
   p.shares = ctas / K::kMaps;
@@ -1064,7 +1117,7 @@ cudaError_t launch_kind(Geometry g, cudaStream_t s) {
   at[1].val.clusterDim = {2, 1, 1};
   cfg.attrs = at;
   cfg.numAttrs = K::kMaps;
-  e = cudaLaunchKernelEx(&cfg, chunk_bf16_kernel<K>, g, maps[0], maps[1]);
+  e = cudaLaunchKernelEx(&cfg, chunk_bf16_kernel<K>, g, maps[0], maps[1], maps[2]);
   return e == cudaSuccess ? launch_chunk_join(p, s) : e;
 }
 

@@ -174,13 +174,13 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_f32_kernel(const __grid_co
           if (r >= it.rows) continue;
           if (tx == 0) {
             slot[r] = m[i];
-            slot[p.block + r] = l[i];
+            slot[p.pitch + r] = l[i];
           }
 #pragma unroll
           for (int j = 0; j < NC; ++j) {
             const int d = tx * 4 + 64 * j;
             if (d < p.dv)
-              reinterpret_cast<float4 *>(slot + 2 * p.block)[(long long)(d / 4) * p.block + r] = make_float4(o[i][j][0], o[i][j][1], o[i][j][2], o[i][j][3]);
+              reinterpret_cast<float4 *>(slot + 2 * p.pitch)[(long long)(d / 4) * p.pitch + r] = make_float4(o[i][j][0], o[i][j][1], o[i][j][2], o[i][j][3]);
           }
         }
         continue;
@@ -252,7 +252,7 @@ cudaError_t launch_f32(ChunkShape p, cudaStream_t s) {
   const int D = p.a.cache.dim;
   const size_t smem = sizeof(SimtShared) + sizeof(float) * ((kSimtRows + kSimtKeys) * (D + kPad) + kSimtKeys * (p.dv + kPad) +
                                                              kSimtRows * (kSimtKeys + kPad) + (p.maps == 2 ? kSimtRows * (p.dv + kPad) : 0));
-  p.block = kSimtRows;
+  p.block = p.pitch = kSimtRows;
   p.tile = kSimtKeys;
   int shares = sm_count() * (int)((227 << 10) / (smem + 1024));
   p.shares = shares < kMaxShares ? shares : kMaxShares;

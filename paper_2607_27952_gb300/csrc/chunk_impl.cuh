@@ -26,6 +26,7 @@ struct ChunkShape {   // the same for every CTA
   ChunkArgs a;
   int units, group;   // kv-heads (diff: pairs of them); query heads (pairs) per unit
   int block, tile;    // rows of an item, keys of a tile
+  int pitch;          // rows of a part: the block's, up to a multiple of 4
   int dv, maps;       // width of a value; 2 for diff
   int shares;
   float scale2;       // times log2(e)
@@ -44,11 +45,12 @@ cudaError_t launch_chunk_bf16(ChunkShape p, float *exchange, cudaStream_t s);
 // Adds up what the cuts have parted.
 cudaError_t launch_chunk_join(const ChunkShape &p, cudaStream_t s);
 
-__host__ __device__ inline size_t chunk_slot_floats(int block, int dv) { return (size_t)block * (dv + 2); }
+// A part: its rows' maxima and sums, then four columns of all rows at a time.
+__host__ __device__ inline size_t chunk_slot_floats(int pitch, int dv) { return (size_t)pitch * (dv + 2); }
 
 #ifdef __CUDACC__
 __device__ __forceinline__ float *chunk_slot(const ChunkShape &p, int share, int map, int second) {
-  return p.parts + (((size_t)share * p.maps + map) * 2 + second) * chunk_slot_floats(p.block, p.dv);
+  return p.parts + (((size_t)share * p.maps + map) * 2 + second) * chunk_slot_floats(p.pitch, p.dv);
 }
 
 __device__ __forceinline__ float chunk_exp2(float x) {
