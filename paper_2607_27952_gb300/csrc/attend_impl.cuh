@@ -22,6 +22,7 @@
 #include "cache_internal.h"
 #include "last_device.cuh"
 #include "last_internal.h"
+#include "mma16816.cuh"
 #include "tensor_map.h"
 
 namespace last {
@@ -126,13 +127,6 @@ __device__ __forceinline__ int tiles_of(Keys k, int tile) {
 // Where a row of a tile lies: boxes of 2^box_log rows, in each the 128-byte columns one after the other.
 __device__ __forceinline__ uint32_t row_at(const Shape &p, int row) {
   return ((row >> p.box_log) * p.chunks << (p.box_log + 7)) + (row & ((1 << p.box_log) - 1)) * 128;
-}
-
-// Two values rounded to bf16, the first in the low half.
-__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
-  return r;
 }
 
 __device__ __forceinline__ float join_factor(float top, float all) { return top == -INFINITY ? 1.0f : exp2_fast(top - all); }

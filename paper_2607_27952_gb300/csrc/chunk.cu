@@ -8,6 +8,11 @@ namespace {
 constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinCtas = 2;
 
+template <int N>
+struct Count {
+  static constexpr int value = N;
+};
+
 template <typename T>
 __device__ __forceinline__ void join_store(T *to, const float (&v)[8], int n) {   // 4 or 8 of v
   if constexpr (sizeof(T) == 4) {
@@ -22,7 +27,7 @@ __device__ __forceinline__ void join_store(T *to, const float (&v)[8], int n) { 
 }
 
 // CTA (w, y) belongs to the item that share w ends within, if any.  The CTAs of all its cuts divide its rows, 32 at a
-// time: a lane has a row, a warp every eighth group of 8 columns.
+// time (8, 16 where blocks have no more): a lane has a row, a warp's 32 / rows lanes of a row and the warps the groups of 8 columns by turns.
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const __grid_constant__ ChunkShape p) {
   __shared__ int first_cut, last_cut, share_of[kMaxShares + 1], parts;
@@ -47,21 +52,26 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const __grid_c
       atomicMax(&last_cut, i);
     }
   __syncthreads();
-  if (tid == 0) {
+  if (warp == 0) {   // the shares with a part: the first, and those that end at another tile than the one before
     int n = 0;
-    for (int i = first_cut; i <= last_cut + 1; ++i) {   // the cuts in between are in the item too
-      const bool some = i == first_cut || i > last_cut || tile_at(i) != tile_at(i - 1);
-      if (some) share_of[n++] = i;
+    for (int i0 = first_cut; i0 <= last_cut + 1; i0 += 32) {   // the cuts in between are in the item too
+      const int i = i0 + lane;
+      const bool some = i <= last_cut + 1 && (i == first_cut || i > last_cut || tile_at(i) != tile_at(i - 1));
+      const unsigned all = __ballot_sync(~0u, some);
+      if (some) share_of[n + __popc(all & ((1u << lane) - 1))] = i;
+      n += __popc(all);
     }
-    parts = n;
+    if (lane == 0) parts = n;
   }
   __syncthreads();
+  const int per = p.block <= 8 ? 8 : p.block <= 16 ? 16 : 32, groups = kJoinWarps * (32 / per);
+  const int in_row = lane & (per - 1), group = warp * (32 / per) + lane / per;
   const int me = (w - first_cut) * gridDim.y + blockIdx.y, ctas = (last_cut - first_cut + 1) * gridDim.y;
   unsigned bad = 0;
   const ChunkSeq s = chunk_seq(a, x.x, &bad);
   const int r0 = x.z * p.block, rows = (int)min((long long)p.block, (long long)s.n * p.group - r0);
-  for (int row0 = me * 32; row0 < rows; row0 += ctas * 32) {
-    const int r = row0 + lane;
+  for (int row0 = me * per; row0 < rows; row0 += ctas * per) {
+    const int r = row0 + in_row;
     const bool live = r < rows;
     const int t = (r0 + (live ? r : 0)) / p.group, h = x.y * p.group + (r0 + (live ? r : 0)) - t * p.group;
     float acc[4][8], sq = 0.0f;
@@ -73,21 +83,23 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const __grid_c
       auto slot = [&](int i) { return chunk_slot(p, share_of[i], map, i == 0); };   // an item begins in its first share
       float all = -INFINITY, sum = 0.0f;
       if (live) {
+#pragma unroll 8
         for (int i = 0; i < parts; ++i) all = fmaxf(all, slot(i)[r]);
+#pragma unroll 8
         for (int i = 0; i < parts; ++i) sum = fmaf(chunk_factor(slot(i)[r], all), slot(i)[p.pitch + r], sum);
       }
       const float weight = map == 0 ? 1.0f : live ? -a.lambda[h] : 0.0f;
-      if (live && p.maps == 1 && a.lse != nullptr && warp == 0) a.lse[(long long)(s.first + t) * a.q_heads + h] = chunk_lse(all, sum);
+      if (live && p.maps == 1 && a.lse != nullptr && group == 0) a.lse[(long long)(s.first + t) * a.q_heads + h] = chunk_lse(all, sum);
       if (!live || sum == 0.0f) continue;
       const float g = weight / sum;
-      for (int i = 0; i < parts; ++i) {
+      auto add = [&](int i, auto last) {   // the groups of 8 columns of the thread: four, or one
         const float *from = slot(i);
         const float f = chunk_factor(from[r], all) * g;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < decltype(last)::value; ++j)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int four = (warp + 8 * j) * 2 + e;
+            const int four = (group + groups * j) * 2 + e;
             if (four * 4 >= p.dv) continue;
             const float4 y = reinterpret_cast<const float4 *>(from + 2 * p.pitch)[(long long)four * p.pitch + r];
             acc[j][4 * e] = fmaf(y.x, f, acc[j][4 * e]);
@@ -95,6 +107,12 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const __grid_c
             acc[j][4 * e + 2] = fmaf(y.z, f, acc[j][4 * e + 2]);
             acc[j][4 * e + 3] = fmaf(y.w, f, acc[j][4 * e + 3]);
           }
+      };
+      if (groups * 8 >= p.dv) {   // parts' loads side by side
+#pragma unroll 8
+        for (int i = 0; i < parts; ++i) add(i, Count<1>{});
+      } else {
+        for (int i = 0; i < parts; ++i) add(i, Count<4>{});
       }
     }
     if (p.maps == 2) {
@@ -106,13 +124,14 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const __grid_c
       squares[warp][lane] = sq;
       __syncthreads();
       sq = 0.0f;
-      for (int i = 0; i < kJoinWarps; ++i) sq += squares[i][lane];
+      for (int i = 0; i < kJoinWarps; ++i)
+        for (int j = in_row; j < 32; j += per) sq += squares[i][j];
       const float f = chunk_norm(a, sq, p.dv);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int d = (warp + 8 * j) * 8 + e;
+          const int d = (group + groups * j) * 8 + e;
           if (d < p.dv) acc[j][e] *= f * (a.norm_weight ? a.norm_weight[d] : 1.0f);
         }
     }
@@ -120,7 +139,7 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const __grid_c
     T *out = reinterpret_cast<T *>(a.out + (long long)(s.first + t) * a.out_stride) + (long long)h * p.dv;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int d = (warp + 8 * j) * 8;
+      const int d = (group + groups * j) * 8;
       if (d < p.dv) join_store(out + d, acc[j], p.dv - d);
     }
   }
@@ -165,7 +184,11 @@ cudaError_t launch_chunk(const ChunkArgs &a, cudaStream_t s) {
   p.cuts = reinterpret_cast<int4 *>(a.ws + kStatusBytes);
   p.parts = reinterpret_cast<float *>(a.ws + kStatusBytes + align256(sizeof(int4) * kMaxShares));
   float *exchange = reinterpret_cast<float *>(reinterpret_cast<char *>(p.parts) + parts_bytes(a.cache.dim, a.elem));
-  return a.elem == 4 ? launch_chunk_f32(p, s) : launch_chunk_bf16(p, exchange, s);
+  if (a.elem == 4) return launch_chunk_f32(p, s);
+  // few rows per sequence, on average: no tile of 128 rows is worth its products
+  const long long rows = a.seq.batch > 0 ? ((long long)a.tokens * p.group + a.seq.batch - 1) / a.seq.batch : 0;
+  if (rows <= (a.diff || a.cache.dim > 128 ? 8 : 16)) return a.diff ? launch_diff_few(p, s) : launch_chunk_few(p, (int)rows, s);
+  return launch_chunk_bf16(p, exchange, s);
 }
 
 }  // namespace last

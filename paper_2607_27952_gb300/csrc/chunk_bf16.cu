@@ -64,34 +64,10 @@ struct alignas(16) Shared {
 };
 static_assert(sizeof(Shared) <= kHead, "the panels begin behind it");
 
-// Waits end after two seconds by the clock.
-constexpr unsigned long long kWaitNanoseconds = 2000000000ull;
-struct Limit {
-  unsigned long long begin = 0;
-  uint32_t tries = 0;
-  __device__ __forceinline__ bool over(const Shared &sm) {
-    if ((tries++ & 63) != 0) return false;
-    unsigned long long now;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-    if (begin == 0) begin = now;
-    return sm.dead != 0 || now - begin > kWaitNanoseconds;
-  }
-};
-// A whole warp waits, with a limit; the first to give up has every other wait of the CTA end too.  The softmax warps go on
-// after a wait that gave up, with whatever is there, to the end of their item, so that no barrier of theirs waits for a warp
-// that has left; the others leave.
-__device__ __forceinline__ bool wait(Shared &sm, unsigned long long *bar, uint32_t parity) {
-  bool ok = mbar_try_wait(bar, parity);
-  if (!ok)
-    for (Limit limit; !ok && !limit.over(sm);) ok = mbar_try_wait(bar, parity);
-  if (__all_sync(~0u, ok)) return true;
-  sm.dead = 1;
-  return false;
-}
 // For what the other CTA of the cluster has written.
 __device__ __forceinline__ bool wait_cluster(Shared &sm, unsigned long long *bar, uint32_t parity) {
   uint32_t ok = 0;
-  for (Limit limit; !ok && !limit.over(sm);)
+  for (ChunkLimit limit; !ok && !limit.over(sm);)
     asm volatile("{\n\t.reg .pred p;\n\t"
                  "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
                  "selp.u32 %0, 1, 0, p;\n\t}"
@@ -157,12 +133,6 @@ __device__ __forceinline__ float2 unpack2(uint64_t v) {
   asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
   return f;
 }
-__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {   // x in the low half
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
-  return r;
-}
-
 // One lane of a converged warp, always the same.
 __device__ __forceinline__ bool elected() {
   uint32_t r;

@@ -19,6 +19,7 @@
 #include "cache_internal.h"
 #include "last_device.cuh"
 #include "last_internal.h"
+#include "mma16816.cuh"
 
 namespace last {
 
@@ -42,6 +43,10 @@ constexpr int kItemKeys = 128, kLeastTiles = 1;
 
 cudaError_t launch_chunk_f32(ChunkShape p, cudaStream_t s);
 cudaError_t launch_chunk_bf16(ChunkShape p, float *exchange, cudaStream_t s);
+// bf16, few rows: `rows` of a sequence and unit on average.
+cudaError_t launch_chunk_few(const ChunkShape &p, int rows, cudaStream_t s);
+cudaError_t launch_chunk_few_wide(const ChunkShape &p, cudaStream_t s);
+cudaError_t launch_diff_few(const ChunkShape &p, cudaStream_t s);
 // Adds up what the cuts have parted.
 cudaError_t launch_chunk_join(const ChunkShape &p, cudaStream_t s);
 
@@ -57,6 +62,33 @@ __device__ __forceinline__ float chunk_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// Waits end after two seconds by the clock.
+constexpr unsigned long long kWaitNanoseconds = 2000000000ull;
+struct ChunkLimit {
+  unsigned long long begin = 0;
+  uint32_t tries = 0;
+  template <typename S>
+  __device__ __forceinline__ bool over(const S &sm) {
+    if ((tries++ & 63) != 0) return false;
+    unsigned long long now;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+    if (begin == 0) begin = now;
+    return sm.dead != 0 || now - begin > kWaitNanoseconds;
+  }
+};
+// A whole warp waits, with a limit; the first to give up has every other wait of the CTA end too.  Warps that meet
+// in barriers go on after a wait that gave up, with whatever is there, to the end of their item, so that no barrier waits for one
+// that has left; the others leave.
+template <typename S>
+__device__ __forceinline__ bool wait(S &sm, unsigned long long *bar, uint32_t parity) {
+  bool ok = mbar_try_wait(bar, parity);
+  if (!ok)
+    for (ChunkLimit limit; !ok && !limit.over(sm);) ok = mbar_try_wait(bar, parity);
+  if (__all_sync(~0u, ok)) return true;
+  sm.dead = 1;
+  return false;
 }
 
 struct ChunkSeq {   // n new tokens from token `first` on, behind `base` cached ones; keys begin .. lens - 1
