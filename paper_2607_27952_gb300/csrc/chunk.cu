@@ -187,7 +187,13 @@ cudaError_t launch_chunk(const ChunkArgs &a, cudaStream_t s) {
   if (a.elem == 4) return launch_chunk_f32(p, s);
   // few rows per sequence, on average: no tile of 128 rows is worth its products
   const long long rows = a.seq.batch > 0 ? ((long long)a.tokens * p.group + a.seq.batch - 1) / a.seq.batch : 0;
-  if (rows <= (a.diff || a.cache.dim > 128 ? 8 : 16)) return a.diff ? launch_diff_few(p, s) : launch_chunk_few(p, (int)rows, s);
+  const int d = a.cache.dim;
+  const bool whole = d == 64 || d == 128;
+  if (rows <= (a.diff || !whole ? 8 : 16)) {
+    if (a.diff) return whole ? launch_diff_few(p, s) : launch_diff_few_any(p, s);
+    if (!whole) return launch_chunk_few_any(p, s);
+    return d == 64 ? launch_chunk_few_64(p, rows > 8, s) : launch_chunk_few_128(p, rows > 8, s);
+  }
   return launch_chunk_bf16(p, exchange, s);
 }
 

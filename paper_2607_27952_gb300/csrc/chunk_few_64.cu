@@ -1,0 +1,11 @@
+// Few rows per sequence, chunk attention: heads of 64 elements.
+#include "chunk_few_impl.cuh"
+
+namespace last {
+
+cudaError_t launch_chunk_few_64(const ChunkShape &p, bool sixteen, cudaStream_t s) {
+  const Few f = few_of(p);
+  return sixteen ? launch_kind<Kind<1, 2, 1, true>>(f, s) : launch_kind<Kind<1, 1, 1, true>>(f, s);
+}
+
+}  // namespace last

@@ -46,9 +46,12 @@ struct alignas(16) Shared {
   volatile unsigned dead;
 };
 
-// CHUNKS: 128-byte columns of a head's row; EIGHTS: groups of 8 rows of a block.
-template <int CHUNKS, int EIGHTS, int MAPS>
+// CHUNKS: 128-byte columns of a head's row; EIGHTS: groups of 8 rows of a block; FULL: the columns are, so that the steps along a
+// row are known and their loads and products go between each other.
+template <int CHUNKS, int EIGHTS, int MAPS, bool FULL>
 struct Kind {
+  static constexpr bool kFull = FULL;
+  static __device__ __forceinline__ int dim(const ChunkShape &p) { return FULL ? CHUNKS * 64 : p.a.cache.dim; }
   static constexpr int kChunks = CHUNKS, kEights = EIGHTS, kMaps = MAPS, kRows = 8 * EIGHTS;
   static constexpr int kConsumers = 4 * MAPS, kThreads = 32 * (kConsumers + MAPS), kCtas = MAPS == 2 || CHUNKS > 2 ? 1 : 2;
   static constexpr int kSteps = CHUNKS * 4;   // 16-wide along a row
@@ -84,7 +87,8 @@ __device__ __forceinline__ void produce(const Few &f, typename K::Sm &sm, char *
   const ChunkShape &p = f.p;
   const CacheLayer &c = p.a.cache;
   const int lane = threadIdx.x & 31, box = 1 << f.box_log, boxes = kTile >> f.box_log, mine = lane & (boxes - 1);
-  const int ops = boxes * (f.joined ? 1 : K::kChunks), size = c.page_size, row_bytes = c.dim * 2;
+  const bool joined = K::kFull || f.joined;
+  const int ops = boxes * (joined ? 1 : K::kChunks), size = c.page_size, row_bytes = c.dim * 2;
   ChunkWalk walk(sm.share);
   ChunkItem it;
   Place at{0, 0};
@@ -160,7 +164,7 @@ __device__ __forceinline__ void produce(const Few &f, typename K::Sm &sm, char *
         if (here) {
           const CUtensorMap *m = is_v ? vmap : kmap;
           char *to = ring + at.slot * K::kPanel + (mine * K::kChunks << (f.box_log + 7));
-          if (f.joined) {
+          if (joined) {
             if (lane < boxes) tma_load_5d(to, m, 0, row, 0, head, page, bar);
           } else {
             for (int i = lane; i < ops; i += 32) {
@@ -226,7 +230,7 @@ struct Part {
 
   // Weights of the warp's 16 keys, row0 .. of the tile and key0 .. of the sequence.
   __device__ __forceinline__ void logits(const Few &f, const Item &it, uint32_t k, int row0, int key0, unsigned skip) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, D = f.p.a.cache.dim, column = 128 << f.box_log;
+    const int lane = threadIdx.x & 31, g = lane >> 2, D = K::dim(f.p), column = 128 << f.box_log;
     const float scale2 = f.p.scale2;
     float s[2][kEights][4] = {};   // even and odd steps
     {   // 8 x 8 blocks (keys 0-7 | 8-15) x (16-byte column even | odd)
@@ -321,7 +325,7 @@ struct Part {
   // o[v] += weights x V.
   template <int V>
   __device__ __forceinline__ void values(const Few &f, uint32_t panel, int row0, int key0) {
-    const int lane = threadIdx.x & 31, D = f.p.a.cache.dim, column = 128 << f.box_log;
+    const int lane = threadIdx.x & 31, D = K::dim(f.p), column = 128 << f.box_log;
     // 8 x 8 blocks, transposed on the way: (keys 0-7 | 8-15) x (16-byte column even | odd)
     const int row = row0 + (lane & 7) + (lane >> 4) * 8, sub = lane >> 3 & 1;
     const uint32_t base = panel + row_at(f, row);
@@ -375,7 +379,7 @@ struct Part {
   // The same on the CUDA cores, each row with the keys that it sees alone.
   template <int V>
   __device__ __forceinline__ void one_by_one(const Few &f, uint32_t panel, int row0, int key0) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, D = f.p.a.cache.dim, column = 128 << f.box_log;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, D = K::dim(f.p), column = 128 << f.box_log;
 #pragma unroll 1
     for (int i = 0; i < 16; ++i) {
       const uint32_t base = panel + row_at(f, row0 + i);
@@ -420,7 +424,7 @@ __device__ __forceinline__ void add_up(const Few &f, typename K::Sm &sm, Part<K>
   constexpr int kMaps = K::kMaps, kEights = K::kEights, kPasses = K::kMaps * K::kChunks;
   const ChunkShape &p = f.p;
   const ChunkArgs &a = p.a;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3, D = a.cache.dim;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3, D = K::dim(p);
 #pragma unroll
   for (int e = 0; e < kEights; ++e)
 #pragma unroll
@@ -546,7 +550,7 @@ __device__ __forceinline__ void add_up(const Few &f, typename K::Sm &sm, Part<K>
 template <typename K>
 __device__ __forceinline__ void consume(const Few &f, typename K::Sm &sm, char *ring, char *qs) {
   const ChunkShape &p = f.p;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, map = warp >> 2, row0 = (warp & 3) * 16, D = p.a.cache.dim;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, map = warp >> 2, row0 = (warp & 3) * 16, D = K::dim(p);
   const uint32_t ring_at = smem_addr(ring);
   Part<K> part;
   Place at{0, 0};

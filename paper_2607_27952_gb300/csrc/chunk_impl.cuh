@@ -43,10 +43,12 @@ constexpr int kItemKeys = 128, kLeastTiles = 1;
 
 cudaError_t launch_chunk_f32(ChunkShape p, cudaStream_t s);
 cudaError_t launch_chunk_bf16(ChunkShape p, float *exchange, cudaStream_t s);
-// bf16, few rows: `rows` of a sequence and unit on average.
-cudaError_t launch_chunk_few(const ChunkShape &p, int rows, cudaStream_t s);
-cudaError_t launch_chunk_few_wide(const ChunkShape &p, cudaStream_t s);
+// bf16, few rows; sixteen: in blocks of 16 instead of 8.
+cudaError_t launch_chunk_few_64(const ChunkShape &p, bool sixteen, cudaStream_t s);
+cudaError_t launch_chunk_few_128(const ChunkShape &p, bool sixteen, cudaStream_t s);
+cudaError_t launch_chunk_few_any(const ChunkShape &p, cudaStream_t s);
 cudaError_t launch_diff_few(const ChunkShape &p, cudaStream_t s);
+cudaError_t launch_diff_few_any(const ChunkShape &p, cudaStream_t s);
 // Adds up what the cuts have parted.
 cudaError_t launch_chunk_join(const ChunkShape &p, cudaStream_t s);
 
