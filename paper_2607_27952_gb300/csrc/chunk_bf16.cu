@@ -64,6 +64,14 @@ struct alignas(16) Shared {
 };
 static_assert(sizeof(Shared) <= kHead, "the panels begin behind it");
 
+// The same for one thread.
+__device__ __forceinline__ bool wait_alone(Shared &sm, unsigned long long *bar, uint32_t parity) {
+  bool ok = mbar_try_wait(bar, parity);
+  if (!ok)
+    for (ChunkLimit limit; !ok && !limit.over(sm);) ok = mbar_try_wait(bar, parity);
+  if (!ok) sm.dead = 1;
+  return ok;
+}
 // For what the other CTA of the cluster has written.
 __device__ __forceinline__ bool wait_cluster(Shared &sm, unsigned long long *bar, uint32_t parity) {
   uint32_t ok = 0;
@@ -368,7 +376,7 @@ __device__ __forceinline__ void load_role(const Geometry &g, Shared &sm, char *r
   }
 }
 
-// ---- warps 8 and 11: the products ----
+// ---- warps 8 and 11: the products, all by one thread: votes and reconvergence took a third of the warps' time ----
 // Each has one of the two accumulators of S: its steps are those of a row tile, or, of an item with one row tile, every other
 // one.  A step's S goes to the tensor cores right behind O of the step before, whose weights lay where it goes: products
 // of one thread run in the order they are issued.  What a warp works out and waits for in between hides behind the other's
@@ -392,14 +400,14 @@ struct Tiles {   // of an item, in registers
 __device__ __forceinline__ void zero_rows(uint32_t panel, int chunks, int from, int to) {
 #pragma unroll 1
   for (int c = 0; c < chunks; ++c)
-#pragma unroll 1
-    for (int i = from * 8 + (threadIdx.x & 31); i < to * 8; i += 32)
+#pragma unroll 8
+    for (int i = from * 8; i < to * 8; ++i)
       asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" :: "r"(panel + c * kChunkBytes + i * 16), "r"(0) : "memory");
 }
 
 template <typename K>
 __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char *qs_, char *ring_, uint32_t tmem, int w) {
-  const int lane = threadIdx.x & 31, D = g.p.a.cache.dim;
+  const int D = g.p.a.cache.dim;
   const uint32_t ring = smem_addr(ring_), panel = (uint32_t)g.panel_chunks * kChunkBytes, rows = (uint32_t)g.chunks * (kChunkBytes >> 4);
   const uint64_t q_desc = umma_desc_sw128(smem_addr(qs_)), k_desc = umma_desc_sw128(ring), v_desc = desc_n_major(ring);
   const uint32_t st = tmem + w * 128;
@@ -407,11 +415,10 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
   Place at{0, 0};
   for (uint32_t n = 0;; ++n) {
     const int e = n % kItems;
-    if (!wait(sm, &sm.item_full[e], n / kItems & 1)) return;
+    if (!wait_alone(sm, &sm.item_full[e], n / kItems & 1)) return;
     const bool end = sm.items[e].seq < 0;
     const Tiles it(sm.items[e]);
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sm.item_empty[e]);
+    mbar_arrive(&sm.item_empty[e]);
     if (end) return;
     const bool two = it.two();
     const int t = two ? w : it.ta[0] < it.tb[0] ? 0 : 1, ta = t == 0 ? it.ta[0] : it.ta[1], tb = t == 0 ? it.tb[0] : it.tb[1];
@@ -423,37 +430,34 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
       const bool own = two ? j >= ta && j < tb : ((j - it.ka) & 1) == w;
       const int key0 = j * kKeys, kmin = max(0, tlo - key0), kmax = min(kKeys, thi - key0);
       const int k0 = kmin >> 4, k1 = (kmax + 15) >> 4;
-      if (own && !begun && !wait(sm, &sm.q_full[q], turn / K::kTiles & 1)) return;
+      if (own && !begun && !wait_alone(sm, &sm.q_full[q], turn / K::kTiles & 1)) return;
 #pragma unroll
       for (int pi = 0; pi < K::kPanels; ++pi) {
-        if (!waited && !wait(sm, &sm.full[at.slot], at.round)) return;
+        if (!waited && !wait_alone(sm, &sm.full[at.slot], at.round)) return;
         if (own) {
-          if (elected()) {
-            const uint64_t k_rows = k_desc + at.slot * (panel >> 4), q_rows = q_desc + q * rows + pi * 2 * (kChunkBytes >> 4);
-            const uint32_t idesc = umma_idesc_bf16(128, k1 * 16);
-            const int steps = (D - pi * 128 + 15) / 16;
-            auto product = [&](int k) {
-              const int off = ((k >> 2) * (int)kChunkBytes + (k & 3) * 32) >> 4;
-              umma_bf16(st, q_rows + off, k_rows + off, idesc, (pi | k) != 0 ? 1u : 0u);
-            };
-            if (steps >= 8) {
+          const uint64_t k_rows = k_desc + at.slot * (panel >> 4), q_rows = q_desc + q * rows + pi * 2 * (kChunkBytes >> 4);
+          const uint32_t idesc = umma_idesc_bf16(128, k1 * 16);
+          const int steps = (D - pi * 128 + 15) / 16;
+          auto product = [&](int k) {
+            const int off = ((k >> 2) * (int)kChunkBytes + (k & 3) * 32) >> 4;
+            umma_bf16(st, q_rows + off, k_rows + off, idesc, (pi | k) != 0 ? 1u : 0u);
+          };
+          if (steps >= 8) {
 #pragma unroll
-              for (int k = 0; k < 8; ++k) product(k);
-            } else {
+            for (int k = 0; k < 8; ++k) product(k);
+          } else {
 #pragma unroll 1
-              for (int k = 0; k < steps; ++k) product(k);
-            }
-            if (pi == K::kPanels - 1) umma_commit(&sm.s_full[w]);
-            umma_commit(&sm.empty[at.slot]);
-            if (pi == K::kPanels - 1 && j + (two ? 1 : 2) >= (two ? tb : it.kb)) {   // the row tile's last
-              umma_commit(&sm.q_empty[q]);
-              if (two) umma_commit(&sm.q_empty[q]);
-            }
+            for (int k = 0; k < steps; ++k) product(k);
           }
-        } else if (lane == 0) {
+          if (pi == K::kPanels - 1) umma_commit(&sm.s_full[w]);
+          umma_commit(&sm.empty[at.slot]);
+          if (pi == K::kPanels - 1 && j + (two ? 1 : 2) >= (two ? tb : it.kb)) {   // the row tile's last
+            umma_commit(&sm.q_empty[q]);
+            if (two) umma_commit(&sm.q_empty[q]);
+          }
+        } else {
           mbar_arrive(&sm.empty[at.slot]);
         }
-        __syncwarp();
         at.skip(g, 1);
       }
       const Place v0 = at;
@@ -461,9 +465,9 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
       const int from = max(0, it.lo - key0), to = min(kKeys, it.hi - key0);
 #pragma unroll
       for (int i = 0; i < K::kValues; ++i) {
-        if (!wait(sm, &sm.full[at.slot], at.round)) return;
+        if (!wait_alone(sm, &sm.full[at.slot], at.round)) return;
         if (!own) {
-          if (lane == 0) mbar_arrive(&sm.empty[at.slot]);
+          mbar_arrive(&sm.empty[at.slot]);
         } else if (((from | to) & 15) != 0 || skip != 0) {   // what no row sees is zeroed (by both warps alike)
           const int chunks = K::kPanels == 1 ? g.chunks : min(2, g.chunks - 2 * (i % K::kPanels));
           zero_rows(ring + at.slot * panel, chunks, from & ~15, from);
@@ -472,7 +476,6 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
           for (unsigned left = skip; left != 0; left &= left - 1)
             zero_rows(ring + at.slot * panel, chunks, (__ffs(left) - 1) * 8, __ffs(left) * 8);
           fence_proxy_async_smem();
-          __syncwarp();
         }
         at.skip(g, 1);
       }
@@ -484,17 +487,17 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
           Place next = at;
 #pragma unroll
           for (int pi = 0; pi < K::kPanels; ++pi) {
-            if (!wait(sm, &sm.full[next.slot], next.round)) return;
+            if (!wait_alone(sm, &sm.full[next.slot], next.round)) return;
             next.skip(g, 1);
           }
           waited = true;
         }
         // one row tile: the other warp's O of the step before goes first
-        if (!two && j > it.ka && !wait(sm, &sm.pv_done[w ^ 1], (others - 1) & 1)) return;
+        if (!two && j > it.ka && !wait_alone(sm, &sm.pv_done[w ^ 1], (others - 1) & 1)) return;
         // the first and second 32 keys of either half
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
-          if (!wait(sm, &sm.p_full[w][part], s & 1)) return;
+          if (!wait_alone(sm, &sm.p_full[w][part], s & 1)) return;
           tc_fence_after();
           Place v = v0;
 #pragma unroll
@@ -503,30 +506,27 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
             const int width = K::kPanels == 1 ? g.columns : min(128, g.columns - pi * 128);
             const uint32_t idesc = umma_idesc_bf16(128, width) | kNMajor, d = o + head * g.columns + pi * 128;
             const uint64_t vd = v_desc + v.slot * (panel >> 4);
-            if (elected()) {
-              if (full) {
+            if (full) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+              for (int h = 0; h < 2; ++h)
 #pragma unroll
-                  for (int k2 = 0; k2 < 2; ++k2) {
-                    const int k = 4 * h + 2 * part + k2;
-#pragma unroll
-                    for (int x = 0; x < K::kParts; ++x)
-                      umma_bf16_ts(d, st + 64 * h + 16 * part + 8 * k2 + 32 * x, vd + k * (2048 >> 4), idesc, part == 0 && h + k2 + x == 0 && j == ta ? 0u : 1u);
-                  }
-              } else if (part == 1) {
-#pragma unroll 1
-                for (int k = k0; k < k1; ++k)
+                for (int k2 = 0; k2 < 2; ++k2) {
+                  const int k = 4 * h + 2 * part + k2;
 #pragma unroll
                   for (int x = 0; x < K::kParts; ++x)
-                    umma_bf16_ts(d, st + 32 * x + (k >> 2) * 64 + (k & 3) * 8, vd + k * (2048 >> 4), idesc, j == ta && k == k0 && x == 0 ? 0u : 1u);
-              }
-              if (part == 1) {
-                if (i == K::kValues - 1) umma_commit(&sm.pv_done[w]);
-                umma_commit(&sm.empty[v.slot]);
-              }
+                    umma_bf16_ts(d, st + 64 * h + 16 * part + 8 * k2 + 32 * x, vd + k * (2048 >> 4), idesc, part == 0 && h + k2 + x == 0 && j == ta ? 0u : 1u);
+                }
+            } else if (part == 1) {
+#pragma unroll 1
+              for (int k = k0; k < k1; ++k)
+#pragma unroll
+                for (int x = 0; x < K::kParts; ++x)
+                  umma_bf16_ts(d, st + 32 * x + (k >> 2) * 64 + (k & 3) * 8, vd + k * (2048 >> 4), idesc, j == ta && k == k0 && x == 0 ? 0u : 1u);
             }
-            __syncwarp();
+            if (part == 1) {
+              if (i == K::kValues - 1) umma_commit(&sm.pv_done[w]);
+              umma_commit(&sm.empty[v.slot]);
+            }
             v.skip(g, 1);
           }
         }
@@ -537,8 +537,8 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
     }
     // an item's only step was the other warp's: it has done with the row tile when both say so
     if (!two && !begun && it.ka < it.kb) {
-      if (!wait(sm, &sm.q_full[q], turn / K::kTiles & 1)) return;
-      if (lane == 0) mbar_arrive(&sm.q_empty[q]);
+      if (!wait_alone(sm, &sm.q_full[q], turn / K::kTiles & 1)) return;
+      mbar_arrive(&sm.q_empty[q]);
     }
     q_tile += (it.ta[0] < it.tb[0]) + (it.ta[1] < it.tb[1]);
   }
@@ -1022,8 +1022,9 @@ chunk_bf16_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CU
     soft_role<K>(g, sm, tmem, rank);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    if (warp == kMmaWarp || warp == kMmaWarp + 3) product_role<K>(g, sm, qs, ring, tmem, warp != kMmaWarp);
-    else if (warp == kLoadWarp) load_role<K>(g, sm, ring, &kmap, &vmap, rank);
+    if (warp == kMmaWarp || warp == kMmaWarp + 3) {
+      if (elected()) product_role<K>(g, sm, qs, ring, tmem, warp != kMmaWarp);
+    } else if (warp == kLoadWarp) load_role<K>(g, sm, ring, &kmap, &vmap, rank);
     else query_role<K>(g, sm, qs, &qmap, rank);
   }
   __syncwarp();

@@ -30,6 +30,7 @@ struct ChunkShape {   // the same for every CTA
   int pitch;          // rows of a part: the block's, up to a multiple of 4
   int dv, maps;       // width of a value; 2 for diff
   int shares;
+  int item_keys;      // what an item costs beside its keys, in keys
   float scale2;       // times log2(e)
   int4 *cuts;         // [shares] where a share ends: sequence, unit, block, tile (0: between two items)
   float *parts;       // [shares][maps][2] parted sums: second one where an item begins in the share
@@ -38,8 +39,7 @@ struct ChunkShape {   // the same for every CTA
 constexpr int kMaxShares = 480, kMaxTensorCtas = 160;   // fp32 and bf16
 constexpr int kMaxKeys = 0x7fffff00;   // of a sequence: the last key's tile ends before 2^31
 constexpr float kChunkLog2e = 1.4426950408889634f, kChunkLn2 = 0.6931471805599453f;
-// What an item costs beside its keys, in keys; parts of fewer tiles are not cut off.
-constexpr int kItemKeys = 128, kLeastTiles = 1;
+constexpr int kLeastTiles = 1;   // parts of fewer tiles are not cut off
 
 cudaError_t launch_chunk_f32(ChunkShape p, cudaStream_t s);
 cudaError_t launch_chunk_bf16(ChunkShape p, float *exchange, cudaStream_t s);
@@ -149,7 +149,7 @@ struct ChunkCost {
   __device__ ChunkCost(const ChunkShape &p, const ChunkSeq &s) {
     const long long g = p.group, all = g * max(0, s.lens - s.begin);
     block = p.block;
-    item = g * kItemKeys;
+    item = g * p.item_keys;
     flat = !p.a.causal;
     a = g * ((long long)s.base - s.begin);
     most = p.a.window > 0 ? min(all, g * p.a.window + p.block) : all;
