@@ -13,6 +13,10 @@
 // boxes of the pages, 10 walks the share's items and fetches rows of Q.  V rows that no row sees are zeroed in
 // shared memory before the product reads them: a weight of zero times an infinity or NaN would show.
 // diff: a cluster of two CTAs, one map each; each finishes half of the rows, with the other's half of O through L2.
+//
+// Bound by the way from S to P: 256 rows by 128 keys by 128 columns take 4600 cycles, of which the products are 2048 (16 x 2944 tokens,
+// 16 heads on 4: 560 us, 1.0 PFLOP/s).  TMEM loads, the exchange of the maxima and the exponentials of a step follow each other;
+// 16 softmax warps (687 us) or four buffers of 64 keys (618 us) made no step shorter.
 #include "chunk_impl.cuh"
 #include "tensor_map.h"
 

@@ -14,7 +14,7 @@ constexpr int kSimtThreads = 256, kSimtRows = 64, kSimtKeys = 64, kPad = 4;
 struct alignas(16) SimtShared {
   ChunkShare share;
   unsigned long long sums[kSimtThreads / 32];
-  float top[kSimtRows], sum[kSimtRows], norm[kSimtThreads / 32][kSimtRows];
+  long long at[kSimtKeys];   // where a key of the tile lies in its head's pages; -1: no row of the block sees it, or its page is out of range
   unsigned flags;
 };
 
@@ -66,34 +66,36 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_f32_kernel(const __grid_co
         for (int k = it.k0; k < it.k1; ++k) {
           const int key0 = (it.t.first + k) * kSimtKeys;
           __syncthreads();
-          // K (and V) rows that no row of the block sees, and those of bad pages, are zeros
-          const int wide = fours + p.dv / 4;
-          unsigned skipped = 0;
-          for (int i = tid; i < kSimtKeys * wide; i += kSimtThreads) {
-            const int r = i / wide, d4 = i - r * wide, key = key0 + r;
-            const bool is_v = d4 >= fours;
-            const int d = (is_v ? d4 - fours : d4) * 4;
-            float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (tid < kSimtKeys) {
+            const int key = key0 + tid;
+            long long at = -1;
             if (key >= it.t.lo && key < it.t.hi) {
               const int page = a.seq.table[it.seq * a.seq.table_stride + key / c.page_size];
-              if ((unsigned)page < (unsigned)c.num_pages) {
-                const int head = is_v ? it.unit * p.maps + d / D : it.unit * p.maps + map;
-                const char *row = (is_v ? c.v : c.k) + page * c.page_stride + head * c.head_stride + key % c.page_size * c.token_stride;
-                x = *reinterpret_cast<const float4 *>(row + (is_v ? d % D : d) * 4);
-              } else {
-                skipped = kErrCacheIndex;
-              }
+              if ((unsigned)page < (unsigned)c.num_pages) at = page * c.page_stride + key % c.page_size * c.token_stride;
+              else atomicOr(&sm.flags, kErrCacheIndex);
             }
-            *reinterpret_cast<float4 *>(is_v ? vs + r * ldv + d : ks + r * ld + d) = x;
+            sm.at[tid] = at;
           }
-          if (skipped) atomicOr(&sm.flags, skipped);
+          __syncthreads();
+          // a warp every eighth row, its lanes the pieces of K and V; rows that are not there are zeros
+          for (int d4 = tid & 31; d4 < fours + p.dv / 4; d4 += 32) {
+            const bool is_v = d4 >= fours;
+            const int d = (is_v ? d4 - fours : d4) * 4, head = it.unit * p.maps + (is_v ? d / D : map);
+            const char *from = (is_v ? c.v : c.k) + head * c.head_stride + (is_v ? d % D : d) * 4;
+            float *to = is_v ? vs + d : ks + d;
+            const int pitch = is_v ? ldv : ld;
+            float4 x[kSimtKeys / 8];
+#pragma unroll
+            for (int i = 0; i < kSimtKeys / 8; ++i) {
+              const long long at = sm.at[i * 8 + (tid >> 5)];
+              x[i] = at >= 0 ? *reinterpret_cast<const float4 *>(from + at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+#pragma unroll
+            for (int i = 0; i < kSimtKeys / 8; ++i) *reinterpret_cast<float4 *>(to + (i * 8 + (tid >> 5)) * pitch) = x[i];
+          }
           bool there[4];   // of keys tx + 16 j
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int key = key0 + tx + 16 * j;
-            there[j] = key >= it.t.lo && key < it.t.hi &&
-                       (unsigned)a.seq.table[it.seq * a.seq.table_stride + key / c.page_size] < (unsigned)c.num_pages;
-          }
+          for (int j = 0; j < 4; ++j) there[j] = sm.at[tx + 16 * j] >= 0;
           __syncthreads();
           float s[4][4] = {};
 #pragma unroll 4
