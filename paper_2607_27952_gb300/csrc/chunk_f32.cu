@@ -18,9 +18,13 @@ struct alignas(16) SimtShared {
   unsigned flags;
 };
 
+// CTAs of an SM, by registers.  All shares run at once: a second wave of them would begin when the first has ended.
+template <int NC>
+constexpr int kSimtCtas = NC <= 2 ? 2 : 1;
+
 // NC: 64-column blocks of a value.
 template <int NC>
-__global__ void __launch_bounds__(kSimtThreads) chunk_f32_kernel(const __grid_constant__ ChunkShape p) {
+__global__ void __launch_bounds__(kSimtThreads, kSimtCtas<NC>) chunk_f32_kernel(const __grid_constant__ ChunkShape p) {
   extern __shared__ float4 smem4[];
   const ChunkArgs &a = p.a;
   const int D = a.cache.dim, ld = D + kPad, ldv = p.dv + kPad, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
@@ -59,9 +63,10 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_f32_kernel(const __grid_co
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = ty * 4 + i, t = (it.r0 + r) / p.group;
-        lo[i] = r < it.rows ? chunk_lo(a, it.s, t) : 0;
-        hi[i] = r < it.rows ? chunk_hi(a, it.s, t) : 0;
+        lo[i] = r < it.rows ? chunk_lo(a, it.s, t) : 0;   // rows of no token see everything, their q is zero
+        hi[i] = r < it.rows ? chunk_hi(a, it.s, t) : 0x7fffffff;
       }
+      const bool works = (tid >> 5) * 8 < it.rows;        // the warp has a row
       if (it.t.count > 0)
         for (int k = it.k0; k < it.k1; ++k) {
           const int key0 = (it.t.first + k) * kSimtKeys;
@@ -99,7 +104,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_f32_kernel(const __grid_co
           __syncthreads();
           float s[4][4] = {};
 #pragma unroll 4
-          for (int d = 0; d < D; d += 4) {
+          for (int d = 0; works && d < D; d += 4) {
             float4 x[4], y[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -142,7 +147,7 @@ __global__ void __launch_bounds__(kSimtThreads) chunk_f32_kernel(const __grid_co
             }
           }
           hidden = __syncthreads_or(hidden);
-          for (int k4 = 0; k4 < kSimtKeys; k4 += 4) {
+          for (int k4 = 0; works && k4 < kSimtKeys; k4 += 4) {
             float4 w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4 *>(ps + (ty * 4 + i) * (kSimtKeys + kPad) + k4);
@@ -256,7 +261,8 @@ cudaError_t launch_f32(ChunkShape p, cudaStream_t s) {
                                                              kSimtRows * (kSimtKeys + kPad) + (p.maps == 2 ? kSimtRows * (p.dv + kPad) : 0));
   p.block = p.pitch = kSimtRows;
   p.tile = kSimtKeys;
-  int shares = sm_count() * (int)((227 << 10) / (smem + 1024));
+  const int ctas = (int)((227 << 10) / (smem + 1024));
+  int shares = sm_count() * (ctas < kSimtCtas<NC> ? ctas : kSimtCtas<NC>);
   p.shares = shares < kMaxShares ? shares : kMaxShares;
   cudaError_t e = allow_smem(reinterpret_cast<const void *>(&chunk_f32_kernel<NC>), smem);
   if (e != cudaSuccess) return e;
