@@ -375,7 +375,8 @@ last_status last_chunk_workspace_size(const last_cache *c, int32_t num_q_heads, 
  * is taken for one without a key; one whose cu_new is out of range or falls is skipped, and rows of no sequence are
  * left as they are.  q-head h reads kv-head h / (num_q_heads / num_kv_heads).  q and out: [num_tokens]
  * [num_q_heads][head_dim], tokens q_stride and out_stride elements apart, both multiples of 16 bytes, 16-byte
- * aligned.  scale <= 0 selects 1/sqrt(head_dim).  bf16: weights are rounded to bf16 before they meet v, with their sum.
+ * aligned.  scale <= 0 selects 1/sqrt(head_dim).  bf16: weights are rounded to bf16
+ * before they meet v where sequences have more than a few rows (new tokens times q-heads per kv-head) on average.
  * Results do not depend on other calls or on timing: repeated calls give the same bits.
  * num_tokens * num_q_heads / num_kv_heads must stay below 2^31, num_tokens * num_q_heads * (max_pages * page_size + 256)
  * below 2^60 (LAST_ERR_UNSUPPORTED). */

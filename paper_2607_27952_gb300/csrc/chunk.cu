@@ -6,7 +6,7 @@ namespace last {
 namespace {
 
 constexpr size_t align256(size_t v) { return (v + 255) / 256 * 256; }
-constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinCtas = 2;
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 
 template <int N>
 struct Count {
@@ -168,7 +168,7 @@ size_t chunk_scratch_bytes(int dim, int elem) {
 }
 
 cudaError_t launch_chunk_join(const ChunkShape &p, cudaStream_t s) {
-  const dim3 grid(p.shares, kJoinCtas);
+  const dim3 grid(p.shares, (p.block + 31) / 32);   // a CTA for 32 rows of an item with one cut
   return p.a.elem == 4 ? launch_early(chunk_join_kernel<float>, grid, kJoinThreads, 0, s, p)
                        : launch_early(chunk_join_kernel<__nv_bfloat16>, grid, kJoinThreads, 0, s, p);
 }

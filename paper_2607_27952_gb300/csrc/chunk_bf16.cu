@@ -51,7 +51,7 @@ struct Item {
   int whole, second;
 };
 
-constexpr size_t kHead = 3072;   // shared memory before the panels, of which seven of 32 KB stand beside it
+constexpr size_t kHead = 3 << 10;   // shared memory before the panels, of which seven of 32 KB stand beside it
 
 struct alignas(16) Shared {
   unsigned long long full[kRingMax], empty[kRingMax], q_full[2], q_empty[2], s_full[2], p_full[2][2], pv_done[2];
