@@ -10,8 +10,10 @@
 // rarely); l sums the weights before they are rounded.
 //
 // Warps: 0-7 softmax and epilogue, 8 and 11 issue the products, 9 fills a ring of K and V panels (128 keys by up to 128 columns) with TMA
-// boxes of the pages, 10 walks the share's items and fetches rows of Q.  V rows that no row sees are zeroed in
-// shared memory before the product reads them: a weight of zero times an infinity or NaN would show.
+// boxes of the pages, 10 walks the share's items and fetches rows of Q.
+// A weight of zero times an infinity or NaN would show.  V rows that no row sees are zeroed in shared memory before the product reads
+// them.  Where some rows of a row tile see a key and others do not (at the mask's edges: one to four key tiles of a row tile), warp 9 looks at
+// its row of V; is something not finite there, the product leaves those groups of 16 keys out and the softmax warps add them up row by row.
 // diff: a cluster of two CTAs, one map each; each finishes half of the rows, with the other's half of O through L2.
 //
 // Bound by the way from S to P: 256 rows by 128 keys by 128 columns take 4600 cycles, of which the products are 2048 (16 x 2944 tokens,
@@ -48,6 +50,9 @@ struct Item {
   int lo, hi;             // keys that some row sees
   int ta[2], tb[2];       // key tiles by row tile
   int tlo[2], thi[2];     // keys by row tile
+  int ca[2], cb[2];       // key tiles by row tile whose keys all rows see (those of no row of the item aside)
+  int qa, qb;             // key tiles for which that holds of all row tiles
+  int alo[2], ahi[2];     // keys that all rows of a row tile see
   int whole, second;
 };
 
@@ -55,13 +60,14 @@ constexpr size_t kHead = 3 << 10;   // shared memory before the panels, of which
 
 struct alignas(16) Shared {
   unsigned long long full[kRingMax], empty[kRingMax], q_full[2], q_empty[2], s_full[2], p_full[2][2], pv_done[2];
-  unsigned long long item_full[kItems], item_empty[kItems], x_full, x_empty, never;
+  unsigned long long item_full[kItems], item_empty[kItems], looked[kTileInfo], x_full, x_empty, never;   // looked: all of `skip` is there
   Item items[kItems];
   float row[2][128];      // a row's value of one half of the columns for the other
   ChunkShare share;
   unsigned long long sums[kThreads / 32];
   alignas(16) int2 boxes[16];   // of the key tile being fetched: first token, page
-  unsigned skip[kTileInfo];   // of the key tiles on their way: groups of 8 keys whose page is out of range
+  // of the key tiles on their way: groups of 8 keys whose page is out of range; from bits 16 and 24 on, by row tile, groups of 16 that the product leaves out
+  volatile unsigned skip[kTileInfo];
   uint32_t tmem;
   unsigned flags;
   volatile unsigned dead;
@@ -215,6 +221,7 @@ __device__ __forceinline__ void query_role(const Geometry &g, Shared &sm, char *
     const bool writes = lane == 0, some = more && it.t.count > 0;
     const int ka = some ? it.t.first + it.k0 : 0, kb = some ? it.t.first + it.k1 : 0;
     unsigned used = 0;   // row tiles with a step
+    int qa = 0, qb = 0x7fffffff;
     if (writes) {
       o.seq = more ? it.seq : -1;
       o.unit = it.unit;
@@ -234,9 +241,12 @@ __device__ __forceinline__ void query_role(const Geometry &g, Shared &sm, char *
 #pragma unroll 1
     for (int t = 0; t < 2; ++t) {
       ChunkTiles x{0, 0, 0, 0};
-      int ta = 0, tb = 0;
+      int ta = 0, tb = 0, alo = 0, ahi = 0;
       if (some && t * g.rows < it.rows) {
-        x = chunk_tiles(p, it.s, it.r0 + t * g.rows, it.r0 + min(it.rows, t * g.rows + g.rows));
+        const int r0 = it.r0 + t * g.rows, r1 = it.r0 + min(it.rows, t * g.rows + g.rows);
+        x = chunk_tiles(p, it.s, r0, r1);
+        alo = chunk_lo(p.a, it.s, (r1 - 1) / p.group);
+        ahi = chunk_hi(p.a, it.s, r0 / p.group);
         ta = max(ka, x.first);
         tb = min(kb, x.first + x.count);
       }
@@ -246,9 +256,22 @@ __device__ __forceinline__ void query_role(const Geometry &g, Shared &sm, char *
         o.tb[t] = tb;
         o.tlo[t] = x.lo;
         o.thi[t] = x.hi;
+        const int ca = alo <= it.t.lo ? 0 : (alo + kKeys - 1) / kKeys, cb = ahi >= it.t.hi ? 0x7fffffff : ahi / kKeys;
+        if (ta < tb) {
+          qa = max(qa, ca);
+          qb = min(qb, cb);
+        }
+        o.ca[t] = ca;
+        o.cb[t] = cb;
+        o.alo[t] = alo;
+        o.ahi[t] = ahi;
       }
     }
-    if (writes) mbar_arrive(&sm.item_full[e]);
+    if (writes) {
+      o.qa = qa;
+      o.qb = qb;
+      mbar_arrive(&sm.item_full[e]);
+    }
     __syncwarp();
     if (!more) return;
 #pragma unroll 1
@@ -298,6 +321,40 @@ __device__ __forceinline__ void query_role(const Geometry &g, Shared &sm, char *
 }
 
 // ---- warp 9: K and V ----
+// Groups of 16 of a step's 128 keys that the product has to leave out: those with a key that some rows of the row tile
+// do not see (below all_lo or from all_hi on), where V's rows of such keys hold an infinity or NaN.  k0 .. k1 - 1: keys that the product reads and
+// warps 8 and 11 do not zero.  v: V's first panel.  This warp has the time, for the ring is full: 16 x 2944 tokens take 577 us, 567 without a look, and
+// 633 where the softmax warps look, which the tensor cores wait for and whose code fills the instruction cache.
+template <typename K>
+__device__ __noinline__ unsigned hidden_values(const Geometry &g, Shared &sm, uint32_t ring, Place v, int k0, int k1, int all_lo, int all_hi, unsigned skip) {
+  const int h0 = min(k1, max(k0, all_lo)), h1 = min(k1, max(h0, all_hi)), n = (h0 - k0 + k1 - h1) * 8;   // pieces of 16 bytes of 64 columns
+  if (n == 0) return 0;
+  __nv_bfloat162 sum = __floats2bfloat162_rn(0.0f, 0.0f);   // of zeros times them: NaN once there was something
+  const __nv_bfloat162 zero = sum;
+#pragma unroll 1
+  for (int i = 0; i < K::kValues; ++i) {
+    if (!wait(sm, &sm.full[v.slot], v.round)) return 0;
+    const int chunks = K::kPanels == 1 ? g.chunks : min(2, g.chunks - 2 * (i % K::kPanels));
+    uint32_t chunk = ring + v.slot * g.panel_chunks * kChunkBytes + k0 * 128;
+#pragma unroll 1
+    for (int c = 0; c < chunks; ++c, chunk += kChunkBytes)
+#pragma unroll 4
+      for (int r = threadIdx.x & 31; r < n; r += 32) {
+        __nv_bfloat162 x[4];
+        uint32_t (&u)[4] = reinterpret_cast<uint32_t (&)[4]>(x);
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(chunk + (r + (r < (h0 - k0) * 8 ? 0 : (h1 - h0) * 8)) * 16) : "memory");
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum = __hfma2(x[e], zero, sum);
+      }
+    v.skip(g, 1);
+  }
+  // rows of pages that are out of range are nobody's, and are zeroed meanwhile
+  if (!__any_sync(~0u, skip != 0 || __low2float(sum) != 0.0f || __high2float(sum) != 0.0f)) return 0;
+  auto groups = [](int from, int to) { return from < to ? (1u << ((to + 15) >> 4)) - (1u << (from >> 4)) : 0u; };
+  return groups(k0, h0) | groups(h1, k1);
+}
+
 // The lanes look the boxes' pages up, a tile ahead; one lane issues all boxes (25 cycles each; a lane per box took 75).
 template <typename K>
 __device__ __forceinline__ void load_role(const Geometry &g, Shared &sm, char *ring, const CUtensorMap *kmap, const CUtensorMap *vmap, int rank) {
@@ -311,9 +368,8 @@ __device__ __forceinline__ void load_role(const Geometry &g, Shared &sm, char *r
   for (uint32_t n = 0;; ++n) {
     const int e = n % kItems;
     if (!wait(sm, &sm.item_full[e], n / kItems & 1)) return;
-    const int seq = sm.items[e].seq, unit = sm.items[e].unit, ka = sm.items[e].ka, kb = sm.items[e].kb, lo = sm.items[e].lo, hi = sm.items[e].hi;
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sm.item_empty[e]);
+    const Item &it = sm.items[e];
+    const int seq = it.seq, unit = it.unit, ka = it.ka, kb = it.kb, lo = it.lo, hi = it.hi, qa = it.qa, qb = it.qb;
     if (seq < 0) return;
     const int32_t *table = p.a.seq.table + seq * p.a.seq.table_stride;
     auto counts = [&](int j) { return lane < boxes && j < kb && j * kKeys + lane * box < hi && j * kKeys + lane * box > lo - box; };
@@ -337,7 +393,8 @@ __device__ __forceinline__ void load_role(const Geometry &g, Shared &sm, char *r
       const int row = g.page_log >= 0 ? (j * kKeys + lane * box) & (size - 1) : (j * kKeys + lane * box) % size;
       if (lane < boxes) sm.boxes[lane] = make_int2(row, page);
       __syncwarp();
-#pragma unroll
+      const Place first = at;
+#pragma unroll 1
       for (int i = 0; i < K::kPanels + K::kValues; ++i) {
         const int pi = i % K::kPanels, value = i / K::kPanels - 1;   // -1: K
         const int chunks = K::kPanels == 1 ? g.chunks : min(2, g.chunks - 2 * pi);
@@ -375,8 +432,23 @@ __device__ __forceinline__ void load_role(const Geometry &g, Shared &sm, char *r
         at.skip(g, 1);
         again |= at.slot < before;
       }
+      unsigned hand = 0;
+#pragma unroll 1
+      for (int t = 0; t < K::kTiles; ++t) {
+        if (j >= qa && j < qb) break;
+        if (j < it.ta[t] || j >= it.tb[t] || (j >= it.ca[t] && j < it.cb[t])) continue;
+        const int key0 = j * kKeys, kmin = max(0, it.tlo[t] - key0), kmax = min(kKeys, it.thi[t] - key0);
+        Place values = first;
+        values.skip(g, K::kPanels);
+        hand |= hidden_values<K>(g, sm, ring_at, values, max(kmin & ~15, lo - key0), min((kmax + 15) & ~15, min(kKeys, hi - key0)),
+                                 it.alo[t] - key0, it.ahi[t] - key0, skip) << (16 + 8 * t);
+      }
+      if (lane == 0 && hand != 0) sm.skip[tile % kTileInfo] = skip | hand;
+      if (lane == 0) mbar_arrive(&sm.looked[tile % kTileInfo]);
       page = next_page;
     }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sm.item_empty[e]);
   }
 }
 
@@ -387,12 +459,14 @@ __device__ __forceinline__ void load_role(const Geometry &g, Shared &sm, char *r
 // products.  A panel's room is free once both say so: a warp that has no use for a panel gives it back as it comes, so that neither
 // mistakes a round of the ring for another.
 struct Tiles {   // of an item, in registers
-  int ka, kb, ta[2], tb[2], tlo[2], thi[2], lo, hi;
+  int ka, kb, ta[2], tb[2], ca[2], cb[2], tlo[2], thi[2], lo, hi;
   __device__ __forceinline__ explicit Tiles(const Item &it) : ka(it.ka), kb(it.kb), lo(it.lo), hi(it.hi) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       ta[t] = it.ta[t];
       tb[t] = it.tb[t];
+      ca[t] = it.ca[t];
+      cb[t] = it.cb[t];
       tlo[t] = it.tlo[t];
       thi[t] = it.thi[t];
     }
@@ -426,7 +500,7 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
     if (end) return;
     const bool two = it.two();
     const int t = two ? w : it.ta[0] < it.tb[0] ? 0 : 1, ta = t == 0 ? it.ta[0] : it.ta[1], tb = t == 0 ? it.tb[0] : it.tb[1];
-    const int tlo = t == 0 ? it.tlo[0] : it.tlo[1], thi = t == 0 ? it.thi[0] : it.thi[1];
+    const int tlo = t == 0 ? it.tlo[0] : it.tlo[1], thi = t == 0 ? it.thi[0] : it.thi[1], ca = t == 0 ? it.ca[0] : it.ca[1], cb = t == 0 ? it.cb[0] : it.cb[1];
     const uint32_t turn = q_tile + (two ? w : 0), q = turn % K::kTiles, o = tmem + kOutColumn + t * 128;
     bool begun = false, waited = false;   // waited: for K of tile j
 #pragma unroll 1
@@ -435,6 +509,8 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
       const int key0 = j * kKeys, kmin = max(0, tlo - key0), kmax = min(kKeys, thi - key0);
       const int k0 = kmin >> 4, k1 = (kmax + 15) >> 4;
       if (own && !begun && !wait_alone(sm, &sm.q_full[q], turn / K::kTiles & 1)) return;
+      // before S is there: who sees it sees all of sm.skip
+      if (own && (j < ca || j >= cb) && !wait_alone(sm, &sm.looked[tile % kTileInfo], tile / kTileInfo & 1)) return;
 #pragma unroll
       for (int pi = 0; pi < K::kPanels; ++pi) {
         if (!waited && !wait_alone(sm, &sm.full[at.slot], at.round)) return;
@@ -465,7 +541,8 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
         at.skip(g, 1);
       }
       const Place v0 = at;
-      const unsigned skip = sm.skip[tile % kTileInfo];   // written before K's panels were asked for
+      const unsigned info = sm.skip[tile % kTileInfo], skip = info & 0xffff;   // of pages: written before K's panels were asked for
+      const unsigned hand = own ? info >> (16 + 8 * t) & 0xff : 0;   // if any, the softmax warps begin O
       const int from = max(0, it.lo - key0), to = min(kKeys, it.hi - key0);
 #pragma unroll
       for (int i = 0; i < K::kValues; ++i) {
@@ -485,7 +562,7 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
       }
       waited = false;
       if (own) {
-        const bool full = k1 - k0 == 8;
+        const bool full = k1 - k0 == 8 && hand == 0;
         // with two row tiles the next step is the next tile's: its K comes before these weights (and wants no room of this V)
         if (two && j + 1 < it.kb) {
           Place next = at;
@@ -522,10 +599,13 @@ __device__ __forceinline__ void product_role(const Geometry &g, Shared &sm, char
                 }
             } else if (part == 1) {
 #pragma unroll 1
-              for (int k = k0; k < k1; ++k)
+              for (int k = k0; k < k1; ++k) {
+                if (hand >> k & 1) continue;
 #pragma unroll
                 for (int x = 0; x < K::kParts; ++x)
-                  umma_bf16_ts(d, st + 32 * x + (k >> 2) * 64 + (k & 3) * 8, vd + k * (2048 >> 4), idesc, j == ta && k == k0 && x == 0 ? 0u : 1u);
+                  umma_bf16_ts(d, st + 32 * x + (k >> 2) * 64 + (k & 3) * 8, vd + k * (2048 >> 4), idesc,
+                               j == ta && k == k0 && x == 0 && hand == 0 ? 0u : 1u);
+              }
             }
             if (part == 1) {
               if (i == K::kValues - 1) umma_commit(&sm.pv_done[w]);
@@ -555,11 +635,64 @@ struct Rows {      // what a thread keeps of a row tile
   bool started;
 };
 
+// O of the warp's 32 rows and its half of the columns, plus their weights times V of `groups`, each row with the keys that it sees
+// (columns from .. to - 1 of the step) alone.  p: TMEM of the step's weights, out: of O; zero: O has not begun.
+template <typename K>
+__device__ __forceinline__ void add_by_hand(const Geometry &g, uint32_t ring, Place v, uint32_t p, uint32_t out, bool zero, int chunk0, int chunk1, unsigned groups,
+                                            int from, int to, unsigned skip) {
+  const int per = g.columns / 16;
+#pragma unroll 1
+  for (int c = chunk0; c < chunk1; ++c) {
+    const int head = K::kMaps == 2 && c >= per, col = (c - head * per) * 16;
+    Place at = v;
+    at.skip(g, head * K::kPanels + (col >> 7));
+    const uint32_t from_v = ring + at.slot * g.panel_chunks * kChunkBytes + (col >> 6 & 1) * kChunkBytes;
+    uint32_t o[16];
+    if (zero) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[i] = 0;
+    } else {
+      tmem_ld16(out + c * 16, o);
+    }
+#pragma unroll 1
+    for (unsigned left = groups; left != 0; left &= left - 1) {
+      const int k = __ffs(left) - 1;
+#pragma unroll 1
+      for (int i = 0; i < 16; i += 2) {
+        uint32_t two, rest = 0;
+        const uint32_t w_at = p + (k >> 2) * 64 + (k & 3) * 8 + i / 2;
+        tmem_ld1(w_at, &two);
+        if (K::kParts == 2) tmem_ld1(w_at + 32, &rest);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int key = k * 16 + i + e;
+          const float w = e ? bf16hi(two) + bf16hi(rest) : bf16lo(two) + bf16lo(rest);
+          const bool sees = key >= from && key < to && !(skip >> (key >> 3) & 1);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t x[4];
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(from_v + key * 128 + ((((col & 63) >> 3) + h) ^ (key & 7)) * 16) : "memory");
+#pragma unroll
+            for (int d = 0; d < 8; ++d) {
+              uint32_t &y = o[h * 8 + d];
+              if (sees) y = __float_as_uint(fmaf(w, d & 1 ? bf16hi(x[d / 2]) : bf16lo(x[d / 2]), __uint_as_float(y)));
+            }
+          }
+        }
+      }
+    }
+    tmem_st16(out + c * 16, o);
+  }
+  tmem_wait_st();
+}
+
 // Weights of the warp's 32 rows and 64 of the step's keys.  from, to: columns of these that the row sees.  There is one
 // copy of this code for all row tiles and masks: with four of them the instruction cache missed all the time.
 template <typename K>
 __device__ __forceinline__ void weights(const Geometry &g, Shared &sm, Rows &r, uint32_t tmem, int t, int chunk0, int chunk1,
-                                        int from, int to, unsigned skip, int b, bool two, uint32_t others) {
+                                        int from, int to, unsigned skip, int b, bool two, uint32_t others, bool by_hand) {
   const bool masked = __any_sync(~0u, from > 0 || to < 64) || skip != 0;
   const int pair = (threadIdx.x >> 5) & 3, half = (threadIdx.x >> 5) >> 2, row = pair * 32 + (threadIdx.x & 31);
   const uint32_t lanes = (uint32_t)(pair * 32) << 16, st = tmem + lanes + b * 128 + half * 64;
@@ -631,50 +764,16 @@ __device__ __forceinline__ void weights(const Geometry &g, Shared &sm, Rows &r, 
     tmem_wait_st();
     tc_fence_before();
     __syncwarp();
-    if ((threadIdx.x & 31) == 0) mbar_arrive(&sm.p_full[b][q]);   // of the half's first, then second 32 keys
+    if ((threadIdx.x & 31) == 0 && (q == 0 || !by_hand)) mbar_arrive(&sm.p_full[b][q]);   // of the half's first, then second 32 keys
   }
   const float2 total = unpack2(add2(sum[0], sum[1]));
   r.l += total.x + total.y;
 }
 
-// Column `lane` of the 32 from col on of a row of O once more, on the CUDA cores, for rows where the sums are not finite though
-// their weights are: a weight of zero times an infinity or NaN in a row of V that the row does not see leaves a NaN.  Here
-// such keys are passed over.  The row sees keys begin .. end - 1 of the item's share; m: its maximum.
-template <typename K>
-__device__ __noinline__ float careful(const Geometry &g, int seq, int begin, int end, float m, const char *q, int k_head, int v_head, int col) {
-  const ChunkShape &p = g.p;
-  const CacheLayer &c = p.a.cache;
-  const int lane = threadIdx.x & 31, D = c.dim;
-  float acc = 0.0f;
-  for (int k0 = begin; k0 < end; k0 += 32) {
-    const int key = k0 + min(lane, end - 1 - k0);
-    const int page = p.a.seq.table[seq * p.a.seq.table_stride + key / c.page_size];
-    const bool sees = lane < end - k0 && (unsigned)page < (unsigned)c.num_pages;
-    const long long at = sees ? page * c.page_stride + key % c.page_size * c.token_stride : 0;
-    float z = 0.0f;
-    for (int d = 0; d < D; d += 8) {
-      float a[8], b[8];
-      Elem<__nv_bfloat16>::widen(ldg(q + d * 2), a);
-      Elem<__nv_bfloat16>::widen(ldg(c.k + k_head * c.head_stride + at + d * 2), b);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) z = fmaf(a[i], b[i], z);
-    }
-    float w = chunk_exp2(fmaf(z, p.scale2, m == -INFINITY ? 0.0f : -m));
-    if (K::kParts == 1) w = bf16lo(pack_bf16(w, 0.0f));
-    for (unsigned left = __ballot_sync(~0u, sees); left != 0; left &= left - 1) {
-      const int i = __ffs(left) - 1;
-      const long long from = (long long)shfl_u64((unsigned long long)at, i);
-      const float f = __shfl_sync(~0u, w, i);
-      if (col + lane < D) acc = fmaf(f, __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(c.v + v_head * c.head_stride + from)[col + lane]), acc);
-    }
-  }
-  return acc;
-}
-
 // A row of a row tile at the end of its item.
 struct RowEnd {
   float m, sum;    // of both warps' keys
-  int lo, hi, tok, head;
+  int tok, head;
   bool live, started;
 };
 
@@ -700,49 +799,20 @@ struct Out {
   __device__ __forceinline__ bool two(int c) const { return c + 1 < chunk1; }
   __device__ __forceinline__ int width(int c) const { return min(two(c) ? 32 : 16, g.p.a.cache.dim - col(c)); }
   __device__ __forceinline__ void load(int c, float (&x)[32]) const {
-    const int lane = threadIdx.x & 31;
     const uint32_t at = tmem + ((threadIdx.x >> 5 & 3) << 21) + kOutColumn + t * 128 + c * 16;
     uint32_t o[32];
-#pragma unroll 1
-    for (bool once_more = false;; once_more = true) {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) o[i] = 0;
-      if (r.started) {
-        if (two(c)) {
-          tmem_ld32(at, o);
-          tmem_wait_ld();
-        } else {
-          tmem_ld16(at, o);
-        }
-      }
-      float zero = 0.0f;   // NaN where some column is not finite
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        x[i] = __uint_as_float(o[i]);
-        zero = fmaf(x[i], 0.0f, zero);
-      }
-      unsigned odd = __ballot_sync(~0u, r.live && zero != 0.0f && r.sum < INFINITY);
-      if (odd == 0 || once_more) break;
-#pragma unroll 1
-      for (; odd != 0; odd &= odd - 1) {
-        const int who = __ffs(odd) - 1;
-        const char *q = g.p.a.q + (long long)(it.first + r.tok) * g.p.a.q_stride + (long long)MapHead<K>::of(r.head, rank) * g.p.a.cache.dim * 2;
-        const float again = careful<K>(g, it.seq, max(it.ka * kKeys, __shfl_sync(~0u, r.lo, who)),
-                                       (int)min((long long)it.kb * kKeys, (long long)__shfl_sync(~0u, r.hi, who)), __shfl_sync(~0u, r.m, who),
-                                       reinterpret_cast<const char *>(shfl_u64(reinterpret_cast<unsigned long long>(q), who)),
-                                       it.unit * K::kMaps + rank, it.unit * K::kMaps + head(), col(c));
-#pragma unroll 1
-        for (int i = 0; i < (two(c) ? 32 : 16); ++i) {   // the row's columns change in TMEM
-          uint32_t y;
-          tmem_ld1(at + i, &y);
-          tmem_wait_ld();
-          const float z = __shfl_sync(~0u, again, i);
-          if (lane == who) y = __float_as_uint(z);
-          asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" :: "r"(at + i), "r"(y) : "memory");
-          tmem_wait_st();
-        }
+    for (int i = 0; i < 32; ++i) o[i] = 0;
+    if (r.started) {
+      if (two(c)) {
+        tmem_ld32(at, o);
+        tmem_wait_ld();
+      } else {
+        tmem_ld16(at, o);
       }
     }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(o[i]);
   }
   // 32 columns, from chunk c on, of every lane's row.  Pieces of 16 bytes change places among 4 lanes, so that these write 64 bytes
   // of one row: a lane per row would touch 32 lines with every store.
@@ -863,7 +933,7 @@ __device__ __forceinline__ void finish_difference(const Geometry &g, Shared &sm,
 }
 
 template <typename K>
-__device__ __forceinline__ void soft_role(const Geometry &g, Shared &sm, uint32_t tmem, int rank) {
+__device__ __forceinline__ void soft_role(const Geometry &g, Shared &sm, char *ring, uint32_t tmem, int rank) {
   const ChunkShape &p = g.p;
   const ChunkArgs &a = p.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp & 3, half = warp >> 2, row = pair * 32 + lane;
@@ -903,9 +973,22 @@ __device__ __forceinline__ void soft_role(const Geometry &g, Shared &sm, uint32_
         tc_fence_after();
         if (t * g.rows + pair * 32 < it.rows) {   // else nobody's rows, whatever becomes of them
           const int key0 = j * kKeys, kmax = min(kKeys, (t == 0 ? it.thi[0] : it.thi[1]) - key0);
+          const unsigned info = sm.skip[tile % kTileInfo], skip = info & 0xffff, hand = info >> (16 + 8 * t) & 0xff;
           // columns past kmax have not been computed
           const int from = max(0, min(kKeys, x.lo - key0)) - half * 64, to = max(0, min(kmax, x.hi - key0)) - half * 64;
-          weights<K>(g, sm, x, tmem, t, chunk0, chunk1, from, to, sm.skip[tile % kTileInfo], b, two, others);
+          weights<K>(g, sm, x, tmem, t, chunk0, chunk1, from, to, skip, b, two, others, hand != 0);
+          if (hand != 0) {   // the product waits for all weights then
+            const uint32_t lanes = (uint32_t)(pair * 32) << 16;
+            pair_sync(pair);   // the other half's are there
+            if (!two && x.started) wait(sm, &sm.pv_done[b ^ 1], (others - 1) & 1);
+            tc_fence_after();
+            const uint32_t panel = tile * (K::kPanels + K::kValues) + K::kPanels;
+            add_by_hand<K>(g, smem_addr(ring), Place{(int)(panel % g.slots), 0}, tmem + lanes + b * 128, tmem + lanes + kOutColumn + t * 128, !x.started, chunk0, chunk1, hand, from + half * 64,
+                           to + half * 64, skip);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.p_full[b][1]);
+          }
         } else if (lane == 0) {
           mbar_arrive(&sm.p_full[b][0]);
           mbar_arrive(&sm.p_full[b][1]);
@@ -934,8 +1017,6 @@ __device__ __forceinline__ void soft_role(const Geometry &g, Shared &sm, uint32_
       end.tok = at / p.group;
       end.head = it.unit * p.group + at - end.tok * p.group;
       end.m = x.m;
-      end.lo = x.lo;
-      end.hi = x.hi;
       end.started = x.started;
       return end;
     };
@@ -997,6 +1078,7 @@ chunk_bf16_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CU
       mbar_init(&sm.item_full[i], 1);
       mbar_init(&sm.item_empty[i], kSoftWarps + 3);
     }
+    for (int i = 0; i < kTileInfo; ++i) mbar_init(&sm.looked[i], 1);
     mbar_init(&sm.x_full, kSoftWarps / 2);
     mbar_init(&sm.x_empty, kSoftWarps / 2);
     mbar_init(&sm.never, 1);
@@ -1023,7 +1105,7 @@ chunk_bf16_kernel(const __grid_constant__ Geometry g, const __grid_constant__ CU
   // 384 x 168 registers at launch = 256 x 200 + 128 x 104
   if (warp < kSoftWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
-    soft_role<K>(g, sm, tmem, rank);
+    soft_role<K>(g, sm, ring, tmem, rank);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == kMmaWarp || warp == kMmaWarp + 3) {
