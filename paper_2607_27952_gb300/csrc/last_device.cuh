@@ -213,6 +213,7 @@ __device__ __forceinline__ bool mbar_wait_bounded(unsigned long long *bar, uint3
 // After a wait has expired: lets asynchronous work in flight finish before its CTA exits
 // (`never`: an initialised barrier that nothing completes).  Bounded like every wait.
 __device__ __forceinline__ void wait_out(unsigned long long *never) {
+#pragma unroll 1
   for (int i = 0; i < 1 << 14; ++i) mbar_try_wait(never, 0);
 }
 
