@@ -372,14 +372,14 @@ last_status last_chunk_workspace_size(const last_cache *c, int32_t num_q_heads, 
  * weight 0.  What a row does not see has no part in it, whatever it holds; pages that no row of a sequence sees
  * are not read (their table entries may be anything).  Keys of a page out of range are left out; a sequence
  * where lens[b] is below n, above 2^31 - 256 or more than its table row has room for, or key_begin[b] is negative,
- * is taken for one without a key; one whose cu_new is out of range or falls is skipped, and rows of no sequence are
- * left as they are.  q-head h reads kv-head h / (num_q_heads / num_kv_heads).  q and out: [num_tokens]
+ * is taken for one without a key; one whose cu_new is out of range or falls is skipped, rows of no sequence are
+ * left as they are, and rows of two get either's result.  q-head h reads kv-head h / (num_q_heads / num_kv_heads).  q and out: [num_tokens]
  * [num_q_heads][head_dim], tokens q_stride and out_stride elements apart, both multiples of 16 bytes, 16-byte
  * aligned.  scale <= 0 selects 1/sqrt(head_dim).  bf16: weights are rounded to bf16
  * before they meet v where sequences have more than a few rows (new tokens times q-heads per kv-head) on average.
  * Results do not depend on other calls or on timing: repeated calls give the same bits.
- * num_tokens * num_q_heads / num_kv_heads must stay below 2^31, num_tokens * num_q_heads * (max_pages * page_size + 256)
- * below 2^60 (LAST_ERR_UNSUPPORTED). */
+ * rows = num_tokens * num_q_heads / num_kv_heads must stay below 2^31, (rows / 8 + batch) * num_q_heads *
+ * (max_pages * page_size + 1024) below 2^62 (LAST_ERR_UNSUPPORTED). */
 last_status last_cache_chunk_attention(const last_cache *c, int32_t layer, const last_sequences *s,
                                        int32_t num_tokens, const int32_t *cu_new, int32_t num_q_heads,
                                        float scale, int32_t causal, int32_t window, const void *q,

@@ -309,10 +309,11 @@ last_status chunk(const last_cache *c, int32_t layer, const last_sequences *s, i
     if (c->head_dim > 128) return fail(LAST_ERR_UNSUPPORTED, "head_dim must be at most 128: values are twice as wide");
   }
   const int e = elem_bytes(c->dtype);
-  const double rows = (double)num_tokens * (num_q_heads / c->num_kv_heads), keys = (double)s->max_pages * c->page_size + 256.0;
-  if (rows >= 2147483648.0 || rows * c->num_kv_heads * keys >= 1152921504606846976.0)
-    return fail(LAST_ERR_UNSUPPORTED, "num_tokens * num_q_heads / num_kv_heads must stay below 2^31, "
-                                      "num_tokens * num_q_heads * (max_pages * page_size + 256) below 2^60");
+  // what the shares' sums count (ChunkCost): a block of 8 rows or more costs a unit's heads times its keys and 1024 at most
+  const double rows = (double)num_tokens * (num_q_heads / c->num_kv_heads), keys = std::fmin((double)s->max_pages * c->page_size, 2147483648.0);
+  if (rows >= 2147483648.0 || (rows / 8 + s->batch) * num_q_heads * (keys + 1024.0) >= 4611686018427387904.0)
+    return fail(LAST_ERR_UNSUPPORTED, "num_tokens * num_q_heads / num_kv_heads must stay below 2^31, an eighth of it and batch, times "
+                                      "num_q_heads * (max_pages * page_size + 1024), below 2^62");
   if (num_tokens > 0 && (q == nullptr || out == nullptr)) return invalid("q and out are required");
   if (!aligned(q, 16) || !aligned(out, 16)) return invalid("q and out must be 16-byte aligned");
   if (!multiple16(q_stride * e) || !multiple16(out_stride * e))

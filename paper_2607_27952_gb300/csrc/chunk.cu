@@ -52,11 +52,12 @@ __global__ void __launch_bounds__(kJoinThreads) chunk_join_kernel(const __grid_c
       atomicMax(&last_cut, i);
     }
   __syncthreads();
+  const int end = min(last_cut + 1, p.shares - 1);   // the last share with a part
   if (warp == 0) {   // the shares with a part: the first, and those that end at another tile than the one before
     int n = 0;
-    for (int i0 = first_cut; i0 <= last_cut + 1; i0 += 32) {   // the cuts in between are in the item too
+    for (int i0 = first_cut; i0 <= end; i0 += 32) {   // the cuts in between are in the item too
       const int i = i0 + lane;
-      const bool some = i <= last_cut + 1 && (i == first_cut || i > last_cut || tile_at(i) != tile_at(i - 1));
+      const bool some = i <= end && (i == first_cut || i > last_cut || tile_at(i) != tile_at(i - 1));
       const unsigned all = __ballot_sync(~0u, some);
       if (some) share_of[n + __popc(all & ((1u << lane) - 1))] = i;
       n += __popc(all);

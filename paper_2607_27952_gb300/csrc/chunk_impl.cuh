@@ -141,7 +141,8 @@ __device__ __forceinline__ int chunk_blocks(const ChunkShape &p, const ChunkSeq 
 }
 
 // Cost of a unit's first x blocks, in keys times group: block y sees, of its last row, base - begin + (y + 1) block /
-// group keys, none below zero and no more than the window (with the block's own tokens) or the sequence has.
+// group keys, none below zero and no more than the window (with the block's own tokens) or the sequence has.  The host refuses calls whose
+// sums could reach 2^62.
 struct ChunkCost {
   long long a, most, item;
   int block;
