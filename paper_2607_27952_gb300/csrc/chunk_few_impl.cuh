@@ -653,6 +653,7 @@ cudaError_t launch_kind(Few f, cudaStream_t s) {
   // CTAs of an SM share its 228 KB: 1 KB each is the system's, 6 KB are room for the join
   constexpr size_t kMost = (size_t)(228 - 6) * 1024 / K::kCtas / 1024 * 1024 - 2048;
   static_assert(offsetof(typename K::Sm, rows) % 16 == 0, "read four floats at a time");
+  static_assert(2 * K::kRows <= 128, "twice the tiles' shares, whose parts have 128 rows and more: room for two of these each");
   const size_t fixed = 1024 + sizeof(typename K::Sm) + (size_t)kItems * K::kMaps * K::kRows * c.dim * 2;
   f.slots = (int)((kMost - fixed) / K::kPanel);   // three at least: K and V of 64 keys, 32 KB each at most
   if (f.slots > kRingMax) f.slots = kRingMax;
@@ -672,7 +673,7 @@ cudaError_t launch_kind(Few f, cudaStream_t s) {
                          f.joined ? box5 : box))
       return cudaErrorInvalidValue;
   p.shares = sm_count() * K::kCtas;
-  if (p.shares > 2 * kMaxTensorCtas / K::kMaps) p.shares = 2 * kMaxTensorCtas / K::kMaps;
+  if (p.shares > kMaxShares / K::kMaps) p.shares = kMaxShares / K::kMaps;
   e = launch_early(chunk_few_kernel<K>, dim3(p.shares), K::kThreads, smem, s, f, maps[0], maps[1]);
   return e == cudaSuccess ? launch_chunk_join(p, s) : e;
 }

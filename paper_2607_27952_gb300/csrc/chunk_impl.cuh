@@ -36,10 +36,10 @@ struct ChunkShape {   // the same for every CTA
   float *parts;       // [shares][maps][2] parted sums: second one where an item begins in the share
 };
 
-constexpr int kMaxShares = 480, kMaxTensorCtas = 160;   // fp32 and bf16
+// bf16 tiles: a CTA per SM.  fp32 and few rows: up to two, with smaller parts.
+constexpr int kMaxTensorCtas = 160, kMaxShares = 2 * kMaxTensorCtas;
 constexpr int kMaxKeys = 0x7fffff00;   // of a sequence: the last key's tile ends before 2^31
 constexpr float kChunkLog2e = 1.4426950408889634f, kChunkLn2 = 0.6931471805599453f;
-constexpr int kLeastTiles = 1;   // parts of fewer tiles are not cut off
 
 cudaError_t launch_chunk_f32(ChunkShape p, cudaStream_t s);
 cudaError_t launch_chunk_bf16(ChunkShape p, float *exchange, cudaStream_t s);
@@ -188,14 +188,11 @@ __device__ inline ChunkPos chunk_locate(const ChunkShape &p, const ChunkSeq &s, 
   const long long before = cost.upto(x);
   const int rows = (int)min((long long)p.block, (long long)s.n * p.group - (long long)x * p.block);
   const int tiles = max(1, chunk_tiles(p, s, x * p.block, x * p.block + rows).count);
-  int k = (int)((double)(rest - before) / (double)(cost.upto(x + 1) - before) * tiles + 0.5);
-  if (k < kLeastTiles) k = 0;
-  if (k > tiles - kLeastTiles) k = tiles;
-  pos.tile = k;
+  pos.tile = (int)((double)(rest - before) / (double)(cost.upto(x + 1) - before) * tiles + 0.5);
   return pos;
 }
 
-// Where this CTA's share begins and ends, by all threads (`sums`: one per warp and two more).  A position behind the
+// Where this CTA's share begins and ends, by all threads (`sums`: one per warp).  A position behind the
 // last item has seq = batch.
 struct ChunkShare {
   ChunkPos begin, end;
