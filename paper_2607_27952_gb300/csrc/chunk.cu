@@ -182,18 +182,24 @@ cudaError_t launch_chunk(const ChunkArgs &a, cudaStream_t s) {
   p.group = a.q_heads / a.cache.heads;
   p.dv = a.cache.dim * p.maps;
   p.scale2 = a.scale * kChunkLog2e;
-  // measured, 128 / 384 / 512 / 1024 / 1536 keys: prompts of 24 x 264 - 4352 tokens 640 / 530 / 528 / 580 / 631 us, differential prefill of
-  // 4 x 2944 tokens 627 / 527 / 494 / 407 / 413 us (its items are 128 rows, and the CTAs of a cluster wait for each other at their ends)
+  // measured, 128 / 384 / 448 / 512 / 1024 / 1536 keys: prompts of 24 x 264 - 4352 tokens 624 / 520 / 523 / 526 / 579 / 629 us, differential prefill of
+  // 4 x 2944 tokens 634 / 523 / 500 / 488 / 422 / 441 us (its items are 128 rows, and the CTAs of a cluster wait for each other at their ends)
   p.item_keys = a.elem == 4 ? 128 : a.diff ? 1024 : 448;
   p.cuts = reinterpret_cast<int4 *>(a.ws + kStatusBytes);
   p.parts = reinterpret_cast<float *>(a.ws + kStatusBytes + align256(sizeof(int4) * kMaxShares));
   float *exchange = reinterpret_cast<float *>(reinterpret_cast<char *>(p.parts) + parts_bytes(a.cache.dim, a.elem));
   if (a.elem == 4) return launch_chunk_f32(p, s);
-  // few rows per sequence, on average: no tile of 128 rows is worth its products
+  // few rows per sequence, on average: no tile of 128 rows is worth its products.  Measured with 4 query heads a kv-head, 64 sequences of 650 keys and 8
+  // of 20000, few rows' kernel against tiles, us: width 128, 16 rows 37 / 47 and 75 / 92, 20 rows 50 / 48 and 122 / 95; 64, 16 rows 29 / 43 and 56 / 77, 20
+  // rows 38 / 44 and 90 / 79; 80, 8 rows 30 / 46 and 63 / 86, 12 rows 42 / 46 and 105 / 88.  Differences, 128, 8 rows 45 / 71 and 87 / 121, 12 rows 61 / 72
+  // and 140 / 126; 64, 8 rows 34 / 59 and 62 / 104, 12 rows 43 / 59 and 96 / 108; 80, 8 rows 53 / 63 and 111 / 116, 12 rows 79 / 63 and 184 / 121.
   const long long rows = a.seq.batch > 0 ? ((long long)a.tokens * p.group + a.seq.batch - 1) / a.seq.batch : 0;
   const int d = a.cache.dim;
   const bool whole = d == 64 || d == 128;
   if (rows <= (a.diff || !whole ? 8 : 16)) {
+    // their items end sooner: differential tokens over 127 x 64 and once 131072 keys 146 / 122 / 129 / 141 us with 128 / 256 / 448 / 1024, over 32
+    // sequences of 64 - 20000 keys 418 / 415 / 417 / 424; chunks 87 / 84 / 86 / 91 and 393 / 392 / 389 / 394
+    p.item_keys = 256;
     if (a.diff) return whole ? launch_diff_few(p, s) : launch_diff_few_any(p, s);
     if (!whole) return launch_chunk_few_any(p, s);
     return d == 64 ? launch_chunk_few_64(p, rows > 8, s) : launch_chunk_few_128(p, rows > 8, s);
