@@ -373,10 +373,13 @@ last_status last_chunk_workspace_size(const last_cache *c, int32_t num_q_heads, 
  * are not read (their table entries may be anything).  Keys of a page out of range are left out; a sequence
  * where lens[b] is below n, above 2^31 - 256 or more than its table row has room for, or key_begin[b] is negative,
  * is taken for one without a key; one whose cu_new is out of range or falls is skipped, rows of no sequence are
- * left as they are, and rows of two get either's result.  q-head h reads kv-head h / (num_q_heads / num_kv_heads).  q and out: [num_tokens]
+ * left as they are, and rows of two are undefined.  q-head h reads kv-head h / (num_q_heads / num_kv_heads).  q and out: [num_tokens]
  * [num_q_heads][head_dim], tokens q_stride and out_stride elements apart, both multiples of 16 bytes, 16-byte
- * aligned.  scale <= 0 selects 1/sqrt(head_dim).  bf16: weights are rounded to bf16
- * before they meet v where sequences have more than a few rows (new tokens times q-heads per kv-head) on average.
+ * aligned.  scale <= 0 selects 1/sqrt(head_dim).  Softmax statistics are fp32.  bf16: weights are held in two bf16 parts (2^-16)
+ * where num_tokens * num_q_heads / num_kv_heads is at most 16 (head_dim 64 and 128) or 8 (others) times batch, and rounded
+ * to bf16 (2^-8 of sum |weight v|) above: which of the two goes by the whole batch.  Sums over n keys are off by up to
+ * n * 2^-27 of sum |weight v|, and are formed before they are divided, with weights of up to 2^8: |v| above 2^119 / n may
+ * come out infinite.
  * Results do not depend on other calls or on timing: repeated calls give the same bits.
  * rows = num_tokens * num_q_heads / num_kv_heads must stay below 2^31, (rows / 8 + batch) * num_q_heads *
  * (max_pages * page_size + 1024) below 2^62 (LAST_ERR_UNSUPPORTED). */
@@ -393,8 +396,8 @@ last_status last_cache_chunk_attention(const last_cache *c, int32_t layer, const
  *   x = sum P1 v - lambda[j] sum P2 v,   out = out_scale x,
  * or, with a norm_weight, out = out_scale norm_weight x / sqrt(mean(x^2) + norm_eps) over the
  * 2 head_dim elements of x (0 where that root is).  out: [num_tokens][num_q_heads / 2][2 head_dim].  num_kv_heads
- * must be even, head_dim at most 128.  Everything else is as for last_cache_chunk_attention.  lambda and norm_weight are
- * DEVICE fp32, the struct is read during the call only. */
+ * must be even, head_dim at most 128.  Everything else is as for last_cache_chunk_attention, but weights are always held in
+ * two parts.  lambda and norm_weight are DEVICE fp32, the struct is read during the call only. */
 typedef struct {
   const float *lambda;       /* [num_q_heads / 2] */
   const float *norm_weight;  /* [2 head_dim]; NULL: no norm */

@@ -3,7 +3,7 @@
 // A CTA holds 256 rows (two tiles of 128) where values are at most 128 wide, else 128.  Steps go key tile by key
 // tile and, within, row tile by row tile:
 //   S = Q K^T into one of two accumulators in TMEM; 8 warps turn it into weights P = 2^(scale2 S - m), rounded to
-//   bf16, a warp and its lanes' rows having 64 of the 128 keys, and put them back over S; O = O + P V in TMEM, P being
+//   bf16 (diff: in two parts), a warp and its lanes' rows having 64 of the 128 keys, and put them back over S; O = O + P V in TMEM, P being
 //   read from there.
 // The next step's S is formed before this one's O, so that the tensor cores work while the weights are formed.
 // The maximum m follows a row's logits only past a factor of 2^8 (weights are then at most 2^8, and O is rescaled by those warps,
@@ -17,7 +17,7 @@
 // diff: a cluster of two CTAs, one map each; each finishes half of the rows, with the other's half of O through L2.
 //
 // Bound by the way from S to P: 256 rows by 128 keys by 128 columns take 4600 cycles, of which the products are 2048 (16 x 2944 tokens,
-// 16 heads on 4: 560 us, 1.0 PFLOP/s).  TMEM loads, the exchange of the maxima and the exponentials of a step follow each other;
+// 16 heads on 4: 575 us, 0.99 PFLOP/s).  TMEM loads, the exchange of the maxima and the exponentials of a step follow each other;
 // 16 softmax warps (687 us) or four buffers of 64 keys (618 us) made no step shorter.
 #include "chunk_impl.cuh"
 #include "tensor_map.h"
