@@ -194,7 +194,7 @@ struct Kind {
   static constexpr int kTiles = TILES, kPanels = PANELS, kMaps = MAPS, kValues = PANELS * MAPS;
   // Weights in two parts (the second what rounding has left) where a difference would magnify the rounding: its terms are
   // alike and cancel.  Else one rounding of the weights, as large as the output's own, because two parts take 28% longer (16 x 2944 tokens 742 us
-  // and not 577): the error against 64 bits, in the norm, is 2.0e-3 for prompts and 2.3e-3 over long caches where it would be 1.6e-3 and 1.7e-3.
+  // and not 577): the error against 64 bits, in the norm, is 2.0e-3 for prompts and 2.3e-3 over long caches, of which the output's own is 1.6e-3 and 1.7e-3.
   static constexpr int kParts = MAPS;
 };
 
